@@ -1260,7 +1260,7 @@ __global__ void __launch_bounds__(kFinThreads) sel_small_kernel(
 
 int select_splits(const Dims& d, int64_t R, int64_t max_len, int sm_count) {
   const int64_t pages = (max_len + kPage - 1) / kPage;
-  int64_t want = (4LL * sm_count + R * d.n_ih - 1) / (R * d.n_ih);
+  int64_t want = (4LL * sm_count + R * std::max(d.n_ih, 1) - 1) / (R * std::max(d.n_ih, 1));
   int64_t cap = (pages + 31) / 32;  // at least 32 pages (2048 keys) per CTA
   int64_t s = want < cap ? want : cap;
   const int64_t least = (pages + 2047) / 2048;   // at most 2048 pages per CTA = 16384 keys per warp (32-bit bin sums)

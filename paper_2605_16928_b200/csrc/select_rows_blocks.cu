@@ -452,7 +452,7 @@ int64_t blocks_padded(int64_t max_len) { return (((max_len + kPage - 1) / kPage)
 
 int stats_splits(const Dims& d, int64_t R, int64_t max_len, int sm_count) {
   const int64_t pages = (max_len + kPage - 1) / kPage;
-  int64_t want = (4LL * sm_count + R * d.n_ih - 1) / (R * d.n_ih);
+  int64_t want = (4LL * sm_count + R * std::max(d.n_ih, 1) - 1) / (R * std::max(d.n_ih, 1));
   const int64_t cap = (pages + 31) / 32;   // at least 32 pages per CTA
   int64_t s = want < cap ? want : cap;
   if (s < 1) s = 1;
