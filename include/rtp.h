@@ -144,10 +144,28 @@ typedef struct rtp_cache {
    * chunk form of rtp_topp_select, rtp_topp_select_blocks and the threshold form of rtp_sparse_attn_prefill need
    * the bf16 cache (RTP_ERR_UNSUPPORTED): the paper's method selects in decode only. */
   int32_t ikey_format;
+  /* Storage type of the K/V cache.  RTP_KV_BF16 (0): the bf16 pages above, 512 bytes per token and KV head.
+   * RTP_KV_FP4 (1): 4-bit floats with a scale per 16 channels, 144 bytes per token and KV head:
+   *   k_pages / v_pages (and k_local_pages / v_local_pages): uint8 [.., .., 64, 64]: codes E2M1 (1 sign, 2 exponent, 1
+   *     mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), channel 2 b in the low half of byte b, channel 2 b + 1 in the high half;
+   *   kv_scales (and kv_local_scales for the local pool): uint8 [.., .., 64, 16]: the 8 scales of the token's K, then the 8
+   *     of its V, unsigned 8-bit floats (5 exponent, 3 mantissa bits, bias 15, subnormals): code << 7 is the fp16 pattern.
+   *     Codes above 226 (10240) are not written; a reader may take them as infinity.
+   * A value is code * scale.  rtp_kv_append quantises: scale = max |x| / 6 over the 16 channels, code = x / scale, each
+   * rounded to the nearest value (ties to even), scales at most 10240; a magnitude beyond 61440 saturates and a NaN is stored
+   * as 0, and RTP_ERR_UNSUPPORTED is recorded in the status word for either.  The decode calls (rtp_sparse_attn_decode,
+   * rtp_sparse_attn_decode_static, rtp_sparse_attn_decode_blocks, rtp_dense_attn_decode, rtp_local_attn with row arrays)
+   * and the list form of rtp_sparse_attn_prefill read such a cache; the other prefill calls need bf16 pages
+   * (RTP_ERR_UNSUPPORTED), which rtp_kv_expand makes of it. */
+  int32_t kv_format;
+  void* kv_scales;       /* DEVICE, RTP_KV_FP4 only */
+  void* kv_local_scales; /* DEVICE, RTP_KV_FP4 with a local pool only */
 } rtp_cache;
 
 #define RTP_IKEY_BF16 0
 #define RTP_IKEY_E4M3 1
+#define RTP_KV_BF16 0
+#define RTP_KV_FP4 1
 
 /* ---- utility ------------------------------------------------------------ */
 
@@ -220,6 +238,17 @@ rtp_status rtp_index_keys(rtp_ctx* ctx, const rtp_params* params, const rtp_cach
 rtp_status rtp_kv_append(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache,
                          const void* k_new, const void* v_new, const int32_t* tok_seq,
                          const int32_t* tok_pos, int64_t T, int32_t* status, void* stream);
+
+/* ---- pages of a 4-bit cache as bf16 pages (the paper has no counterpart) -----------
+ * Page src_pages[i] of the cache's main pool, decoded, goes to page dst_pages[i] of a bf16 pool (dst_pages == NULL: to
+ * page i); exact, every value of the format is a bf16 number.  A chunked prefill over a 4-bit cache appends its chunk,
+ * expands the pages of its sequence into a scratch pool and runs the prefill calls on a cache that describes that pool.
+ * src_pages, dst_pages DEVICE int32 [n]; k_out, v_out DEVICE bf16 [n_out_pages, KV heads of the main pool, 64, 128].  Page
+ * numbers out of range are skipped and RTP_ERR_INVALID is recorded; a page named twice in dst_pages is left with a mixture
+ * of its sources.  All 64 rows of a page are written, whatever of them is in use. */
+rtp_status rtp_kv_expand(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, const int32_t* src_pages,
+                         const int32_t* dst_pages, int64_t n, void* k_out, void* v_out, int32_t n_out_pages,
+                         int32_t* status, void* stream);
 
 /* ---- S1: query projection (Eq. 4, the W^Q q_pre factor) --------------------
  * q_pre  DEVICE bf16 [R, n_q_heads, 128] pre-RoPE queries (all heads; only the

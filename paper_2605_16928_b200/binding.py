@@ -17,12 +17,13 @@ LIB_PATH = os.path.join(_PKG_DIR, "librtp.so")
 
 RTP_OK, RTP_ERR_INVALID, RTP_ERR_CAPACITY, RTP_ERR_UNSUPPORTED, RTP_ERR_CUDA, RTP_ERR_TIMEOUT = range(6)
 RTP_IKEY_BF16, RTP_IKEY_E4M3 = 0, 1
+RTP_KV_BF16, RTP_KV_FP4 = 0, 1
 _STATUS_NAMES = ["RTP_OK", "RTP_ERR_INVALID", "RTP_ERR_CAPACITY", "RTP_ERR_UNSUPPORTED", "RTP_ERR_CUDA",
                  "RTP_ERR_TIMEOUT"]
 
 EXPORTS = [
     "rtp_version", "rtp_struct_bytes", "rtp_create", "rtp_destroy", "rtp_last_error", "rtp_debug_wait_test", "rtp_debug_select_path", "rtp_workspace_bytes", "rtp_check_status",
-    "rtp_kv_append", "rtp_index_keys", "rtp_index_queries", "rtp_index_score", "rtp_topp_select", "rtp_sparse_attn_decode", "rtp_sparse_attn_decode_static",
+    "rtp_kv_append", "rtp_kv_expand", "rtp_index_keys", "rtp_index_queries", "rtp_index_score", "rtp_topp_select", "rtp_sparse_attn_decode", "rtp_sparse_attn_decode_static",
     "rtp_sparse_attn_prefill", "rtp_local_attn", "rtp_dense_attn_prefill", "rtp_dense_attn_decode",
     "rtp_block_workspace_bytes", "rtp_topp_select_blocks", "rtp_sparse_attn_prefill_blocks",
     "rtp_topp_select_blocks_rows", "rtp_sparse_attn_decode_blocks",
@@ -56,7 +57,7 @@ class RtpCache(C.Structure):
         ("num_pages", C.c_int32), ("batch", C.c_int32), ("max_pages", C.c_int32),
         ("k_local_pages", C.c_void_p), ("v_local_pages", C.c_void_p), ("local_block_table", C.c_void_p),
         ("n_local_pages", C.c_int32), ("sink_pages", C.c_int32), ("ring_pages", C.c_int32),
-        ("ikey_format", C.c_int32),
+        ("ikey_format", C.c_int32), ("kv_format", C.c_int32), ("kv_scales", C.c_void_p), ("kv_local_scales", C.c_void_p),
     ]
 
 
@@ -97,6 +98,8 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.rtp_index_keys.argtypes = [vp, PP, PC, vp, vp, vp, vp, i64, vp]
     lib.rtp_kv_append.restype = i32
     lib.rtp_kv_append.argtypes = [vp, PP, PC, vp, vp, vp, vp, i64, vp, vp]
+    lib.rtp_kv_expand.restype = i32
+    lib.rtp_kv_expand.argtypes = [vp, PP, PC, vp, vp, i64, vp, vp, i32, vp, vp]
     lib.rtp_index_queries.restype = i32
     lib.rtp_index_queries.argtypes = [vp, PP, vp, vp, i64, vp, vp]
     lib.rtp_index_score.restype = i32
@@ -192,10 +195,12 @@ class Params:
 
 
 def make_cache(k_pages, v_pages, ikey_pages, block_table, seq_lens, k_local_pages=None, v_local_pages=None,
-               local_block_table=None, sink_pages: int = 0, ikey_format: Optional[int] = None) -> RtpCache:
+               local_block_table=None, sink_pages: int = 0, ikey_format: Optional[int] = None, kv_scales=None,
+               kv_local_scales=None) -> RtpCache:
     """Describes caller-owned paged caches (torch CUDA tensors) to the library.  With ``k_local_pages`` the cache is
     truncated for local heads: ``k_pages`` / ``v_pages`` hold the other KV heads only, the local heads live in the
-    local pool behind ``local_block_table`` [batch, sink_pages + ring_pages]."""
+    local pool behind ``local_block_table`` [batch, sink_pages + ring_pages].  With ``kv_scales`` the K/V pages are 4-bit codes
+    (uint8 [.., .., 64, 64], scales uint8 [.., .., 64, 16]; ``kv_local_scales`` goes with a local pool)."""
     num_pages = int((k_pages if k_pages is not None else ikey_pages).shape[0])
     if ikey_format is None:   # the tensor's element size says which: uint8 pages are E4M3 codes
         ikey_format = RTP_IKEY_E4M3 if (ikey_pages is not None and ikey_pages.element_size() == 1) else RTP_IKEY_BF16
@@ -206,7 +211,8 @@ def make_cache(k_pages, v_pages, ikey_pages, block_table, seq_lens, k_local_page
     return RtpCache(_ptr(k_pages), _ptr(v_pages), _ptr(ikey_pages), _ptr(block_table), _ptr(seq_lens),
                     num_pages, int(block_table.shape[0]), int(block_table.shape[1]),
                     _ptr(k_local_pages), _ptr(v_local_pages), _ptr(local_block_table), n_local, int(sink_pages), ring,
-                    int(ikey_format))
+                    int(ikey_format), RTP_KV_FP4 if kv_scales is not None else RTP_KV_BF16, _ptr(kv_scales),
+                    _ptr(kv_local_scales))
 
 
 class Context:
@@ -267,6 +273,13 @@ def rtp_kv_append(ctx, params, cache, k_new, v_new, tok_seq, tok_pos, status, st
     ctx._check(ctx.lib.rtp_kv_append(ctx.h, params.ref(), C.byref(cache), _ptr(k_new), _ptr(v_new), _ptr(tok_seq),
                                      _ptr(tok_pos), int(tok_seq.shape[0]), _ptr(status), _stream(stream)),
                "rtp_kv_append")
+
+
+def rtp_kv_expand(ctx, params, cache, src_pages, dst_pages, k_out, v_out, status, stream=None):
+    """src_pages, dst_pages (or None: page i): int32 [n]; k_out, v_out: bf16 [pages, KV heads of the main pool, 64, 128]."""
+    ctx._check(ctx.lib.rtp_kv_expand(ctx.h, params.ref(), C.byref(cache), _ptr(src_pages), _ptr(dst_pages),
+                                     int(src_pages.shape[0]), _ptr(k_out), _ptr(v_out), int(k_out.shape[0]), _ptr(status),
+                                     _stream(stream)), "rtp_kv_expand")
 
 
 def rtp_index_queries(ctx, params, q_pre, w_q, qt_out, stream=None):

@@ -1,0 +1,482 @@
+// Decode attention (the sets of attn_rows.cu) on a 4-bit K/V cache: o = softmax(sm_scale q K^T) V with K and V taken
+// as codes and scales, 144 bytes per (token, KV head) where the bf16 cache has 512.
+//
+// Layout of the work: a (row, KV head or listed query head) is split over CTAs, a CTA over four warps, a warp takes tiles
+// of 16 tokens.  Tiles are copied to a ring in shared memory by 16-byte cp.async, three tiles ahead.
+//
+// The contractions run with the TOKENS as the 16 rows of the MMA (m16n8k16, fp16 -> fp32) and the up to eight query heads
+// of the group as its columns:
+//   S^T = K Q^T   A = 16 tokens x 16 channels.  The channels of a k-step may be any as long as Q has the same, so lane
+//                 (g, c) of the fragment takes channels 32 c .. 32 c + 31 of its two tokens: one 16-byte read each.
+//   O^T = V^T P^T A = 16 channels x 16 tokens.  Lane (g, c) takes channels 16 g .. 16 g + 15 (one scale group) of four
+//                 tokens; the nibbles of two tokens are interleaved into bytes, so that one conversion gives the pair
+//                 (token, token') that an MMA register holds.  P^T comes from S^T by movmatrix.
+// Everything that is decoded this way is exact in fp16 (kv4.cuh).  Queries are scaled by a power of two per head, so that
+// their largest channel is near 2^9: the rounding to fp16 then costs 2^-34 of it at most, for any bf16 input.
+// Probabilities are relative to a reference that trails the running maximum by at most 2^8 and are shifted up by 2^7: they
+// fit fp16 (11 bits; bf16 has 8), down to 2^-21 of the reference without a loss.  Sums are fp32.
+#include "attn_split.cuh"
+#include "kv4.cuh"
+
+namespace rtp {
+
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
+constexpr int kTileTok = 16;
+constexpr int kTilesPerPage = kPage / kTileTok;
+constexpr int kStages = 4;                                   // tiles of a warp in shared memory
+constexpr int kTileV = kTileTok * kKv4TokBytes;              // K codes, V codes (from here), scales (from kTileS)
+constexpr int kTileS = 2 * kTileV;
+constexpr int kTileBytes = kTileS + kTileTok * kKv4ScaleBytes;   // 2304
+constexpr int kSmemBytes = kWarps * kStages * kTileBytes;    // 36 KB
+constexpr float kLag = 8.f;    // the reference of the softmax may trail the maximum by this much (log2)
+constexpr float kLift = 7.f;   // probabilities are multiplied by 2^kLift: at most 2^15 < 65504
+
+__device__ __forceinline__ void cp16z(uint32_t dst, const void* src, bool valid) {
+  const int sz = valid ? 16 : 0;
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(sz) : "memory");
+}
+__device__ __forceinline__ uint4 lds_v4(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds_v2(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds_u16(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds_u8(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  const __half2 r = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ void mma_acc(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <int G, int SET>
+__global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
+    const __grid_constant__ CacheView cv, const __grid_constant__ Dims d, const __grid_constant__ HeadMaps hm,
+    const __grid_constant__ Rows rows, const int n_units,
+    const __nv_bfloat16* __restrict__ q, const int32_t* __restrict__ sel_idx, const int64_t sel_stride,
+    const int32_t* __restrict__ sel_count, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
+    float* __restrict__ partial, const int n_splits, int32_t* status) {
+  chain_wait();
+  static_assert(G >= 1 && G <= 8, "the query heads of a KV group are the eight columns of the MMA");
+  extern __shared__ __align__(128) unsigned char smem_rows4[];
+
+  const int64_t r = blockIdx.x / n_units;
+  const int u = blockIdx.x % n_units;
+  const int split = blockIdx.y;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int g = lane >> 2, c = lane & 3;
+
+  int qh0, kvh;
+  if (SET == kSetList || SET == kSetPages) {
+    qh0 = hm.ret_q_head[u];
+    kvh = qh0 / d.group;
+  } else {
+    kvh = hm.kv_list[u];
+    qh0 = kvh * d.group;
+  }
+  const int seq = rows.row_seq(r);
+  int n_keys = rows.row_pos(r) + 1;
+  {
+    const int sl = (seq >= 0 && seq < cv.batch) ? min(cv.seq_lens[seq], cv.cap_tokens) : 0;   // (never beyond the block table)
+    if (n_keys > sl) {
+      if (threadIdx.x == 0) set_status(status, RTP_ERR_INVALID);
+      n_keys = sl;
+    }
+    if (n_keys < 0) n_keys = 0;
+  }
+
+  // The set as tiles of 16: entries of the list, or 16 tokens of one page that start at a multiple of 16 (of which those
+  // outside the set are masked).
+  int n_ent = 0, ns = 0, wlo = 0, sink_tiles = 0, n_total;
+  const int32_t* ids = nullptr;
+  if (SET == kSetList || SET == kSetPages || SET == kSetUnion) {
+    const int64_t at = r * (SET == kSetUnion ? n_units : d.n_ret) + u;
+    n_ent = (int)max(min((int64_t)sel_count[at], sel_stride), (int64_t)0);
+    ids = sel_idx + at * sel_stride;
+    n_total = SET == kSetList ? (n_ent + kTileTok - 1) / kTileTok : n_ent * kTilesPerPage;
+  } else if (SET == kSetLocal) {
+    ns = min(d.n_sink, n_keys);
+    wlo = max(ns, n_keys - d.window);
+    sink_tiles = (ns + kTileTok - 1) / kTileTok;
+    n_total = sink_tiles + (n_keys > wlo ? (n_keys + kTileTok - 1) / kTileTok - wlo / kTileTok : 0);
+  } else {
+    n_total = (n_keys + kTileTok - 1) / kTileTok;
+  }
+  const int per = ((n_total + n_splits - 1) / n_splits + kTilesPerPage - 1) / kTilesPerPage * kTilesPerPage;
+  const int first = min(n_total, split * per);
+  const int n_tiles = min(n_total, first + per) - first;
+  const int n_mine = n_tiles > warp ? (n_tiles - warp + kWarps - 1) / kWarps : 0;   // tiles first + warp, + 4, ...
+
+  // B fragments of the queries: column g = head g of the group, channels 32 c + 4 ks .. + 3 in k-step ks
+  uint32_t qb[8][2];
+  float sc[2];   // logits in log2 units: factor of heads 2 c and 2 c + 1
+  {
+    uint32_t w[16];
+    float mx = 0.f;
+    if (g < G) {
+      const uint4* qp = reinterpret_cast<const uint4*>(q + ((int64_t)r * d.n_q + qh0 + g) * kHeadDim + 32 * c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint4 v = __ldg(qp + i);
+        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] = 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+    const int e = max((int)(__float_as_uint(mx) >> 23), 27) - 127;            // floor(log2 mx), at least -100
+    const float up = __uint_as_float((uint32_t)(9 - e + 127) << 23);          // 2^(9 - e)
+    const float down = d.sm_scale * kLog2e * __uint_as_float((uint32_t)max(e - 9 + 127, 1) << 23);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      qb[i >> 1][i & 1] = pack_f16x2(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xffff0000u) * up);
+    sc[0] = __shfl_sync(0xffffffffu, down, 8 * c);       // (lane of head 2 c, channel quarter 0)
+    sc[1] = __shfl_sync(0xffffffffu, down, 8 * c + 4);
+  }
+  float o[8][4];   // tile i: channels 16 g + 2 i (elements 0, 1: heads 2 c, 2 c + 1) and 16 g + 2 i + 1 (2, 3)
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  float m_ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+  const int64_t bt_base = (int64_t)seq * cv.max_pages;
+  const int kslot = cv.kv_slot[kvh];
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem_rows4) + warp * kStages * kTileBytes;
+  const uint8_t* kp = reinterpret_cast<const uint8_t*>(cv.k);
+  const uint8_t* vp = reinterpret_cast<const uint8_t*>(cv.v);
+  const int tok_k = (g >> 1) + 4 * (g & 1);   // token of MMA row g (row g + 8: tok_k + 8)
+
+  // Where a tile lives is found in steps, each a tile after the one that requested it: entry -> token -> page -> row.
+  // List sets: lane t (and t + 16) looks after token t of the tile.  Other sets: all lanes look after the tile's page.
+  auto raw_entry = [&](int i) -> int {
+    if (i >= n_mine) return -1;
+    const int tile = first + warp + i * kWarps;
+    if (SET == kSetList) {
+      const int t = tile * kTileTok + (lane & 15);
+      return t < n_ent ? __ldg(ids + t) : -1;
+    }
+    if (SET == kSetPages || SET == kSetUnion) return __ldg(ids + tile / kTilesPerPage);
+    return 0;
+  };
+  // the token of this lane (list), or the first token of the tile; -1: none
+  auto token_of = [&](int i, int entry) -> int {
+    if (i >= n_mine) return -1;
+    const int tile = first + warp + i * kWarps;
+    if (SET == kSetList) {
+      if (entry >= 0 && entry < n_keys) return entry;
+      if (entry != -1 || tile * kTileTok + (lane & 15) < n_ent) set_status(status, RTP_ERR_INVALID);
+      return -1;
+    }
+    if (SET == kSetPages || SET == kSetUnion) {
+      const int page = SET == kSetUnion ? entry & 0xffffff : entry;
+      if (page < 0 || n_keys == 0 || page > ((n_keys - 1) >> kPageShift)) {
+        set_status(status, RTP_ERR_INVALID);
+        return -1;
+      }
+      return page * kPage + (tile % kTilesPerPage) * kTileTok;
+    }
+    if (SET == kSetLocal) return tile < sink_tiles ? tile * kTileTok : (wlo / kTileTok + tile - sink_tiles) * kTileTok;
+    return tile * kTileTok;
+  };
+  auto raw_phys = [&](int tok) -> int { return tok >= 0 ? __ldg(cv.block_table + bt_base + page_entry(cv, tok >> kPageShift)) : 0; };
+  // tokens of the tile that belong to the set, one bit each
+  auto valid_mask = [&](int i, int tok) -> uint32_t {
+    if (SET == kSetList) return __ballot_sync(0xffffffffu, tok >= 0) & 0xffffu;
+    if (tok < 0) return 0u;
+    int lo = 0, hi = n_keys;
+    if (SET == kSetLocal) {
+      if (first + warp + i * kWarps < sink_tiles) hi = ns; else lo = wlo;
+    }
+    const int a = min(max(lo - tok, 0), kTileTok), b = min(max(hi - tok, 0), kTileTok);
+    return ((1u << b) - 1u) & ~((1u << a) - 1u);
+  };
+  // Copies a tile to its stage.  Lane (t, chunk) = (lane / 4, lane % 4) takes chunk `chunk` of tokens t and t + 8; lanes
+  // 0 .. 15 take the scales.  K rows lie in the order of the MMA rows, the chunks of a V row are exchanged in pairs by bit 1
+  // of the token number: either way the reads below touch every bank once.  Tokens outside the set are filled with zeros.
+  // (A row number fits 32 bits: 2^32 rows of 144 bytes are more than the device's memory.)
+  auto issue = [&](int stage, int tok, int phys, uint32_t mask) {
+    if ((unsigned)phys >= (unsigned)cv.num_pages) {
+      set_status(status, RTP_ERR_INVALID);
+      phys = 0;
+    }
+    const uint32_t dst = ring + stage * kTileBytes;
+    const uint32_t row = ((uint32_t)phys * cv.n_kv + kslot) * kPage + (tok & (kPage - 1));
+    const int t = lane >> 2, ch = lane & 3;
+    const uint32_t dk = dst + (2 * (t & 3) + (t >> 2)) * kKv4TokBytes + ch * 16;
+    const uint32_t dv = dst + kTileV + t * kKv4TokBytes + ((ch ^ (t & 2)) << 4);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool ok = (mask >> (t + 8 * h)) & 1u;
+      const uint32_t rt = SET == kSetList ? __shfl_sync(0xffffffffu, row, t + 8 * h) : row + t + 8 * h;
+      const int64_t off = ok ? (int64_t)rt * kKv4TokBytes + ch * 16 : 0;
+      cp16z(dk + h * 8 * kKv4TokBytes, kp + off, ok);
+      cp16z(dv + h * 8 * kKv4TokBytes, vp + off, ok);
+    }
+    if (lane < kTileTok) {
+      const bool ok = (mask >> lane) & 1u;
+      const uint32_t rt = SET == kSetList ? row : row + lane;
+      cp16z(dst + kTileS + lane * kKv4ScaleBytes, cv.kv_scales + (ok ? (int64_t)rt * kKv4ScaleBytes : 0), ok);
+    }
+  };
+
+  uint32_t mask_st[kStages], flag_st[kStages];   // of the tiles in the ring
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) {
+    const int e = raw_entry(s), tok = token_of(s, e);
+    mask_st[s] = valid_mask(s, tok);
+    flag_st[s] = (uint32_t)e >> 24;
+    issue(s, tok, raw_phys(tok), mask_st[s]);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  mask_st[kStages - 1] = flag_st[kStages - 1] = 0u;
+  int ent_a = raw_entry(kStages - 1);                       // the next tile to be copied: its entry, token and page
+  int tok_a = token_of(kStages - 1, ent_a), phys_a = raw_phys(tok_a);
+  int ent_b = raw_entry(kStages);
+
+#pragma unroll 1
+  for (int i0 = 0; i0 < n_mine; i0 += kStages) {
+#pragma unroll
+    for (int sgi = 0; sgi < kStages; ++sgi) {
+      const int i = i0 + sgi;
+      if (i < n_mine) {   // uniform in the warp
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+        __syncwarp();
+        {   // tile i + 3 goes where tile i - 1 was
+          const int next = (sgi + kStages - 1) % kStages;
+          mask_st[next] = valid_mask(i + kStages - 1, tok_a);
+          flag_st[next] = (uint32_t)ent_a >> 24;
+          issue(next, tok_a, phys_a, mask_st[next]);
+          asm volatile("cp.async.commit_group;" ::: "memory");
+          ent_a = ent_b;
+          tok_a = token_of(i + kStages, ent_a);
+          phys_a = raw_phys(tok_a);
+          ent_b = raw_entry(i + kStages + 1);
+        }
+        const uint32_t tile = ring + sgi * kTileBytes;
+        // ---- S^T = K Q^T ----
+        float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        {
+          const uint4 ka = lds_v4(tile + lane * 16), kb = lds_v4(tile + 8 * kKv4TokBytes + lane * 16);
+          const uint32_t ua = lds_u16(tile + kTileS + tok_k * kKv4ScaleBytes + 2 * c);
+          const uint32_t ub = lds_u16(tile + kTileS + (tok_k + 8) * kKv4ScaleBytes + 2 * c);
+          const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t fa = (((w < 2 ? ua : ua >> 8) & 0xffu) << 7) * 0x10001u, fb = (((w < 2 ? ub : ub >> 8) & 0xffu) << 7) * 0x10001u;
+            uint32_t a[4], b[4];
+            e2m1x8_to_f16x2(wa[w], a);
+            e2m1x8_to_f16x2(wb[w], b);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              a[j] = mul_f16x2(a[j], fa);
+              b[j] = mul_f16x2(b[j], fb);
+            }
+            mma_acc(s[0], a[0], b[0], a[1], b[1], qb[2 * w][0], qb[2 * w][1]);
+            mma_acc(s[1], a[2], b[2], a[3], b[3], qb[2 * w + 1][0], qb[2 * w + 1][1]);
+          }
+        }
+        // ---- softmax: elements 0, 1 = heads 2 c, 2 c + 1 of token tok_k; 2, 3 = of token tok_k + 8 ----
+        float t[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[j] = (s[0][j] + s[1][j]) * sc[j & 1];
+        const uint32_t vm = mask_st[sgi];
+        if (SET == kSetUnion || vm != 0xffffu) {
+          const bool v0 = (vm >> tok_k) & 1u, v1 = (vm >> (tok_k + 8)) & 1u;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            bool on = j < 2 ? v0 : v1;
+            if (SET == kSetUnion) on = on && ((flag_st[sgi] >> (2 * c + (j & 1))) & 1u);
+            if (!on) t[j] = -INFINITY;
+          }
+        }
+        const float top0 = fmaxf(t[0], t[2]), top1 = fmaxf(t[1], t[3]);
+        if (__any_sync(0xffffffffu, top0 > m_ref[0] + kLag || top1 > m_ref[1] + kLag)) {
+          float top[2] = {top0, top1};
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int x = 4; x <= 16; x <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], x));
+            const float m_new = fmaxf(m_ref[j], top[j]);
+            const float corr = m_ref[j] == -INFINITY ? 0.f : fast_ex2(m_ref[j] - m_new);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+              o[x][j] *= corr;
+              o[x][2 + j] *= corr;
+            }
+            l[j] *= corr;
+            m_ref[j] = m_new;
+          }
+        }
+        const float mb0 = m_ref[0] == -INFINITY ? 0.f : m_ref[0] - kLift, mb1 = m_ref[1] == -INFINITY ? 0.f : m_ref[1] - kLift;
+        const float p0 = fast_ex2(t[0] - mb0), p1 = fast_ex2(t[1] - mb1), p2 = fast_ex2(t[2] - mb0), p3 = fast_ex2(t[3] - mb1);
+        l[0] += p0 + p2;
+        l[1] += p1 + p3;
+        const uint32_t pb0 = transpose8x8(pack_f16x2(p0, p1)), pb1 = transpose8x8(pack_f16x2(p2, p3));
+        // ---- O^T += V^T P^T: tokens c, c + 4, c + 8, c + 12 of the tile ----
+        {
+          const uint32_t va = tile + kTileV + c * kKv4TokBytes + (((g >> 1) ^ (c & 2)) << 4) + (g & 1) * 8;
+          const uint32_t vs = tile + kTileS + c * kKv4ScaleBytes + kKv4ScaleBytes / 2 + g;
+          uint2 w[4];
+          uint32_t f[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            w[j] = lds_v2(va + j * 4 * kKv4TokBytes);
+            f[j] = lds_u8(vs + j * 4 * kKv4ScaleBytes);
+          }
+          const uint32_t f01 = (f[0] << 7) | (f[1] << 23), f23 = (f[2] << 7) | (f[3] << 23);
+          constexpr uint32_t kLow = 0x0f0f0f0fu;
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            const uint32_t w0 = hh ? w[0].y : w[0].x, w1 = hh ? w[1].y : w[1].x, w2 = hh ? w[2].y : w[2].x, w3 = hh ? w[3].y : w[3].x;
+            uint32_t e01[4], d01[4], e23[4], d23[4];   // even and odd channels of the token pairs
+            e2m1x8_to_f16x2((w0 & kLow) | ((w1 << 4) & ~kLow), e01);
+            e2m1x8_to_f16x2(((w0 >> 4) & kLow) | (w1 & ~kLow), d01);
+            e2m1x8_to_f16x2((w2 & kLow) | ((w3 << 4) & ~kLow), e23);
+            e2m1x8_to_f16x2(((w2 >> 4) & kLow) | (w3 & ~kLow), d23);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              mma_acc(o[4 * hh + j], mul_f16x2(e01[j], f01), mul_f16x2(d01[j], f01), mul_f16x2(e23[j], f23), mul_f16x2(d23[j], f23), pb0, pb1);
+          }
+        }
+      }
+    }
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();   // the rings are free: they now hold the warps' partial results
+
+  float* red = reinterpret_cast<float*>(smem_rows4);   // [kWarps][G][kPartial]
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+#pragma unroll
+    for (int x = 4; x <= 16; x <<= 1) l[j] += __shfl_xor_sync(0xffffffffu, l[j], x);
+    const int h = 2 * c + j;
+    if (h < G) {
+      float* rw = red + (warp * G + h) * kPartial;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        rw[16 * g + 2 * i] = o[i][j];
+        rw[16 * g + 2 * i + 1] = o[i][2 + j];
+      }
+      if (g == 0) {
+        rw[kHeadDim] = m_ref[j] - kLift;   // (the lift goes into the reference)
+        rw[kHeadDim + 1] = l[j];
+      }
+    }
+  }
+  __syncthreads();
+  const int dim = threadIdx.x;  // 128 threads = 128 dims
+#pragma unroll
+  for (int gg = 0; gg < G; ++gg) {
+    float mt = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) mt = fmaxf(mt, red[(w * G + gg) * kPartial + kHeadDim]);
+    float lt = 0.f, a = 0.f;
+    if (mt != -INFINITY) {
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float* rw = red + (w * G + gg) * kPartial;
+        const float wgt = fast_ex2(rw[kHeadDim] - mt);
+        lt += rw[kHeadDim + 1] * wgt;
+        a += rw[dim] * wgt;
+      }
+    }
+    const int64_t oh = (int64_t)r * d.n_q + qh0 + gg;
+    // (a retrieval head inside a local group is not a local call's; a local head inside a retrieval group not a union call's)
+    if ((SET == kSetLocal || SET == kSetUnion) && hm.skips(qh0 + gg)) continue;
+    if (n_splits == 1) {
+      out[oh * kHeadDim + dim] = __float2bfloat16_rn(lt > 0.f ? a / lt : 0.f);
+      if (lse && dim == 0) lse[oh] = lt > 0.f ? (mt + log2f(lt)) * kLn2 : -INFINITY;
+    } else {
+      float* p = partial + (((int64_t)blockIdx.x * G + gg) * n_splits + split) * kPartial;
+      p[dim] = a;
+      if (dim == 0) {
+        p[kHeadDim] = mt;
+        p[kHeadDim + 1] = lt;
+      }
+    }
+  }
+}
+
+template <int G, int SET>
+cudaError_t launch_typed4(const CacheView& cv, const Dims& d, const HeadMaps& hm, const Rows& rows, int n_units,
+                          const __nv_bfloat16* q, const int32_t* sel_idx, int64_t sel_stride, const int32_t* sel_count,
+                          __nv_bfloat16* out, float* lse, float* partial, int n_splits, int32_t* status, cudaStream_t st) {
+  const dim3 grid((unsigned)(rows.R * n_units), n_splits);
+  (void)launch_chained(attn_rows4_kernel<G, SET>, grid, dim3(kThreads), kSmemBytes, st, cv, d, hm, rows, n_units, q, sel_idx,
+                       sel_stride, sel_count, out, lse, partial, n_splits, status);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || n_splits == 1) return e;
+  (void)launch_chained(attn_merge_kernel<SET>, dim3((unsigned)(rows.R * n_units * G)), dim3(kHeadDim), 0, st, d, hm, n_units, G,
+                       partial, n_splits, out, lse);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+// Split count of a call: one round of the four resident CTAs per SM, at least 512 tokens (eight tiles per warp) each.
+int plan_splits4(int64_t units, int64_t max_set, int sm_count) {
+  if (units <= 0) return 1;
+  const int64_t want = 4LL * sm_count / units, cap = (max_set + 511) / 512;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, cap), 512));
+}
+
+cudaError_t launch_attn_rows4(const CacheView& cv, const Dims& d, const HeadMaps& hm, const Rows& rows, int set, int n_units,
+                              const __nv_bfloat16* q, const int32_t* sel_idx, int64_t sel_stride,
+                              const int32_t* sel_count, __nv_bfloat16* out, float* lse, float* partial, int n_splits,
+                              int32_t* status, cudaStream_t st) {
+#define RTP_LAUNCH4(GG, SS)                                                                                               \
+  return launch_typed4<GG, SS>(cv, d, hm, rows, n_units, q, sel_idx, sel_stride, sel_count, out, lse, partial, n_splits, \
+                               status, st)
+#define RTP_GROUPS4(SS)                 \
+  switch (d.group) {                    \
+    case 1: RTP_LAUNCH4(1, SS);         \
+    case 2: RTP_LAUNCH4(2, SS);         \
+    case 4: RTP_LAUNCH4(4, SS);         \
+    case 8: RTP_LAUNCH4(8, SS);         \
+    default: return cudaErrorInvalidValue; \
+  }
+  switch (set) {
+    case kSetList: RTP_LAUNCH4(1, kSetList);
+    case kSetPages: RTP_LAUNCH4(1, kSetPages);
+    case kSetUnion: RTP_GROUPS4(kSetUnion)
+    case kSetLocal: RTP_GROUPS4(kSetLocal)
+    default: RTP_GROUPS4(kSetDense)
+  }
+#undef RTP_GROUPS4
+#undef RTP_LAUNCH4
+}
+
+}  // namespace rtp

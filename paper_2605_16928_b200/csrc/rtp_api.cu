@@ -117,11 +117,18 @@ const char* check_cache(const rtp_cache* c, const rtp_params* p, bool need_kv, b
   cv->ring_pages = 0;
   if (c->ikey_format != RTP_IKEY_BF16 && c->ikey_format != RTP_IKEY_E4M3) return "unknown ikey_format";
   cv->ikey_fp8 = c->ikey_format == RTP_IKEY_E4M3;
+  if (c->kv_format != RTP_KV_BF16 && c->kv_format != RTP_KV_FP4) return "unknown kv_format";
+  cv->kv_fp4 = c->kv_format == RTP_KV_FP4;
+  cv->kv_scales = cv->kv_fp4 ? reinterpret_cast<const uint8_t*>(c->kv_scales) : nullptr;
+  if (cv->kv_fp4 && need_kv && !c->kv_scales) return "kv_scales is NULL";
+  if (cv->kv_fp4 && !aligned16(c->kv_scales)) return "kv_scales must be 16-byte aligned";
   for (int h = 0; h < 32; ++h) cv->kv_slot[h] = h < p->n_kv_heads ? (uint8_t)h : (uint8_t)0xff;
   if (c->k_local_pages) {
     // truncated layout: the main pool holds the KV heads that are not local, in increasing order
     if (!c->v_local_pages || !c->local_block_table) return "v_local_pages / local_block_table is NULL";
     if (!aligned16(c->k_local_pages) || !aligned16(c->v_local_pages)) return "local cache pages must be 16-byte aligned";
+    if (cv->kv_fp4 && !c->kv_local_scales) return "kv_local_scales is NULL";
+    if (cv->kv_fp4 && !aligned16(c->kv_local_scales)) return "kv_local_scales must be 16-byte aligned";
     if (c->n_local_pages <= 0 || c->ring_pages <= 0 || c->sink_pages < 0) return "local cache sizes must be positive";
     if ((int64_t)c->sink_pages * kPage < p->n_sink) return "sink_pages does not cover n_sink";
     if (p->n_local_kv_heads <= 0) return "a local cache without local KV heads";
@@ -144,6 +151,7 @@ CacheView local_view(const CacheView& main, const rtp_cache* c, const rtp_params
   v.k = reinterpret_cast<const __nv_bfloat16*>(c->k_local_pages);
   v.v = reinterpret_cast<const __nv_bfloat16*>(c->v_local_pages);
   v.ikey = nullptr;
+  v.kv_scales = v.kv_fp4 ? reinterpret_cast<const uint8_t*>(c->kv_local_scales) : nullptr;
   v.block_table = c->local_block_table;
   v.num_pages = c->n_local_pages;
   v.max_pages = c->sink_pages + c->ring_pages;
@@ -195,7 +203,7 @@ constexpr int kFallbackSm = 148;
 
 extern "C" {
 
-int32_t rtp_version(void) { return 100; }
+int32_t rtp_version(void) { return 200; }
 
 size_t rtp_struct_bytes(int32_t what) { return what == 0 ? sizeof(rtp_params) : (what == 1 ? sizeof(rtp_cache) : 0); }
 
@@ -307,13 +315,28 @@ rtp_status rtp_kv_append(rtp_ctx* ctx, const rtp_params* params, const rtp_cache
   if (!aligned16(k_new) || !aligned16(v_new)) return fail(ctx, RTP_ERR_INVALID, "k_new / v_new must be 16-byte aligned");
   (void)hm;
   cudaError_t e = cudaSuccess;
+  const auto launch = cv.kv_fp4 ? launch_kv4_append : launch_kv_append;
   if (cv.n_kv > 0)
-    e = launch_kv_append(cv, d.n_kv, reinterpret_cast<const __nv_bfloat16*>(k_new),
-                         reinterpret_cast<const __nv_bfloat16*>(v_new), tok_seq, tok_pos, T, status, st);
+    e = launch(cv, d.n_kv, reinterpret_cast<const __nv_bfloat16*>(k_new),
+               reinterpret_cast<const __nv_bfloat16*>(v_new), tok_seq, tok_pos, T, status, st);
   if (e == cudaSuccess && cache->k_local_pages)
-    e = launch_kv_append(local_view(cv, cache, params), d.n_kv, reinterpret_cast<const __nv_bfloat16*>(k_new),
-                         reinterpret_cast<const __nv_bfloat16*>(v_new), tok_seq, tok_pos, T, status, st);
+    e = launch(local_view(cv, cache, params), d.n_kv, reinterpret_cast<const __nv_bfloat16*>(k_new),
+               reinterpret_cast<const __nv_bfloat16*>(v_new), tok_seq, tok_pos, T, status, st);
   return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_kv_append");
+}
+
+rtp_status rtp_kv_expand(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, const int32_t* src_pages,
+                         const int32_t* dst_pages, int64_t n, void* k_out, void* v_out, int32_t n_out_pages,
+                         int32_t* status, void* stream) {
+  RTP_COMMON_PROLOGUE(true, false)
+  (void)hm;
+  if (n < 0 || n_out_pages < 0) return fail(ctx, RTP_ERR_INVALID, "page count is negative");
+  if (!cv.kv_fp4) return fail(ctx, RTP_ERR_UNSUPPORTED, "the cache is not a 4-bit cache");
+  if (n == 0) return RTP_OK;
+  if (!src_pages || !k_out || !v_out) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
+  if (!aligned16(k_out) || !aligned16(v_out)) return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
+  cudaError_t e = launch_kv4_expand(cv, src_pages, dst_pages, n, k_out, v_out, n_out_pages, status, st);
+  return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_kv_expand");
 }
 
 rtp_status rtp_index_queries(rtp_ctx* ctx, const rtp_params* params, const void* q_pre, const void* w_q, int64_t R,
@@ -459,6 +482,7 @@ rtp_status rtp_sparse_attn_prefill(rtp_ctx* ctx, const rtp_params* params, const
                                      workspace ? workspace_bytes : 0, max_len, status, ctx->sm_count, st);
     return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_sparse_attn_prefill(lists)");
   }
+  if (cv.kv_fp4) return fail(ctx, RTP_ERR_UNSUPPORTED, "4-bit K/V cache: list form only (or rtp_kv_expand its pages)");
   if (!sel_thresh || !sel_tie_last || !q_pre || !w_q || !workspace)
     return fail(ctx, RTP_ERR_INVALID, "threshold mode needs sel_thresh, sel_tie_last, q_pre, w_q and a workspace");
   if (cv.ikey_fp8) return fail(ctx, RTP_ERR_UNSUPPORTED, "8-bit index keys: list form only");
@@ -601,6 +625,7 @@ rtp_status rtp_sparse_attn_prefill_blocks(rtp_ctx* ctx, const rtp_params* params
   int64_t max_len = 0;
   if (const char* m = check_rows(nullptr, nullptr, seq_id, q_start, C, cache, &rows, &max_len)) return fail(ctx, RTP_ERR_INVALID, m);
   if (C == 0 || d.n_ret == 0) return RTP_OK;
+  if (cv.kv_fp4) return fail(ctx, RTP_ERR_UNSUPPORTED, "4-bit K/V cache: decode calls only (or rtp_kv_expand its pages)");
   if (!q || !out || !block_mask) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
   if (!aligned16(q) || !aligned16(out)) return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
   if (mask_words * 32 < ((int64_t)q_start + C + kPage - 1) / kPage) return fail(ctx, RTP_ERR_INVALID, "mask_words too small for the chunk's pages");
@@ -622,6 +647,7 @@ rtp_status rtp_local_attn(rtp_ctx* ctx, const rtp_params* params, const rtp_cach
   if (R == 0 || params->n_local_kv_heads == 0) return RTP_OK;
   if (!q || !out) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
+  if (cv.kv_fp4 && !row_seq) return fail(ctx, RTP_ERR_UNSUPPORTED, "4-bit K/V cache: row arrays only (or rtp_kv_expand its pages)");
   hm.n_kv_list = params->n_local_kv_heads;
   for (int i = 0; i < hm.n_kv_list; ++i) hm.kv_list[i] = (uint8_t)params->local_kv_heads[i];
   // a mixed group: its retrieval heads are written by the sparse call, not by this one
@@ -676,6 +702,7 @@ rtp_status rtp_dense_attn_prefill(rtp_ctx* ctx, const rtp_params* params, const 
     if (cv.kv_slot[hm.kv_list[i]] == 0xff)
       return fail(ctx, RTP_ERR_UNSUPPORTED, "the cache is truncated for local heads: a dense call may only name the other KV heads");
   if (C == 0 || hm.n_kv_list == 0) return RTP_OK;
+  if (cv.kv_fp4) return fail(ctx, RTP_ERR_UNSUPPORTED, "4-bit K/V cache: decode calls only (or rtp_kv_expand its pages)");
   if (!q || !out) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
   if (!aligned16(q) || !aligned16(out)) return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
   cudaError_t e = launch_attn_prefill(cv, d, hm, kPrefillDense, reinterpret_cast<const __nv_bfloat16*>(q), nullptr,

@@ -57,6 +57,9 @@ struct CacheView {
   uint8_t kv_slot[32];
   // != 0: the index-key cache holds 8-bit floats (E4M3), 16 bytes per token and index head, instead of bf16
   int32_t ikey_fp8;
+  // != 0: k / v point to 4-bit codes, uint8 [num_pages, n_kv, 64, 64], and kv_scales to their scales, uint8 [.., 64, 16]
+  int32_t kv_fp4;
+  const uint8_t* kv_scales;
 };
 
 struct Dims {
@@ -173,6 +176,11 @@ cudaError_t launch_index_keys(const CacheView& cv, const Dims& d, const __nv_bfl
 cudaError_t launch_kv_append(const CacheView& cv, int n_src_heads, const __nv_bfloat16* k_new, const __nv_bfloat16* v_new,
                              const int32_t* tok_seq, const int32_t* tok_pos, int64_t T, int32_t* status,
                              cudaStream_t st);
+cudaError_t launch_kv4_append(const CacheView& cv, int n_src_heads, const __nv_bfloat16* k_new, const __nv_bfloat16* v_new,
+                              const int32_t* tok_seq, const int32_t* tok_pos, int64_t T, int32_t* status,
+                              cudaStream_t st);
+cudaError_t launch_kv4_expand(const CacheView& cv, const int32_t* src_pages, const int32_t* dst_pages, int64_t n, void* k_out,
+                              void* v_out, int32_t n_out_pages, int32_t* status, cudaStream_t st);
 cudaError_t launch_index_queries(const Dims& d, const HeadMaps& hm, const __nv_bfloat16* q_pre,
                                  const __nv_bfloat16* w_q, int64_t R, __nv_bfloat16* qt, cudaStream_t st);
 
@@ -204,6 +212,13 @@ cudaError_t launch_attn_rows(const CacheView& cv, const Dims& d, const HeadMaps&
                              const __nv_bfloat16* q, const int32_t* sel_idx, int64_t sel_stride,
                              const int32_t* sel_count, __nv_bfloat16* out, float* lse, void* ws,
                              size_t ws_bytes, int64_t max_len, int32_t* status, int sm_count, cudaStream_t st);
+
+// The same call on a 4-bit cache (cv.kv_fp4): `partial` holds R * n_units * group * n_splits partial results when n_splits > 1.
+int plan_splits4(int64_t units, int64_t max_set, int sm_count);
+cudaError_t launch_attn_rows4(const CacheView& cv, const Dims& d, const HeadMaps& hm, const Rows& rows, int set, int n_units,
+                              const __nv_bfloat16* q, const int32_t* sel_idx, int64_t sel_stride,
+                              const int32_t* sel_count, __nv_bfloat16* out, float* lse, float* partial, int n_splits,
+                              int32_t* status, cudaStream_t st);
 
 size_t attn_rows_static_scratch_bytes();
 cudaError_t launch_attn_rows_static(const CacheView& cv, const Dims& d, const HeadMaps& hm, const Rows& rows,
