@@ -250,6 +250,55 @@ rtp_status rtp_kv_expand(rtp_ctx* ctx, const rtp_params* params, const rtp_cache
                          const int32_t* dst_pages, int64_t n, void* k_out, void* v_out, int32_t n_out_pages,
                          int32_t* status, void* stream);
 
+/* ---- pages: copies, shared sequences, allocation, release, compaction (the paper has no counterpart) ----
+ * The calls below manage the pages of the MAIN pool: every array that the cache names (k_pages, v_pages, kv_scales,
+ * ikey_pages; NULL ones are left out) is treated alike.  Apart from rtp_cache_copy_pages they own
+ *   page_refs          DEVICE int32 [num_pages]: the number of block-table entries that name each page; 0 = free.  A caller
+ *                      that starts with an empty cache sets it to 0, block_table to -1 and seq_lens to 0;
+ *   cache->block_table and cache->seq_lens, which they WRITE: an unmapped entry is -1, and the mapped entries of a sequence
+ *                      come first in its row.
+ * Everything happens on the device in stream order (a captured decode step can reserve its own pages), and results do not
+ * depend on timing: free pages are handed out in the order of their numbers.  These calls refuse a cache with a local pool
+ * (RTP_ERR_UNSUPPORTED), whose rings belong to one sequence each.  Rows named by an index out of range are skipped
+ * and RTP_ERR_INVALID is recorded in the status word.
+ *
+ * rtp_cache_copy_pages: page src_pages[i] -> page dst_pages[i], DEVICE int32 [n].  No page may be named twice in dst_pages, nor
+ *   be both a destination and another pair's source (such pages are left with a mixture); a page copied to itself is left alone.
+ *
+ * rtp_cache_fork: sequence dst_seqs[i] becomes a copy of sequence src_seqs[i] that shares its pages (the ceil(len / 64) ones that
+ *   hold tokens): entries copied, references counted, seq_lens[dst] = seq_lens[src].  No contents move; reserve
+ *   copies the one page that both may write.  dst must be empty (length 0, no entry mapped).  A dst named before in the same
+ *   call, a src that is also a dst of the call, a dst that is not empty or a src with an unmapped page: skipped,
+ *   RTP_ERR_INVALID.  DEVICE int32 [n]; n <= 65535.
+ *
+ * rtp_cache_reserve: room for n_tokens[i] more tokens in sequence seqs[i] (positions seq_lens .. seq_lens + n_tokens - 1; seq_lens
+ *   itself is left to the caller, as in rtp_kv_append).  Unmapped pages up to there are taken from the free ones, and a
+ *   partly filled last page that other sequences share is replaced by a copy of its own, contents included, if at
+ *   least one token is asked for.  Requests are served in the order of the list: of r sequences that share a page and are all
+ *   listed, the first r - 1 get copies.  If the free pages or a table row do not suffice for ALL requests, nothing changes and
+ *   RTP_ERR_CAPACITY is recorded.  A sequence named twice counts the first time (RTP_ERR_INVALID).  n <= 4096
+ *   (RTP_ERR_UNSUPPORTED).  workspace: rtp_cache_workspace_bytes(cache, n).
+ *
+ * rtp_cache_free: gives back every page of sequences seqs[i], sets their entries to -1 and their lengths to 0.  Freeing an
+ *   empty sequence, or one twice, is allowed.  n <= 65535.
+ *
+ * rtp_cache_compact: moves pages so that the n pages in use become pages 0 .. n - 1: the k-th used page at or above n goes to
+ *   the k-th free page below it; contents, references and table entries follow, *n_used (DEVICE int32) = n.  Pages n .. are
+ *   free afterwards (their old contents are left), so that the pool can be cut there.  An entry that names a page without
+ *   references: left, RTP_ERR_INVALID.  workspace: rtp_cache_workspace_bytes(cache, 0). */
+size_t rtp_cache_workspace_bytes(const rtp_cache* cache, int64_t n_seqs);
+rtp_status rtp_cache_copy_pages(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, const int32_t* src_pages,
+                                const int32_t* dst_pages, int64_t n, int32_t* status, void* stream);
+rtp_status rtp_cache_fork(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
+                          const int32_t* src_seqs, const int32_t* dst_seqs, int64_t n, int32_t* status, void* stream);
+rtp_status rtp_cache_reserve(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
+                             const int32_t* seqs, const int32_t* n_tokens, int64_t n, void* workspace,
+                             size_t workspace_bytes, int32_t* status, void* stream);
+rtp_status rtp_cache_free(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
+                          const int32_t* seqs, int64_t n, int32_t* status, void* stream);
+rtp_status rtp_cache_compact(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
+                             int32_t* n_used, void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
 /* ---- S1: query projection (Eq. 4, the W^Q q_pre factor) --------------------
  * q_pre  DEVICE bf16 [R, n_q_heads, 128] pre-RoPE queries (all heads; only the
  *        retrieval heads are read)

@@ -23,7 +23,8 @@ _STATUS_NAMES = ["RTP_OK", "RTP_ERR_INVALID", "RTP_ERR_CAPACITY", "RTP_ERR_UNSUP
 
 EXPORTS = [
     "rtp_version", "rtp_struct_bytes", "rtp_create", "rtp_destroy", "rtp_last_error", "rtp_debug_wait_test", "rtp_debug_select_path", "rtp_workspace_bytes", "rtp_check_status",
-    "rtp_kv_append", "rtp_kv_expand", "rtp_index_keys", "rtp_index_queries", "rtp_index_score", "rtp_topp_select", "rtp_sparse_attn_decode", "rtp_sparse_attn_decode_static",
+    "rtp_kv_append", "rtp_kv_expand", "rtp_cache_workspace_bytes", "rtp_cache_copy_pages", "rtp_cache_fork", "rtp_cache_reserve",
+    "rtp_cache_free", "rtp_cache_compact", "rtp_index_keys", "rtp_index_queries", "rtp_index_score", "rtp_topp_select", "rtp_sparse_attn_decode", "rtp_sparse_attn_decode_static",
     "rtp_sparse_attn_prefill", "rtp_local_attn", "rtp_dense_attn_prefill", "rtp_dense_attn_decode",
     "rtp_block_workspace_bytes", "rtp_topp_select_blocks", "rtp_sparse_attn_prefill_blocks",
     "rtp_topp_select_blocks_rows", "rtp_sparse_attn_decode_blocks",
@@ -100,6 +101,18 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.rtp_kv_append.argtypes = [vp, PP, PC, vp, vp, vp, vp, i64, vp, vp]
     lib.rtp_kv_expand.restype = i32
     lib.rtp_kv_expand.argtypes = [vp, PP, PC, vp, vp, i64, vp, vp, i32, vp, vp]
+    lib.rtp_cache_workspace_bytes.restype = sz
+    lib.rtp_cache_workspace_bytes.argtypes = [PC, i64]
+    lib.rtp_cache_copy_pages.restype = i32
+    lib.rtp_cache_copy_pages.argtypes = [vp, PP, PC, vp, vp, i64, vp, vp]
+    lib.rtp_cache_fork.restype = i32
+    lib.rtp_cache_fork.argtypes = [vp, PP, PC, vp, vp, vp, i64, vp, vp]
+    lib.rtp_cache_reserve.restype = i32
+    lib.rtp_cache_reserve.argtypes = [vp, PP, PC, vp, vp, vp, i64, vp, sz, vp, vp]
+    lib.rtp_cache_free.restype = i32
+    lib.rtp_cache_free.argtypes = [vp, PP, PC, vp, vp, i64, vp, vp]
+    lib.rtp_cache_compact.restype = i32
+    lib.rtp_cache_compact.argtypes = [vp, PP, PC, vp, vp, vp, sz, vp, vp]
     lib.rtp_index_queries.restype = i32
     lib.rtp_index_queries.argtypes = [vp, PP, vp, vp, i64, vp, vp]
     lib.rtp_index_score.restype = i32
@@ -280,6 +293,40 @@ def rtp_kv_expand(ctx, params, cache, src_pages, dst_pages, k_out, v_out, status
     ctx._check(ctx.lib.rtp_kv_expand(ctx.h, params.ref(), C.byref(cache), _ptr(src_pages), _ptr(dst_pages),
                                      int(src_pages.shape[0]), _ptr(k_out), _ptr(v_out), int(k_out.shape[0]), _ptr(status),
                                      _stream(stream)), "rtp_kv_expand")
+
+
+def rtp_cache_workspace_bytes(cache, n_seqs: int) -> int:
+    return int(load_library().rtp_cache_workspace_bytes(C.byref(cache), int(n_seqs)))
+
+
+def rtp_cache_copy_pages(ctx, params, cache, src_pages, dst_pages, status, stream=None):
+    ctx._check(ctx.lib.rtp_cache_copy_pages(ctx.h, params.ref(), C.byref(cache), _ptr(src_pages), _ptr(dst_pages),
+                                            int(src_pages.shape[0]), _ptr(status), _stream(stream)), "rtp_cache_copy_pages")
+
+
+def rtp_cache_fork(ctx, params, cache, page_refs, src_seqs, dst_seqs, status, stream=None):
+    """Writes page_refs and the block table and sequence lengths that ``cache`` describes (as the three calls below do)."""
+    ctx._check(ctx.lib.rtp_cache_fork(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(src_seqs), _ptr(dst_seqs),
+                                      int(src_seqs.shape[0]), _ptr(status), _stream(stream)), "rtp_cache_fork")
+
+
+def rtp_cache_reserve(ctx, params, cache, page_refs, seqs, n_tokens, workspace, status, stream=None):
+    ctx._check(ctx.lib.rtp_cache_reserve(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(seqs), _ptr(n_tokens),
+                                         int(seqs.shape[0]), _ptr(workspace),
+                                         int(workspace.numel() * workspace.element_size()), _ptr(status), _stream(stream)),
+               "rtp_cache_reserve")
+
+
+def rtp_cache_free(ctx, params, cache, page_refs, seqs, status, stream=None):
+    ctx._check(ctx.lib.rtp_cache_free(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(seqs), int(seqs.shape[0]),
+                                      _ptr(status), _stream(stream)), "rtp_cache_free")
+
+
+def rtp_cache_compact(ctx, params, cache, page_refs, n_used, workspace, status, stream=None):
+    """n_used: int32 [1] on the device, written."""
+    ctx._check(ctx.lib.rtp_cache_compact(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(n_used), _ptr(workspace),
+                                         int(workspace.numel() * workspace.element_size()), _ptr(status), _stream(stream)),
+               "rtp_cache_compact")
 
 
 def rtp_index_queries(ctx, params, q_pre, w_q, qt_out, stream=None):

@@ -1,0 +1,514 @@
+// Pages of a cache: copies, sequences that share pages (fork), room for new tokens with copies of shared pages that are going
+// to be written (reserve), release (free) and the move of all used pages to the front of the pool (compact).
+//
+// A page is free iff its reference count is zero, so there is no other state to keep in step: the free pages in the order of
+// their numbers are found by a scan over the counts (4 bytes a page: 64 KB for a pool of 16K pages, which one CTA reads from
+// L2 in a few microseconds), and what a call hands out does not depend on the order in which threads arrive.  Decisions that
+// need an order are taken by one CTA; page contents, the only bytes that matter, are then copied by all SMs.
+#include "rtp_device.cuh"
+
+namespace rtp {
+
+namespace {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanWarps = kPlanThreads / 32;
+constexpr int kRowThreads = 256;
+constexpr int kCopyThreads = 256;
+constexpr int kCopyVec = 4;                                       // 16-byte pieces in flight per thread
+constexpr int kPiece = kCopyThreads * kCopyVec * 16;              // bytes of a page that a CTA copies at a time
+
+// Workspace: counts, then lists.
+struct PlanHead {
+  int32_t n_pairs, n_used;
+};
+
+__device__ __forceinline__ bool page_ok(int p, int num_pages) { return (unsigned)p < (unsigned)num_pages; }
+
+// ---- contents ------------------------------------------------------------------------------------
+// Copies piece `piece` (counted over the arrays of a page) of page src to page dst.
+__device__ __forceinline__ void copy_piece(const PageArrays& pa, int64_t src, int64_t dst, int piece) {
+  int a = 0;
+#pragma unroll
+  for (; a < kPageArrays - 1; ++a) {
+    if (piece < pa.pieces[a]) break;
+    piece -= pa.pieces[a];
+  }
+  const char* s = pa.base[a] + src * pa.bytes[a];
+  char* d = pa.base[a] + dst * pa.bytes[a];
+  const int64_t at = (int64_t)piece * kPiece + threadIdx.x * 16;
+  uint4 v[kCopyVec];
+#pragma unroll
+  for (int i = 0; i < kCopyVec; ++i)
+    if (at + i * kCopyThreads * 16 < pa.bytes[a]) v[i] = ld_stream_v4(s + at + i * kCopyThreads * 16);
+#pragma unroll
+  for (int i = 0; i < kCopyVec; ++i)
+    if (at + i * kCopyThreads * 16 < pa.bytes[a]) *reinterpret_cast<uint4*>(d + at + i * kCopyThreads * 16) = v[i];
+}
+
+// n pairs given by the caller, or as many as head->n_pairs says.
+__global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_constant__ PageArrays pa, const int num_pages,
+                                                                  const int32_t* __restrict__ src,
+                                                                  const int32_t* __restrict__ dst, const int64_t n,
+                                                                  const PlanHead* __restrict__ head, int32_t* status) {
+  chain_wait();
+  const int64_t total = (head ? (int64_t)head->n_pairs : n) * pa.total_pieces;
+  for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
+    const int64_t i = u / pa.total_pieces;
+    const int s = src[i], d = dst[i];
+    if (!page_ok(s, num_pages) || !page_ok(d, num_pages)) {
+      if (threadIdx.x == 0) set_status(status, RTP_ERR_INVALID);
+      continue;
+    }
+    if (s != d) copy_piece(pa, s, d, (int)(u % pa.total_pieces));
+  }
+}
+
+// ---- fork, free: one CTA per sequence -------------------------------------------------------------
+__global__ void __launch_bounds__(kRowThreads) fork_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_lens,
+                                                           int32_t* __restrict__ refs, const int num_pages, const int batch,
+                                                           const int max_pages, const int32_t* __restrict__ src_seqs,
+                                                           const int32_t* __restrict__ dst_seqs, const int n, int32_t* status) {
+  chain_wait();
+  const int i = blockIdx.x, src = src_seqs[i], dst = dst_seqs[i];
+  bool bad = (unsigned)src >= (unsigned)batch || (unsigned)dst >= (unsigned)batch;
+  // named as a destination before, or a source that is somebody's destination: what it holds would depend on the order
+  for (int j = threadIdx.x; j < n; j += kRowThreads) bad = bad || (j < i && dst_seqs[j] == dst) || dst_seqs[j] == src;
+  if (__syncthreads_or(bad)) {
+    if (threadIdx.x == 0) set_status(status, RTP_ERR_INVALID);
+    return;
+  }
+  const int len = seq_lens[src];
+  const int np = len < 0 ? 0 : (int)(((int64_t)len + kPage - 1) >> kPageShift);
+  const int32_t* from = table + (int64_t)src * max_pages;
+  int32_t* to = table + (int64_t)dst * max_pages;
+  bad = len < 0 || np > max_pages || seq_lens[dst] != 0;
+  if (!bad)
+    for (int p = threadIdx.x; p < max_pages; p += kRowThreads) {
+      bad = bad || to[p] >= 0;
+      if (p < np) bad = bad || !page_ok(from[p], num_pages) || refs[from[p]] <= 0;
+    }
+  if (__syncthreads_or(bad)) {
+    if (threadIdx.x == 0) set_status(status, RTP_ERR_INVALID);
+    return;
+  }
+  for (int p = threadIdx.x; p < np; p += kRowThreads) {
+    const int e = from[p];
+    to[p] = e;
+    atomicAdd(refs + e, 1);
+  }
+  if (threadIdx.x == 0) seq_lens[dst] = len;
+}
+
+__global__ void __launch_bounds__(kRowThreads) free_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_lens,
+                                                           int32_t* __restrict__ refs, const int num_pages, const int batch,
+                                                           const int max_pages, const int32_t* __restrict__ seqs,
+                                                           int32_t* status) {
+  chain_wait();
+  const int seq = seqs[blockIdx.x];
+  if ((unsigned)seq >= (unsigned)batch) {
+    if (threadIdx.x == 0) set_status(status, RTP_ERR_INVALID);
+    return;
+  }
+  int32_t* row = table + (int64_t)seq * max_pages;
+  for (int p = threadIdx.x; p < max_pages; p += kRowThreads) {
+    if (row[p] < 0) continue;
+    const int e = atomicExch(row + p, -1);   // (a sequence named twice gives each page back once)
+    if (e < 0) continue;
+    if (!page_ok(e, num_pages)) {
+      set_status(status, RTP_ERR_INVALID);
+    } else if (atomicSub(refs + e, 1) <= 0) {   // nobody held it
+      atomicAdd(refs + e, 1);
+      set_status(status, RTP_ERR_INVALID);
+    }
+  }
+  if (threadIdx.x == 0) seq_lens[seq] = 0;
+}
+
+// ---- the scan over the reference counts ------------------------------------------------------------
+// The pool is cut into one contiguous segment per warp of the CTA, a multiple of 128 pages (four per lane).
+struct Segment {
+  int lo, hi;
+};
+__device__ __forceinline__ Segment warp_segment(int num_pages, int warp) {
+  const int64_t per = (((int64_t)num_pages + kPlanWarps - 1) / kPlanWarps + 127) / 128 * 128;
+  const int64_t lo = per * warp, hi = lo + per;
+  return {(int)(lo < num_pages ? lo : num_pages), (int)(hi < num_pages ? hi : num_pages)};
+}
+// Bit j: page at + 4 lane + j is in use; pages at or beyond hi are not.
+__device__ __forceinline__ uint32_t used_bits(const int32_t* refs, int at, int hi, int lane) {
+  const int p = at + 4 * lane;
+  uint32_t b = 0;
+  if (p + 3 < hi) {
+    const int4 v = *reinterpret_cast<const int4*>(refs + p);
+    b = (v.x != 0 ? 1u : 0u) | (v.y != 0 ? 2u : 0u) | (v.z != 0 ? 4u : 0u) | (v.w != 0 ? 8u : 0u);
+  } else {
+    for (int j = 0; j < 4; ++j)
+      if (p + j < hi && refs[p + j] != 0) b |= 1u << j;
+  }
+  return b;
+}
+__device__ __forceinline__ int count_used(const int32_t* refs, int lo, int hi, int lane) {
+  int n = 0;
+#pragma unroll 4
+  for (int at = lo; at < hi; at += 128) n += __popc(used_bits(refs, at, hi, lane));
+  return __reduce_add_sync(0xffffffffu, n);
+}
+__device__ __forceinline__ int lanes_before(int x, int lane) {   // exclusive sum over the warp
+  int s = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += y;
+  }
+  return s - x;
+}
+// Used pages before each warp's segment; returns those of the whole pool.  Called by the whole CTA.
+__device__ __forceinline__ int scan_segments(int mine, int* s_before, int lane, int warp) {
+  if (lane == 0) s_before[warp] = mine;
+  __syncthreads();
+  if (warp == 0) {
+    const int x = s_before[lane], b = lanes_before(x, lane);
+    __syncwarp();
+    s_before[lane] = b;
+    if (lane == 31) s_before[32] = b + x;
+  }
+  __syncthreads();
+  return s_before[32];
+}
+
+// ---- reserve -----------------------------------------------------------------------------------------
+struct ReserveShared {
+  int seq[kReserveMax];       // -1: the entry asks for nothing
+  int cow[kReserveMax];       // shared page that the sequence is going to write into, or -1
+  int first[kReserveMax];     // first table entry that has to be filled
+  int off[kReserveMax + 1];   // pages handed out before this entry's
+  int before[33];
+  int n_pairs;
+  unsigned long long total;   // (the sum in 32 bits may wrap)
+};
+
+__global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restrict__ table, const int32_t* __restrict__ seq_lens,
+                                                               int32_t* __restrict__ refs, const int num_pages, const int batch,
+                                                               const int max_pages, const int32_t* __restrict__ seqs,
+                                                               const int32_t* __restrict__ n_tokens, const int n,
+                                                               PlanHead* __restrict__ head, int32_t* __restrict__ pair_src,
+                                                               int32_t* __restrict__ pair_dst, int32_t* status) {
+  chain_wait();
+  extern __shared__ __align__(16) unsigned char smem_reserve[];
+  ReserveShared& s = *reinterpret_cast<ReserveShared*>(smem_reserve);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) {
+    s.n_pairs = 0;
+    s.total = 0;
+  }
+  bool invalid = false, full = false, shared_page = false;
+  for (int i = tid; i < n; i += kPlanThreads) {
+    const int seq = seqs[i];
+    const bool ok = (unsigned)seq < (unsigned)batch && n_tokens[i] >= 0 && seq_lens[seq] >= 0;
+    invalid = invalid || !ok;
+    s.seq[i] = ok ? seq : -1;
+  }
+  __syncthreads();
+  for (int i = tid; i < n; i += kPlanThreads) {   // a sequence named twice: the first one counts
+    const int seq = s.seq[i];
+    bool twice = false;
+    for (int j = 0; j < i && seq >= 0; ++j) twice = twice || s.seq[j] == seq;
+    s.first[i] = twice;
+  }
+  __syncthreads();
+  for (int i = tid; i < n; i += kPlanThreads)
+    if (s.first[i]) {
+      s.seq[i] = -1;
+      invalid = true;
+    }
+  __syncthreads();
+  // one warp per entry: the table entries from the sequence's length up to what it is going to need
+  for (int i = warp; i < n; i += kPlanWarps) {
+    const int seq = s.seq[i];
+    int need = 0, cow = -1, first = 0;
+    if (seq >= 0) {
+      const int64_t len = seq_lens[seq], end = len + n_tokens[i];
+      const int64_t want = (end + kPage - 1) >> kPageShift;
+      const int32_t* row = table + (int64_t)seq * max_pages;
+      if (want > max_pages) {
+        full = true;
+      } else {
+        bool bad = false;
+        int mapped = 0;
+        first = (int)((len + kPage - 1) >> kPageShift);
+        for (int p = first + lane; p < want; p += 32) {   // mapped entries come first, then unmapped ones
+          const bool m = row[p] >= 0;
+          mapped += m;
+          bad = bad || (m && p > first && row[p - 1] < 0);
+        }
+        mapped = __reduce_add_sync(0xffffffffu, mapped);
+        first += mapped;
+        need = (int)want - first;
+        if (need < 0) need = 0;
+        if (n_tokens[i] > 0 && (len & (kPage - 1))) {
+          const int last = row[len >> kPageShift];
+          if (!page_ok(last, num_pages)) bad = true;
+          else if (refs[last] > 1) cow = last;
+        }
+        if (__any_sync(0xffffffffu, bad)) {
+          invalid = true;
+          need = 0;
+          cow = -1;
+          if (lane == 0) s.seq[i] = -1;
+        }
+      }
+    }
+    if (lane == 0) {
+      s.first[i] = first;
+      s.cow[i] = cow;
+      s.off[i] = need;
+    }
+    shared_page = shared_page || cow >= 0;
+  }
+  if (__syncthreads_or(shared_page)) {
+    // A page with r holders is copied by the first r - 1 of them at most: the last one to write it has it alone.
+    int mine[(kReserveMax + kPlanThreads - 1) / kPlanThreads];
+#pragma unroll
+    for (int k = 0; k < (kReserveMax + kPlanThreads - 1) / kPlanThreads; ++k) {
+      const int i = tid + k * kPlanThreads;
+      mine[k] = 0;
+      if (i < n && s.cow[i] >= 0) {
+        int earlier = 0;
+        for (int j = 0; j < i; ++j) earlier += s.cow[j] == s.cow[i];
+        mine[k] = refs[s.cow[i]] - earlier > 1 ? 1 : -1;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < (kReserveMax + kPlanThreads - 1) / kPlanThreads; ++k) {
+      const int i = tid + k * kPlanThreads;
+      if (i < n && mine[k] > 0) s.off[i] += 1;
+      if (i < n && mine[k] < 0) s.cow[i] = -1;
+    }
+  }
+  __syncthreads();
+  // exclusive sums of the needs: thread t takes entries t * per ..
+  const int per = (n + kPlanThreads - 1) / kPlanThreads;
+  int sum = 0;
+  unsigned long long wide = 0;
+  for (int k = 0; k < per; ++k) {
+    const int i = tid * per + k;
+    if (i < n) {
+      const int x = s.off[i];
+      s.off[i] = sum;
+      sum += x;
+      wide += x;
+    }
+  }
+  if (wide) atomicAdd(&s.total, wide);
+  const int in_warp = lanes_before(sum, lane);
+  const int total = scan_segments(__shfl_sync(0xffffffffu, in_warp + sum, 31), s.before, lane, warp);
+  for (int k = 0; k < per; ++k) {
+    const int i = tid * per + k;
+    if (i < n) s.off[i] += s.before[warp] + in_warp;
+  }
+  if (tid == 0) s.off[n] = total;
+  if (invalid) set_status(status, RTP_ERR_INVALID);
+  if (__syncthreads_or(full) || s.total > (unsigned)num_pages) {   // a row or the pool is too short: nothing is handed out
+    if (tid == 0) {
+      set_status(status, RTP_ERR_CAPACITY);
+      head->n_pairs = 0;
+    }
+    return;
+  }
+  if (total > 0) {
+    const Segment seg = warp_segment(num_pages, warp);
+    const int used = count_used(refs, seg.lo, seg.hi, lane);
+    const int all_used = scan_segments(used, s.before, lane, warp);
+    if (num_pages - all_used < total) {   // not enough free pages: nothing is handed out
+      if (tid == 0) {
+        set_status(status, RTP_ERR_CAPACITY);
+        head->n_pairs = 0;
+      }
+      return;
+    }
+    int rank = seg.lo - s.before[warp];   // free pages before this segment
+    for (int at = seg.lo; at < seg.hi && rank < total; at += 128) {
+      const int valid = min(4, max(0, seg.hi - (at + 4 * lane)));
+      const uint32_t free_bits = ~used_bits(refs, at, seg.hi, lane) & ((1u << valid) - 1u);
+      const int cnt = __popc(free_bits);
+      int u = rank + lanes_before(cnt, lane);
+      for (int j = 0; j < 4; ++j) {
+        if (!((free_bits >> j) & 1u)) continue;
+        if (u < total) {
+          int a = 0, b = n;   // the last entry with off <= u
+          while (a + 1 < b) {
+            const int mid = (a + b) >> 1;
+            if (s.off[mid] <= u) a = mid; else b = mid;
+          }
+          const int page = at + 4 * lane + j, seq = s.seq[a], cow = s.cow[a];
+          int k = u - s.off[a];
+          int32_t* row = table + (int64_t)seq * max_pages;
+          refs[page] = 1;
+          if (cow >= 0 && k == 0) {
+            atomicSub(refs + cow, 1);
+            row[seq_lens[seq] >> kPageShift] = page;
+            const int slot = atomicAdd(&s.n_pairs, 1);
+            pair_src[slot] = cow;
+            pair_dst[slot] = page;
+          } else {
+            row[s.first[a] + k - (cow >= 0)] = page;
+          }
+        }
+        ++u;
+      }
+      rank += __reduce_add_sync(0xffffffffu, cnt);
+    }
+  }
+  __syncthreads();
+  if (tid == 0) head->n_pairs = s.n_pairs;
+}
+
+// ---- compact -----------------------------------------------------------------------------------------
+// With n_used pages in use, the k-th used page at or above n_used goes to the k-th free page below it.
+__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const int32_t* __restrict__ refs, const int num_pages,
+                                                                    PlanHead* __restrict__ head, int32_t* __restrict__ src,
+                                                                    int32_t* __restrict__ dst, int32_t* __restrict__ move,
+                                                                    int32_t* __restrict__ n_used_out) {
+  chain_wait();
+  __shared__ int s_before[33], s_below;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const Segment seg = warp_segment(num_pages, warp);
+  if (threadIdx.x == 0) s_below = 0;
+  const int n_used = scan_segments(count_used(refs, seg.lo, seg.hi, lane), s_before, lane, warp);
+  if (seg.lo < n_used) {
+    const int below = count_used(refs, seg.lo, min(seg.hi, n_used), lane);
+    if (lane == 0) atomicAdd(&s_below, below);
+  }
+  __syncthreads();
+  const int below = s_below;   // used pages that stay
+  int before = s_before[warp];
+  for (int at = seg.lo; at < seg.hi; at += 128) {
+    const uint32_t used = used_bits(refs, at, seg.hi, lane);
+    const int cnt = __popc(used);
+    int u = before + lanes_before(cnt, lane);   // used pages before page p
+    for (int j = 0; j < 4; ++j) {
+      const int p = at + 4 * lane + j;
+      if (p >= seg.hi) break;
+      const bool is_used = (used >> j) & 1u;
+      if (p < n_used) {
+        if (!is_used) dst[p - u] = p;
+      } else {
+        move[p] = is_used ? u - below : -1;
+        if (is_used) src[u - below] = p;
+      }
+      u += is_used;
+    }
+    before += __reduce_add_sync(0xffffffffu, cnt);
+  }
+  if (threadIdx.x == 0) {
+    head->n_pairs = n_used - below;
+    head->n_used = n_used;
+    *n_used_out = n_used;
+  }
+}
+
+__global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const __grid_constant__ PageArrays pa, const int num_pages,
+                                                                    int32_t* __restrict__ table, const int64_t n_entries,
+                                                                    int32_t* __restrict__ refs, const PlanHead* __restrict__ head,
+                                                                    const int32_t* __restrict__ src,
+                                                                    const int32_t* __restrict__ dst,
+                                                                    const int32_t* __restrict__ move, int32_t* status) {
+  chain_wait();
+  const int n_pairs = head->n_pairs, n_used = head->n_used;
+  const int64_t t0 = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x, step = (int64_t)gridDim.x * kCopyThreads;
+  for (int64_t i = t0; i < n_entries; i += step) {
+    const int e = table[i];
+    if (e < n_used) continue;
+    const int k = e < num_pages ? move[e] : -1;
+    if (k >= 0) table[i] = dst[k];
+    else set_status(status, RTP_ERR_INVALID);   // (an entry whose page nobody holds, or no page at all)
+  }
+  for (int64_t i = t0; i < n_pairs; i += step) {
+    refs[dst[i]] = refs[src[i]];
+    refs[src[i]] = 0;
+  }
+  const int64_t total = (int64_t)n_pairs * pa.total_pieces;
+  for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
+    const int64_t i = u / pa.total_pieces;
+    copy_piece(pa, src[i], dst[i], (int)(u % pa.total_pieces));
+  }
+}
+
+unsigned copy_grid(const PageArrays& pa, int64_t pairs) {
+  return (unsigned)std::max<int64_t>(1, std::min<int64_t>(pairs * pa.total_pieces, (int64_t)current_sm_count(148) * 8));
+}
+
+}  // namespace
+
+void finish_page_arrays(PageArrays* pa) {
+  pa->total_pieces = 0;
+  for (int a = 0; a < kPageArrays; ++a) {
+    pa->pieces[a] = (int)((pa->bytes[a] + kPiece - 1) / kPiece);
+    pa->total_pieces += pa->pieces[a];
+  }
+}
+
+size_t pages_workspace_bytes(int64_t num_pages, int64_t n_seqs) {
+  return 256 + sizeof(int32_t) * (size_t)(3 * ((num_pages + 63) & ~(int64_t)63) + 2 * ((n_seqs + 63) & ~(int64_t)63));
+}
+
+cudaError_t launch_copy_pages(const PageArrays& pa, int num_pages, const int32_t* src, const int32_t* dst, int64_t n,
+                              int32_t* status, cudaStream_t st) {
+  if (n == 0 || pa.total_pieces == 0) return cudaSuccess;
+  (void)launch_chained(copy_pages_kernel, dim3(copy_grid(pa, n)), dim3(kCopyThreads), 0, st, pa, num_pages, src, dst, n,
+                       (const PlanHead*)nullptr, status);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_fork(int32_t* table, int32_t* seq_lens, int32_t* refs, int num_pages, int batch, int max_pages,
+                        const int32_t* src, const int32_t* dst, int n, int32_t* status, cudaStream_t st) {
+  if (n == 0) return cudaSuccess;
+  (void)launch_chained(fork_kernel, dim3(n), dim3(kRowThreads), 0, st, table, seq_lens, refs, num_pages, batch, max_pages, src,
+                       dst, n, status);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_free(int32_t* table, int32_t* seq_lens, int32_t* refs, int num_pages, int batch, int max_pages,
+                        const int32_t* seqs, int n, int32_t* status, cudaStream_t st) {
+  if (n == 0) return cudaSuccess;
+  (void)launch_chained(free_kernel, dim3(n), dim3(kRowThreads), 0, st, table, seq_lens, refs, num_pages, batch, max_pages, seqs,
+                       status);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_reserve(const PageArrays& pa, int32_t* table, const int32_t* seq_lens, int32_t* refs, int num_pages, int batch,
+                           int max_pages, const int32_t* seqs, const int32_t* n_tokens, int n, void* ws, int32_t* status,
+                           cudaStream_t st) {
+  if (n == 0) return cudaSuccess;
+  static PerDeviceOnce once;
+  cudaError_t e = set_dyn_smem_once(reserve_kernel, (int)sizeof(ReserveShared), once);
+  if (e != cudaSuccess) return e;
+  PlanHead* head = reinterpret_cast<PlanHead*>(ws);
+  int32_t* src = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(ws) + 256);
+  int32_t* dst = src + ((n + 63) & ~63);
+  (void)launch_chained(reserve_kernel, dim3(1), dim3(kPlanThreads), sizeof(ReserveShared), st, table, seq_lens, refs, num_pages,
+                       batch, max_pages, seqs, n_tokens, n, head, src, dst, status);
+  e = cudaGetLastError();
+  if (e != cudaSuccess || pa.total_pieces == 0) return e;
+  (void)launch_chained(copy_pages_kernel, dim3(copy_grid(pa, n)), dim3(kCopyThreads), 0, st, pa, num_pages, src, dst, (int64_t)0,
+                       (const PlanHead*)head, status);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_compact(const PageArrays& pa, int32_t* table, int64_t n_entries, int32_t* refs, int num_pages,
+                           int32_t* n_used, void* ws, int32_t* status, cudaStream_t st) {
+  PlanHead* head = reinterpret_cast<PlanHead*>(ws);
+  const int64_t pad = ((int64_t)num_pages + 63) & ~(int64_t)63;
+  int32_t* src = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(ws) + 256);
+  int32_t *dst = src + pad, *move = dst + pad;
+  (void)launch_chained(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, refs, num_pages, head, src, dst, move, n_used);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  (void)launch_chained(compact_move_kernel, dim3((unsigned)current_sm_count(148) * 8), dim3(kCopyThreads), 0, st, pa, num_pages,
+                       table, n_entries, refs, head, src, dst, move, status);
+  return cudaGetLastError();
+}
+
+}  // namespace rtp

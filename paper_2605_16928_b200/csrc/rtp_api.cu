@@ -183,6 +183,18 @@ const char* check_rows(const int32_t* row_seq, const int32_t* row_pos, int32_t s
   return nullptr;
 }
 
+// The arrays that a page of the main pool consists of.  Returns NULL on success, else a message.
+const char* page_arrays(const rtp_cache* c, const CacheView& cv, PageArrays* pa) {
+  if ((c->k_pages == nullptr) != (c->v_pages == nullptr)) return "k_pages and v_pages must both be given or both be NULL";
+  if (c->k_pages && cv.kv_fp4 && !c->kv_scales) return "kv_scales is NULL";
+  const int64_t kv = c->k_pages ? (int64_t)cv.n_kv * kPage * (cv.kv_fp4 ? kHeadDim / 2 : kHeadDim * 2) : 0;
+  const int64_t sc = c->k_pages && cv.kv_fp4 ? (int64_t)cv.n_kv * kPage * (kHeadDim / 8) : 0;
+  const int64_t ik = c->ikey_pages ? (int64_t)cv.n_ih * kPage * kIndexDim * (cv.ikey_fp8 ? 1 : 2) : 0;
+  *pa = PageArrays{{(char*)c->k_pages, (char*)c->v_pages, (char*)c->kv_scales, (char*)c->ikey_pages}, {kv, kv, sc, ik}, {}, 0};
+  finish_page_arrays(pa);
+  return nullptr;
+}
+
 struct WsCarver {
   char* base;
   size_t off = 0;
@@ -337,6 +349,81 @@ rtp_status rtp_kv_expand(rtp_ctx* ctx, const rtp_params* params, const rtp_cache
   if (!aligned16(k_out) || !aligned16(v_out)) return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
   cudaError_t e = launch_kv4_expand(cv, src_pages, dst_pages, n, k_out, v_out, n_out_pages, status, st);
   return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_kv_expand");
+}
+
+size_t rtp_cache_workspace_bytes(const rtp_cache* cache, int64_t n_seqs) {
+  if (!cache || cache->num_pages <= 0 || n_seqs < 0 || n_seqs > kReserveMax) return 0;
+  return pages_workspace_bytes(cache->num_pages, n_seqs);
+}
+
+rtp_status rtp_cache_copy_pages(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, const int32_t* src_pages,
+                                const int32_t* dst_pages, int64_t n, int32_t* status, void* stream) {
+  RTP_COMMON_PROLOGUE(false, false)
+  (void)hm;
+  PageArrays pa;
+  if (const char* m = page_arrays(cache, cv, &pa)) return fail(ctx, RTP_ERR_INVALID, m);
+  if (n < 0) return fail(ctx, RTP_ERR_INVALID, "page count is negative");
+  if (n == 0) return RTP_OK;
+  if (!src_pages || !dst_pages) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
+  cudaError_t e = launch_copy_pages(pa, cv.num_pages, src_pages, dst_pages, n, status, st);
+  return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_cache_copy_pages");
+}
+
+// What the calls on reference counts share: the cache must not have a local pool.
+#define RTP_PAGES_PROLOGUE(limit)                                                                                          \
+  RTP_COMMON_PROLOGUE(false, false)                                                                                        \
+  (void)hm;                                                                                                                \
+  PageArrays pa;                                                                                                           \
+  if (const char* m_ = page_arrays(cache, cv, &pa)) return fail(ctx, RTP_ERR_INVALID, m_);                                 \
+  if (cache->k_local_pages) return fail(ctx, RTP_ERR_UNSUPPORTED, "a cache with a local pool: its pages are the caller's"); \
+  if (!page_refs) return fail(ctx, RTP_ERR_INVALID, "page_refs is NULL");                                                  \
+  if (!aligned16(page_refs)) return fail(ctx, RTP_ERR_INVALID, "page_refs must be 16-byte aligned");                       \
+  if (n < 0) return fail(ctx, RTP_ERR_INVALID, "sequence count is negative");                                              \
+  if (n > (limit)) return fail(ctx, RTP_ERR_UNSUPPORTED, "too many sequences in one call");                                \
+  int32_t* table = const_cast<int32_t*>(cv.block_table);                                                                   \
+  int32_t* lens = const_cast<int32_t*>(cv.seq_lens);                                                                       \
+  (void)lens;
+
+rtp_status rtp_cache_fork(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
+                          const int32_t* src_seqs, const int32_t* dst_seqs, int64_t n, int32_t* status, void* stream) {
+  RTP_PAGES_PROLOGUE(65535)
+  if (n == 0) return RTP_OK;
+  if (!src_seqs || !dst_seqs) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
+  cudaError_t e = launch_fork(table, lens, page_refs, cv.num_pages, cv.batch, cv.max_pages, src_seqs, dst_seqs, (int)n, status, st);
+  return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_cache_fork");
+}
+
+rtp_status rtp_cache_reserve(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
+                             const int32_t* seqs, const int32_t* n_tokens, int64_t n, void* workspace,
+                             size_t workspace_bytes, int32_t* status, void* stream) {
+  RTP_PAGES_PROLOGUE(kReserveMax)
+  if (n == 0) return RTP_OK;
+  if (!seqs || !n_tokens || !workspace) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
+  if (!aligned16(workspace)) return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
+  if (workspace_bytes < pages_workspace_bytes(cv.num_pages, n)) return fail(ctx, RTP_ERR_CAPACITY, "workspace too small");
+  cudaError_t e = launch_reserve(pa, table, lens, page_refs, cv.num_pages, cv.batch, cv.max_pages, seqs, n_tokens, (int)n,
+                                 workspace, status, st);
+  return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_cache_reserve");
+}
+
+rtp_status rtp_cache_free(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
+                          const int32_t* seqs, int64_t n, int32_t* status, void* stream) {
+  RTP_PAGES_PROLOGUE(65535)
+  if (n == 0) return RTP_OK;
+  if (!seqs) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
+  cudaError_t e = launch_free(table, lens, page_refs, cv.num_pages, cv.batch, cv.max_pages, seqs, (int)n, status, st);
+  return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_cache_free");
+}
+
+rtp_status rtp_cache_compact(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
+                             int32_t* n_used, void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
+  const int64_t n = 0;
+  RTP_PAGES_PROLOGUE(0)
+  if (!n_used || !workspace) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
+  if (!aligned16(workspace)) return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
+  if (workspace_bytes < pages_workspace_bytes(cv.num_pages, 0)) return fail(ctx, RTP_ERR_CAPACITY, "workspace too small");
+  cudaError_t e = launch_compact(pa, table, (int64_t)cv.batch * cv.max_pages, page_refs, cv.num_pages, n_used, workspace, status, st);
+  return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_cache_compact");
 }
 
 rtp_status rtp_index_queries(rtp_ctx* ctx, const rtp_params* params, const void* q_pre, const void* w_q, int64_t R,

@@ -181,6 +181,29 @@ cudaError_t launch_kv4_append(const CacheView& cv, int n_src_heads, const __nv_b
                               cudaStream_t st);
 cudaError_t launch_kv4_expand(const CacheView& cv, const int32_t* src_pages, const int32_t* dst_pages, int64_t n, void* k_out,
                               void* v_out, int32_t n_out_pages, int32_t* status, cudaStream_t st);
+
+// Pages of the main pool: the arrays that a page consists of (keys, values, 4-bit scales, index keys; absent ones have no bytes).
+constexpr int kPageArrays = 4;
+constexpr int kReserveMax = 4096;   // sequences of one reserve call
+struct PageArrays {
+  char* base[kPageArrays];
+  int64_t bytes[kPageArrays];   // of one page
+  int32_t pieces[kPageArrays], total_pieces;
+};
+void finish_page_arrays(PageArrays* pa);
+size_t pages_workspace_bytes(int64_t num_pages, int64_t n_seqs);
+cudaError_t launch_copy_pages(const PageArrays& pa, int num_pages, const int32_t* src, const int32_t* dst, int64_t n,
+                              int32_t* status, cudaStream_t st);
+cudaError_t launch_fork(int32_t* table, int32_t* seq_lens, int32_t* refs, int num_pages, int batch, int max_pages,
+                        const int32_t* src, const int32_t* dst, int n, int32_t* status, cudaStream_t st);
+cudaError_t launch_free(int32_t* table, int32_t* seq_lens, int32_t* refs, int num_pages, int batch, int max_pages,
+                        const int32_t* seqs, int n, int32_t* status, cudaStream_t st);
+cudaError_t launch_reserve(const PageArrays& pa, int32_t* table, const int32_t* seq_lens, int32_t* refs, int num_pages, int batch,
+                           int max_pages, const int32_t* seqs, const int32_t* n_tokens, int n, void* ws, int32_t* status,
+                           cudaStream_t st);
+cudaError_t launch_compact(const PageArrays& pa, int32_t* table, int64_t n_entries, int32_t* refs, int num_pages,
+                           int32_t* n_used, void* ws, int32_t* status, cudaStream_t st);
+
 cudaError_t launch_index_queries(const Dims& d, const HeadMaps& hm, const __nv_bfloat16* q_pre,
                                  const __nv_bfloat16* w_q, int64_t R, __nv_bfloat16* qt, cudaStream_t st);
 

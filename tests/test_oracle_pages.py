@@ -1,0 +1,48 @@
+"""Pins of the page operations' oracle: small written-out cases, and invariants over random sequences of calls."""
+import numpy as np
+
+from oracle.pages_oracle import Pool
+
+
+def test_written_out_case():
+    p = Pool(8, 4, 4)
+    p.reserve([0, 1], [70, 64])
+    assert p.table[0].tolist() == [0, 1, -1, -1] and p.table[1].tolist() == [2, -1, -1, -1]
+    p.lens[:2] = 70, 64
+    p.fork([0, 0, 1], [2, 3, 2])              # the third names 2 again
+    assert p.invalid and p.refs.tolist() == [3, 3, 1, 0, 0, 0, 0, 0]
+    p.reserve([2, 0, 3], [1, 1, 1])            # page 1 has three holders, all of which write: the first two get copies
+    assert [p.table[s, 1] for s in (2, 0, 3)] == [3, 4, 1] and p.contents[3] == 1 and p.refs[1] == 1
+    p.free([0, 1])
+    assert p.refs.tolist() == [2, 1, 0, 1, 0, 0, 0, 0]
+    assert p.compact() == 3 and p.refs.tolist() == [2, 1, 1, 0, 0, 0, 0, 0] and p.table[2, 1] == 2
+    p.check()
+    before = p.table.copy()
+    p.reserve([2, 3], [64 * 2, 64 * 3])        # the row of 3 is too short: nothing happens for 2 either
+    assert p.capacity and np.array_equal(before, p.table)
+
+
+def test_invariants_under_random_calls():
+    rng = np.random.default_rng(0)
+    for _ in range(50):
+        p = Pool(40, 6, 9)
+        for _ in range(60):
+            kind = rng.integers(4)
+            seqs = rng.permutation(6)[:rng.integers(1, 4)].tolist()
+            if kind == 0:
+                p.fork(seqs, rng.permutation(6)[:len(seqs)].tolist())
+            elif kind == 1:
+                n = rng.integers(0, 150, len(seqs)).tolist()
+                p.capacity = False
+                p.reserve(seqs, n)
+                if not p.capacity:
+                    for s, k in zip(seqs, n):
+                        p.lens[s] += k
+                        if k:                  # what is written next is nobody else's
+                            assert p.refs[p.table[s, (p.lens[s] - k) // 64]] == 1
+            elif kind == 2:
+                p.free(seqs[:1])
+            else:
+                n = p.compact()
+                assert (p.refs[:n] > 0).all() and not p.refs[n:].any()
+            p.check()
