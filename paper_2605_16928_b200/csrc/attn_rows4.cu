@@ -2,7 +2,7 @@
 // as codes and scales, 144 bytes per (token, KV head) where the bf16 cache has 512.
 //
 // Layout of the work: a (row, KV head or listed query head) is split over CTAs, a CTA over four warps, a warp takes tiles
-// of 16 tokens.  Tiles are copied to a ring in shared memory by 16-byte cp.async, three tiles ahead.
+// of 32 tokens.  Tiles are copied to a ring in shared memory by 16-byte cp.async, two tiles ahead.
 //
 // The contractions run with the TOKENS as the 16 rows of the MMA (m16n8k16, fp16 -> fp32) and the up to eight query heads
 // of the group as its columns:
@@ -24,19 +24,23 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
-constexpr int kTileTok = 16;
+constexpr int kTileTok = 32;                                 // two MMA tiles of 16 tokens
 constexpr int kTilesPerPage = kPage / kTileTok;
-constexpr int kStages = 4;                                   // tiles of a warp in shared memory
+constexpr int kStages = 3;                                   // tiles of a warp in shared memory
 constexpr int kTileV = kTileTok * kKv4TokBytes;              // K codes, V codes (from here), scales (from kTileS)
 constexpr int kTileS = 2 * kTileV;
-constexpr int kTileBytes = kTileS + kTileTok * kKv4ScaleBytes;   // 2304
-constexpr int kSmemBytes = kWarps * kStages * kTileBytes;    // 36 KB
+constexpr int kTileBytes = kTileS + kTileTok * kKv4ScaleBytes;   // 4608
+constexpr int kSmemBytes = kWarps * kStages * kTileBytes;    // 54 KB: four CTAs per SM
+constexpr uint32_t kFull = 0xffffffffu;
 constexpr float kLag = 8.f;    // the reference of the softmax may trail the maximum by this much (log2)
 constexpr float kLift = 7.f;   // probabilities are multiplied by 2^kLift: at most 2^15 < 65504
 
 __device__ __forceinline__ void cp16z(uint32_t dst, const void* src, bool valid) {
   const int sz = valid ? 16 : 0;
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(sz) : "memory");
+}
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ uint4 lds_v4(uint32_t a) {
   uint4 v;
@@ -114,8 +118,7 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
     if (n_keys < 0) n_keys = 0;
   }
 
-  // The set as tiles of 16: entries of the list, or 16 tokens of one page that start at a multiple of 16 (of which those
-  // outside the set are masked).
+  // The set as tiles of 32: entries of the list, or half a page (of which the tokens outside the set are masked).
   int n_ent = 0, ns = 0, wlo = 0, sink_tiles = 0, n_total;
   const int32_t* ids = nullptr;
   if (SET == kSetList || SET == kSetPages || SET == kSetUnion) {
@@ -170,7 +173,10 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
   float o[8][4];   // tile i: channels 16 g + 2 i (elements 0, 1: heads 2 c, 2 c + 1) and 16 g + 2 i + 1 (2, 3)
 #pragma unroll
   for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-  float m_ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  // Reference of the softmax, less the lift, for heads 2 c and 2 c + 1; none before a head's first token.  While a column of
+  // the warp has none, every tile goes through the branch that sets it (limit = -inf).
+  float base[2] = {0.f, 0.f}, l[2] = {0.f, 0.f}, limit = 2 * c < G ? -INFINITY : kLift + kLag;
+  bool empty[2] = {2 * c < G, 2 * c + 1 < G};   // (columns beyond the group count as set)
 
   const int64_t bt_base = (int64_t)seq * cv.max_pages;
   const int kslot = cv.kv_slot[kvh];
@@ -180,14 +186,11 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
   const int tok_k = (g >> 1) + 4 * (g & 1);   // token of MMA row g (row g + 8: tok_k + 8)
 
   // Where a tile lives is found in steps, each a tile after the one that requested it: entry -> token -> page -> row.
-  // List sets: lane t (and t + 16) looks after token t of the tile.  Other sets: all lanes look after the tile's page.
+  // List sets: lane t looks after token t of the tile.  Other sets: all lanes look after the tile's page.
   auto raw_entry = [&](int i) -> int {
     if (i >= n_mine) return -1;
     const int tile = first + warp + i * kWarps;
-    if (SET == kSetList) {
-      const int t = tile * kTileTok + (lane & 15);
-      return t < n_ent ? __ldg(ids + t) : -1;
-    }
+    if (SET == kSetList) return tile * kTileTok + lane < n_ent ? __ldg(ids + tile * kTileTok + lane) : -1;
     if (SET == kSetPages || SET == kSetUnion) return __ldg(ids + tile / kTilesPerPage);
     return 0;
   };
@@ -197,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
     const int tile = first + warp + i * kWarps;
     if (SET == kSetList) {
       if (entry >= 0 && entry < n_keys) return entry;
-      if (entry != -1 || tile * kTileTok + (lane & 15) < n_ent) set_status(status, RTP_ERR_INVALID);
+      if (tile * kTileTok + lane < n_ent) set_status(status, RTP_ERR_INVALID);
       return -1;
     }
     if (SET == kSetPages || SET == kSetUnion) {
@@ -214,163 +217,208 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
   auto raw_phys = [&](int tok) -> int { return tok >= 0 ? __ldg(cv.block_table + bt_base + page_entry(cv, tok >> kPageShift)) : 0; };
   // tokens of the tile that belong to the set, one bit each
   auto valid_mask = [&](int i, int tok) -> uint32_t {
-    if (SET == kSetList) return __ballot_sync(0xffffffffu, tok >= 0) & 0xffffu;
+    if (SET == kSetList) return __ballot_sync(kFull, tok >= 0);
     if (tok < 0) return 0u;
     int lo = 0, hi = n_keys;
     if (SET == kSetLocal) {
       if (first + warp + i * kWarps < sink_tiles) hi = ns; else lo = wlo;
     }
-    const int a = min(max(lo - tok, 0), kTileTok), b = min(max(hi - tok, 0), kTileTok);
-    return ((1u << b) - 1u) & ~((1u << a) - 1u);
+    const int a = lo - tok, b = tok + kTileTok - hi;   // tokens missing at the front and at the end
+    uint32_t m = kFull;
+    if (a > 0) m = a < kTileTok ? m << a : 0u;
+    if (b > 0) m = b < kTileTok ? m & (kFull >> b) : 0u;
+    return m;
   };
-  // Copies a tile to its stage.  Lane (t, chunk) = (lane / 4, lane % 4) takes chunk `chunk` of tokens t and t + 8; lanes
-  // 0 .. 15 take the scales.  K rows lie in the order of the MMA rows, the chunks of a V row are exchanged in pairs by bit 1
-  // of the token number: either way the reads below touch every bank once.  Tokens outside the set are filled with zeros.
-  // (A row number fits 32 bits: 2^32 rows of 144 bytes are more than the device's memory.)
-  auto issue = [&](int stage, int tok, int phys, uint32_t mask) {
+  // Copies a tile to its stage.  Lane (t, chunk) = (lane / 4, lane % 4) takes chunk `chunk` of tokens t, t + 8, ..; lane t the
+  // scales of token t.  The K rows of 16 tokens lie in the order of the MMA rows, the chunks of a V row are exchanged in pairs
+  // by bit 1 of the token number: either way the reads below touch every bank once.  Tokens outside the set are filled with
+  // zeros.  (A row number fits 32 bits: 2^32 rows of 144 bytes are more than the device's memory.)
+  const uint32_t dk = ring + (2 * (g & 3) + (g >> 2)) * kKv4TokBytes + c * 16;
+  const uint32_t dv = ring + kTileV + g * kKv4TokBytes + ((c ^ (g & 2)) << 4);
+  const uint32_t ds = ring + kTileS + lane * kKv4ScaleBytes;
+  auto issue = [&](uint32_t at, int tok, int phys, uint32_t mask) {
     if ((unsigned)phys >= (unsigned)cv.num_pages) {
       set_status(status, RTP_ERR_INVALID);
       phys = 0;
     }
-    const uint32_t dst = ring + stage * kTileBytes;
     const uint32_t row = ((uint32_t)phys * cv.n_kv + kslot) * kPage + (tok & (kPage - 1));
-    const int t = lane >> 2, ch = lane & 3;
-    const uint32_t dk = dst + (2 * (t & 3) + (t >> 2)) * kKv4TokBytes + ch * 16;
-    const uint32_t dv = dst + kTileV + t * kKv4TokBytes + ((ch ^ (t & 2)) << 4);
+    if (SET == kSetList) {
+      const uint32_t mine = mask >> lane & 1u ? row : 0u;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const bool ok = (mask >> (t + 8 * h)) & 1u;
-      const uint32_t rt = SET == kSetList ? __shfl_sync(0xffffffffu, row, t + 8 * h) : row + t + 8 * h;
-      const int64_t off = ok ? (int64_t)rt * kKv4TokBytes + ch * 16 : 0;
-      cp16z(dk + h * 8 * kKv4TokBytes, kp + off, ok);
-      cp16z(dv + h * 8 * kKv4TokBytes, vp + off, ok);
+      for (int j = 0; j < 4; ++j) {
+        const bool ok = (mask >> (g + 8 * j)) & 1u;
+        const int64_t off = (int64_t)__shfl_sync(kFull, mine, g + 8 * j) * kKv4TokBytes + c * 16;
+        cp16z(dk + at + j * 8 * kKv4TokBytes, kp + off, ok);
+        cp16z(dv + at + j * 8 * kKv4TokBytes, vp + off, ok);
+      }
+      cp16z(ds + at, cv.kv_scales + (int64_t)mine * kKv4ScaleBytes, mask >> lane & 1u);
+      return;
     }
-    if (lane < kTileTok) {
+    const int64_t off = (int64_t)row * kKv4TokBytes + lane * 16, off_s = (int64_t)(row + lane) * kKv4ScaleBytes;
+    if (mask == kFull) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        cp16(dk + at + j * 8 * kKv4TokBytes, kp + off + j * 8 * kKv4TokBytes);
+        cp16(dv + at + j * 8 * kKv4TokBytes, vp + off + j * 8 * kKv4TokBytes);
+      }
+      cp16(ds + at, cv.kv_scales + off_s);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool ok = (mask >> (g + 8 * j)) & 1u;
+        const int64_t o_j = ok ? off + j * 8 * kKv4TokBytes : 0;
+        cp16z(dk + at + j * 8 * kKv4TokBytes, kp + o_j, ok);
+        cp16z(dv + at + j * 8 * kKv4TokBytes, vp + o_j, ok);
+      }
       const bool ok = (mask >> lane) & 1u;
-      const uint32_t rt = SET == kSetList ? row : row + lane;
-      cp16z(dst + kTileS + lane * kKv4ScaleBytes, cv.kv_scales + (ok ? (int64_t)rt * kKv4ScaleBytes : 0), ok);
+      cp16z(ds + at, cv.kv_scales + (ok ? off_s : 0), ok);
     }
   };
 
-  uint32_t mask_st[kStages], flag_st[kStages];   // of the tiles in the ring
+  uint32_t mask_st[kStages - 1], flag_st[kStages - 1];   // of the tiles in the ring
 #pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) {
-    const int e = raw_entry(s), tok = token_of(s, e);
-    mask_st[s] = valid_mask(s, tok);
-    flag_st[s] = (uint32_t)e >> 24;
-    issue(s, tok, raw_phys(tok), mask_st[s]);
+  for (int x = 0; x < kStages - 1; ++x) {
+    const int e = raw_entry(x), tok = token_of(x, e);
+    mask_st[x] = valid_mask(x, tok);
+    flag_st[x] = (uint32_t)e >> 24;
+    issue(x * kTileBytes, tok, raw_phys(tok), mask_st[x]);
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
-  mask_st[kStages - 1] = flag_st[kStages - 1] = 0u;
   int ent_a = raw_entry(kStages - 1);                       // the next tile to be copied: its entry, token and page
   int tok_a = token_of(kStages - 1, ent_a), phys_a = raw_phys(tok_a);
   int ent_b = raw_entry(kStages);
+  uint32_t rd = 0, wr = (kStages - 1) * kTileBytes;         // stage that is read, stage that is filled
 
 #pragma unroll 1
-  for (int i0 = 0; i0 < n_mine; i0 += kStages) {
+  for (int i = 0; i < n_mine; ++i) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+    __syncwarp();
+    const uint32_t vm = mask_st[0], flags = flag_st[0];
+    {   // tile i + 2 goes where tile i - 1 was
 #pragma unroll
-    for (int sgi = 0; sgi < kStages; ++sgi) {
-      const int i = i0 + sgi;
-      if (i < n_mine) {   // uniform in the warp
-        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-        __syncwarp();
-        {   // tile i + 3 goes where tile i - 1 was
-          const int next = (sgi + kStages - 1) % kStages;
-          mask_st[next] = valid_mask(i + kStages - 1, tok_a);
-          flag_st[next] = (uint32_t)ent_a >> 24;
-          issue(next, tok_a, phys_a, mask_st[next]);
-          asm volatile("cp.async.commit_group;" ::: "memory");
-          ent_a = ent_b;
-          tok_a = token_of(i + kStages, ent_a);
-          phys_a = raw_phys(tok_a);
-          ent_b = raw_entry(i + kStages + 1);
+      for (int x = 0; x + 1 < kStages - 1; ++x) {
+        mask_st[x] = mask_st[x + 1];
+        flag_st[x] = flag_st[x + 1];
+      }
+      const uint32_t m_next = valid_mask(i + kStages - 1, tok_a);
+      mask_st[kStages - 2] = m_next;
+      flag_st[kStages - 2] = (uint32_t)ent_a >> 24;
+      if (i + kStages - 1 < n_mine) issue(wr, tok_a, phys_a, m_next);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      ent_a = ent_b;
+      tok_a = token_of(i + kStages, ent_a);
+      phys_a = raw_phys(tok_a);
+      ent_b = raw_entry(i + kStages + 1);
+      wr = rd;
+    }
+    const uint32_t tile = ring + rd;
+    rd = rd == (kStages - 1) * kTileBytes ? 0u : rd + kTileBytes;
+    // ---- S^T = K Q^T: s[x] elements 0, 1 = heads 2 c, 2 c + 1 of token 16 x + tok_k; 2, 3 = of token 16 x + tok_k + 8 ----
+    float s[2][4];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
+      const uint32_t kt = tile + x * 16 * kKv4TokBytes + lane * 16, st = tile + kTileS + (16 * x + tok_k) * kKv4ScaleBytes + 2 * c;
+      const uint4 ka = lds_v4(kt), kb = lds_v4(kt + 8 * kKv4TokBytes);
+      const uint32_t ua = lds_u16(st), ub = lds_u16(st + 8 * kKv4ScaleBytes);
+      const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t fa = __byte_perm(ua, 0u, w < 2 ? 0x4040 : 0x4141) << 7, fb = __byte_perm(ub, 0u, w < 2 ? 0x4040 : 0x4141) << 7;
+        uint32_t a[4], b[4];
+        e2m1x8_to_f16x2(wa[w], a);
+        e2m1x8_to_f16x2(wb[w], b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          a[j] = mul_f16x2(a[j], fa);
+          b[j] = mul_f16x2(b[j], fb);
         }
-        const uint32_t tile = ring + sgi * kTileBytes;
-        // ---- S^T = K Q^T ----
-        float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-        {
-          const uint4 ka = lds_v4(tile + lane * 16), kb = lds_v4(tile + 8 * kKv4TokBytes + lane * 16);
-          const uint32_t ua = lds_u16(tile + kTileS + tok_k * kKv4ScaleBytes + 2 * c);
-          const uint32_t ub = lds_u16(tile + kTileS + (tok_k + 8) * kKv4ScaleBytes + 2 * c);
-          const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+        mma_acc(s[x], a[0], b[0], a[1], b[1], qb[2 * w][0], qb[2 * w][1]);
+        mma_acc(s[x], a[2], b[2], a[3], b[3], qb[2 * w + 1][0], qb[2 * w + 1][1]);
+      }
+    }
+    // ---- softmax: exponents relative to the reference, lifted ----
+    float t[2][4];
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const uint32_t fa = (((w < 2 ? ua : ua >> 8) & 0xffu) << 7) * 0x10001u, fb = (((w < 2 ? ub : ub >> 8) & 0xffu) << 7) * 0x10001u;
-            uint32_t a[4], b[4];
-            e2m1x8_to_f16x2(wa[w], a);
-            e2m1x8_to_f16x2(wb[w], b);
+    for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              a[j] = mul_f16x2(a[j], fa);
-              b[j] = mul_f16x2(b[j], fb);
-            }
-            mma_acc(s[0], a[0], b[0], a[1], b[1], qb[2 * w][0], qb[2 * w][1]);
-            mma_acc(s[1], a[2], b[2], a[3], b[3], qb[2 * w + 1][0], qb[2 * w + 1][1]);
-          }
+      for (int j = 0; j < 4; ++j) t[x][j] = fmaf(s[x][j], sc[j & 1], -base[j & 1]);
+    if (SET == kSetUnion || vm != kFull) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          bool on = (vm >> (16 * x + tok_k + (j < 2 ? 0 : 8))) & 1u;
+          if (SET == kSetUnion) on = on && ((flags >> (2 * c + (j & 1))) & 1u);
+          if (!on) t[x][j] = -INFINITY;
         }
-        // ---- softmax: elements 0, 1 = heads 2 c, 2 c + 1 of token tok_k; 2, 3 = of token tok_k + 8 ----
-        float t[4];
+    }
+    const float top0 = fmaxf(fmaxf(t[0][0], t[0][2]), fmaxf(t[1][0], t[1][2])), top1 = fmaxf(fmaxf(t[0][1], t[0][3]), fmaxf(t[1][1], t[1][3]));
+    if (__any_sync(kFull, fmaxf(top0, top1) > limit)) {
+      // a score lies further above the reference than it may (or there is none yet): the maximum becomes the reference
+      limit = kLift + kLag;
+      float top[2] = {top0, top1};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) t[j] = (s[0][j] + s[1][j]) * sc[j & 1];
-        const uint32_t vm = mask_st[sgi];
-        if (SET == kSetUnion || vm != 0xffffu) {
-          const bool v0 = (vm >> tok_k) & 1u, v1 = (vm >> (tok_k + 8)) & 1u;
+      for (int j = 0; j < 2; ++j) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            bool on = j < 2 ? v0 : v1;
-            if (SET == kSetUnion) on = on && ((flag_st[sgi] >> (2 * c + (j & 1))) & 1u);
-            if (!on) t[j] = -INFINITY;
-          }
+        for (int x = 4; x <= 16; x <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(kFull, top[j], x));
+        // (a column without a token so far has the reference -inf, for which `base` holds 0)
+        const float above = empty[j] ? (top[j] == -INFINITY ? 0.f : top[j] - kLift) : fmaxf(top[j] - kLift, 0.f);
+        const float raised = base[j] + above, rise = raised - base[j];   // (what the sum's rounding leaves of it)
+        const float corr = empty[j] ? 0.f : fast_ex2(-rise);
+        if (top[j] == -INFINITY && empty[j]) limit = -INFINITY; else empty[j] = false;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          o[x][j] *= corr;
+          o[x][2 + j] *= corr;
         }
-        const float top0 = fmaxf(t[0], t[2]), top1 = fmaxf(t[1], t[3]);
-        if (__any_sync(0xffffffffu, top0 > m_ref[0] + kLag || top1 > m_ref[1] + kLag)) {
-          float top[2] = {top0, top1};
+        l[j] *= corr;
+        base[j] = raised;
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-#pragma unroll
-            for (int x = 4; x <= 16; x <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], x));
-            const float m_new = fmaxf(m_ref[j], top[j]);
-            const float corr = m_ref[j] == -INFINITY ? 0.f : fast_ex2(m_ref[j] - m_new);
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-              o[x][j] *= corr;
-              o[x][2 + j] *= corr;
-            }
-            l[j] *= corr;
-            m_ref[j] = m_new;
-          }
+        for (int x = 0; x < 2; ++x) {
+          t[x][j] -= rise;
+          t[x][2 + j] -= rise;
         }
-        const float mb0 = m_ref[0] == -INFINITY ? 0.f : m_ref[0] - kLift, mb1 = m_ref[1] == -INFINITY ? 0.f : m_ref[1] - kLift;
-        const float p0 = fast_ex2(t[0] - mb0), p1 = fast_ex2(t[1] - mb1), p2 = fast_ex2(t[2] - mb0), p3 = fast_ex2(t[3] - mb1);
-        l[0] += p0 + p2;
-        l[1] += p1 + p3;
-        const uint32_t pb0 = transpose8x8(pack_f16x2(p0, p1)), pb1 = transpose8x8(pack_f16x2(p2, p3));
-        // ---- O^T += V^T P^T: tokens c, c + 4, c + 8, c + 12 of the tile ----
-        {
-          const uint32_t va = tile + kTileV + c * kKv4TokBytes + (((g >> 1) ^ (c & 2)) << 4) + (g & 1) * 8;
-          const uint32_t vs = tile + kTileS + c * kKv4ScaleBytes + kKv4ScaleBytes / 2 + g;
-          uint2 w[4];
-          uint32_t f[4];
+      }
+    }
+    uint32_t pb[2][2];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            w[j] = lds_v2(va + j * 4 * kKv4TokBytes);
-            f[j] = lds_u8(vs + j * 4 * kKv4ScaleBytes);
-          }
-          const uint32_t f01 = (f[0] << 7) | (f[1] << 23), f23 = (f[2] << 7) | (f[3] << 23);
-          constexpr uint32_t kLow = 0x0f0f0f0fu;
+    for (int x = 0; x < 2; ++x) {
+      float p[4];
 #pragma unroll
-          for (int hh = 0; hh < 2; ++hh) {
-            const uint32_t w0 = hh ? w[0].y : w[0].x, w1 = hh ? w[1].y : w[1].x, w2 = hh ? w[2].y : w[2].x, w3 = hh ? w[3].y : w[3].x;
-            uint32_t e01[4], d01[4], e23[4], d23[4];   // even and odd channels of the token pairs
-            e2m1x8_to_f16x2((w0 & kLow) | ((w1 << 4) & ~kLow), e01);
-            e2m1x8_to_f16x2(((w0 >> 4) & kLow) | (w1 & ~kLow), d01);
-            e2m1x8_to_f16x2((w2 & kLow) | ((w3 << 4) & ~kLow), e23);
-            e2m1x8_to_f16x2(((w2 >> 4) & kLow) | (w3 & ~kLow), d23);
+      for (int j = 0; j < 4; ++j) {
+        p[j] = fast_ex2(t[x][j]);
+        l[j & 1] += p[j];
+      }
+      pb[x][0] = transpose8x8(pack_f16x2(p[0], p[1]));
+      pb[x][1] = transpose8x8(pack_f16x2(p[2], p[3]));
+    }
+    // ---- O^T += V^T P^T: tokens c, c + 4, c + 8, c + 12 of each 16 ----
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              mma_acc(o[4 * hh + j], mul_f16x2(e01[j], f01), mul_f16x2(d01[j], f01), mul_f16x2(e23[j], f23), mul_f16x2(d23[j], f23), pb0, pb1);
-          }
-        }
+    for (int x = 0; x < 2; ++x) {
+      const uint32_t va = tile + kTileV + (16 * x + c) * kKv4TokBytes + (((g >> 1) ^ (c & 2)) << 4) + (g & 1) * 8;
+      const uint32_t vs = tile + kTileS + (16 * x + c) * kKv4ScaleBytes + kKv4ScaleBytes / 2 + g;
+      uint2 w[4];
+      uint32_t f[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        w[j] = lds_v2(va + j * 4 * kKv4TokBytes);
+        f[j] = lds_u8(vs + j * 4 * kKv4ScaleBytes);
+      }
+      const uint32_t f01 = __byte_perm(f[0], f[1], 0x5410) << 7, f23 = __byte_perm(f[2], f[3], 0x5410) << 7;
+      constexpr uint32_t kLow = 0x0f0f0f0fu;
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        const uint32_t w0 = hh ? w[0].y : w[0].x, w1 = hh ? w[1].y : w[1].x, w2 = hh ? w[2].y : w[2].x, w3 = hh ? w[3].y : w[3].x;
+        uint32_t e01[4], d01[4], e23[4], d23[4];   // even and odd channels of the token pairs
+        e2m1x8_to_f16x2((w0 & kLow) | ((w1 << 4) & ~kLow), e01);
+        e2m1x8_to_f16x2(((w0 >> 4) & kLow) | (w1 & ~kLow), d01);
+        e2m1x8_to_f16x2((w2 & kLow) | ((w3 << 4) & ~kLow), e23);
+        e2m1x8_to_f16x2(((w2 >> 4) & kLow) | (w3 & ~kLow), d23);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          mma_acc(o[4 * hh + j], mul_f16x2(e01[j], f01), mul_f16x2(d01[j], f01), mul_f16x2(e23[j], f23), mul_f16x2(d23[j], f23),
+                  pb[x][0], pb[x][1]);
       }
     }
   }
@@ -391,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
         rw[16 * g + 2 * i + 1] = o[i][2 + j];
       }
       if (g == 0) {
-        rw[kHeadDim] = m_ref[j] - kLift;   // (the lift goes into the reference)
+        rw[kHeadDim] = empty[j] ? -INFINITY : base[j];
         rw[kHeadDim + 1] = l[j];
       }
     }
@@ -435,6 +483,9 @@ cudaError_t launch_typed4(const CacheView& cv, const Dims& d, const HeadMaps& hm
                           const __nv_bfloat16* q, const int32_t* sel_idx, int64_t sel_stride, const int32_t* sel_count,
                           __nv_bfloat16* out, float* lse, float* partial, int n_splits, int32_t* status, cudaStream_t st) {
   const dim3 grid((unsigned)(rows.R * n_units), n_splits);
+  static PerDeviceOnce once;   // (one per instantiation)
+  const cudaError_t attr = set_dyn_smem_once(attn_rows4_kernel<G, SET>, kSmemBytes, once, true);
+  if (attr != cudaSuccess) return attr;
   (void)launch_chained(attn_rows4_kernel<G, SET>, grid, dim3(kThreads), kSmemBytes, st, cv, d, hm, rows, n_units, q, sel_idx,
                        sel_stride, sel_count, out, lse, partial, n_splits, status);
   cudaError_t e = cudaGetLastError();
@@ -446,7 +497,7 @@ cudaError_t launch_typed4(const CacheView& cv, const Dims& d, const HeadMaps& hm
 
 }  // namespace
 
-// Split count of a call: one round of the four resident CTAs per SM, at least 512 tokens (eight tiles per warp) each.
+// Split count of a call: one round of the four resident CTAs per SM, at least 512 tokens (four tiles per warp) each.
 int plan_splits4(int64_t units, int64_t max_set, int sm_count) {
   if (units <= 0) return 1;
   const int64_t want = 4LL * sm_count / units, cap = (max_set + 511) / 512;
