@@ -55,11 +55,6 @@ __device__ __forceinline__ uint2 lds_v2(uint32_t a) {
   asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
   return v;
 }
-__device__ __forceinline__ uint32_t lds_u16(uint32_t a) {
-  uint16_t v;
-  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
-  return v;
-}
 __device__ __forceinline__ uint32_t lds_u8(uint32_t a) {
   uint32_t v;
   asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
@@ -323,18 +318,23 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
       s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
       const uint32_t kt = tile + x * 16 * kKv4TokBytes + lane * 16, st = tile + kTileS + (16 * x + tok_k) * kKv4ScaleBytes + 2 * c;
       const uint4 ka = lds_v4(kt), kb = lds_v4(kt + 8 * kKv4TokBytes);
-      const uint32_t ua = lds_u16(st), ub = lds_u16(st + 8 * kKv4ScaleBytes);
+      // scales as fp16 pairs (s, s): code << 7 in both halves, by a product (the ALU is the busiest unit here, see below)
+      uint32_t fa[2], fb[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        fa[h] = lds_u8(st + h) * 0x00800080u;
+        fb[h] = lds_u8(st + 8 * kKv4ScaleBytes + h) * 0x00800080u;
+      }
       const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const uint32_t fa = __byte_perm(ua, 0u, w < 2 ? 0x4040 : 0x4141) << 7, fb = __byte_perm(ub, 0u, w < 2 ? 0x4040 : 0x4141) << 7;
         uint32_t a[4], b[4];
         e2m1x8_to_f16x2(wa[w], a);
         e2m1x8_to_f16x2(wb[w], b);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          a[j] = mul_f16x2(a[j], fa);
-          b[j] = mul_f16x2(b[j], fb);
+          a[j] = mul_f16x2(a[j], fa[w >> 1]);
+          b[j] = mul_f16x2(b[j], fb[w >> 1]);
         }
         mma_acc(s[x], a[0], b[0], a[1], b[1], qb[2 * w][0], qb[2 * w][1]);
         mma_acc(s[x], a[2], b[2], a[3], b[3], qb[2 * w + 1][0], qb[2 * w + 1][1]);
@@ -408,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
         w[j] = lds_v2(va + j * 4 * kKv4TokBytes);
         f[j] = lds_u8(vs + j * 4 * kKv4ScaleBytes);
       }
-      const uint32_t f01 = __byte_perm(f[0], f[1], 0x5410) << 7, f23 = __byte_perm(f[2], f[3], 0x5410) << 7;
+      const uint32_t f01 = f[1] * 0x00800000u + f[0] * 0x80u, f23 = f[3] * 0x00800000u + f[2] * 0x80u;
       constexpr uint32_t kLow = 0x0f0f0f0fu;
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) {
