@@ -392,6 +392,7 @@ rtp_status rtp_sparse_attn_decode(rtp_ctx* ctx, const rtp_params* params, const 
  *    split per 512 listed tokens, nothing at all for a single split; on a 148-SM device a decode
  *    batch of up to 63 sequences x 8 retrieval heads always fits).  Larger calls return RTP_ERR_CAPACITY before anything is launched
  *    and rtp_last_error says how many bytes were needed.
+ *    (On a 4-bit K/V cache a call that would not fit is cut into fewer splits instead.)
  *  - The first call on each device looks up the array's device address (once per device, with that
  *    device current); make that first call outside any CUDA stream capture.
  *  - All calls share the one array.  Nothing in it has to start at zero (every slot that is read was

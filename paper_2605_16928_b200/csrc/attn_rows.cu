@@ -484,7 +484,10 @@ cudaError_t launch_attn_rows_static(const CacheView& cv, const Dims& d, const He
                                     int32_t* status, int sm_count, size_t* needed_bytes, cudaStream_t st) {
   *needed_bytes = 0;
   if (rows.R == 0 || d.n_ret == 0) return cudaSuccess;
-  const int n_splits = plan_splits(rows.R * d.n_ret, max_set_len(d, kSetList, sel_stride, max_len), sm_count, true);
+  const int64_t longest = max_set_len(d, kSetList, sel_stride, max_len);
+  int n_splits = cv.kv_fp4 ? plan_splits4(rows.R * d.n_ret, longest, sm_count) : plan_splits(rows.R * d.n_ret, longest, sm_count, true);
+  if (cv.kv_fp4)   // (never more splits than fit)
+    n_splits = std::max(1, (int)std::min<size_t>(n_splits, kStaticScratchBytes / ((size_t)rows.R * d.n_ret * kPartial * sizeof(float))));
   const size_t need = n_splits > 1 ? (size_t)rows.R * d.n_ret * n_splits * kPartial * sizeof(float) : 0;
   *needed_bytes = need;
   if (need > kStaticScratchBytes) return cudaErrorMemoryAllocation;   // reported as RTP_ERR_CAPACITY by the caller

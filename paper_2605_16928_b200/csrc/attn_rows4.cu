@@ -425,6 +425,7 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
       }
     }
   }
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the merge may be set up meanwhile (it waits, too)
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();   // the rings are free: they now hold the warps' partial results
 

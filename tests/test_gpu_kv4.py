@@ -140,6 +140,44 @@ def test_dense_named_heads_positions_and_splits():
     assert torch.equal(a, c.out) and torch.equal(b, c.lse)       # the same call, the same bits
 
 
+def test_long_contexts_in_many_splits():
+    """The results of all splits, of as many as the workspace has room for, and of a single one."""
+    h = _h()
+    L = 20000
+    rng = np.random.default_rng(0)
+    k, v = (np.tile(rng.standard_normal((500, 1, 128)), (40, 1, 1)) for _ in range(2))
+    c = h.Cache4([L], n_kv=1, group=4, k=[k], v=[v], seed=9)
+    full = rb.rtp_workspace_bytes(c.params, 1, L)
+    for room in (full, 4 * 130 * 4 * 33, 4 * 130 * 4 * 17 + 5, 16):
+        ws = torch.empty(room, dtype=torch.uint8, device="cuda")
+        c.out.fill_(-77), c.lse.fill_(-77)
+        rb.rtp_dense_attn_decode(*c.args(), None, c.out, c.lse, ws, c.status)
+        c.check(range(4), lambda r, hd: range(L))
+    idx = rng.permutation(L)[:9001]
+    d_idx, d_cnt = h.dev_i32(np.tile(idx, (1, 4, 1))), h.dev_i32([[9001, 9000, 1, 0]])
+    sets = lambda r, hd: idx[:[9001, 9000, 1, 0][hd]]
+    for call in (rb.rtp_sparse_attn_decode, None):
+        c.out.fill_(-77), c.lse.fill_(-77)
+        if call:
+            call(*c.args(), d_idx, d_cnt, c.out, c.lse, c.ws, c.status)
+        else:
+            rb.rtp_sparse_attn_decode_static(*c.args(), d_idx, d_cnt, c.out, c.lse, c.status)
+        c.check(range(4), sets)
+    assert c.code() == rb.RTP_OK
+
+
+def test_static_scratch_takes_any_number_of_rows():
+    """Where the built-in scratch would not hold the splits of a call, a 4-bit cache is read in fewer."""
+    h = _h()
+    c = h.Cache4([9000], n_kv=1, group=1, k=[np.tile(np.random.default_rng(1).standard_normal((300, 1, 128)), (30, 1, 1))])
+    R = 700
+    c.set_rows(np.random.default_rng(2).standard_normal((R, 1, 128)), [0] * R, [8999] * R)
+    idx = np.stack([np.random.default_rng(r).permutation(9000)[:8500] for r in range(R)])[:, None]
+    rb.rtp_sparse_attn_decode_static(*c.args(), h.dev_i32(idx), h.dev_i32(np.full((R, 1), 8500)), c.out, c.lse, c.status)
+    assert c.code() == rb.RTP_OK
+    c.check([0], lambda r, hd: idx[r, 0], rows=[0, 33, 699])
+
+
 @pytest.mark.parametrize("scale", [1e-30, 1e-4, 1.0, 300.0, 1e20])
 def test_query_magnitudes(scale):
     """Queries of any bf16 magnitude: they are scaled by a power of two on their way to fp16."""
