@@ -56,29 +56,35 @@ __device__ __forceinline__ uint32_t f32_to_e2m1x8(const float (&x)[8]) {
 // Sixteen bf16 channels -> their codes and their scale.  Values beyond 61440 in magnitude saturate, a NaN is stored as 0;
 // `bad` is set for either.
 __device__ __forceinline__ uint2 kv4_encode(const uint4& lo, const uint4& hi, uint32_t& scale, bool& bad) {
-  float x[16];
-  const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-  float amax = 0.f;
+  uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  uint32_t mx = 0;   // the magnitudes' bit patterns order like the magnitudes, two at a time
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float f = __uint_as_float((i & 1) ? (w[i >> 1] & 0xffff0000u) : (w[i >> 1] << 16));
-    bad = bad || !(fabsf(f) <= kKv4MaxValue);
-    x[i] = f != f ? 0.f : fminf(fmaxf(f, -kKv4MaxValue), kKv4MaxValue);
-    amax = fmaxf(amax, fabsf(x[i]));
-  }
-  scale = kv4_scale_code(__fdiv_rn(amax, 6.0f));
-  const float s = kv4_scale_value(scale), inv = s > 0.f ? __frcp_rn(s) : 0.f;
-  // x / s with one correction step: the plain product x * inv is off a tie by one bit for scales of 15/8 * 2^n
+  for (int i = 0; i < 8; ++i) mx = __vmaxu2(mx, w[i] & 0x7fff7fffu);
+  mx = max(mx & 0xffffu, mx >> 16);
+  if (mx > 0x4770u) {   // 61440; infinities and NaN lie above it
+    bad = true;
+    mx = 0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float y = x[i] * inv;
-    x[i] = fmaf(fmaf(-y, s, x[i]), inv, y);
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int h = 0; h < 32; h += 16) {
+        const uint32_t mag = (w[i] >> h) & 0x7fffu, put = mag > 0x7f80u ? 0u : min(mag, 0x4770u);
+        w[i] = (w[i] & ~(0x7fffu << h)) | (put << h);
+        mx = max(mx, put);
+      }
+    }
   }
+  scale = kv4_scale_code(__fdiv_rn(__uint_as_float(mx << 16), 6.0f));
+  // x / s as x * (inv + err), inv + err the reciprocal to 48 bits: the product with inv alone is off a tie by one bit for
+  // scales of 15/8 * 2^n, the one below is exact at every tie
+  const float s = kv4_scale_value(scale), inv = s > 0.f ? __frcp_rn(s) : 0.f, err = fmaf(-inv, s, 1.0f) * inv;
   float a[8], b[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    a[i] = x[i];
-    b[i] = x[8 + i];
+    const float x = __uint_as_float((i & 1) ? (w[i >> 1] & 0xffff0000u) : (w[i >> 1] << 16));
+    const float y = __uint_as_float((i & 1) ? (w[4 + (i >> 1)] & 0xffff0000u) : (w[4 + (i >> 1)] << 16));
+    a[i] = fmaf(x, inv, x * err);
+    b[i] = fmaf(y, inv, y * err);
   }
   return make_uint2(f32_to_e2m1x8(a), f32_to_e2m1x8(b));
 }

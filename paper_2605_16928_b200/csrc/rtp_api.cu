@@ -329,6 +329,7 @@ rtp_status rtp_kv_append(rtp_ctx* ctx, const rtp_params* params, const rtp_cache
   if (!aligned16(k_new) || !aligned16(v_new)) return fail(ctx, RTP_ERR_INVALID, "k_new / v_new must be 16-byte aligned");
   (void)hm;
   cudaError_t e = cudaSuccess;
+  if (cv.kv_fp4 && T >= ((int64_t)1 << 31) / d.n_kv) return fail(ctx, RTP_ERR_UNSUPPORTED, "2^31 or more (token, head) rows in one call");
   const auto launch = cv.kv_fp4 ? launch_kv4_append : launch_kv_append;
   if (cv.n_kv > 0)
     e = launch(cv, d.n_kv, reinterpret_cast<const __nv_bfloat16*>(k_new),
@@ -346,6 +347,7 @@ rtp_status rtp_kv_expand(rtp_ctx* ctx, const rtp_params* params, const rtp_cache
   (void)hm;
   if (n < 0 || n_out_pages < 0) return fail(ctx, RTP_ERR_INVALID, "page count is negative");
   if (!cv.kv_fp4) return fail(ctx, RTP_ERR_UNSUPPORTED, "the cache is not a 4-bit cache");
+  if (n >= ((int64_t)1 << 31) / d.n_kv) return fail(ctx, RTP_ERR_UNSUPPORTED, "2^31 or more (page, head) pairs in one call");
   if (n == 0) return RTP_OK;
   if (!src_pages || !k_out || !v_out) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
   if (!aligned16(k_out) || !aligned16(v_out)) return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
