@@ -19,6 +19,7 @@ __global__ void __launch_bounds__(kThreads) kv4_append_kernel(const __grid_const
                                                               const int32_t* __restrict__ tok_seq,
                                                               const int32_t* __restrict__ tok_pos, const int64_t T,
                                                               int32_t* status) {
+  chain_wait();
   uint8_t* kp = const_cast<uint8_t*>(reinterpret_cast<const uint8_t*>(cv.k));
   uint8_t* vp = const_cast<uint8_t*>(reinterpret_cast<const uint8_t*>(cv.v));
   uint8_t* sp = const_cast<uint8_t*>(cv.kv_scales);
@@ -58,6 +59,7 @@ __global__ void __launch_bounds__(kThreads) kv4_expand_kernel(const __grid_const
                                                               const int32_t* __restrict__ src_pages,
                                                               const int32_t* __restrict__ dst_pages, uint4* __restrict__ k_out,
                                                               uint4* __restrict__ v_out, const int n_out_pages, int32_t* status) {
+  chain_wait();
   constexpr int kChunks = kHeadDim / 8;                     // 16-byte pieces of an expanded row
   constexpr int kSteps = kPage * kChunks / kThreads;
   const unsigned p = blockIdx.x / cv.n_kv, head = blockIdx.x % cv.n_kv;
@@ -104,15 +106,16 @@ cudaError_t launch_kv4_append(const CacheView& cv, int n_src_heads, const __nv_b
   if (T == 0) return cudaSuccess;
   int64_t blocks = (T * n_src_heads * kGroupsPerRow + kThreads - 1) / kThreads;
   blocks = std::min<int64_t>(blocks, (int64_t)current_sm_count(148) * 32);
-  kv4_append_kernel<<<(unsigned)blocks, kThreads, 0, st>>>(cv, n_src_heads, k_new, v_new, tok_seq, tok_pos, T, status);
+  (void)launch_chained(kv4_append_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, st, cv, n_src_heads, k_new, v_new, tok_seq,
+                       tok_pos, T, status);
   return cudaGetLastError();
 }
 
 cudaError_t launch_kv4_expand(const CacheView& cv, const int32_t* src_pages, const int32_t* dst_pages, int64_t n, void* k_out,
                               void* v_out, int32_t n_out_pages, int32_t* status, cudaStream_t st) {
   if (n == 0 || cv.n_kv == 0) return cudaSuccess;
-  kv4_expand_kernel<<<(unsigned)(n * cv.n_kv), kThreads, 0, st>>>(cv, src_pages, dst_pages, reinterpret_cast<uint4*>(k_out),
-                                                                  reinterpret_cast<uint4*>(v_out), n_out_pages, status);
+  (void)launch_chained(kv4_expand_kernel, dim3((unsigned)(n * cv.n_kv)), dim3(kThreads), 0, st, cv, src_pages, dst_pages,
+                       reinterpret_cast<uint4*>(k_out), reinterpret_cast<uint4*>(v_out), n_out_pages, status);
   return cudaGetLastError();
 }
 

@@ -15,7 +15,7 @@ constexpr int kPlanThreads = 1024;
 constexpr int kPlanWarps = kPlanThreads / 32;
 constexpr int kRowThreads = 256;
 constexpr int kCopyThreads = 256;
-constexpr int kCopyVec = 4;                                       // 16-byte pieces in flight per thread
+constexpr int kCopyVec = 8;                                       // 16-byte pieces in flight per thread
 constexpr int kPiece = kCopyThreads * kCopyVec * 16;              // bytes of a page that a CTA copies at a time
 
 // Workspace: counts, then lists.
@@ -457,7 +457,8 @@ size_t pages_workspace_bytes(int64_t num_pages, int64_t n_seqs) {
 cudaError_t launch_copy_pages(const PageArrays& pa, int num_pages, const int32_t* src, const int32_t* dst, int64_t n,
                               int32_t* status, cudaStream_t st) {
   if (n == 0 || pa.total_pieces == 0) return cudaSuccess;
-  (void)launch_chained(copy_pages_kernel, dim3(copy_grid(pa, n)), dim3(kCopyThreads), 0, st, pa, num_pages, src, dst, n,
+  const unsigned grid = (unsigned)std::min<int64_t>(n * pa.total_pieces, 1 << 20);
+  (void)launch_chained(copy_pages_kernel, dim3(grid), dim3(kCopyThreads), 0, st, pa, num_pages, src, dst, n,
                        (const PlanHead*)nullptr, status);
   return cudaGetLastError();
 }
