@@ -5,6 +5,8 @@
 // their numbers are found by a scan over the counts (4 bytes a page: 64 KB for a pool of 16K pages, which one CTA reads from
 // L2 in a few microseconds), and what a call hands out does not depend on the order in which threads arrive.  Decisions that
 // need an order are taken by one CTA; page contents, the only bytes that matter, are then copied by all SMs.
+#include <type_traits>
+
 #include "rtp_device.cuh"
 
 namespace rtp {
@@ -13,7 +15,9 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWarps = kPlanThreads / 32;
+constexpr int kEarlyPages = kPlanWarps * 8 * 128;
 constexpr int kRowThreads = 256;
+constexpr int kRowVec = 4;                                        // table entries in flight per thread
 constexpr int kCopyThreads = 256;
 constexpr int kCopyVec = 8;                                       // 16-byte pieces in flight per thread
 constexpr int kPiece = kCopyThreads * kCopyVec * 16;              // bytes of a page that a CTA copies at a time
@@ -84,9 +88,19 @@ __global__ void __launch_bounds__(kRowThreads) fork_kernel(int32_t* __restrict__
   int32_t* to = table + (int64_t)dst * max_pages;
   bad = len < 0 || np > max_pages || seq_lens[dst] != 0;
   if (!bad)
-    for (int p = threadIdx.x; p < max_pages; p += kRowThreads) {
-      bad = bad || to[p] >= 0;
-      if (p < np) bad = bad || !page_ok(from[p], num_pages) || refs[from[p]] <= 0;
+    for (int p0 = threadIdx.x; p0 < max_pages; p0 += kRowThreads * kRowVec) {   // (loads of a step side by side)
+      int e[kRowVec], t[kRowVec];
+#pragma unroll
+      for (int k = 0; k < kRowVec; ++k) {
+        const int p = p0 + k * kRowThreads;
+        e[k] = p < np ? from[p] : -1;
+        t[k] = p < max_pages ? to[p] : -1;
+      }
+#pragma unroll
+      for (int k = 0; k < kRowVec; ++k) {
+        bad = bad || t[k] >= 0;
+        if (p0 + k * kRowThreads < np) bad = bad || !page_ok(e[k], num_pages) || refs[e[k]] <= 0;
+      }
     }
   if (__syncthreads_or(bad)) {
     if (threadIdx.x == 0) set_status(status, RTP_ERR_INVALID);
@@ -111,14 +125,19 @@ __global__ void __launch_bounds__(kRowThreads) free_kernel(int32_t* __restrict__
     return;
   }
   int32_t* row = table + (int64_t)seq * max_pages;
-  for (int p = threadIdx.x; p < max_pages; p += kRowThreads) {
-    if (row[p] < 0) continue;
-    const int e = atomicExch(row + p, -1);   // (a sequence named twice gives each page back once)
-    if (e < 0) continue;
-    if (!page_ok(e, num_pages)) {
-      set_status(status, RTP_ERR_INVALID);
-    } else if (atomicSub(refs + e, 1) <= 0) {   // nobody held it
-      atomicAdd(refs + e, 1);
+  for (int p0 = threadIdx.x; p0 < max_pages; p0 += kRowThreads * kRowVec) {   // (requests of a step side by side)
+    int e[kRowVec], held[kRowVec];
+#pragma unroll
+    for (int k = 0; k < kRowVec; ++k) e[k] = p0 + k * kRowThreads < max_pages ? row[p0 + k * kRowThreads] : -1;
+#pragma unroll
+    for (int k = 0; k < kRowVec; ++k)   // (a sequence named twice gives each page back once)
+      if (e[k] >= 0) e[k] = atomicExch(row + p0 + k * kRowThreads, -1);
+#pragma unroll
+    for (int k = 0; k < kRowVec; ++k) held[k] = e[k] >= 0 && page_ok(e[k], num_pages) ? atomicSub(refs + e[k], 1) : 0;
+#pragma unroll
+    for (int k = 0; k < kRowVec; ++k) {
+      if (e[k] < 0 || held[k] > 0) continue;
+      if (page_ok(e[k], num_pages)) atomicAdd(refs + e[k], 1);   // nobody held it
       set_status(status, RTP_ERR_INVALID);
     }
   }
@@ -180,6 +199,8 @@ __device__ __forceinline__ int scan_segments(int mine, int* s_before, int lane, 
 // ---- reserve -----------------------------------------------------------------------------------------
 struct ReserveShared {
   int seq[kReserveMax];       // -1: the entry asks for nothing
+  int len[kReserveMax], add[kReserveMax];
+  int held[kReserveMax];      // references of `cow`
   int cow[kReserveMax];       // shared page that the sequence is going to write into, or -1
   int first[kReserveMax];     // first table entry that has to be filled
   int off[kReserveMax + 1];   // pages handed out before this entry's
@@ -187,6 +208,18 @@ struct ReserveShared {
   int n_pairs;
   unsigned long long total;   // (the sum in 32 bits may wrap)
 };
+
+// How many of v[0 .. i - 1] equal v[i] (v 16-byte aligned).
+__device__ __forceinline__ int earlier_equal(const int* v, int i) {
+  const int x = v[i];
+  int n = 0;
+#pragma unroll 4
+  for (int j = 0; j < i; j += 4) {
+    const int4 y = *reinterpret_cast<const int4*>(v + j);
+    n += (y.x == x) + (y.y == x && j + 1 < i) + (y.z == x && j + 2 < i) + (y.w == x && j + 3 < i);
+  }
+  return n;
+}
 
 __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restrict__ table, const int32_t* __restrict__ seq_lens,
                                                                int32_t* __restrict__ refs, const int num_pages, const int batch,
@@ -202,70 +235,88 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
     s.n_pairs = 0;
     s.total = 0;
   }
-  bool invalid = false, full = false, shared_page = false;
+  // Pools of up to 32K pages: every lane asks for its reference counts first, next to the requests, and keeps four bits for
+  // each of up to eight pieces of its warp's segment.
+  const Segment seg = warp_segment(num_pages, warp);
+  const bool early = num_pages <= kEarlyPages;
+  uint32_t used4 = 0;
+  if (early) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) used4 |= (seg.lo + 128 * k < seg.hi ? used_bits(refs, seg.lo + 128 * k, seg.hi, lane) : 0u) << (4 * k);
+  }
+  bool invalid = false, full = false, shared_page = false, many = false;
   for (int i = tid; i < n; i += kPlanThreads) {
-    const int seq = seqs[i];
-    const bool ok = (unsigned)seq < (unsigned)batch && n_tokens[i] >= 0 && seq_lens[seq] >= 0;
+    const int seq = seqs[i], add = n_tokens[i];
+    const int len = (unsigned)seq < (unsigned)batch ? seq_lens[seq] : -1;
+    const bool ok = add >= 0 && len >= 0;
     invalid = invalid || !ok;
+    many = many || (ok && add > 32 * kPage);
     s.seq[i] = ok ? seq : -1;
+    s.len[i] = len;
+    s.add[i] = add;
   }
+  many = __syncthreads_or(many);
+  for (int i = tid; i < n; i += kPlanThreads) s.first[i] = s.seq[i] >= 0 && earlier_equal(s.seq, i) > 0;
   __syncthreads();
-  for (int i = tid; i < n; i += kPlanThreads) {   // a sequence named twice: the first one counts
-    const int seq = s.seq[i];
-    bool twice = false;
-    for (int j = 0; j < i && seq >= 0; ++j) twice = twice || s.seq[j] == seq;
-    s.first[i] = twice;
-  }
-  __syncthreads();
-  for (int i = tid; i < n; i += kPlanThreads)
+  for (int i = tid; i < n; i += kPlanThreads)   // a sequence named twice: the first one counts
     if (s.first[i]) {
       s.seq[i] = -1;
       invalid = true;
     }
   __syncthreads();
-  // one warp per entry: the table entries from the sequence's length up to what it is going to need
-  for (int i = warp; i < n; i += kPlanWarps) {
-    const int seq = s.seq[i];
-    int need = 0, cow = -1, first = 0;
-    if (seq >= 0) {
-      const int64_t len = seq_lens[seq], end = len + n_tokens[i];
-      const int64_t want = (end + kPage - 1) >> kPageShift;
-      const int32_t* row = table + (int64_t)seq * max_pages;
-      if (want > max_pages) {
-        full = true;
-      } else {
-        bool bad = false;
-        int mapped = 0;
-        first = (int)((len + kPage - 1) >> kPageShift);
-        for (int p = first + lane; p < want; p += 32) {   // mapped entries come first, then unmapped ones
-          const bool m = row[p] >= 0;
-          mapped += m;
-          bad = bad || (m && p > first && row[p - 1] < 0);
-        }
-        mapped = __reduce_add_sync(0xffffffffu, mapped);
-        first += mapped;
-        need = (int)want - first;
-        if (need < 0) need = 0;
-        if (n_tokens[i] > 0 && (len & (kPage - 1))) {
-          const int last = row[len >> kPageShift];
-          if (!page_ok(last, num_pages)) bad = true;
-          else if (refs[last] > 1) cow = last;
-        }
-        if (__any_sync(0xffffffffu, bad)) {
-          invalid = true;
-          need = 0;
-          cow = -1;
-          if (lane == 0) s.seq[i] = -1;
+  // The table entries from a sequence's length up to what it is going to need: eight lanes per sequence, a warp where somebody
+  // asks for more than 32 pages.
+  auto look_at_rows = [&](auto width) {
+    constexpr int W = decltype(width)::value;
+    const uint32_t lanes = W == 32 ? 0xffffffffu : ((1u << (W & 31)) - 1u) << (lane / W * W);
+    const int sub = lane % W;
+    for (int i = tid / W; i < n; i += kPlanThreads / W) {
+      const int seq = s.seq[i];
+      int need = 0, cow = -1, first = 0, held = 0;
+      if (seq >= 0) {
+        const int64_t len = s.len[i], end = len + s.add[i];
+        const int64_t want = (end + kPage - 1) >> kPageShift;
+        const int32_t* row = table + (int64_t)seq * max_pages;
+        if (want > max_pages) {
+          full = true;
+        } else {
+          bool bad = false;
+          int mapped = 0;
+          first = (int)((len + kPage - 1) >> kPageShift);
+          const bool part = s.add[i] > 0 && (len & (kPage - 1));
+          const int last = part ? row[len >> kPageShift] : -1;   // (requested together with the entries below)
+          for (int p = first + sub; p < want; p += W) {   // mapped entries come first, then unmapped ones
+            const bool m = row[p] >= 0;
+            mapped += m;
+            bad = bad || (m && p > first && row[p - 1] < 0);
+          }
+          mapped = __reduce_add_sync(lanes, mapped);
+          first += mapped;
+          need = (int)want - first;
+          if (need < 0) need = 0;
+          if (part) {
+            if (!page_ok(last, num_pages)) bad = true;
+            else held = refs[last];
+            if (held > 1) cow = last;
+          }
+          if (__any_sync(lanes, bad)) {
+            invalid = true;
+            need = 0;
+            cow = -1;
+            if (sub == 0) s.seq[i] = -1;
+          }
         }
       }
+      if (sub == 0) {
+        s.first[i] = first;
+        s.cow[i] = cow;
+        s.held[i] = held;
+        s.off[i] = need;
+      }
+      shared_page = shared_page || cow >= 0;
     }
-    if (lane == 0) {
-      s.first[i] = first;
-      s.cow[i] = cow;
-      s.off[i] = need;
-    }
-    shared_page = shared_page || cow >= 0;
-  }
+  };
+  if (many) look_at_rows(std::integral_constant<int, 32>()); else look_at_rows(std::integral_constant<int, 8>());
   if (__syncthreads_or(shared_page)) {
     // A page with r holders is copied by the first r - 1 of them at most: the last one to write it has it alone.
     int mine[(kReserveMax + kPlanThreads - 1) / kPlanThreads];
@@ -274,9 +325,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
       const int i = tid + k * kPlanThreads;
       mine[k] = 0;
       if (i < n && s.cow[i] >= 0) {
-        int earlier = 0;
-        for (int j = 0; j < i; ++j) earlier += s.cow[j] == s.cow[i];
-        mine[k] = refs[s.cow[i]] - earlier > 1 ? 1 : -1;
+        mine[k] = s.held[i] - earlier_equal(s.cow, i) > 1 ? 1 : -1;
       }
     }
     __syncthreads();
@@ -318,8 +367,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
     return;
   }
   if (total > 0) {
-    const Segment seg = warp_segment(num_pages, warp);
-    const int used = count_used(refs, seg.lo, seg.hi, lane);
+    const int used = early ? __reduce_add_sync(0xffffffffu, __popc(used4)) : count_used(refs, seg.lo, seg.hi, lane);
     const int all_used = scan_segments(used, s.before, lane, warp);
     if (num_pages - all_used < total) {   // not enough free pages: nothing is handed out
       if (tid == 0) {
@@ -331,7 +379,8 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
     int rank = seg.lo - s.before[warp];   // free pages before this segment
     for (int at = seg.lo; at < seg.hi && rank < total; at += 128) {
       const int valid = min(4, max(0, seg.hi - (at + 4 * lane)));
-      const uint32_t free_bits = ~used_bits(refs, at, seg.hi, lane) & ((1u << valid) - 1u);
+      const uint32_t used_here = early ? used4 >> ((at - seg.lo) / 128 * 4) : used_bits(refs, at, seg.hi, lane);
+      const uint32_t free_bits = ~used_here & ((1u << valid) - 1u);
       const int cnt = __popc(free_bits);
       int u = rank + lanes_before(cnt, lane);
       for (int j = 0; j < 4; ++j) {
@@ -348,7 +397,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
           refs[page] = 1;
           if (cow >= 0 && k == 0) {
             atomicSub(refs + cow, 1);
-            row[seq_lens[seq] >> kPageShift] = page;
+            row[s.len[a] >> kPageShift] = page;
             const int slot = atomicAdd(&s.n_pairs, 1);
             pair_src[slot] = cow;
             pair_dst[slot] = page;
