@@ -75,7 +75,7 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 }
 __device__ __forceinline__ void mma_acc(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                         uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -356,6 +356,16 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
           if (!on) t[x][j] = -INFINITY;
         }
     }
+    // (V of the first 16 tokens is read here, so that the loads have arrived behind the branch)
+    const uint32_t va = tile + kTileV + c * kKv4TokBytes + (((g >> 1) ^ (c & 2)) << 4) + (g & 1) * 8;
+    const uint32_t vs = tile + kTileS + c * kKv4ScaleBytes + kKv4ScaleBytes / 2 + g;
+    uint2 w[4];
+    uint32_t f[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      w[j] = lds_v2(va + j * 4 * kKv4TokBytes);
+      f[j] = lds_u8(vs + j * 4 * kKv4ScaleBytes);
+    }
     const float top0 = fmaxf(fmaxf(t[0][0], t[0][2]), fmaxf(t[1][0], t[1][2])), top1 = fmaxf(fmaxf(t[0][1], t[0][3]), fmaxf(t[1][1], t[1][3]));
     if (__any_sync(kFull, fmaxf(top0, top1) > limit)) {
       // a score lies further above the reference than it may (or there is none yet): the maximum becomes the reference
@@ -399,14 +409,12 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
     // ---- O^T += V^T P^T: tokens c, c + 4, c + 8, c + 12 of each 16 ----
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const uint32_t va = tile + kTileV + (16 * x + c) * kKv4TokBytes + (((g >> 1) ^ (c & 2)) << 4) + (g & 1) * 8;
-      const uint32_t vs = tile + kTileS + (16 * x + c) * kKv4ScaleBytes + kKv4ScaleBytes / 2 + g;
-      uint2 w[4];
-      uint32_t f[4];
+      if (x > 0) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        w[j] = lds_v2(va + j * 4 * kKv4TokBytes);
-        f[j] = lds_u8(vs + j * 4 * kKv4ScaleBytes);
+        for (int j = 0; j < 4; ++j) {
+          w[j] = lds_v2(va + (16 * x + 4 * j) * kKv4TokBytes);
+          f[j] = lds_u8(vs + (16 * x + 4 * j) * kKv4ScaleBytes);
+        }
       }
       const uint32_t f01 = f[1] * 0x00800000u + f[0] * 0x80u, f23 = f[3] * 0x00800000u + f[2] * 0x80u;
       constexpr uint32_t kLow = 0x0f0f0f0fu;
