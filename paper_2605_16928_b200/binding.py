@@ -149,11 +149,9 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
 
 
 def _ptr(t) -> Optional[int]:
-    if t is None:
-        return None
-    if isinstance(t, int):
+    if t is None or isinstance(t, int):
         return t
-    return int(t.data_ptr())
+    return t.data_ptr()
 
 
 def _stream(stream) -> Optional[int]:
