@@ -9,9 +9,16 @@
 //   S^T = K Q^T   A = 16 tokens x 16 channels.  The channels of a k-step may be any as long as Q has the same, so lane
 //                 (g, c) of the fragment takes channels 32 c .. 32 c + 31 of its two tokens: one 16-byte read each.
 //   O^T = V^T P^T A = 16 channels x 16 tokens.  Lane (g, c) takes channels 16 g .. 16 g + 15 (one scale group) of four
-//                 tokens; the nibbles of two tokens are interleaved into bytes, so that one conversion gives the pair
-//                 (token, token') that an MMA register holds.  P^T comes from S^T by movmatrix.
-// Everything that is decoded this way is exact in fp16 (kv4.cuh).  Queries are scaled by a power of two per head, so that
+//                 tokens.  P^T comes from S^T by movmatrix.  An MMA register holds two values of the contracted index, a
+//                 conversion gives two channels of one token:
+//     groups of 8   the nibbles of two tokens are interleaved into bytes first, so that the pair is (token, token');
+//     groups <= 4   half of the eight columns would be idle.  The pair is (even channel, odd channel) of one token, columns
+//                   0 .. 3 have P of the heads in the even place and 0 in the odd one, columns 4 .. 7 the reverse: they
+//                   come out as the sums of the even and of the odd channels.  As many MMAs, no interleaving, and half
+//                   the accumulators.
+// A single head (lists and pages of one query head) has eight columns to itself: column n of S^T gets the channels of scale
+// group 2 n (or 2 n - 7) alone, K goes in without its scales, and eight products per token bring them in afterwards.
+// What is decoded is exact in fp16 (kv4.cuh).  Queries are scaled by a power of two per head, so that
 // their largest channel is near 2^9: the rounding to fp16 then costs 2^-34 of it at most, for any bf16 input.
 // Probabilities are relative to a reference that trails the running maximum by at most 2^8 and are shifted up by 2^7: they
 // fit fp16 (11 bits; bf16 has 8), down to 2^-21 of the reference without a loss.  Sums are fp32.
@@ -137,14 +144,20 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
   const int n_tiles = min(n_total, first + per) - first;
   const int n_mine = n_tiles > warp ? (n_tiles - warp + kWarps - 1) / kWarps : 0;   // tiles first + warp, + 4, ...
 
-  // B fragments of the queries: column g = head g of the group, channels 32 c + 4 ks .. + 3 in k-step ks
+  // B fragments of the queries: channels 32 c + 4 ks .. + 3 of column g's head in k-step ks.  Head of column n: n, or n % 4 in
+  // groups of up to four.  `head`: of this lane's columns 2 c and 2 c + 1 in the results.
+  constexpr bool kPairs = G <= 4, kSingle = G == 1;
+  constexpr int H = kSingle ? 1 : 2;     // heads per lane
+  constexpr int kTilesO = kPairs ? 4 : 8;
+  const int head_b = kSingle ? 0 : kPairs ? g & 3 : g;
+  const int head[2] = {kSingle ? 0 : kPairs ? (2 * c) & 3 : 2 * c, kSingle ? 0 : kPairs ? (2 * c + 1) & 3 : 2 * c + 1};
   uint32_t qb[8][2];
-  float sc[2];   // logits in log2 units: factor of heads 2 c and 2 c + 1
+  float sc[H];   // logits in log2 units: factors of the lane's heads
   {
     uint32_t w[16];
     float mx = 0.f;
-    if (g < G) {
-      const uint4* qp = reinterpret_cast<const uint4*>(q + ((int64_t)r * d.n_q + qh0 + g) * kHeadDim + 32 * c);
+    if (head_b < G) {
+      const uint4* qp = reinterpret_cast<const uint4*>(q + ((int64_t)r * d.n_q + qh0 + head_b) * kHeadDim + 32 * c);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint4 v = __ldg(qp + i);
@@ -165,16 +178,28 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       qb[i >> 1][i & 1] = pack_f16x2(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xffff0000u) * up);
-    sc[0] = __shfl_sync(0xffffffffu, down, 8 * c);       // (lane of head 2 c, channel quarter 0)
-    sc[1] = __shfl_sync(0xffffffffu, down, 8 * c + 4);
-  }
-  float o[8][4];   // tile i: channels 16 g + 2 i (elements 0, 1: heads 2 c, 2 c + 1) and 16 g + 2 i + 1 (2, 3)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-  // Reference of the softmax, less the lift, for heads 2 c and 2 c + 1; none before a head's first token.  While a column of
+    for (int j = 0; j < H; ++j) sc[j] = __shfl_sync(0xffffffffu, down, 8 * c + 4 * j);   // (from the lane of column 2 c + j)
+    if (kSingle) {   // column n < 4: group 2 n, the first half of lane n's channels; column 4 + n: group 2 n + 1
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (g != c + (i < 8 ? 0 : 4)) qb[i >> 1][i & 1] = 0u;
+    }
+  }
+  // O^T, rows of tile i: byte 8 g + 2 i (elements 0, 1: columns 2 c, 2 c + 1) and byte 8 g + 2 i + 1 (2, 3), the column's half
+  // of either; in groups of 8: channels 16 g + 2 i and 16 g + 2 i + 1
+  float o[kTilesO][4];
+#pragma unroll
+  for (int i = 0; i < kTilesO; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  // Reference of the softmax, less the lift, for the lane's heads; none before a head's first token.  While a column of
   // the warp has none, every tile goes through the branch that sets it (limit = -inf).
-  float base[2] = {0.f, 0.f}, l[2] = {0.f, 0.f}, limit = 2 * c < G ? -INFINITY : kLift + kLag;
-  bool empty[2] = {2 * c < G, 2 * c + 1 < G};   // (columns beyond the group count as set)
+  float base[H], l[H], limit = head[0] < G ? -INFINITY : kLift + kLag;
+  bool empty[H];   // (columns beyond the group count as set)
+#pragma unroll
+  for (int j = 0; j < H; ++j) {
+    base[j] = l[j] = 0.f;
+    empty[j] = head[j] < G;
+  }
 
   const int64_t bt_base = (int64_t)seq * cv.max_pages;
   const int kslot = cv.kv_slot[kvh];
@@ -182,6 +207,8 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
   const uint8_t* kp = reinterpret_cast<const uint8_t*>(cv.k);
   const uint8_t* vp = reinterpret_cast<const uint8_t*>(cv.v);
   const int tok_k = (g >> 1) + 4 * (g & 1);   // token of MMA row g (row g + 8: tok_k + 8)
+  // groups of up to four: the first or second of two packed probabilities into the half that column g multiplies
+  const uint32_t place[2] = {g < 4 ? 0x4410u : 0x1044u, g < 4 ? 0x4432u : 0x3244u};
 
   // Where a tile lives is found in steps, each a tile after the one that requested it: entry -> token -> page -> row.
   // List sets: lane t looks after token t of the tile.  Other sets: all lanes look after the tile's page.
@@ -311,50 +338,63 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
     }
     const uint32_t tile = ring + rd;
     rd = rd == (kStages - 1) * kTileBytes ? 0u : rd + kTileBytes;
-    // ---- S^T = K Q^T: s[x] elements 0, 1 = heads 2 c, 2 c + 1 of token 16 x + tok_k; 2, 3 = of token 16 x + tok_k + 8 ----
-    float s[2][4];
+    // ---- S^T = K Q^T, as exponents relative to the reference: t[x][h][j] = head j of token 16 x + 8 h + tok_k ----
+    float t[2][2][H];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
-      const uint32_t kt = tile + x * 16 * kKv4TokBytes + lane * 16, st = tile + kTileS + (16 * x + tok_k) * kKv4ScaleBytes + 2 * c;
-      const uint4 ka = lds_v4(kt), kb = lds_v4(kt + 8 * kKv4TokBytes);
-      // scales as fp16 pairs (s, s): code << 7 in both halves, by a product (the ALU is the busiest unit here, see below)
-      uint32_t fa[2], fb[2];
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+      const uint32_t kt = tile + x * 16 * kKv4TokBytes + lane * 16, st = tile + kTileS + (16 * x + tok_k) * kKv4ScaleBytes;
+      const uint4 kk[2] = {lds_v4(kt), lds_v4(kt + 8 * kKv4TokBytes)};
+      const int grp = kSingle ? 4 * (c & 1) + (c >> 1) : 2 * c;   // scale groups: of columns 2 c and 2 c + 1, or of the lane's channels
+      uint32_t f[2][2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        fa[h] = lds_u8(st + h) * 0x00800080u;
-        fb[h] = lds_u8(st + 8 * kKv4ScaleBytes + h) * 0x00800080u;
+        f[h][0] = lds_u8(st + 8 * h * kKv4ScaleBytes + grp);
+        f[h][1] = lds_u8(st + 8 * h * kKv4ScaleBytes + grp + (kSingle ? 2 : 1));
+        if (!kSingle) {   // fp16 pairs (scale, scale): code << 7 in both halves, by a product (the ALU is the busiest unit here)
+          f[h][0] *= 0x00800080u;
+          f[h][1] *= 0x00800080u;
+        }
       }
-      const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         uint32_t a[4], b[4];
-        e2m1x8_to_f16x2(wa[w], a);
-        e2m1x8_to_f16x2(wb[w], b);
+        e2m1x8_to_f16x2(w == 0 ? kk[0].x : w == 1 ? kk[0].y : w == 2 ? kk[0].z : kk[0].w, a);
+        e2m1x8_to_f16x2(w == 0 ? kk[1].x : w == 1 ? kk[1].y : w == 2 ? kk[1].z : kk[1].w, b);
+        if (!kSingle) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          a[j] = mul_f16x2(a[j], fa[w >> 1]);
-          b[j] = mul_f16x2(b[j], fb[w >> 1]);
+          for (int j = 0; j < 4; ++j) {
+            a[j] = mul_f16x2(a[j], f[0][w >> 1]);
+            b[j] = mul_f16x2(b[j], f[1][w >> 1]);
+          }
         }
-        mma_acc(s[x], a[0], b[0], a[1], b[1], qb[2 * w][0], qb[2 * w][1]);
-        mma_acc(s[x], a[2], b[2], a[3], b[3], qb[2 * w + 1][0], qb[2 * w + 1][1]);
+        mma_acc(s, a[0], b[0], a[1], b[1], qb[2 * w][0], qb[2 * w][1]);
+        mma_acc(s, a[2], b[2], a[3], b[3], qb[2 * w + 1][0], qb[2 * w + 1][1]);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (kSingle) {   // the two groups of this lane's columns, then the other lanes' (a code << 20 is scale * 2^-112 in fp32)
+          float v = s[2 * h] * (__uint_as_float(f[h][0] << 20) * 0x1p112f);
+          v = fmaf(s[2 * h + 1], __uint_as_float(f[h][1] << 20) * 0x1p112f, v);
+          v += __shfl_xor_sync(kFull, v, 1);
+          v += __shfl_xor_sync(kFull, v, 2);
+          s[2 * h] = v;
+        }
+#pragma unroll
+        for (int j = 0; j < H; ++j) t[x][h][j] = fmaf(s[2 * h + j], sc[j], -base[j]);
       }
     }
-    // ---- softmax: exponents relative to the reference, lifted ----
-    float t[2][4];
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) t[x][j] = fmaf(s[x][j], sc[j & 1], -base[j & 1]);
     if (SET == kSetUnion || vm != kFull) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          bool on = (vm >> (16 * x + tok_k + (j < 2 ? 0 : 8))) & 1u;
-          if (SET == kSetUnion) on = on && ((flags >> (2 * c + (j & 1))) & 1u);
-          if (!on) t[x][j] = -INFINITY;
-        }
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < H; ++j) {
+            bool on = (vm >> (16 * x + 8 * h + tok_k)) & 1u;
+            if (SET == kSetUnion) on = on && ((flags >> head[j]) & 1u);
+            if (!on) t[x][h][j] = -INFINITY;
+          }
     }
     // (V of the first 16 tokens is read here, so that the loads have arrived behind the branch)
     const uint32_t va = tile + kTileV + c * kKv4TokBytes + (((g >> 1) ^ (c & 2)) << 4) + (g & 1) * 8;
@@ -366,13 +406,14 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
       w[j] = lds_v2(va + j * 4 * kKv4TokBytes);
       f[j] = lds_u8(vs + j * 4 * kKv4ScaleBytes);
     }
-    const float top0 = fmaxf(fmaxf(t[0][0], t[0][2]), fmaxf(t[1][0], t[1][2])), top1 = fmaxf(fmaxf(t[0][1], t[0][3]), fmaxf(t[1][1], t[1][3]));
-    if (__any_sync(kFull, fmaxf(top0, top1) > limit)) {
+    float top[H];
+#pragma unroll
+    for (int j = 0; j < H; ++j) top[j] = fmaxf(fmaxf(t[0][0][j], t[0][1][j]), fmaxf(t[1][0][j], t[1][1][j]));
+    if (__any_sync(kFull, fmaxf(top[0], top[H - 1]) > limit)) {
       // a score lies further above the reference than it may (or there is none yet): the maximum becomes the reference
       limit = kLift + kLag;
-      float top[2] = {top0, top1};
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < H; ++j) {
 #pragma unroll
         for (int x = 4; x <= 16; x <<= 1) top[j] = fmaxf(top[j], __shfl_xor_sync(kFull, top[j], x));
         // (a column without a token so far has the reference -inf, for which `base` holds 0)
@@ -381,31 +422,36 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
         const float corr = empty[j] ? 0.f : fast_ex2(-rise);
         if (top[j] == -INFINITY && empty[j]) limit = -INFINITY; else empty[j] = false;
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
+        for (int x = 0; x < kTilesO; ++x) {
           o[x][j] *= corr;
           o[x][2 + j] *= corr;
+          if (kSingle) {
+            o[x][1] *= corr;
+            o[x][3] *= corr;
+          }
         }
         l[j] *= corr;
         base[j] = raised;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          t[x][j] -= rise;
-          t[x][2 + j] -= rise;
+          t[x][0][j] -= rise;
+          t[x][1][j] -= rise;
         }
       }
     }
-    uint32_t pb[2][2];
+    uint32_t pb[2][2];   // P^T of 16 tokens: rows 2 c, 2 c + 1 (and + 8) of column g
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      float p[4];
+    for (int x = 0; x < 2; ++x)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        p[j] = fast_ex2(t[x][j]);
-        l[j & 1] += p[j];
+      for (int h = 0; h < 2; ++h) {
+        float p[H];
+#pragma unroll
+        for (int j = 0; j < H; ++j) {
+          p[j] = fast_ex2(t[x][h][j]);
+          l[j] += p[j];
+        }
+        pb[x][h] = transpose8x8(pack_f16x2(p[0], p[H - 1]));
       }
-      pb[x][0] = transpose8x8(pack_f16x2(p[0], p[1]));
-      pb[x][1] = transpose8x8(pack_f16x2(p[2], p[3]));
-    }
     // ---- O^T += V^T P^T: tokens c, c + 4, c + 8, c + 12 of each 16 ----
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -416,20 +462,38 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
           f[j] = lds_u8(vs + (16 * x + 4 * j) * kKv4ScaleBytes);
         }
       }
-      const uint32_t f01 = f[1] * 0x00800000u + f[0] * 0x80u, f23 = f[3] * 0x00800000u + f[2] * 0x80u;
-      constexpr uint32_t kLow = 0x0f0f0f0fu;
+      if constexpr (kPairs) {
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh) {
-        const uint32_t w0 = hh ? w[0].y : w[0].x, w1 = hh ? w[1].y : w[1].x, w2 = hh ? w[2].y : w[2].x, w3 = hh ? w[3].y : w[3].x;
-        uint32_t e01[4], d01[4], e23[4], d23[4];   // even and odd channels of the token pairs
-        e2m1x8_to_f16x2((w0 & kLow) | ((w1 << 4) & ~kLow), e01);
-        e2m1x8_to_f16x2(((w0 >> 4) & kLow) | (w1 & ~kLow), d01);
-        e2m1x8_to_f16x2((w2 & kLow) | ((w3 << 4) & ~kLow), e23);
-        e2m1x8_to_f16x2(((w2 >> 4) & kLow) | (w3 & ~kLow), d23);
+        for (int k = 0; k < 2; ++k) {   // tokens c + 4 k and c + 4 k + 8
+          const uint32_t b0 = __byte_perm(pb[x][0], 0u, place[k]), b1 = __byte_perm(pb[x][1], 0u, place[k]);
+          const uint32_t s0 = f[k] * 0x00800080u, s1 = f[k + 2] * 0x00800080u;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          mma_acc(o[4 * hh + j], mul_f16x2(e01[j], f01), mul_f16x2(d01[j], f01), mul_f16x2(e23[j], f23), mul_f16x2(d23[j], f23),
-                  pb[x][0], pb[x][1]);
+          for (int hh = 0; hh < 2; ++hh) {
+            uint32_t a[4], b[4];
+            e2m1x8_to_f16x2(hh ? w[k].y : w[k].x, a);
+            e2m1x8_to_f16x2(hh ? w[k + 2].y : w[k + 2].x, b);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              mma_acc(o[2 * hh + i], mul_f16x2(a[2 * i], s0), mul_f16x2(a[2 * i + 1], s0), mul_f16x2(b[2 * i], s1),
+                      mul_f16x2(b[2 * i + 1], s1), b0, b1);
+          }
+        }
+      } else {
+        const uint32_t f01 = f[1] * 0x00800000u + f[0] * 0x80u, f23 = f[3] * 0x00800000u + f[2] * 0x80u;
+        constexpr uint32_t kLow = 0x0f0f0f0fu;
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          const uint32_t w0 = hh ? w[0].y : w[0].x, w1 = hh ? w[1].y : w[1].x, w2 = hh ? w[2].y : w[2].x, w3 = hh ? w[3].y : w[3].x;
+          uint32_t e01[4], d01[4], e23[4], d23[4];   // even and odd channels of the token pairs
+          e2m1x8_to_f16x2((w0 & kLow) | ((w1 << 4) & ~kLow), e01);
+          e2m1x8_to_f16x2(((w0 >> 4) & kLow) | (w1 & ~kLow), d01);
+          e2m1x8_to_f16x2((w2 & kLow) | ((w3 << 4) & ~kLow), e23);
+          e2m1x8_to_f16x2(((w2 >> 4) & kLow) | (w3 & ~kLow), d23);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            mma_acc(o[4 * hh + j], mul_f16x2(e01[j], f01), mul_f16x2(d01[j], f01), mul_f16x2(e23[j], f23), mul_f16x2(d23[j], f23),
+                    pb[x][0], pb[x][1]);
+        }
       }
     }
   }
@@ -439,18 +503,23 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
 
   float* red = reinterpret_cast<float*>(smem_rows4);   // [kWarps][G][kPartial]
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+  for (int j = 0; j < H; ++j) {
 #pragma unroll
     for (int x = 4; x <= 16; x <<= 1) l[j] += __shfl_xor_sync(0xffffffffu, l[j], x);
-    const int h = 2 * c + j;
-    if (h < G) {
-      float* rw = red + (warp * G + h) * kPartial;
+    // (the column is the head's first, or of a pair that counts; a single head's columns are all alike: 0 and 4 count)
+    if (head[j] < G && !(kSingle && (c & 1))) {
+      float* rw = red + (warp * G + head[j]) * kPartial;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        rw[16 * g + 2 * i] = o[i][j];
-        rw[16 * g + 2 * i + 1] = o[i][2 + j];
+      for (int i = 0; i < kTilesO; ++i) {
+        if (kPairs) {
+          rw[16 * g + 4 * i + (c >> 1)] = o[i][j];
+          rw[16 * g + 4 * i + 2 + (c >> 1)] = o[i][2 + j];
+        } else {
+          rw[16 * g + 2 * i] = o[i][j];
+          rw[16 * g + 2 * i + 1] = o[i][2 + j];
+        }
       }
-      if (g == 0) {
+      if (g == 0 && (!kPairs || c < 2)) {
         rw[kHeadDim] = empty[j] ? -INFINITY : base[j];
         rw[kHeadDim + 1] = l[j];
       }
