@@ -234,7 +234,8 @@ rtp_status rtp_index_keys(rtp_ctx* ctx, const rtp_params* params, const rtp_cach
  * tok_seq, tok_pos DEVICE int32 [T].  Copies every row to
  * k_pages / v_pages[block_table[seq][pos/64], head, pos%64, :].  Tokens whose sequence or page
  * is out of range are skipped and RTP_ERR_INVALID is recorded in *status.  seq_lens is not
- * modified (it belongs to the caller). */
+ * modified (it belongs to the caller).  A position named twice in one call is left with a mixture of both rows (of their codes
+ * and scales on a 4-bit cache, which is then neither's value). */
 rtp_status rtp_kv_append(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache,
                          const void* k_new, const void* v_new, const int32_t* tok_seq,
                          const int32_t* tok_pos, int64_t T, int32_t* status, void* stream);

@@ -402,6 +402,58 @@ def test_prompt_through_expanded_pages():
     assert (pre.float() - c.out.float()).abs().max() <= 2e-2
 
 
+def test_offsets_beyond_32_bits():
+    """A pool whose codes take more than 4 GB: append, attention, expansion and page copies at its far end."""
+    h = _h()
+    n_kv, N, L = 8, 140000, 200                                # 32 KB of K codes a page: 4.6 GB
+    rng = np.random.default_rng(0)
+    k, v = (rng.standard_normal((L, n_kv, 128)) for _ in range(2))
+    c = h.Cache4([L], n_kv=n_kv, group=2, ret_kv=(7,), local_kv=(3,), window=90, k=[k], v=[v])
+    kp, vp = (torch.empty((N, n_kv, 64, 64), dtype=torch.uint8, device="cuda") for _ in range(2))
+    sp = torch.empty((N, n_kv, 64, 16), dtype=torch.uint8, device="cuda")
+    table = h.dev_i32([[N - 1, N - 3, 5, N - 2]])
+    cache = rb.make_cache(kp, vp, None, table, c.d_lens, kv_scales=sp)
+    p = (c.ctx, c.params, cache)
+    rb.rtp_kv_append(*p, h.dev_bf16(k), h.dev_bf16(v), h.dev_i32([0] * L), h.dev_i32(range(L)), c.status)
+    rb.rtp_cache_copy_pages(*p, h.dev_i32([N - 1, 5]), h.dev_i32([7, N - 9]), c.status)
+    for row in ([N - 1, N - 3, 5, N - 2], [7, N - 3, N - 9, N - 2]):
+        table.copy_(h.dev_i32([row]))
+        c.out.fill_(-77), c.lse.fill_(-77)
+        rb.rtp_dense_attn_decode(*p, *c.args()[3:], None, c.out, c.lse, c.ws, c.status)
+        c.check(range(16), lambda r, hd: range(L))
+        idx = rng.permutation(L)[:77]
+        rb.rtp_sparse_attn_decode(*p, *c.args()[3:], h.dev_i32(np.tile(idx, (1, 2, 1))), h.dev_i32([[77, 77]]), c.out, c.lse, c.ws, c.status)
+        rb.rtp_local_attn(*p, *c.args()[3:], 0, 0, 1, c.out, c.lse, c.ws, c.status)
+        c.check(range(16), lambda r, hd: idx if hd >= 14 else [t for t in range(L) if hd not in (6, 7) or t < 4 or t >= L - 90])
+    kx, vx = (torch.zeros((4, n_kv, 64, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    rb.rtp_kv_expand(*p, table[0], None, kx, vx, c.status)
+    got = vx.transpose(1, 2).reshape(256, n_kv, 128)[:L].double().cpu().numpy()
+    assert np.array_equal(got, c.v[0]) and c.code() == rb.RTP_OK
+
+
+def test_two_calls_at_once():
+    """Calls on two streams, each with a workspace of its own, over the same cache."""
+    h = _h()
+    c = h.Cache4([3000, 2500], n_kv=2, group=4, ret_kv=(0,), local_kv=(1,), window=1000, seed=12)
+    idx, cnt = _lists(c, np.random.default_rng(0), [700, 900], 1000)
+    d_idx, d_cnt = h.dev_i32(idx), h.dev_i32(cnt)
+    other = torch.empty_like(c.ws)
+    side = torch.cuda.Stream()
+    sets = lambda r, hd: idx[r, hd, :cnt[r, hd]] if hd < 4 else [t for t in range(c.lens[r]) if t < 4 or t >= c.lens[r] - 1000]
+    ref = None
+    for _ in range(20):
+        c.out.fill_(-77), c.lse.fill_(-77)
+        side.wait_stream(torch.cuda.current_stream())
+        rb.rtp_local_attn(*c.args(), 0, 0, 2, c.out, c.lse, other, c.status, stream=side)
+        rb.rtp_sparse_attn_decode(*c.args(), d_idx, d_cnt, c.out, c.lse, c.ws, c.status)
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        if ref is None:
+            c.check(range(8), sets)
+            ref = c.out.clone(), c.lse.clone()
+        assert torch.equal(c.out, ref[0]) and torch.equal(c.lse, ref[1])
+
+
 def test_refusals():
     h = _h()
     c = h.Cache4([200], n_kv=2, group=2, ret_kv=(0,), local_kv=(1,))

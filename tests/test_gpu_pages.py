@@ -173,6 +173,53 @@ def test_wrong_requests_are_reported_and_skipped():
     d.same()
 
 
+def test_thousands_of_requests_in_one_call():
+    """More requests than the planning block has threads, sharing pages in groups of three."""
+    n = 3000
+    pool = Pool(9000, n, 3)
+    for i in range(0, n, 3):
+        pool.table[i:i + 3, 0] = i
+        pool.refs[i] = 3
+        pool.lens[i:i + 3] = 1 + i % 63
+    d = Device(pool, n_kv=1, n_ih=1, kv=False)
+    order = np.random.default_rng(0).permutation(n)
+    add = np.random.default_rng(1).integers(0, 100, n)
+    for x in (d, pool):
+        x.reserve(order, add)
+    assert d.code() == rb.RTP_OK
+    d.same()
+    pool.check()
+
+
+def test_broken_tables_are_reported():
+    """Entries that name no page, or a page that nobody holds: reported, and nothing outside the arrays is touched."""
+    pool = Pool(40, 3, 4)
+    for x in (pool,):
+        x.reserve([0, 1], [200, 100])
+    d = Device(pool)
+    table = d.table.clone()
+    d.table[0, 1] = 1 << 20
+    d.table[1, 1] = 39                                     # free
+    refs = d.refs.clone()
+    d.compact()
+    assert d.code() == rb.RTP_ERR_INVALID
+    assert d.table[0, 1] == 1 << 20 and d.table[1, 1] == 39 and torch.equal(d.refs, refs)
+    d.free([0, 1])
+    assert d.code() == rb.RTP_ERR_INVALID
+    assert (d.table == -1).all() and int(d.refs.sum()) == 2      # the two pages whose entries were overwritten
+    d.table.copy_(table)
+    d.lens[0] = 130
+    d.table[0, 2] = 40                                     # the page that the next token would go to does not exist
+    d.reserve([0, 2], [1, 64])
+    assert d.code() == rb.RTP_ERR_INVALID and d.table[0, 2] == 40 and d.table[2, 0] >= 0
+    d.table[0] = torch.tensor([-1, -1, -1, 3])             # mapped behind an unmapped entry
+    d.lens[0] = 0
+    d.reserve([0], [256])
+    assert d.code() == rb.RTP_ERR_INVALID and d.table[0].tolist() == [-1, -1, -1, 3]
+    d.fork([0], [1])                                       # (1 has the pages that were put back above)
+    assert d.code() == rb.RTP_ERR_INVALID and torch.equal(d.table[1], table[1])
+
+
 @pytest.mark.parametrize("kind", range(len(KINDS)))
 def test_copy_pages(kind):
     pool = Pool(60, 1, 1)
