@@ -428,7 +428,7 @@ cudaError_t launch_attn_rows(const CacheView& cv, const Dims& d, const HeadMaps&
   if (rows.R == 0 || n_units == 0) return cudaSuccess;
   const int G = per_head ? 1 : d.group;
   const int64_t longest = max_set_len(d, set, sel_stride, max_len);
-  int n_splits = cv.kv_fp4 ? plan_splits4(rows.R * n_units, longest, sm_count)
+  int n_splits = cv.kv_fp4 ? plan_splits4(rows.R * n_units, longest, sm_count, set == kSetList)
                            : plan_splits(rows.R * n_units, longest, sm_count, set == kSetList);
   // never plan more splits than the workspace holds
   const size_t per_split = (size_t)rows.R * n_units * G * kPartial * sizeof(float);
@@ -485,7 +485,7 @@ cudaError_t launch_attn_rows_static(const CacheView& cv, const Dims& d, const He
   *needed_bytes = 0;
   if (rows.R == 0 || d.n_ret == 0) return cudaSuccess;
   const int64_t longest = max_set_len(d, kSetList, sel_stride, max_len);
-  int n_splits = cv.kv_fp4 ? plan_splits4(rows.R * d.n_ret, longest, sm_count) : plan_splits(rows.R * d.n_ret, longest, sm_count, true);
+  int n_splits = cv.kv_fp4 ? plan_splits4(rows.R * d.n_ret, longest, sm_count, true) : plan_splits(rows.R * d.n_ret, longest, sm_count, true);
   if (cv.kv_fp4)   // (never more splits than fit)
     n_splits = std::max(1, (int)std::min<size_t>(n_splits, kStaticScratchBytes / ((size_t)rows.R * d.n_ret * kPartial * sizeof(float))));
   const size_t need = n_splits > 1 ? (size_t)rows.R * d.n_ret * n_splits * kPartial * sizeof(float) : 0;

@@ -642,11 +642,23 @@ cudaError_t launch_typed4(const CacheView& cv, const Dims& d, const HeadMaps& hm
 
 }  // namespace
 
-// Split count of a call: one round of the four resident CTAs per SM, at least 128 tokens (a tile per warp) each.
-int plan_splits4(int64_t units, int64_t max_set, int sm_count) {
+// Split count of a call.  Long sets get one round of the four resident CTAs per SM.  Shorter ones get one or two CTAs per SM:
+// they finish as early, with fewer partial results to merge (8 KV heads, us with 1 / 2 / 4 CTAs per SM: 4K tokens 7.7 / 9.2 /
+// 11.6, 8K 9.2 / 9.7 / 12.4, 32K 17.5 / 15.7 / 17.4, 64K and more best with 4), as long as a CTA has at most 512 tokens (four
+// tiles per warp) per resident CTA; a list, whose tokens come one by one, 128.  No CTA gets fewer than 128 tokens (a tile per
+// warp), and the four warps equally many tiles where the count is free.
+int plan_splits4(int64_t units, int64_t max_set, int sm_count, bool list) {
   if (units <= 0) return 1;
-  const int64_t want = 4LL * sm_count / units, cap = (max_set + 127) / 128;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, cap), kMaxSplits));
+  const int64_t tiles = (max_set + kTileTok - 1) / kTileTok, cap = std::max<int64_t>(1, (tiles + kWarps - 1) / kWarps);
+  const int64_t limit = (list ? 1 : 4) * kWarps;   // tiles
+  int64_t s = 1, step = kTilesPerPage;
+  for (int k : {1, 2, 4}) {
+    s = std::min<int64_t>(std::max<int64_t>(1, k * (int64_t)sm_count / units), cap);
+    step = k < 4 ? kWarps : kTilesPerPage;
+    if (tiles <= s * k * limit) break;
+  }
+  const int64_t per = std::max<int64_t>(1, (tiles + s * step - 1) / (s * step)) * step;
+  return (int)std::min<int64_t>(std::max<int64_t>(1, (tiles + per - 1) / per), kMaxSplits);
 }
 
 cudaError_t launch_attn_rows4(const CacheView& cv, const Dims& d, const HeadMaps& hm, const Rows& rows, int set, int n_units,
