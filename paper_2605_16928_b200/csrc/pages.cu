@@ -18,9 +18,20 @@ constexpr int kPlanWarps = kPlanThreads / 32;
 constexpr int kEarlyPages = kPlanWarps * 8 * 128;
 constexpr int kRowThreads = 256;
 constexpr int kRowVec = 4;                                        // table entries in flight per thread
-constexpr int kCopyThreads = 256;
-constexpr int kCopyVec = 8;                                       // 16-byte pieces in flight per thread
-constexpr int kPiece = kCopyThreads * kCopyVec * 16;              // bytes of a page that a CTA copies at a time
+// Bytes of a page that a CTA copies at a time: its threads x 16-byte loads in flight per thread.  A few pages (the copies of
+// a reserve call, 64 pages) are spread over more SMs by small CTAs; a long move runs better in large ones whose stores do
+// not stay in L2 (1.6 GB moved: 265 us with 256 x 8, 256 with 512 x 4, 250 with 1024 x 4, and 247 = 6.5 TB/s with 32 CTAs per SM
+// in the grid instead of 8: the last pieces are dealt more evenly).
+struct SmallCopy {
+  static constexpr int kThreads = 256, kVec = 8;
+  static constexpr bool kStream = false;
+};
+struct LargeCopy {
+  static constexpr int kThreads = 1024, kVec = 4;
+  static constexpr bool kStream = true;
+};
+template <class C>
+constexpr int kPieceOf = C::kThreads * C::kVec * 16;
 
 // Workspace: counts, then lists.
 struct PlanHead {
@@ -31,6 +42,7 @@ __device__ __forceinline__ bool page_ok(int p, int num_pages) { return (unsigned
 
 // ---- contents ------------------------------------------------------------------------------------
 // Copies piece `piece` (counted over the arrays of a page) of page src to page dst.
+template <class C>
 __device__ __forceinline__ void copy_piece(const PageArrays& pa, int64_t src, int64_t dst, int piece) {
   int a = 0;
 #pragma unroll
@@ -40,18 +52,22 @@ __device__ __forceinline__ void copy_piece(const PageArrays& pa, int64_t src, in
   }
   const char* s = pa.base[a] + src * pa.bytes[a];
   char* d = pa.base[a] + dst * pa.bytes[a];
-  const int64_t at = (int64_t)piece * kPiece + threadIdx.x * 16;
-  uint4 v[kCopyVec];
+  constexpr int kStep = C::kThreads * 16;
+  const int64_t at = (int64_t)piece * kPieceOf<C> + threadIdx.x * 16;
+  uint4 v[C::kVec];
 #pragma unroll
-  for (int i = 0; i < kCopyVec; ++i)
-    if (at + i * kCopyThreads * 16 < pa.bytes[a]) v[i] = ld_stream_v4(s + at + i * kCopyThreads * 16);
+  for (int i = 0; i < C::kVec; ++i)
+    if (at + i * kStep < pa.bytes[a]) v[i] = ld_stream_v4(s + at + i * kStep);
 #pragma unroll
-  for (int i = 0; i < kCopyVec; ++i)
-    if (at + i * kCopyThreads * 16 < pa.bytes[a]) *reinterpret_cast<uint4*>(d + at + i * kCopyThreads * 16) = v[i];
+  for (int i = 0; i < C::kVec; ++i)
+    if (at + i * kStep < pa.bytes[a]) {
+      uint4* to = reinterpret_cast<uint4*>(d + at + i * kStep);
+      if (C::kStream) __stcs(to, v[i]); else *to = v[i];
+    }
 }
 
 // n pairs given by the caller, or as many as head->n_pairs says.
-__global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_constant__ PageArrays pa, const int num_pages,
+__global__ void __launch_bounds__(SmallCopy::kThreads) copy_pages_kernel(const __grid_constant__ PageArrays pa, const int num_pages,
                                                                   const int32_t* __restrict__ src,
                                                                   const int32_t* __restrict__ dst, const int64_t n,
                                                                   const PlanHead* __restrict__ head, int32_t* status) {
@@ -64,7 +80,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_c
       if (threadIdx.x == 0) set_status(status, RTP_ERR_INVALID);
       continue;
     }
-    if (s != d) copy_piece(pa, s, d, (int)(u % pa.total_pieces));
+    if (s != d) copy_piece<SmallCopy>(pa, s, d, (int)(u % pa.total_pieces));
   }
 }
 
@@ -458,7 +474,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const int32_
   }
 }
 
-__global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const __grid_constant__ PageArrays pa, const int num_pages,
+__global__ void __launch_bounds__(LargeCopy::kThreads) compact_move_kernel(const __grid_constant__ PageArrays pa, const int num_pages,
                                                                     int32_t* __restrict__ table, const int64_t n_entries,
                                                                     int32_t* __restrict__ refs, const PlanHead* __restrict__ head,
                                                                     const int32_t* __restrict__ src,
@@ -466,7 +482,7 @@ __global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const __grid
                                                                     const int32_t* __restrict__ move, int32_t* status) {
   chain_wait();
   const int n_pairs = head->n_pairs, n_used = head->n_used;
-  const int64_t t0 = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x, step = (int64_t)gridDim.x * kCopyThreads;
+  const int64_t t0 = (int64_t)blockIdx.x * LargeCopy::kThreads + threadIdx.x, step = (int64_t)gridDim.x * LargeCopy::kThreads;
   for (int64_t i = t0; i < n_entries; i += step) {
     const int e = table[i];
     if (e < n_used) continue;
@@ -481,7 +497,7 @@ __global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const __grid
   const int64_t total = (int64_t)n_pairs * pa.total_pieces;
   for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
     const int64_t i = u / pa.total_pieces;
-    copy_piece(pa, src[i], dst[i], (int)(u % pa.total_pieces));
+    copy_piece<LargeCopy>(pa, src[i], dst[i], (int)(u % pa.total_pieces));
   }
 }
 
@@ -489,25 +505,29 @@ unsigned copy_grid(const PageArrays& pa, int64_t pairs) {
   return (unsigned)std::max<int64_t>(1, std::min<int64_t>(pairs * pa.total_pieces, (int64_t)current_sm_count(148) * 8));
 }
 
-}  // namespace
-
-void finish_page_arrays(PageArrays* pa) {
-  pa->total_pieces = 0;
+// Cuts the arrays into the pieces of the copies.
+template <class C>
+PageArrays in_pieces(PageArrays pa) {
+  pa.total_pieces = 0;
   for (int a = 0; a < kPageArrays; ++a) {
-    pa->pieces[a] = (int)((pa->bytes[a] + kPiece - 1) / kPiece);
-    pa->total_pieces += pa->pieces[a];
+    pa.pieces[a] = (int)((pa.bytes[a] + kPieceOf<C> - 1) / kPieceOf<C>);
+    pa.total_pieces += pa.pieces[a];
   }
+  return pa;
 }
+
+}  // namespace
 
 size_t pages_workspace_bytes(int64_t num_pages, int64_t n_seqs) {
   return 256 + sizeof(int32_t) * (size_t)(3 * ((num_pages + 63) & ~(int64_t)63) + 2 * ((n_seqs + 63) & ~(int64_t)63));
 }
 
-cudaError_t launch_copy_pages(const PageArrays& pa, int num_pages, const int32_t* src, const int32_t* dst, int64_t n,
+cudaError_t launch_copy_pages(const PageArrays& arrays, int num_pages, const int32_t* src, const int32_t* dst, int64_t n,
                               int32_t* status, cudaStream_t st) {
+  const PageArrays pa = in_pieces<SmallCopy>(arrays);
   if (n == 0 || pa.total_pieces == 0) return cudaSuccess;
   const unsigned grid = (unsigned)std::min<int64_t>(n * pa.total_pieces, 1 << 20);
-  (void)launch_chained(copy_pages_kernel, dim3(grid), dim3(kCopyThreads), 0, st, pa, num_pages, src, dst, n,
+  (void)launch_chained(copy_pages_kernel, dim3(grid), dim3(SmallCopy::kThreads), 0, st, pa, num_pages, src, dst, n,
                        (const PlanHead*)nullptr, status);
   return cudaGetLastError();
 }
@@ -528,10 +548,11 @@ cudaError_t launch_free(int32_t* table, int32_t* seq_lens, int32_t* refs, int nu
   return cudaGetLastError();
 }
 
-cudaError_t launch_reserve(const PageArrays& pa, int32_t* table, const int32_t* seq_lens, int32_t* refs, int num_pages, int batch,
+cudaError_t launch_reserve(const PageArrays& arrays, int32_t* table, const int32_t* seq_lens, int32_t* refs, int num_pages, int batch,
                            int max_pages, const int32_t* seqs, const int32_t* n_tokens, int n, void* ws, int32_t* status,
                            cudaStream_t st) {
   if (n == 0) return cudaSuccess;
+  const PageArrays pa = in_pieces<SmallCopy>(arrays);
   static PerDeviceOnce once;
   cudaError_t e = set_dyn_smem_once(reserve_kernel, (int)sizeof(ReserveShared), once);
   if (e != cudaSuccess) return e;
@@ -542,13 +563,14 @@ cudaError_t launch_reserve(const PageArrays& pa, int32_t* table, const int32_t* 
                        batch, max_pages, seqs, n_tokens, n, head, src, dst, status);
   e = cudaGetLastError();
   if (e != cudaSuccess || pa.total_pieces == 0) return e;
-  (void)launch_chained(copy_pages_kernel, dim3(copy_grid(pa, n)), dim3(kCopyThreads), 0, st, pa, num_pages, src, dst, (int64_t)0,
+  (void)launch_chained(copy_pages_kernel, dim3(copy_grid(pa, n)), dim3(SmallCopy::kThreads), 0, st, pa, num_pages, src, dst, (int64_t)0,
                        (const PlanHead*)head, status);
   return cudaGetLastError();
 }
 
-cudaError_t launch_compact(const PageArrays& pa, int32_t* table, int64_t n_entries, int32_t* refs, int num_pages,
+cudaError_t launch_compact(const PageArrays& arrays, int32_t* table, int64_t n_entries, int32_t* refs, int num_pages,
                            int32_t* n_used, void* ws, int32_t* status, cudaStream_t st) {
+  const PageArrays pa = in_pieces<LargeCopy>(arrays);
   PlanHead* head = reinterpret_cast<PlanHead*>(ws);
   const int64_t pad = ((int64_t)num_pages + 63) & ~(int64_t)63;
   int32_t* src = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(ws) + 256);
@@ -556,7 +578,7 @@ cudaError_t launch_compact(const PageArrays& pa, int32_t* table, int64_t n_entri
   (void)launch_chained(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, refs, num_pages, head, src, dst, move, n_used);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  (void)launch_chained(compact_move_kernel, dim3((unsigned)current_sm_count(148) * 8), dim3(kCopyThreads), 0, st, pa, num_pages,
+  (void)launch_chained(compact_move_kernel, dim3((unsigned)current_sm_count(148) * 32), dim3(LargeCopy::kThreads), 0, st, pa, num_pages,
                        table, n_entries, refs, head, src, dst, move, status);
   return cudaGetLastError();
 }

@@ -191,7 +191,6 @@ const char* page_arrays(const rtp_cache* c, const CacheView& cv, PageArrays* pa)
   const int64_t sc = c->k_pages && cv.kv_fp4 ? (int64_t)cv.n_kv * kPage * (kHeadDim / 8) : 0;
   const int64_t ik = c->ikey_pages ? (int64_t)cv.n_ih * kPage * kIndexDim * (cv.ikey_fp8 ? 1 : 2) : 0;
   *pa = PageArrays{{(char*)c->k_pages, (char*)c->v_pages, (char*)c->kv_scales, (char*)c->ikey_pages}, {kv, kv, sc, ik}, {}, 0};
-  finish_page_arrays(pa);
   return nullptr;
 }
 

@@ -188,9 +188,8 @@ constexpr int kReserveMax = 4096;   // sequences of one reserve call
 struct PageArrays {
   char* base[kPageArrays];
   int64_t bytes[kPageArrays];   // of one page
-  int32_t pieces[kPageArrays], total_pieces;
+  int32_t pieces[kPageArrays], total_pieces;   // (filled in by the launchers)
 };
-void finish_page_arrays(PageArrays* pa);
 size_t pages_workspace_bytes(int64_t num_pages, int64_t n_seqs);
 cudaError_t launch_copy_pages(const PageArrays& pa, int num_pages, const int32_t* src, const int32_t* dst, int64_t n,
                               int32_t* status, cudaStream_t st);
