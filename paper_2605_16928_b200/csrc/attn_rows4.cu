@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
   const int64_t r = blockIdx.x / n_units;
   const int u = blockIdx.x % n_units;
   const int split = blockIdx.y;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = __shfl_sync(kFull, (int)(threadIdx.x >> 5), 0);   // (uniform for the compiler)
   const int g = lane >> 2, c = lane & 3;
 
   int qh0, kvh;
@@ -201,7 +201,6 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
     empty[j] = head[j] < G;
   }
 
-  const int64_t bt_base = (int64_t)seq * cv.max_pages;
   const int kslot = cv.kv_slot[kvh];
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem_rows4) + warp * kStages * kTileBytes;
   const uint8_t* kp = reinterpret_cast<const uint8_t*>(cv.k);
@@ -239,7 +238,11 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
     if (SET == kSetLocal) return tile < sink_tiles ? tile * kTileTok : (wlo / kTileTok + tile - sink_tiles) * kTileTok;
     return tile * kTileTok;
   };
-  auto raw_phys = [&](int tok) -> int { return tok >= 0 ? __ldg(cv.block_table + bt_base + page_entry(cv, tok >> kPageShift)) : 0; };
+  const int32_t* table = cv.block_table + (int64_t)seq * cv.max_pages;
+  auto raw_phys = [&](int tok) -> int {   // (only the local heads' pool can be a ring)
+    const int page = tok >> kPageShift;
+    return tok >= 0 ? __ldg(table + (SET == kSetLocal ? page_entry(cv, page) : page)) : 0;
+  };
   // tokens of the tile that belong to the set, one bit each
   auto valid_mask = [&](int i, int tok) -> uint32_t {
     if (SET == kSetList) return __ballot_sync(kFull, tok >= 0);
@@ -250,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
     }
     const int a = lo - tok, b = tok + kTileTok - hi;   // tokens missing at the front and at the end
     uint32_t m = kFull;
-    if (a > 0) m = a < kTileTok ? m << a : 0u;
+    if (SET == kSetLocal && a > 0) m = a < kTileTok ? m << a : 0u;
     if (b > 0) m = b < kTileTok ? m & (kFull >> b) : 0u;
     return m;
   };
