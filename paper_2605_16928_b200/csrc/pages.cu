@@ -69,18 +69,18 @@ __device__ __forceinline__ void copy_piece(const PageArrays& pa, int64_t src, in
 // n pairs given by the caller, or as many as head->n_pairs says.
 __global__ void __launch_bounds__(SmallCopy::kThreads) copy_pages_kernel(const __grid_constant__ PageArrays pa, const int num_pages,
                                                                   const int32_t* __restrict__ src,
-                                                                  const int32_t* __restrict__ dst, const int64_t n,
+                                                                  const int32_t* __restrict__ dst, const int n,
                                                                   const PlanHead* __restrict__ head, int32_t* status) {
   chain_wait();
-  const int64_t total = (head ? (int64_t)head->n_pairs : n) * pa.total_pieces;
-  for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
-    const int64_t i = u / pa.total_pieces;
+  const unsigned pieces = pa.total_pieces, total = (head ? head->n_pairs : n) * pieces;   // (below 2^31: checked by the caller)
+  for (unsigned u = blockIdx.x; u < total; u += gridDim.x) {
+    const unsigned i = u / pieces;
     const int s = src[i], d = dst[i];
     if (!page_ok(s, num_pages) || !page_ok(d, num_pages)) {
       if (threadIdx.x == 0) set_status(status, RTP_ERR_INVALID);
       continue;
     }
-    if (s != d) copy_piece<SmallCopy>(pa, s, d, (int)(u % pa.total_pieces));
+    if (s != d) copy_piece<SmallCopy>(pa, s, d, (int)(u - i * pieces));
   }
 }
 
@@ -494,10 +494,10 @@ __global__ void __launch_bounds__(LargeCopy::kThreads) compact_move_kernel(const
     refs[dst[i]] = refs[src[i]];
     refs[src[i]] = 0;
   }
-  const int64_t total = (int64_t)n_pairs * pa.total_pieces;
-  for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
-    const int64_t i = u / pa.total_pieces;
-    copy_piece<LargeCopy>(pa, src[i], dst[i], (int)(u % pa.total_pieces));
+  const unsigned pieces = pa.total_pieces, total = n_pairs * pieces;   // (below 2^31: checked by the caller)
+  for (unsigned u = blockIdx.x; u < total; u += gridDim.x) {
+    const unsigned i = u / pieces;
+    copy_piece<LargeCopy>(pa, src[i], dst[i], (int)(u - i * pieces));
   }
 }
 
@@ -526,8 +526,9 @@ cudaError_t launch_copy_pages(const PageArrays& arrays, int num_pages, const int
                               int32_t* status, cudaStream_t st) {
   const PageArrays pa = in_pieces<SmallCopy>(arrays);
   if (n == 0 || pa.total_pieces == 0) return cudaSuccess;
+  if (n >= ((int64_t)1 << 31) / pa.total_pieces) return cudaErrorNotSupported;
   const unsigned grid = (unsigned)std::min<int64_t>(n * pa.total_pieces, 1 << 20);
-  (void)launch_chained(copy_pages_kernel, dim3(grid), dim3(SmallCopy::kThreads), 0, st, pa, num_pages, src, dst, n,
+  (void)launch_chained(copy_pages_kernel, dim3(grid), dim3(SmallCopy::kThreads), 0, st, pa, num_pages, src, dst, (int)n,
                        (const PlanHead*)nullptr, status);
   return cudaGetLastError();
 }
@@ -563,7 +564,7 @@ cudaError_t launch_reserve(const PageArrays& arrays, int32_t* table, const int32
                        batch, max_pages, seqs, n_tokens, n, head, src, dst, status);
   e = cudaGetLastError();
   if (e != cudaSuccess || pa.total_pieces == 0) return e;
-  (void)launch_chained(copy_pages_kernel, dim3(copy_grid(pa, n)), dim3(SmallCopy::kThreads), 0, st, pa, num_pages, src, dst, (int64_t)0,
+  (void)launch_chained(copy_pages_kernel, dim3(copy_grid(pa, n)), dim3(SmallCopy::kThreads), 0, st, pa, num_pages, src, dst, 0,
                        (const PlanHead*)head, status);
   return cudaGetLastError();
 }
@@ -571,6 +572,7 @@ cudaError_t launch_reserve(const PageArrays& arrays, int32_t* table, const int32
 cudaError_t launch_compact(const PageArrays& arrays, int32_t* table, int64_t n_entries, int32_t* refs, int num_pages,
                            int32_t* n_used, void* ws, int32_t* status, cudaStream_t st) {
   const PageArrays pa = in_pieces<LargeCopy>(arrays);
+  if ((int64_t)num_pages * pa.total_pieces >= (int64_t)1 << 31) return cudaErrorNotSupported;
   PlanHead* head = reinterpret_cast<PlanHead*>(ws);
   const int64_t pad = ((int64_t)num_pages + 63) & ~(int64_t)63;
   int32_t* src = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(ws) + 256);

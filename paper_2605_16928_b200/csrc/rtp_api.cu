@@ -369,6 +369,7 @@ rtp_status rtp_cache_copy_pages(rtp_ctx* ctx, const rtp_params* params, const rt
   if (n == 0) return RTP_OK;
   if (!src_pages || !dst_pages) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
   cudaError_t e = launch_copy_pages(pa, cv.num_pages, src_pages, dst_pages, n, status, st);
+  if (e == cudaErrorNotSupported) return fail(ctx, RTP_ERR_UNSUPPORTED, "too many pages in one call");
   return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_cache_copy_pages");
 }
 
@@ -426,6 +427,7 @@ rtp_status rtp_cache_compact(rtp_ctx* ctx, const rtp_params* params, const rtp_c
   if (!aligned16(workspace)) return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
   if (workspace_bytes < pages_workspace_bytes(cv.num_pages, 0)) return fail(ctx, RTP_ERR_CAPACITY, "workspace too small");
   cudaError_t e = launch_compact(pa, table, (int64_t)cv.batch * cv.max_pages, page_refs, cv.num_pages, n_used, workspace, status, st);
+  if (e == cudaErrorNotSupported) return fail(ctx, RTP_ERR_UNSUPPORTED, "too many pages in one call");
   return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_cache_compact");
 }
 
