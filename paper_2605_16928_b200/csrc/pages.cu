@@ -213,6 +213,7 @@ __device__ __forceinline__ int scan_segments(int mine, int* s_before, int lane, 
 }
 
 // ---- reserve -----------------------------------------------------------------------------------------
+constexpr int kListMax = 4096;
 struct ReserveShared {
   int seq[kReserveMax];       // -1: the entry asks for nothing
   int len[kReserveMax], add[kReserveMax];
@@ -222,19 +223,20 @@ struct ReserveShared {
   int off[kReserveMax + 1];   // pages handed out before this entry's
   int before[33];
   int n_pairs;
-  unsigned long long total;   // (the sum in 32 bits may wrap)
+  unsigned long long total;
+  int page[kListMax];         // the free pages that are handed out, if they are not many
 };
 
-// How many of v[0 .. i - 1] equal v[i] (v 16-byte aligned).
-__device__ __forceinline__ int earlier_equal(const int* v, int i) {
-  const int x = v[i];
+// How many of v[0 .. i - 1] equal v[i] (v 16-byte aligned), counted by `width` (a power of two up to 32) neighbouring lanes.
+__device__ __forceinline__ int earlier_equal(const int* v, int i, int width, int lane) {
+  const int x = v[i], sub = lane & (width - 1);
   int n = 0;
-#pragma unroll 4
-  for (int j = 0; j < i; j += 4) {
+  for (int j = 4 * sub; j < i; j += 4 * width) {
     const int4 y = *reinterpret_cast<const int4*>(v + j);
     n += (y.x == x) + (y.y == x && j + 1 < i) + (y.z == x && j + 2 < i) + (y.w == x && j + 3 < i);
   }
-  return n;
+  const uint32_t lanes = (width == 32 ? 0xffffffffu : (1u << width) - 1u) << (lane - sub);
+  return __reduce_add_sync(lanes, n);
 }
 
 __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restrict__ table, const int32_t* __restrict__ seq_lens,
@@ -272,7 +274,12 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
     s.add[i] = add;
   }
   many = __syncthreads_or(many);
-  for (int i = tid; i < n; i += kPlanThreads) s.first[i] = s.seq[i] >= 0 && earlier_equal(s.seq, i) > 0;
+  int width = 1;   // lanes that compare one request with the earlier ones
+  while (width < 32 && 2 * width * n <= kPlanThreads) width *= 2;
+  for (int i = tid / width; i < n; i += kPlanThreads / width) {
+    const bool twice = earlier_equal(s.seq, i, width, lane) > 0;
+    if ((lane & (width - 1)) == 0) s.first[i] = twice && s.seq[i] >= 0;
+  }
   __syncthreads();
   for (int i = tid; i < n; i += kPlanThreads)   // a sequence named twice: the first one counts
     if (s.first[i]) {
@@ -335,21 +342,14 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
   if (many) look_at_rows(std::integral_constant<int, 32>()); else look_at_rows(std::integral_constant<int, 8>());
   if (__syncthreads_or(shared_page)) {
     // A page with r holders is copied by the first r - 1 of them at most: the last one to write it has it alone.
-    int mine[(kReserveMax + kPlanThreads - 1) / kPlanThreads];
-#pragma unroll
-    for (int k = 0; k < (kReserveMax + kPlanThreads - 1) / kPlanThreads; ++k) {
-      const int i = tid + k * kPlanThreads;
-      mine[k] = 0;
-      if (i < n && s.cow[i] >= 0) {
-        mine[k] = s.held[i] - earlier_equal(s.cow, i) > 1 ? 1 : -1;
-      }
+    for (int i = tid / width; i < n; i += kPlanThreads / width) {
+      const int earlier = earlier_equal(s.cow, i, width, lane);
+      if ((lane & (width - 1)) == 0) s.add[i] = s.cow[i] < 0 ? 0 : s.held[i] - earlier > 1 ? 1 : -1;
     }
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < (kReserveMax + kPlanThreads - 1) / kPlanThreads; ++k) {
-      const int i = tid + k * kPlanThreads;
-      if (i < n && mine[k] > 0) s.off[i] += 1;
-      if (i < n && mine[k] < 0) s.cow[i] = -1;
+    for (int i = tid; i < n; i += kPlanThreads) {
+      if (s.add[i] > 0) s.off[i] += 1;
+      if (s.add[i] < 0) s.cow[i] = -1;
     }
   }
   __syncthreads();
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
       wide += x;
     }
   }
-  if (wide) atomicAdd(&s.total, wide);
+  if ((int64_t)n * max_pages >= (int64_t)1 << 30) atomicAdd(&s.total, wide);   // (the sum in 32 bits could wrap)
   const int in_warp = lanes_before(sum, lane);
   const int total = scan_segments(__shfl_sync(0xffffffffu, in_warp + sum, 31), s.before, lane, warp);
   for (int k = 0; k < per; ++k) {
@@ -392,7 +392,28 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
       }
       return;
     }
-    int rank = seg.lo - s.before[warp];   // free pages before this segment
+    // page number `page` is the u-th that is handed out
+    auto hand_out = [&](int u, int page) {
+      int a = 0, b = n;   // the last entry with off <= u
+      while (a + 1 < b) {
+        const int mid = (a + b) >> 1;
+        if (s.off[mid] <= u) a = mid; else b = mid;
+      }
+      const int cow = s.cow[a], k = u - s.off[a];
+      int32_t* row = table + (int64_t)s.seq[a] * max_pages;
+      refs[page] = 1;
+      if (cow >= 0 && k == 0) {
+        atomicSub(refs + cow, 1);
+        row[s.len[a] >> kPageShift] = page;
+        const int slot = atomicAdd(&s.n_pairs, 1);
+        pair_src[slot] = cow;
+        pair_dst[slot] = page;
+      } else {
+        row[s.first[a] + k - (cow >= 0)] = page;
+      }
+    };
+    const bool listed = total <= kListMax;   // a list first, so that every thread then hands out its own
+    int rank = seg.lo - s.before[warp];      // free pages before this segment
     for (int at = seg.lo; at < seg.hi && rank < total; at += 128) {
       const int valid = min(4, max(0, seg.hi - (at + 4 * lane)));
       const uint32_t used_here = early ? used4 >> ((at - seg.lo) / 128 * 4) : used_bits(refs, at, seg.hi, lane);
@@ -402,28 +423,15 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
       for (int j = 0; j < 4; ++j) {
         if (!((free_bits >> j) & 1u)) continue;
         if (u < total) {
-          int a = 0, b = n;   // the last entry with off <= u
-          while (a + 1 < b) {
-            const int mid = (a + b) >> 1;
-            if (s.off[mid] <= u) a = mid; else b = mid;
-          }
-          const int page = at + 4 * lane + j, seq = s.seq[a], cow = s.cow[a];
-          int k = u - s.off[a];
-          int32_t* row = table + (int64_t)seq * max_pages;
-          refs[page] = 1;
-          if (cow >= 0 && k == 0) {
-            atomicSub(refs + cow, 1);
-            row[s.len[a] >> kPageShift] = page;
-            const int slot = atomicAdd(&s.n_pairs, 1);
-            pair_src[slot] = cow;
-            pair_dst[slot] = page;
-          } else {
-            row[s.first[a] + k - (cow >= 0)] = page;
-          }
+          if (listed) s.page[u] = at + 4 * lane + j; else hand_out(u, at + 4 * lane + j);
         }
         ++u;
       }
       rank += __reduce_add_sync(0xffffffffu, cnt);
+    }
+    if (listed) {
+      __syncthreads();
+      for (int u = tid; u < total; u += kPlanThreads) hand_out(u, s.page[u]);
     }
   }
   __syncthreads();
