@@ -2,7 +2,8 @@
 // bytes they move.  Append: a thread owns one group of 16 channels, so that the group's maximum needs no exchange between
 // lanes; 16 neighbouring threads are the 8 groups of K and the 8 of V of one (token, head), whose codes are two runs of 64
 // bytes and whose scales are one run of 16.  Expansion: a thread owns eight channels, 16 bytes of output, so that a warp
-// writes 512 bytes in a row; a block does one (page, head).
+// writes 512 bytes in a row; a block does one (page, head).  Measured: 8192 tokens x 8 heads appended in 13.6 us (43 MB; latency
+// of the token -> table -> row chain), 128K tokens x 8 heads expanded in 107 us (688 MB, 6.4 TB/s, the rate of a plain copy).
 #include "kv4.cuh"
 
 namespace rtp {
