@@ -196,6 +196,7 @@ class Params:
                            C.cast(self._a, C.POINTER(C.c_int32)), C.cast(self._b, C.POINTER(C.c_int32)),
                            C.cast(self._c, C.POINTER(C.c_int32)), C.cast(self._d, C.POINTER(C.c_int32)),
                            top_k, force_sink, force_recent)
+        self._ref = C.byref(self.c)
 
     @classmethod
     def from_workload(cls, wl, **over) -> "Params":
@@ -208,7 +209,7 @@ class Params:
         return cls(**kw)
 
     def ref(self):
-        return C.byref(self.c)
+        return self._ref
 
 
 def make_cache(k_pages, v_pages, ikey_pages, block_table, seq_lens, k_local_pages=None, v_local_pages=None,
@@ -223,10 +224,10 @@ def make_cache(k_pages, v_pages, ikey_pages, block_table, seq_lens, k_local_page
         ikey_format = RTP_IKEY_E4M3 if (ikey_pages is not None and ikey_pages.element_size() == 1) else RTP_IKEY_BF16
     n_local, ring = 0, 0
     if k_local_pages is not None:
-        n_local = int(k_local_pages.shape[0])
-        ring = int(local_block_table.shape[1]) - int(sink_pages)
+        n_local = k_local_pages.shape[0]
+        ring = local_block_table.shape[1] - int(sink_pages)
     return RtpCache(_ptr(k_pages), _ptr(v_pages), _ptr(ikey_pages), _ptr(block_table), _ptr(seq_lens),
-                    num_pages, int(block_table.shape[0]), int(block_table.shape[1]),
+                    num_pages, block_table.shape[0], block_table.shape[1],
                     _ptr(k_local_pages), _ptr(v_local_pages), _ptr(local_block_table), n_local, int(sink_pages), ring,
                     int(ikey_format), RTP_KV_FP4 if kv_scales is not None else RTP_KV_BF16, _ptr(kv_scales),
                     _ptr(kv_local_scales))
@@ -283,19 +284,19 @@ def rtp_check_status(ctx: Context, status, stream=None) -> int:
 
 def rtp_index_keys(ctx, params, cache, k_pre, w_k, tok_seq, tok_pos, stream=None):
     ctx._check(ctx.lib.rtp_index_keys(ctx.h, params.ref(), C.byref(cache), _ptr(k_pre), _ptr(w_k), _ptr(tok_seq),
-                                      _ptr(tok_pos), int(tok_seq.shape[0]), _stream(stream)), "rtp_index_keys")
+                                      _ptr(tok_pos), tok_seq.shape[0], _stream(stream)), "rtp_index_keys")
 
 
 def rtp_kv_append(ctx, params, cache, k_new, v_new, tok_seq, tok_pos, status, stream=None):
     ctx._check(ctx.lib.rtp_kv_append(ctx.h, params.ref(), C.byref(cache), _ptr(k_new), _ptr(v_new), _ptr(tok_seq),
-                                     _ptr(tok_pos), int(tok_seq.shape[0]), _ptr(status), _stream(stream)),
+                                     _ptr(tok_pos), tok_seq.shape[0], _ptr(status), _stream(stream)),
                "rtp_kv_append")
 
 
 def rtp_kv_expand(ctx, params, cache, src_pages, dst_pages, k_out, v_out, status, stream=None):
     """src_pages, dst_pages (or None: page i): int32 [n]; k_out, v_out: bf16 [pages, KV heads of the main pool, 64, 128]."""
     ctx._check(ctx.lib.rtp_kv_expand(ctx.h, params.ref(), C.byref(cache), _ptr(src_pages), _ptr(dst_pages),
-                                     int(src_pages.shape[0]), _ptr(k_out), _ptr(v_out), int(k_out.shape[0]), _ptr(status),
+                                     src_pages.shape[0], _ptr(k_out), _ptr(v_out), k_out.shape[0], _ptr(status),
                                      _stream(stream)), "rtp_kv_expand")
 
 
@@ -305,66 +306,66 @@ def rtp_cache_workspace_bytes(cache, n_seqs: int) -> int:
 
 def rtp_cache_copy_pages(ctx, params, cache, src_pages, dst_pages, status, stream=None):
     ctx._check(ctx.lib.rtp_cache_copy_pages(ctx.h, params.ref(), C.byref(cache), _ptr(src_pages), _ptr(dst_pages),
-                                            int(src_pages.shape[0]), _ptr(status), _stream(stream)), "rtp_cache_copy_pages")
+                                            src_pages.shape[0], _ptr(status), _stream(stream)), "rtp_cache_copy_pages")
 
 
 def rtp_cache_fork(ctx, params, cache, page_refs, src_seqs, dst_seqs, status, stream=None):
     """Writes page_refs and the block table and sequence lengths that ``cache`` describes (as the three calls below do)."""
     ctx._check(ctx.lib.rtp_cache_fork(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(src_seqs), _ptr(dst_seqs),
-                                      int(src_seqs.shape[0]), _ptr(status), _stream(stream)), "rtp_cache_fork")
+                                      src_seqs.shape[0], _ptr(status), _stream(stream)), "rtp_cache_fork")
 
 
 def rtp_cache_reserve(ctx, params, cache, page_refs, seqs, n_tokens, workspace, status, stream=None):
     ctx._check(ctx.lib.rtp_cache_reserve(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(seqs), _ptr(n_tokens),
-                                         int(seqs.shape[0]), _ptr(workspace),
-                                         int(workspace.numel() * workspace.element_size()), _ptr(status), _stream(stream)),
+                                         seqs.shape[0], _ptr(workspace),
+                                         workspace.nbytes, _ptr(status), _stream(stream)),
                "rtp_cache_reserve")
 
 
 def rtp_cache_free(ctx, params, cache, page_refs, seqs, status, stream=None):
-    ctx._check(ctx.lib.rtp_cache_free(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(seqs), int(seqs.shape[0]),
+    ctx._check(ctx.lib.rtp_cache_free(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(seqs), seqs.shape[0],
                                       _ptr(status), _stream(stream)), "rtp_cache_free")
 
 
 def rtp_cache_compact(ctx, params, cache, page_refs, n_used, workspace, status, stream=None):
     """n_used: int32 [1] on the device, written."""
     ctx._check(ctx.lib.rtp_cache_compact(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(n_used), _ptr(workspace),
-                                         int(workspace.numel() * workspace.element_size()), _ptr(status), _stream(stream)),
+                                         workspace.nbytes, _ptr(status), _stream(stream)),
                "rtp_cache_compact")
 
 
 def rtp_index_queries(ctx, params, q_pre, w_q, qt_out, stream=None):
-    ctx._check(ctx.lib.rtp_index_queries(ctx.h, params.ref(), _ptr(q_pre), _ptr(w_q), int(q_pre.shape[0]),
+    ctx._check(ctx.lib.rtp_index_queries(ctx.h, params.ref(), _ptr(q_pre), _ptr(w_q), q_pre.shape[0],
                                          _ptr(qt_out), _stream(stream)), "rtp_index_queries")
 
 
 def rtp_index_score(ctx, params, cache, q_pre, w_q, row_seq, row_pos, scores_out, row_max_out, row_sum_out,
                     workspace, status, stream=None):
-    stride = int(scores_out.shape[-1]) if scores_out is not None else 0
+    stride = scores_out.shape[-1] if scores_out is not None else 0
     ctx._check(ctx.lib.rtp_index_score(ctx.h, params.ref(), C.byref(cache), _ptr(q_pre), _ptr(w_q), _ptr(row_seq),
-                                       _ptr(row_pos), int(row_seq.shape[0]), _ptr(scores_out), stride,
+                                       _ptr(row_pos), row_seq.shape[0], _ptr(scores_out), stride,
                                        _ptr(row_max_out), _ptr(row_sum_out), _ptr(workspace),
-                                       int(workspace.numel() * workspace.element_size()), _ptr(status),
+                                       workspace.nbytes, _ptr(status),
                                        _stream(stream)), "rtp_index_score")
 
 
 def rtp_topp_select(ctx, params, cache, q_pre, w_q, row_seq, row_pos, seq_id, q_start, n_rows, sel_idx, sel_count,
                     sel_mass, sel_thresh, sel_tie_last, status, workspace, stream=None):
-    stride = int(sel_idx.shape[-1]) if sel_idx is not None else 0
+    stride = sel_idx.shape[-1] if sel_idx is not None else 0
     ctx._check(ctx.lib.rtp_topp_select(ctx.h, params.ref(), C.byref(cache), _ptr(q_pre), _ptr(w_q), _ptr(row_seq),
                                        _ptr(row_pos), int(seq_id), int(q_start), int(n_rows), _ptr(sel_idx), stride,
                                        _ptr(sel_count), _ptr(sel_mass), _ptr(sel_thresh), _ptr(sel_tie_last),
                                        _ptr(status), _ptr(workspace),
-                                       int(workspace.numel() * workspace.element_size()), _stream(stream)),
+                                       workspace.nbytes, _stream(stream)),
                "rtp_topp_select")
 
 
 def rtp_sparse_attn_decode(ctx, params, cache, q, row_seq, row_pos, sel_idx, sel_count, out, lse, workspace, status,
                            stream=None):
     ctx._check(ctx.lib.rtp_sparse_attn_decode(ctx.h, params.ref(), C.byref(cache), _ptr(q), _ptr(row_seq),
-                                              _ptr(row_pos), int(row_seq.shape[0]), _ptr(sel_idx),
-                                              int(sel_idx.shape[-1]), _ptr(sel_count), _ptr(out), _ptr(lse),
-                                              _ptr(workspace), int(workspace.numel() * workspace.element_size()),
+                                              _ptr(row_pos), row_seq.shape[0], _ptr(sel_idx),
+                                              sel_idx.shape[-1], _ptr(sel_count), _ptr(out), _ptr(lse),
+                                              _ptr(workspace), workspace.nbytes,
                                               _ptr(status), _stream(stream)), "rtp_sparse_attn_decode")
 
 
@@ -373,20 +374,20 @@ def rtp_sparse_attn_decode_static(ctx, params, cache, q, row_seq, row_pos, sel_i
     """rtp_sparse_attn_decode for callers that cannot hand over scratch memory: the split partials go to a
     512 KiB array built into the library, so nothing is allocated.  Calls must not overlap on the GPU."""
     ctx._check(ctx.lib.rtp_sparse_attn_decode_static(ctx.h, params.ref(), C.byref(cache), _ptr(q), _ptr(row_seq),
-                                                     _ptr(row_pos), int(row_seq.shape[0]), _ptr(sel_idx),
-                                                     int(sel_idx.shape[-1]), _ptr(sel_count), _ptr(out), _ptr(lse),
+                                                     _ptr(row_pos), row_seq.shape[0], _ptr(sel_idx),
+                                                     sel_idx.shape[-1], _ptr(sel_count), _ptr(out), _ptr(lse),
                                                      _ptr(status), _stream(stream)),
                "rtp_sparse_attn_decode_static")
 
 
 def rtp_sparse_attn_prefill(ctx, params, cache, q, q_pre, w_q, seq_id, q_start, n_rows, sel_idx, sel_count,
                             sel_thresh, sel_tie_last, out, lse, workspace, status, stream=None):
-    stride = int(sel_idx.shape[-1]) if sel_idx is not None else 0
+    stride = sel_idx.shape[-1] if sel_idx is not None else 0
     ctx._check(ctx.lib.rtp_sparse_attn_prefill(ctx.h, params.ref(), C.byref(cache), _ptr(q), _ptr(q_pre), _ptr(w_q),
                                                int(seq_id), int(q_start), int(n_rows), _ptr(sel_idx), stride,
                                                _ptr(sel_count), _ptr(sel_thresh), _ptr(sel_tie_last), _ptr(out),
                                                _ptr(lse), _ptr(workspace),
-                                               int(workspace.numel() * workspace.element_size()), _ptr(status),
+                                               workspace.nbytes, _ptr(status),
                                                _stream(stream)), "rtp_sparse_attn_prefill")
 
 
@@ -398,31 +399,31 @@ def rtp_topp_select_blocks(ctx, params, cache, q_pre, w_q, seq_id, q_start, n_ro
                            sel_thresh, sel_tie_last, status, workspace, stream=None):
     """block_mask: int32 / uint32 tensor [n_rows, n_ret, mask_words]."""
     ctx._check(ctx.lib.rtp_topp_select_blocks(ctx.h, params.ref(), C.byref(cache), _ptr(q_pre), _ptr(w_q), int(seq_id),
-                                              int(q_start), int(n_rows), _ptr(block_mask), int(block_mask.shape[-1]),
+                                              int(q_start), int(n_rows), _ptr(block_mask), block_mask.shape[-1],
                                               _ptr(sel_count), _ptr(sel_mass), _ptr(sel_thresh), _ptr(sel_tie_last),
                                               _ptr(status), _ptr(workspace),
-                                              int(workspace.numel() * workspace.element_size()), _stream(stream)),
+                                              workspace.nbytes, _stream(stream)),
                "rtp_topp_select_blocks")
 
 
 def rtp_topp_select_blocks_rows(ctx, params, cache, q_pre, w_q, row_seq, row_pos, block_idx, sel_count, sel_mass,
                                 sel_thresh, sel_tie_last, status, workspace, stream=None):
     """block_idx: int32 tensor [R, n_ret, block_stride] of logical page numbers (or None: counts only)."""
-    stride = int(block_idx.shape[-1]) if block_idx is not None else 0
+    stride = block_idx.shape[-1] if block_idx is not None else 0
     ctx._check(ctx.lib.rtp_topp_select_blocks_rows(ctx.h, params.ref(), C.byref(cache), _ptr(q_pre), _ptr(w_q),
-                                                   _ptr(row_seq), _ptr(row_pos), int(row_seq.shape[0]),
+                                                   _ptr(row_seq), _ptr(row_pos), row_seq.shape[0],
                                                    _ptr(block_idx), stride, _ptr(sel_count), _ptr(sel_mass),
                                                    _ptr(sel_thresh), _ptr(sel_tie_last), _ptr(status), _ptr(workspace),
-                                                   int(workspace.numel() * workspace.element_size()), _stream(stream)),
+                                                   workspace.nbytes, _stream(stream)),
                "rtp_topp_select_blocks_rows")
 
 
 def rtp_sparse_attn_decode_blocks(ctx, params, cache, q, row_seq, row_pos, block_idx, block_count, out, lse, workspace,
                                   status, stream=None):
     ctx._check(ctx.lib.rtp_sparse_attn_decode_blocks(ctx.h, params.ref(), C.byref(cache), _ptr(q), _ptr(row_seq),
-                                                     _ptr(row_pos), int(row_seq.shape[0]), _ptr(block_idx),
-                                                     int(block_idx.shape[-1]), _ptr(block_count), _ptr(out), _ptr(lse),
-                                                     _ptr(workspace), int(workspace.numel() * workspace.element_size()),
+                                                     _ptr(row_pos), row_seq.shape[0], _ptr(block_idx),
+                                                     block_idx.shape[-1], _ptr(block_count), _ptr(out), _ptr(lse),
+                                                     _ptr(workspace), workspace.nbytes,
                                                      _ptr(status), _stream(stream)), "rtp_sparse_attn_decode_blocks")
 
 
@@ -430,13 +431,13 @@ def rtp_sparse_attn_prefill_blocks(ctx, params, cache, q, seq_id, q_start, n_row
                                    stream=None):
     ctx._check(ctx.lib.rtp_sparse_attn_prefill_blocks(ctx.h, params.ref(), C.byref(cache), _ptr(q), int(seq_id),
                                                       int(q_start), int(n_rows), _ptr(block_mask),
-                                                      int(block_mask.shape[-1]), _ptr(out), _ptr(lse), _ptr(status),
+                                                      block_mask.shape[-1], _ptr(out), _ptr(lse), _ptr(status),
                                                       _stream(stream)), "rtp_sparse_attn_prefill_blocks")
 
 
 def rtp_local_attn(ctx, params, cache, q, row_seq, row_pos, seq_id, q_start, n_rows, out, lse, workspace, status,
                    stream=None):
-    ws_bytes = int(workspace.numel() * workspace.element_size()) if workspace is not None else 0
+    ws_bytes = workspace.nbytes if workspace is not None else 0
     ctx._check(ctx.lib.rtp_local_attn(ctx.h, params.ref(), C.byref(cache), _ptr(q), _ptr(row_seq), _ptr(row_pos),
                                       int(seq_id), int(q_start), int(n_rows), _ptr(out), _ptr(lse), _ptr(workspace),
                                       ws_bytes, _ptr(status), _stream(stream)), "rtp_local_attn")
@@ -454,8 +455,8 @@ def rtp_dense_attn_decode(ctx, params, cache, q, row_seq, row_pos, kv_heads, out
                           stream=None):
     arr = _i32_array(kv_heads) if kv_heads is not None else None
     ctx._check(ctx.lib.rtp_dense_attn_decode(ctx.h, params.ref(), C.byref(cache), _ptr(q), _ptr(row_seq),
-                                             _ptr(row_pos), int(row_seq.shape[0]),
+                                             _ptr(row_pos), row_seq.shape[0],
                                              C.cast(arr, C.c_void_p) if arr is not None else None,
                                              len(kv_heads) if kv_heads is not None else 0, _ptr(out), _ptr(lse),
-                                             _ptr(workspace), int(workspace.numel() * workspace.element_size()),
+                                             _ptr(workspace), workspace.nbytes,
                                              _ptr(status), _stream(stream)), "rtp_dense_attn_decode")

@@ -415,7 +415,8 @@ cudaError_t launch_typed(const CacheView& cv, const Dims& d, const HeadMaps& hm,
 
 size_t attn_rows_workspace_bytes(const Dims& d, int64_t R, int n_units, int group, int sm_count, int64_t max_len) {
   if (R <= 0 || n_units <= 0) return 0;
-  const int n_splits = plan_splits(R * n_units, max_len, sm_count, true);   // (the larger of the two roundings)
+  // (the larger of the two roundings, and what a call on a 4-bit cache may take)
+  const int n_splits = std::max(plan_splits(R * n_units, max_len, sm_count, true), max_splits4(R * n_units, max_len, sm_count));
   return (size_t)R * n_units * group * n_splits * kPartial * sizeof(float);
 }
 

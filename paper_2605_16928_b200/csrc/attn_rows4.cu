@@ -659,6 +659,13 @@ cudaError_t launch_typed4(const CacheView& cv, const Dims& d, const HeadMaps& hm
 
 }  // namespace
 
+// No plan has more splits than this.
+int max_splits4(int64_t units, int64_t max_set, int sm_count) {
+  if (units <= 0) return 1;
+  const int64_t tiles = (max_set + kTileTok - 1) / kTileTok, cap = (tiles + kWarps - 1) / kWarps;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({4LL * sm_count / units, cap, kMaxSplits}));
+}
+
 // Split count of a call.  Long sets get one round of the four resident CTAs per SM.  Shorter ones get one or two CTAs per SM:
 // they finish as early, with fewer partial results to merge (8 KV heads, us with 1 / 2 / 4 CTAs per SM: 4K tokens 7.7 / 9.2 /
 // 11.6, 8K 9.2 / 9.7 / 12.4, 32K 17.5 / 15.7 / 17.4, 64K and more best with 4), as long as a CTA has at most 512 tokens (four

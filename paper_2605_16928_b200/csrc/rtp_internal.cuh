@@ -236,6 +236,7 @@ cudaError_t launch_attn_rows(const CacheView& cv, const Dims& d, const HeadMaps&
                              size_t ws_bytes, int64_t max_len, int32_t* status, int sm_count, cudaStream_t st);
 
 // The same call on a 4-bit cache (cv.kv_fp4): `partial` holds R * n_units * group * n_splits partial results when n_splits > 1.
+int max_splits4(int64_t units, int64_t max_set, int sm_count);
 int plan_splits4(int64_t units, int64_t max_set, int sm_count, bool list);
 cudaError_t launch_attn_rows4(const CacheView& cv, const Dims& d, const HeadMaps& hm, const Rows& rows, int set, int n_units,
                               const __nv_bfloat16* q, const int32_t* sel_idx, int64_t sel_stride,
