@@ -117,6 +117,18 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
     kvh = hm.kv_list[u];
     qh0 = kvh * d.group;
   }
+  // Head of column n of the MMAs: n, or n % 4 in groups of up to four.  head_b: of column g (queries), head: of this lane's
+  // columns 2 c and 2 c + 1 in the results.
+  constexpr bool kPairs = G <= 4, kSingle = G == 1;
+  constexpr int H = kSingle ? 1 : 2;     // heads per lane
+  constexpr int kTilesO = kPairs ? 4 : 8;
+  const int head_b = kSingle ? 0 : kPairs ? g & 3 : g;
+  const int head[2] = {kSingle ? 0 : kPairs ? (2 * c) & 3 : 2 * c, kSingle ? 0 : kPairs ? (2 * c + 1) & 3 : 2 * c + 1};
+  uint4 qv[4];   // requested now, looked at when the first tiles are on their way
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    qv[i] = head_b < G ? __ldg(reinterpret_cast<const uint4*>(q + ((int64_t)r * d.n_q + qh0 + head_b) * kHeadDim + 32 * c) + i)
+                       : make_uint4(0u, 0u, 0u, 0u);
   const int seq = rows.row_seq(r);
   int n_keys = rows.row_pos(r) + 1;
   {
@@ -149,48 +161,6 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
   const int n_tiles = min(n_total, first + per) - first;
   const int n_mine = n_tiles > warp ? (n_tiles - warp + kWarps - 1) / kWarps : 0;   // tiles first + warp, + 4, ...
 
-  // B fragments of the queries: channels 32 c + 4 ks .. + 3 of column g's head in k-step ks.  Head of column n: n, or n % 4 in
-  // groups of up to four.  `head`: of this lane's columns 2 c and 2 c + 1 in the results.
-  constexpr bool kPairs = G <= 4, kSingle = G == 1;
-  constexpr int H = kSingle ? 1 : 2;     // heads per lane
-  constexpr int kTilesO = kPairs ? 4 : 8;
-  const int head_b = kSingle ? 0 : kPairs ? g & 3 : g;
-  const int head[2] = {kSingle ? 0 : kPairs ? (2 * c) & 3 : 2 * c, kSingle ? 0 : kPairs ? (2 * c + 1) & 3 : 2 * c + 1};
-  uint32_t qb[8][2];
-  float sc[H];   // logits in log2 units: factors of the lane's heads
-  {
-    uint32_t w[16];
-    float mx = 0.f;
-    if (head_b < G) {
-      const uint4* qp = reinterpret_cast<const uint4*>(q + ((int64_t)r * d.n_q + qh0 + head_b) * kHeadDim + 32 * c);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint4 v = __ldg(qp + i);
-        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w[i] = 0u;
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-    const int e = max((int)(__float_as_uint(mx) >> 23), 27) - 127;            // floor(log2 mx), at least -100
-    const float up = __uint_as_float((uint32_t)(9 - e + 127) << 23);          // 2^(9 - e)
-    const float down = d.sm_scale * kLog2e * __uint_as_float((uint32_t)max(e - 9 + 127, 1) << 23);
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      qb[i >> 1][i & 1] = pack_f16x2(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xffff0000u) * up);
-#pragma unroll
-    for (int j = 0; j < H; ++j) sc[j] = __shfl_sync(0xffffffffu, down, 8 * c + 4 * j);   // (from the lane of column 2 c + j)
-    if (kSingle) {   // column n < 4: group 2 n, the first half of lane n's channels; column 4 + n: group 2 n + 1
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (g != c + (i < 8 ? 0 : 4)) qb[i >> 1][i & 1] = 0u;
-    }
-  }
   // O^T, rows of tile i: byte 8 g + 2 i (elements 0, 1: columns 2 c, 2 c + 1) and byte 8 g + 2 i + 1 (2, 3), the column's half
   // of either; in groups of 8: channels 16 g + 2 i and 16 g + 2 i + 1
   float o[kTilesO][4];
@@ -316,6 +286,32 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
     flag_st[x] = (uint32_t)e >> 24;
     issue(x * kTileBytes, tok, raw_phys(tok), mask_st[x]);
     asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  // B fragments of the queries: channels 32 c + 4 ks .. + 3 of column g's head in k-step ks
+  uint32_t qb[8][2];
+  float sc[H];   // logits in log2 units: factors of the lane's heads
+  {
+    const uint32_t w[16] = {qv[0].x, qv[0].y, qv[0].z, qv[0].w, qv[1].x, qv[1].y, qv[1].z, qv[1].w,
+                            qv[2].x, qv[2].y, qv[2].z, qv[2].w, qv[3].x, qv[3].y, qv[3].z, qv[3].w};
+    float mx = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+    const int e = max((int)(__float_as_uint(mx) >> 23), 27) - 127;            // floor(log2 mx), at least -100
+    const float up = __uint_as_float((uint32_t)(9 - e + 127) << 23);          // 2^(9 - e)
+    const float down = d.sm_scale * kLog2e * __uint_as_float((uint32_t)max(e - 9 + 127, 1) << 23);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      qb[i >> 1][i & 1] = pack_f16x2(__uint_as_float(w[i] << 16) * up, __uint_as_float(w[i] & 0xffff0000u) * up);
+#pragma unroll
+    for (int j = 0; j < H; ++j) sc[j] = __shfl_sync(0xffffffffu, down, 8 * c + 4 * j);   // (from the lane of column 2 c + j)
+    if (kSingle) {   // column n < 4: group 2 n, the first half of lane n's channels; column 4 + n: group 2 n + 1
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (g != c + (i < 8 ? 0 : 4)) qb[i >> 1][i & 1] = 0u;
+    }
   }
   int ent_a = raw_entry(kStages - 1);                       // the next tile to be copied: its entry, token and page
   int tok_a = token_of(kStages - 1, ent_a), phys_a = raw_phys(tok_a);
@@ -534,35 +530,47 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
     }
   }
   __syncthreads();
-  const int dim = threadIdx.x;  // 128 threads = 128 dims
+  // a warp for each head (the next four heads after that), four channels per lane: 2 lane, 2 lane + 1 and 64 more of each
 #pragma unroll
-  for (int gg = 0; gg < G; ++gg) {
+  for (int gg0 = 0; gg0 < G; gg0 += kWarps) {
+    const int gg = gg0 + warp;
+    if (gg >= G) break;
+    // (a retrieval head inside a local group is not a local call's; a local head inside a retrieval group not a union call's)
+    if ((SET == kSetLocal || SET == kSetUnion) && hm.skips(qh0 + gg)) continue;
+    float2 ml[kWarps];
     float mt = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) mt = fmaxf(mt, red[(w * G + gg) * kPartial + kHeadDim]);
-    float lt = 0.f, a = 0.f;
+    for (int w = 0; w < kWarps; ++w) {
+      ml[w] = *reinterpret_cast<const float2*>(red + (w * G + gg) * kPartial + kHeadDim);
+      mt = fmaxf(mt, ml[w].x);
+    }
+    float lt = 0.f;
+    float2 a0 = {0.f, 0.f}, a1 = {0.f, 0.f};
     if (mt != -INFINITY) {
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const float* rw = red + (w * G + gg) * kPartial;
-        const float wgt = fast_ex2(rw[kHeadDim] - mt);
-        lt += rw[kHeadDim + 1] * wgt;
-        a += rw[dim] * wgt;
+        const float2* rw = reinterpret_cast<const float2*>(red + (w * G + gg) * kPartial) + lane;
+        const float wgt = fast_ex2(ml[w].x - mt);
+        const float2 x = rw[0], y = rw[32];
+        lt += ml[w].y * wgt;
+        a0.x += x.x * wgt;
+        a0.y += x.y * wgt;
+        a1.x += y.x * wgt;
+        a1.y += y.y * wgt;
       }
     }
-    const int64_t oh = (int64_t)r * d.n_q + qh0 + gg;
-    // (a retrieval head inside a local group is not a local call's; a local head inside a retrieval group not a union call's)
-    if ((SET == kSetLocal || SET == kSetUnion) && hm.skips(qh0 + gg)) continue;
     if (n_splits == 1) {
-      out[oh * kHeadDim + dim] = __float2bfloat16_rn(lt > 0.f ? a / lt : 0.f);
-      if (lse && dim == 0) lse[oh] = lt > 0.f ? (mt + log2f(lt)) * kLn2 : -INFINITY;
+      const int64_t oh = (int64_t)r * d.n_q + qh0 + gg;
+      const float inv = lt > 0.f ? 1.f / lt : 0.f;
+      __nv_bfloat162* to = reinterpret_cast<__nv_bfloat162*>(out + oh * kHeadDim) + lane;
+      to[0] = __floats2bfloat162_rn(a0.x * inv, a0.y * inv);
+      to[32] = __floats2bfloat162_rn(a1.x * inv, a1.y * inv);
+      if (lse && lane == 0) lse[oh] = lt > 0.f ? (mt + log2f(lt)) * kLn2 : -INFINITY;
     } else {
-      float* p = partial + (((int64_t)blockIdx.x * G + gg) * n_splits + split) * kPartial;
-      p[dim] = a;
-      if (dim == 0) {
-        p[kHeadDim] = mt;
-        p[kHeadDim + 1] = lt;
-      }
+      float2* p = reinterpret_cast<float2*>(partial + (((int64_t)blockIdx.x * G + gg) * n_splits + split) * kPartial);
+      p[lane] = a0;
+      p[32 + lane] = a1;
+      if (lane == 0) p[kHeadDim / 2] = make_float2(mt, lt);
     }
   }
 }
