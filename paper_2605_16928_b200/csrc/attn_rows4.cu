@@ -593,6 +593,16 @@ __global__ void __launch_bounds__(32 * W) attn_merge4_kernel(
   if ((SET == kSetLocal || SET == kSetUnion) && hm.skips(qh)) return;
   const float* p = partial + ((unit * G + g) * (int64_t)n_splits) * kPartial;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  // the warp's first four results are requested together with the maxima
+  constexpr int kAhead = 4;
+  float2 x0[kAhead], y0[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const int s = warp + k * W;
+    const float2* row = reinterpret_cast<const float2*>(p + (int64_t)s * kPartial) + lane;
+    x0[k] = s < n_splits ? row[0] : make_float2(0.f, 0.f);
+    y0[k] = s < n_splits ? row[32] : make_float2(0.f, 0.f);
+  }
   float m[kPer], l[kPer], mt = -INFINITY;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
@@ -623,8 +633,16 @@ __global__ void __launch_bounds__(32 * W) attn_merge4_kernel(
 #pragma unroll
   for (int k = 0; k < W; ++k) lt += red_l[k];
   float2 a0 = {0.f, 0.f}, a1 = {0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const float w = warp + k * W < n_splits ? wgt[warp + k * W] : 0.f;
+    a0.x = fmaf(x0[k].x, w, a0.x);
+    a0.y = fmaf(x0[k].y, w, a0.y);
+    a1.x = fmaf(y0[k].x, w, a1.x);
+    a1.y = fmaf(y0[k].y, w, a1.y);
+  }
 #pragma unroll 4
-  for (int s = warp; s < n_splits; s += W) {
+  for (int s = warp + kAhead * W; s < n_splits; s += W) {
     const float w = wgt[s];
     const float2* q = reinterpret_cast<const float2*>(p + (int64_t)s * kPartial) + lane;
     const float2 x = q[0], y = q[32];
