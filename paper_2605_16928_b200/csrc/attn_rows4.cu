@@ -693,8 +693,8 @@ int max_splits4(int64_t units, int64_t max_set, int sm_count) {
 }
 
 // Split count of a call.  Long sets get one round of the four resident CTAs per SM.  Shorter ones get one or two CTAs per SM:
-// they finish as early, with fewer partial results to merge (8 KV heads, us with 1 / 2 / 4 CTAs per SM: 4K tokens 7.7 / 9.2 /
-// 11.6, 8K 9.2 / 9.7 / 12.4, 32K 17.5 / 15.7 / 17.4, 64K and more best with 4), as long as a CTA has at most 512 tokens (four
+// they finish as early, with fewer partial results to merge (8 KV heads, us with 1 / 2 / 4 CTAs per SM: 4K tokens 5.8 / 6.7 /
+// 8.2, 8K 7.1 / 7.5 / 8.6, 32K 14.2 / 12.3 / 13.1, 64K and more best with 4), as long as a CTA has at most 512 tokens (four
 // tiles per warp) per resident CTA; a list, whose tokens come one by one, 128.  No CTA gets fewer than 128 tokens (a tile per
 // warp), and the four warps equally many tiles where the count is free.
 int plan_splits4(int64_t units, int64_t max_set, int sm_count, bool list) {
