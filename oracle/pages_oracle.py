@@ -48,6 +48,10 @@ class Pool:
             if self.used(ln + n) > self.table.shape[1]:
                 self.capacity = True
                 return
+            behind = self.table[s, self.used(ln):self.used(ln + n)]
+            if (self.refs[behind[behind >= 0]] > 1).any():     # pages that somebody else holds, behind the last token
+                self.invalid = True
+                continue
             if n and ln % PAGE:
                 p = self.table[s, ln // PAGE]
                 if refs[p] > 1:

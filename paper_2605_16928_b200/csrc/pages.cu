@@ -311,9 +311,11 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
           const bool part = s.add[i] > 0 && (len & (kPage - 1));
           const int last = part ? row[len >> kPageShift] : -1;   // (requested together with the entries below)
           for (int p = first + sub; p < want; p += W) {   // mapped entries come first, then unmapped ones
-            const bool m = row[p] >= 0;
+            const int e = row[p];
+            const bool m = e >= 0;
             mapped += m;
             bad = bad || (m && p > first && row[p - 1] < 0);
+            bad = bad || (m && (!page_ok(e, num_pages) || refs[e] > 1));   // (somebody else's tokens would be written over)
           }
           mapped = __reduce_add_sync(lanes, mapped);
           first += mapped;

@@ -191,6 +191,32 @@ def test_thousands_of_requests_in_one_call():
     pool.check()
 
 
+def test_a_shortened_sequence_does_not_write_into_shared_pages():
+    """A forked sequence made shorter by its owner: pages behind its end are still the source's, so room in them is refused."""
+    pool = Pool(30, 3, 8)
+    d = Device(pool)
+    for x in (d, pool):
+        x.reserve([0], [300])
+    pool.lens[0] = 300
+    d.lens.copy_(_i32(pool.lens))
+    for x in (d, pool):
+        x.fork([0], [1])
+    for ln, add, ok in ((10, 54, True), (10, 55, False), (64, 1, False), (300, 20, True), (128, 0, True)):
+        for x in (d, pool):
+            x.free([1])
+            x.fork([0], [1])
+        pool.lens[1] = ln
+        d.lens.copy_(_i32(pool.lens))
+        pool.invalid = False
+        for x in (d, pool):
+            x.reserve([1, 2], [add, 70])
+        assert pool.invalid == (not ok) and d.code() == (rb.RTP_OK if ok else rb.RTP_ERR_INVALID)
+        d.same()
+        pool.check()
+        for x in (d, pool):
+            x.free([2])
+
+
 def test_broken_tables_are_reported():
     """Entries that name no page, or a page that nobody holds: reported, and nothing outside the arrays is touched."""
     pool = Pool(40, 3, 4)
