@@ -387,22 +387,18 @@ __global__ void __launch_bounds__(kUniThreads) blk_union_kernel(const CacheView 
     }
   }
   __syncthreads();
-  int max_cnt = 0;
-  for (int g = 0; g < d.group; ++g) max_cnt = max(max_cnt, s_cnt[g]);
-  for (int j0 = tid; j0 < max_cnt; j0 += kUniThreads * kUniLoads) {
-    for (int g = 0; g < d.group; ++g) {   // (the loads of a head are in flight together; heads follow each other closely)
-      const int cnt = s_cnt[g];
-      if (j0 - tid >= cnt) continue;      // uniform
-      const int32_t* lst = s_lst[g];
+  // the threads are dealt to the heads, so that the loads of all heads are in flight together (groups of 1, 2, 4 or 8)
+  {
+    const int per = kUniThreads / d.group, g = tid / per, t = tid % per;
+    const int cnt = s_cnt[g];
+    const int32_t* lst = s_lst[g];
+    for (int j0 = t; j0 < cnt; j0 += per * kUniLoads) {
       int page[kUniLoads];
 #pragma unroll
-      for (int k = 0; k < kUniLoads; ++k) {
-        const int j = j0 + k * kUniThreads;
-        page[k] = j < cnt ? __ldg(lst + j) : -1;
-      }
+      for (int k = 0; k < kUniLoads; ++k) page[k] = j0 + k * per < cnt ? __ldg(lst + j0 + k * per) : -1;
 #pragma unroll
       for (int k = 0; k < kUniLoads; ++k) {
-        if (j0 + k * kUniThreads >= cnt) continue;
+        if (j0 + k * per >= cnt) continue;
         if ((unsigned)page[k] >= (unsigned)nb) {
           set_status(status, RTP_ERR_INVALID);   // a page outside the row's causal pages is left out
           continue;
@@ -413,11 +409,12 @@ __global__ void __launch_bounds__(kUniThreads) blk_union_kernel(const CacheView 
   }
   __syncthreads();
   int32_t* out = uni_idx + (int64_t)blockIdx.x * uni_stride;
-  for (int w0 = 0; w0 < nbw; w0 += kUniThreads) {
-    const int w = w0 + tid;
+  for (int w0 = 0; w0 < nbw; w0 += kUniThreads / 4) {   // (a thread writes the pages of a quarter of a word)
+    const int w = w0 + (tid >> 2);
     uint32_t any = 0u;
     if (w < nbw)
       for (int g = 0; g < d.group; ++g) any |= uni_bits[g * nbw_max + w];
+    any &= 0xffu << (8 * (tid & 3));
     const int mine = __popc(any);
     int inc = mine;
 #pragma unroll
