@@ -207,7 +207,7 @@ def test_rising_and_falling_scores():
 
 
 @pytest.mark.parametrize("L,window,n_sink", [(1, 1, 0), (40, 5, 3), (100, 100, 4), (1000, 64, 4), (1000, 1, 70), (3000, 517, 17), (300, 4096, 4), (65, 64, 0)])
-@pytest.mark.parametrize("group", [1, 4])
+@pytest.mark.parametrize("group", [1, 2, 4, 8])
 def test_local(L, window, n_sink, group):
     c = _h().Cache4([L, max(1, L // 2)], n_kv=3, group=group, ret_kv=(0,), local_kv=(2, 1), window=window, n_sink=n_sink, seed=L)
     rb.rtp_local_attn(*c.args(), 0, 0, c.R, c.out, c.lse, c.ws, c.status)
@@ -307,6 +307,30 @@ def test_pages(group):
     rb.rtp_sparse_attn_decode_blocks(*c.args(), d_idx, d_cnt, c.out, c.lse, tiny, c.status)
     assert c.code() == rb.RTP_OK
     c.check(c.ret, sets)
+
+
+@pytest.mark.parametrize("group", [2, 4, 8])
+def test_mixed_group(group):
+    """A KV head with retrieval and local query heads: each call writes its own heads and leaves the others."""
+    h = _h()
+    c = h.Cache4([900, 70], n_kv=2, group=group, seed=group)
+    ret = [0] if group == 2 else [0, 2]
+    c.params = rb.Params(c.n_q, 2, ret, [0] * len(ret), [0], [0, 1], window=100, n_sink=3)
+    c.ret = ret
+    rb.rtp_local_attn(*c.args(), 0, 0, 2, c.out, c.lse, c.ws, c.status)
+    local = lambda r, hd: [t for t in range(c.lens[r]) if t < 3 or t >= c.lens[r] - 100]
+    c.check([hd for hd in range(c.n_q) if hd not in ret], local)
+    c.out.fill_(-77), c.lse.fill_(-77)
+    pages = [np.array([3, 0, 14, 7]), np.array([1])]
+    idx = np.zeros((2, len(ret), 15), np.int32)
+    for r in range(2):
+        for i in range(len(ret)):
+            idx[r, i, :len(pages[r]) - i * (r == 0)] = pages[r][:len(pages[r]) - i * (r == 0)]
+    cnt = [[4 - i for i in range(len(ret))], [1] * len(ret)]
+    sets = lambda r, hd: [t for p in idx[r, ret.index(hd), :cnt[r][ret.index(hd)]] for t in range(64 * p, min(64 * p + 64, c.lens[r]))]
+    rb.rtp_sparse_attn_decode_blocks(*c.args(), h.dev_i32(idx), h.dev_i32(cnt), c.out, c.lse, c.ws, c.status)
+    assert c.code() == rb.RTP_OK
+    c.check(ret, sets)
 
 
 def test_truncated_local_pool():

@@ -99,7 +99,7 @@ def test_random_calls(kind):
         pool.check()
 
 
-@pytest.mark.parametrize("num_pages", [1, 3, 127, 128, 129, 4095, 5000])
+@pytest.mark.parametrize("num_pages", [1, 3, 127, 128, 129, 4095, 5000, 32768, 32769, 70001])
 def test_pool_sizes(num_pages):
     """The scan over the counts at every kind of pool size, down to a pool of one page, filled to the last page."""
     pool = Pool(num_pages, 3, num_pages + 1)
