@@ -196,7 +196,8 @@ def _handle(s, c, n_loc=(), n_ret_kv=0, **over):
     Hkv, G = c["Hkv"], c.get("group", 1)
     ret = list(range(n_ret_kv * G))
     s["rb"], s["ctx"] = rb, rb.Context()
-    s["params"] = rb.Params(Hkv * G, Hkv, ret, [i // G for i in ret], list(range(max(n_ret_kv, c.get("n_ih", 0)))), list(n_loc), **over)
+    index_kv = [i % Hkv for i in range(max(n_ret_kv, c.get("n_ih", 0)))]
+    s["params"] = rb.Params(Hkv * G, Hkv, ret, [i // G for i in ret], index_kv, list(n_loc), **over)
     s["cache"] = rb.make_cache(s["k"], s["v"], s.get("ikey"), s["table"], s["lens"], kv_scales=s.get("scales"))
     s["status"] = torch.zeros(1, dtype=torch.int32, device="cuda")
 
