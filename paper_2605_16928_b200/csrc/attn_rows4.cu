@@ -705,7 +705,7 @@ int plan_splits4(int64_t units, int64_t max_set, int sm_count, bool list) {
   for (int k : {1, 2, 4}) {
     s = std::min<int64_t>(std::max<int64_t>(1, k * (int64_t)sm_count / units), cap);
     step = k < 4 ? kWarps : kTilesPerPage;
-    if (tiles <= s * k * limit) break;
+    if (tiles <= s * k * limit * (s == 1 ? 2 : 1)) break;   // (a single split needs no merge)
   }
   const int64_t per = std::max<int64_t>(1, (tiles + s * step - 1) / (s * step)) * step;
   return (int)std::min<int64_t>(std::max<int64_t>(1, (tiles + per - 1) / per), kMaxSplits);
