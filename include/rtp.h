@@ -287,8 +287,9 @@ rtp_status rtp_kv_expand(rtp_ctx* ctx, const rtp_params* params, const rtp_cache
  *
  * rtp_cache_compact: moves pages so that the n pages in use become pages 0 .. n - 1: the k-th used page at or above n goes to
  *   the k-th free page below it; contents, references and table entries follow, *n_used (DEVICE int32) = n.  Pages n .. are
- *   free afterwards (their old contents are left), so that the pool can be cut there.  An entry that names a page without
- *   references: left, RTP_ERR_INVALID.  workspace: rtp_cache_workspace_bytes(cache, 0). */
+ *   free afterwards (their old contents are left), so that the pool can be cut there.  If an entry names a page without
+ *   references, or no page of the pool, nothing moves: RTP_ERR_INVALID, and *n_used = num_pages.
+ *   workspace: rtp_cache_workspace_bytes(cache, 0). */
 size_t rtp_cache_workspace_bytes(const rtp_cache* cache, int64_t n_seqs);
 rtp_status rtp_cache_copy_pages(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, const int32_t* src_pages,
                                 const int32_t* dst_pages, int64_t n, int32_t* status, void* stream);

@@ -81,6 +81,10 @@ class Pool:
             self.lens[s] = 0
 
     def compact(self) -> int:
+        named = self.table[self.table >= 0]
+        if (named >= len(self.refs)).any() or (self.refs[named] <= 0).any():   # the table is wrong: nothing moves
+            self.invalid = True
+            return len(self.refs)
         n = int((self.refs > 0).sum())
         gaps = [p for p in range(n) if self.refs[p] == 0]
         for p in range(n, len(self.refs)):

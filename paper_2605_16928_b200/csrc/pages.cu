@@ -35,10 +35,14 @@ struct LargeCopy {
 template <class C>
 constexpr int kPieceOf = C::kThreads * C::kVec * 16;
 
-// Workspace: counts, then lists.
+// Workspace: counts and the verdicts of the table checks (256 bytes), then lists.
+constexpr int kCheckMax = 60;    // CTAs that look through the table before a compaction
+constexpr int kCheckVec = 4;     // table entries in flight per thread
 struct PlanHead {
   int32_t n_pairs, n_used;
+  int32_t bad[kCheckMax];
 };
+static_assert(sizeof(PlanHead) <= 256, "the lists begin 256 bytes into the workspace");
 
 __device__ __forceinline__ bool page_ok(int p, int num_pages) { return (unsigned)p < (unsigned)num_pages; }
 
@@ -443,12 +447,30 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
 }
 
 // ---- compact -----------------------------------------------------------------------------------------
-// With n_used pages in use, the k-th used page at or above n_used goes to the k-th free page below it.
-__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const int32_t* __restrict__ refs, const int num_pages,
+// With n_used pages in use, the k-th used page at or above n_used goes to the k-th free page below it.  That is CTA 0's work;
+// the others look meanwhile for table entries that name a page without references (one below n_used would be filled with somebody
+// else's tokens, which its row would then read, and give away when it is freed) or no page at all, and leave a verdict each.
+__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const int32_t* __restrict__ table, const int64_t n_entries,
+                                                                    const int32_t* __restrict__ refs, const int num_pages,
                                                                     PlanHead* __restrict__ head, int32_t* __restrict__ src,
                                                                     int32_t* __restrict__ dst, int32_t* __restrict__ move,
                                                                     int32_t* __restrict__ n_used_out) {
   chain_wait();
+  if (blockIdx.x > 0) {
+    const int64_t step = (int64_t)(gridDim.x - 1) * kPlanThreads;
+    bool bad = false;
+    for (int64_t i = (int64_t)(blockIdx.x - 1) * kPlanThreads + threadIdx.x; i < n_entries; i += step * kCheckVec) {
+      int e[kCheckVec];   // (loads of a step side by side)
+#pragma unroll
+      for (int k = 0; k < kCheckVec; ++k) e[k] = i + k * step < n_entries ? table[i + k * step] : -1;
+#pragma unroll
+      for (int k = 0; k < kCheckVec; ++k)
+        if (e[k] >= 0) bad = bad || !page_ok(e[k], num_pages) || refs[e[k]] <= 0;
+    }
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) head->bad[blockIdx.x - 1] = bad;
+    return;
+  }
   __shared__ int s_before[33], s_below;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const Segment seg = warp_segment(num_pages, warp);
@@ -489,18 +511,23 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const int32_
 __global__ void __launch_bounds__(LargeCopy::kThreads) compact_move_kernel(const __grid_constant__ PageArrays pa, const int num_pages,
                                                                     int32_t* __restrict__ table, const int64_t n_entries,
                                                                     int32_t* __restrict__ refs, const PlanHead* __restrict__ head,
-                                                                    const int32_t* __restrict__ src,
+                                                                    const int n_checks, const int32_t* __restrict__ src,
                                                                     const int32_t* __restrict__ dst,
-                                                                    const int32_t* __restrict__ move, int32_t* status) {
+                                                                    const int32_t* __restrict__ move,
+                                                                    int32_t* __restrict__ n_used_out, int32_t* status) {
   chain_wait();
+  if (__syncthreads_or(threadIdx.x < n_checks && head->bad[threadIdx.x])) {   // the table is wrong: nothing moves, no page may be cut
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+      set_status(status, RTP_ERR_INVALID);
+      *n_used_out = num_pages;
+    }
+    return;
+  }
   const int n_pairs = head->n_pairs, n_used = head->n_used;
   const int64_t t0 = (int64_t)blockIdx.x * LargeCopy::kThreads + threadIdx.x, step = (int64_t)gridDim.x * LargeCopy::kThreads;
   for (int64_t i = t0; i < n_entries; i += step) {
     const int e = table[i];
-    if (e < n_used) continue;
-    const int k = e < num_pages ? move[e] : -1;
-    if (k >= 0) table[i] = dst[k];
-    else set_status(status, RTP_ERR_INVALID);   // (an entry whose page nobody holds, or no page at all)
+    if (e >= n_used) table[i] = dst[move[e]];   // (a page in use: checked above)
   }
   for (int64_t i = t0; i < n_pairs; i += step) {
     refs[dst[i]] = refs[src[i]];
@@ -589,11 +616,13 @@ cudaError_t launch_compact(const PageArrays& arrays, int32_t* table, int64_t n_e
   const int64_t pad = ((int64_t)num_pages + 63) & ~(int64_t)63;
   int32_t* src = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(ws) + 256);
   int32_t *dst = src + pad, *move = dst + pad;
-  (void)launch_chained(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, refs, num_pages, head, src, dst, move, n_used);
+  const int n_checks = (int)std::min<int64_t>(kCheckMax, (n_entries + kPlanThreads * kCheckVec - 1) / (kPlanThreads * kCheckVec));
+  (void)launch_chained(compact_plan_kernel, dim3(1 + n_checks), dim3(kPlanThreads), 0, st, (const int32_t*)table, n_entries,
+                       (const int32_t*)refs, num_pages, head, src, dst, move, n_used);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   (void)launch_chained(compact_move_kernel, dim3((unsigned)current_sm_count(148) * 32), dim3(LargeCopy::kThreads), 0, st, pa, num_pages,
-                       table, n_entries, refs, head, src, dst, move, status);
+                       table, n_entries, refs, head, n_checks, src, dst, move, n_used, status);
   return cudaGetLastError();
 }
 

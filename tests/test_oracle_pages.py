@@ -46,3 +46,14 @@ def test_invariants_under_random_calls():
                 n = p.compact()
                 assert (p.refs[:n] > 0).all() and not p.refs[n:].any()
             p.check()
+
+
+def test_compaction_of_a_wrong_table_moves_nothing():
+    for entry in (1, 2, 7, 8):
+        p = Pool(8, 3, 4)
+        p.reserve([0, 1], [128, 128])
+        p.free([0])
+        p.table[2, 3] = entry
+        before = p.table.copy()
+        assert p.compact() == (2 if entry == 2 else 8) and p.invalid == (entry != 2)
+        assert np.array_equal(before, p.table) == (entry != 2)
