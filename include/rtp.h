@@ -276,8 +276,8 @@ rtp_status rtp_kv_expand(rtp_ctx* ctx, const rtp_params* params, const rtp_cache
  *   itself is left to the caller, as in rtp_kv_append).  Unmapped pages up to there are taken from the free ones, and a
  *   partly filled last page that other sequences share is replaced by a copy of its own, contents included, if at
  *   least one token is asked for.  (So every append behind a fork needs a reserve before it.)  A request is skipped and
- *   RTP_ERR_INVALID recorded if the tokens would also go to further pages that are mapped already and shared: a sequence that
- *   the caller made shorter than what it shares has to be freed and forked anew.  Requests are served in the order of the list: of r sequences that share a page and are all
+ *   RTP_ERR_INVALID recorded if the tokens would also go to further pages that are mapped already and shared (a sequence that
+ *   the caller made shorter than what it shares has to be freed and forked anew), or to a page without references.  Requests are served in the order of the list: of r sequences that share a page and are all
  *   listed, the first r - 1 get copies.  If the free pages or a table row do not suffice for ALL requests, nothing changes and
  *   RTP_ERR_CAPACITY is recorded.  A sequence named twice counts the first time (RTP_ERR_INVALID).  n <= 4096
  *   (RTP_ERR_UNSUPPORTED).  workspace: rtp_cache_workspace_bytes(cache, n).

@@ -49,11 +49,14 @@ class Pool:
                 self.capacity = True
                 return
             behind = self.table[s, self.used(ln):self.used(ln + n)]
-            if (self.refs[behind[behind >= 0]] > 1).any():     # pages that somebody else holds, behind the last token
+            if (self.refs[behind[behind >= 0]] != 1).any():    # pages that somebody else holds, or nobody, behind the last token
                 self.invalid = True
                 continue
             if n and ln % PAGE:
                 p = self.table[s, ln // PAGE]
+                if self.refs[p] <= 0:
+                    self.invalid = True
+                    continue
                 if refs[p] > 1:
                     refs[p] -= 1
                     todo.append((s, ln // PAGE, p))

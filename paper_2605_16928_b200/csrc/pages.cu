@@ -319,7 +319,8 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
             const bool m = e >= 0;
             mapped += m;
             bad = bad || (m && p > first && row[p - 1] < 0);
-            bad = bad || (m && (!page_ok(e, num_pages) || refs[e] > 1));   // (somebody else's tokens would be written over)
+            // (held by others: their tokens would be written over; held by nobody: it may be handed out to another sequence)
+            bad = bad || (m && (!page_ok(e, num_pages) || refs[e] != 1));
           }
           mapped = __reduce_add_sync(lanes, mapped);
           first += mapped;
@@ -328,6 +329,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
           if (part) {
             if (!page_ok(last, num_pages)) bad = true;
             else held = refs[last];
+            if (held <= 0) bad = true;
             if (held > 1) cow = last;
           }
           if (__any_sync(lanes, bad)) {

@@ -35,3 +35,19 @@ def test_compaction_of_a_wrong_table_moves_nothing(batch, max_pages, page):
     assert pool.compact() == 2 == int(d.n_used) and d.code() == rb.RTP_OK
     d.same()
     pool.check()
+
+
+def test_room_in_a_page_that_nobody_holds_is_refused():
+    """A mapped page whose count is zero, as the partly filled last page of a sequence or as a page reserved behind it: the
+    request is skipped, and the page may go to somebody else."""
+    for table, refs, ln, add in (([[3, -1]], [], 10, 5), ([[0, 1]], [0], 64, 10), ([[0, 1]], [0], 20, 100), ([[2, -1]], [], 63, 1)):
+        pool = Pool(6, 2, 2)
+        pool.table[0] = table[0]
+        pool.refs[refs] = 1
+        pool.lens[0] = ln
+        d = Device(pool, n_kv=1, n_ih=1, kv=False)
+        for x in (d, pool):
+            x.reserve([0, 1], [add, 128])
+        assert pool.invalid and d.code() == rb.RTP_ERR_INVALID
+        d.same()
+        assert pool.table[0].tolist() == table[0] and (pool.table[1] >= 0).all()

@@ -57,3 +57,12 @@ def test_compaction_of_a_wrong_table_moves_nothing():
         before = p.table.copy()
         assert p.compact() == (2 if entry == 2 else 8) and p.invalid == (entry != 2)
         assert np.array_equal(before, p.table) == (entry != 2)
+
+
+def test_room_in_a_page_that_nobody_holds_is_refused():
+    for table, refs, ln, add in (([3, -1], [], 10, 5), ([0, 1], [0], 64, 10), ([0, 1], [0], 20, 100)):
+        p = Pool(6, 2, 2)
+        p.table[0], p.lens[0] = table, ln
+        p.refs[refs] = 1
+        p.reserve([0], [add])
+        assert p.invalid and p.table[0].tolist() == table and p.refs.sum() == len(refs)
