@@ -160,6 +160,10 @@ typedef struct rtp_cache {
   int32_t kv_format;
   void* kv_scales;       /* DEVICE, RTP_KV_FP4 only */
   void* kv_local_scales; /* DEVICE, RTP_KV_FP4 with a local pool only */
+  /* Optional: the reference counts of the main pool's pages (see rtp_cache_fork).  When not NULL, rtp_kv_append and rtp_index_keys
+   * write to pages that exactly one block-table entry names and skip every other row (rtp_kv_append then records
+   * RTP_ERR_INVALID): a row never goes to a page that sequences share, whatever became of the reserve call in front. */
+  const int32_t* page_refs; /* DEVICE int32 [num_pages] */
 } rtp_cache;
 
 #define RTP_IKEY_BF16 0
@@ -223,7 +227,7 @@ rtp_status rtp_check_status(rtp_ctx* ctx, const int32_t* status, void* stream);
  * tok_seq DEVICE int32 [T] sequence of each token; tok_pos DEVICE int32 [T] its position
  * Writes ikey_pages[block_table[seq][pos/64], j, pos%64, :] for every token and
  * index head j: fp32 accumulation, rounded to bf16.  Pages must already be
- * mapped in block_table.  Nothing else is written. */
+ * mapped in block_table; with page_refs, rows of pages that are not their sequence's alone are skipped.  Nothing else is written. */
 rtp_status rtp_index_keys(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache,
                           const void* k_pre, const void* w_k, const int32_t* tok_seq,
                           const int32_t* tok_pos, int64_t T, void* stream);
@@ -233,7 +237,8 @@ rtp_status rtp_index_keys(rtp_ctx* ctx, const rtp_params* params, const rtp_cach
  * k_new, v_new DEVICE bf16 [T, n_kv_heads, 128] post-RoPE keys / values of T new tokens;
  * tok_seq, tok_pos DEVICE int32 [T].  Copies every row to
  * k_pages / v_pages[block_table[seq][pos/64], head, pos%64, :].  Tokens whose sequence or page
- * is out of range are skipped and RTP_ERR_INVALID is recorded in *status.  seq_lens is not
+ * is out of range (or, with page_refs, whose page is not their sequence's alone) are skipped and RTP_ERR_INVALID is recorded in
+ * *status.  seq_lens is not
  * modified (it belongs to the caller).  A position named twice in one call is left with a mixture of both rows (of their codes
  * and scales on a 4-bit cache, which is then neither's value). */
 rtp_status rtp_kv_append(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache,
@@ -258,8 +263,10 @@ rtp_status rtp_kv_expand(rtp_ctx* ctx, const rtp_params* params, const rtp_cache
  *                      that starts with an empty cache sets it to 0, block_table to -1 and seq_lens to 0;
  *   cache->block_table and cache->seq_lens, which they WRITE: an unmapped entry is -1, and the mapped entries of a sequence
  *                      come first in its row.
- * Everything happens on the device in stream order (a captured decode step can reserve its own pages), and results do not
- * depend on timing: free pages are handed out in the order of their numbers.  These calls refuse a cache with a local pool
+ * Everything happens on the device in stream order, and results do not depend on timing: free pages are handed out in the order
+ * of their numbers.  A captured decode step can reserve its own pages, but a reserve that finds the pool full only says so in the
+ * status word, and the appends behind it run all the same: such a step names the counts in cache->page_refs too, so that they
+ * leave shared pages alone.  (The calls below refuse a page_refs that differs from it.)  These calls refuse a cache with a local pool
  * (RTP_ERR_UNSUPPORTED), whose rings belong to one sequence each.  Rows named by an index out of range are skipped
  * and RTP_ERR_INVALID is recorded in the status word.
  *
@@ -275,7 +282,8 @@ rtp_status rtp_kv_expand(rtp_ctx* ctx, const rtp_params* params, const rtp_cache
  * rtp_cache_reserve: room for n_tokens[i] more tokens in sequence seqs[i] (positions seq_lens .. seq_lens + n_tokens - 1; seq_lens
  *   itself is left to the caller, as in rtp_kv_append).  Unmapped pages up to there are taken from the free ones, and a
  *   partly filled last page that other sequences share is replaced by a copy of its own, contents included, if at
- *   least one token is asked for.  (So every append behind a fork needs a reserve before it.)  A request is skipped and
+ *   least one token is asked for.  (So every append behind a fork needs a reserve before it, and must not run if that failed:
+ *   cache->page_refs sees to both.)  A request is skipped and
  *   RTP_ERR_INVALID recorded if the tokens would also go to further pages that are mapped already and shared (a sequence that
  *   the caller made shorter than what it shares has to be freed and forked anew), or to a page without references.  Requests are served in the order of the list: of r sequences that share a page and are all
  *   listed, the first r - 1 get copies.  If the free pages or a table row do not suffice for ALL requests, nothing changes and

@@ -60,6 +60,7 @@ class RtpCache(C.Structure):
         ("k_local_pages", C.c_void_p), ("v_local_pages", C.c_void_p), ("local_block_table", C.c_void_p),
         ("n_local_pages", C.c_int32), ("sink_pages", C.c_int32), ("ring_pages", C.c_int32),
         ("ikey_format", C.c_int32), ("kv_format", C.c_int32), ("kv_scales", C.c_void_p), ("kv_local_scales", C.c_void_p),
+        ("page_refs", C.c_void_p),
     ]
 
 
@@ -214,11 +215,12 @@ class Params:
 
 def make_cache(k_pages, v_pages, ikey_pages, block_table, seq_lens, k_local_pages=None, v_local_pages=None,
                local_block_table=None, sink_pages: int = 0, ikey_format: Optional[int] = None, kv_scales=None,
-               kv_local_scales=None) -> RtpCache:
+               kv_local_scales=None, page_refs=None) -> RtpCache:
     """Describes caller-owned paged caches (torch CUDA tensors) to the library.  With ``k_local_pages`` the cache is
     truncated for local heads: ``k_pages`` / ``v_pages`` hold the other KV heads only, the local heads live in the
     local pool behind ``local_block_table`` [batch, sink_pages + ring_pages].  With ``kv_scales`` the K/V pages are 4-bit codes
-    (uint8 [.., .., 64, 64], scales uint8 [.., .., 64, 16]; ``kv_local_scales`` goes with a local pool)."""
+    (uint8 [.., .., 64, 64], scales uint8 [.., .., 64, 16]; ``kv_local_scales`` goes with a local pool).  With ``page_refs`` (int32
+    [num_pages], the counts that the rtp_cache_* calls keep) rows are only appended to pages that one sequence alone holds."""
     num_pages = int((k_pages if k_pages is not None else ikey_pages).shape[0])
     if ikey_format is None:   # the tensor's element size says which: uint8 pages are E4M3 codes
         ikey_format = RTP_IKEY_E4M3 if (ikey_pages is not None and ikey_pages.element_size() == 1) else RTP_IKEY_BF16
@@ -230,7 +232,7 @@ def make_cache(k_pages, v_pages, ikey_pages, block_table, seq_lens, k_local_page
                     num_pages, block_table.shape[0], block_table.shape[1],
                     _ptr(k_local_pages), _ptr(v_local_pages), _ptr(local_block_table), n_local, int(sink_pages), ring,
                     int(ikey_format), RTP_KV_FP4 if kv_scales is not None else RTP_KV_BF16, _ptr(kv_scales),
-                    _ptr(kv_local_scales))
+                    _ptr(kv_local_scales), _ptr(page_refs))
 
 
 class Context:

@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(kProjThreads) project_kernel(
     const int seq = tok_seq[t], pos = tok_pos[t];
     if (seq < 0 || seq >= cv.batch || pos < 0 || (pos >> kPageShift) >= cv.max_pages) return;
     const int phys = cv.block_table[(int64_t)seq * cv.max_pages + (pos >> kPageShift)];
-    if (phys < 0 || phys >= cv.num_pages) return;
+    if (phys < 0 || phys >= cv.num_pages || !page_writable(cv, phys)) return;
     const int64_t at = (((int64_t)phys * cv.n_ih + head) * kPage + (pos & (kPage - 1))) * kIndexDim + j;
     if (cv.ikey_fp8)   // the fp32 sum straight to E4M3: nearest, ties to even, saturating at 448
       reinterpret_cast<uint8_t*>(cv.ikey)[at] = (uint8_t)__nv_cvt_float_to_fp8(acc, __NV_SATFINITE, __NV_E4M3);
@@ -88,7 +88,7 @@ __global__ void kv_append_kernel(CacheView cv, const int n_src_heads, const __nv
       continue;
     }
     const int phys = cv.block_table[(int64_t)seq * cv.max_pages + page_entry(cv, pos >> kPageShift)];
-    if (phys < 0 || phys >= cv.num_pages) {
+    if (phys < 0 || phys >= cv.num_pages || !page_writable(cv, phys)) {
       set_status(status, RTP_ERR_INVALID);
       continue;
     }

@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(kThreads) kv4_append_kernel(const __grid_const
       continue;
     }
     const int phys = __ldg(cv.block_table + (int64_t)seq * cv.max_pages + page_entry(cv, pos >> kPageShift));
-    if (phys < 0 || phys >= cv.num_pages) {
+    if (phys < 0 || phys >= cv.num_pages || !page_writable(cv, phys)) {
       set_status(status, RTP_ERR_INVALID);
       continue;
     }

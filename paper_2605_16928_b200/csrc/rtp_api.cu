@@ -122,6 +122,7 @@ const char* check_cache(const rtp_cache* c, const rtp_params* p, bool need_kv, b
   cv->kv_scales = cv->kv_fp4 ? reinterpret_cast<const uint8_t*>(c->kv_scales) : nullptr;
   if (cv->kv_fp4 && need_kv && !c->kv_scales) return "kv_scales is NULL";
   if (cv->kv_fp4 && !aligned16(c->kv_scales)) return "kv_scales must be 16-byte aligned";
+  cv->page_refs = c->page_refs;
   for (int h = 0; h < 32; ++h) cv->kv_slot[h] = h < p->n_kv_heads ? (uint8_t)h : (uint8_t)0xff;
   if (c->k_local_pages) {
     // truncated layout: the main pool holds the KV heads that are not local, in increasing order
@@ -152,6 +153,7 @@ CacheView local_view(const CacheView& main, const rtp_cache* c, const rtp_params
   v.v = reinterpret_cast<const __nv_bfloat16*>(c->v_local_pages);
   v.ikey = nullptr;
   v.kv_scales = v.kv_fp4 ? reinterpret_cast<const uint8_t*>(c->kv_local_scales) : nullptr;
+  v.page_refs = nullptr;   // (the counts are the main pool's)
   v.block_table = c->local_block_table;
   v.num_pages = c->n_local_pages;
   v.max_pages = c->sink_pages + c->ring_pages;
@@ -214,7 +216,7 @@ constexpr int kFallbackSm = 148;
 
 extern "C" {
 
-int32_t rtp_version(void) { return 200; }
+int32_t rtp_version(void) { return 201; }
 
 size_t rtp_struct_bytes(int32_t what) { return what == 0 ? sizeof(rtp_params) : (what == 1 ? sizeof(rtp_cache) : 0); }
 
@@ -381,6 +383,7 @@ rtp_status rtp_cache_copy_pages(rtp_ctx* ctx, const rtp_params* params, const rt
   if (const char* m_ = page_arrays(cache, cv, &pa)) return fail(ctx, RTP_ERR_INVALID, m_);                                 \
   if (cache->k_local_pages) return fail(ctx, RTP_ERR_UNSUPPORTED, "a cache with a local pool: its pages are the caller's"); \
   if (!page_refs) return fail(ctx, RTP_ERR_INVALID, "page_refs is NULL");                                                  \
+  if (cv.page_refs && cv.page_refs != page_refs) return fail(ctx, RTP_ERR_INVALID, "page_refs is not the cache's");         \
   if (!aligned16(page_refs)) return fail(ctx, RTP_ERR_INVALID, "page_refs must be 16-byte aligned");                       \
   if (n < 0) return fail(ctx, RTP_ERR_INVALID, "sequence count is negative");                                              \
   if (n > (limit)) return fail(ctx, RTP_ERR_UNSUPPORTED, "too many sequences in one call");                                \

@@ -220,6 +220,11 @@ __device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait
 __device__ __forceinline__ int page_entry(const CacheView& cv, int page) {
   return (cv.ring_pages > 0 && page >= cv.sink_pages) ? cv.sink_pages + (page - cv.sink_pages) % cv.ring_pages : page;
 }
+// Whether a row may be written to page `phys` (in range): nobody else's tokens lie there.  (Counts are read from L2: an earlier
+// kernel of the stream may just have changed them.)
+__device__ __forceinline__ bool page_writable(const CacheView& cv, int phys) {
+  return cv.page_refs == nullptr || __ldcg(cv.page_refs + phys) == 1;
+}
 __device__ __forceinline__ int safe_phys(const CacheView& cv, int64_t entry, int32_t* status = nullptr) {
   const int phys = __ldg(cv.block_table + entry);
   if ((unsigned)phys < (unsigned)cv.num_pages) return phys;

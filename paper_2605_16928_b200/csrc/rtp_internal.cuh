@@ -60,6 +60,8 @@ struct CacheView {
   // != 0: k / v point to 4-bit codes, uint8 [num_pages, n_kv, 64, 64], and kv_scales to their scales, uint8 [.., 64, 16]
   int32_t kv_fp4;
   const uint8_t* kv_scales;
+  // block-table entries that name each page of this pool, or NULL: rows are then only written to pages with a count of one
+  const int32_t* page_refs;
 };
 
 struct Dims {

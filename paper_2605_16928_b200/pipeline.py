@@ -212,7 +212,9 @@ class DecodePath(_Base):
 
 class PagePool:
     """Block table, sequence lengths and reference counts of a pool of pages, on the device.  ``cache_of`` gives the arrays of
-    the pool the description that the other calls take; every method is one call in stream order, nothing is read back.
+    the pool the description that the other calls take; every method is one call in stream order, nothing is read back.  The
+    description names the reference counts, so that appends leave pages alone that sequences share (after a reserve that found
+    the pool full, for instance).
     ``status`` collects what only the device can see (a full pool: RTP_ERR_CAPACITY)."""
 
     def __init__(self, params: rb.Params, num_pages: int, batch: int, max_pages: int, device="cuda:0"):
@@ -226,7 +228,8 @@ class PagePool:
         self.cache = self.workspace = None
 
     def cache_of(self, k_pages, v_pages, ikey_pages=None, kv_scales=None) -> rb.RtpCache:
-        self.cache = rb.make_cache(k_pages, v_pages, ikey_pages, self.block_table, self.seq_lens, kv_scales=kv_scales)
+        self.cache = rb.make_cache(k_pages, v_pages, ikey_pages, self.block_table, self.seq_lens, kv_scales=kv_scales,
+                                   page_refs=self.page_refs)
         self.workspace = torch.empty(rb.rtp_cache_workspace_bytes(self.cache, min(4096, int(self.seq_lens.shape[0]))),
                                      dtype=torch.uint8, device=self.seq_lens.device)
         return self.cache

@@ -51,3 +51,85 @@ def test_room_in_a_page_that_nobody_holds_is_refused():
         assert pool.invalid and d.code() == rb.RTP_ERR_INVALID
         d.same()
         assert pool.table[0].tolist() == table[0] and (pool.table[1] >= 0).all()
+
+
+def _page_pool(num_pages, batch, max_pages, kv4, n_ih=1):
+    """A PagePool over one KV head with index keys, and what appends a row of ones to a list of sequences."""
+    from paper_2605_16928_b200 import pipeline
+    params = rb.Params(2, 1, [0] * n_ih, [0] * n_ih, [0] * n_ih, [])
+    pool = pipeline.PagePool(params, num_pages=num_pages, batch=batch, max_pages=max_pages)
+    w = 64 if kv4 else 128
+    t = torch.uint8 if kv4 else torch.bfloat16
+    k, v = (torch.zeros((num_pages, 1, 64, w), dtype=t, device="cuda") for _ in range(2))
+    scales = torch.zeros((num_pages, 1, 64, 16), dtype=torch.uint8, device="cuda") if kv4 else None
+    ik = torch.zeros((num_pages, 1, 64, 16), dtype=torch.bfloat16, device="cuda")
+    cache = pool.cache_of(k, v, ik, kv_scales=scales)
+    w_k = torch.ones((1, 128, 16), dtype=torch.bfloat16, device="cuda")
+
+    def append(seqs, pos):
+        rows = torch.ones((len(seqs), 1, 128), dtype=torch.bfloat16, device="cuda") * (1 + torch.arange(len(seqs), device="cuda"))[:, None, None]
+        rb.rtp_kv_append(pool.ctx, params, cache, rows, -rows, _i32(seqs), _i32(pos), pool.status)
+        rb.rtp_index_keys(pool.ctx, params, cache, rows, w_k, _i32(seqs), _i32(pos))
+
+    return pool, append, [x for x in (k, v, scales, ik) if x is not None]
+
+
+@pytest.mark.parametrize("kv4", [False, True])
+def test_a_full_pool_keeps_shared_pages_as_they_are(kv4):
+    """Samples of a prompt whose reserve finds the pool full: the appends behind it leave the page that they share alone."""
+    pool, append, arrays = _page_pool(3, 4, 4, kv4)
+    pool.reserve(_i32([0]), _i32([100]))
+    append([0] * 100, list(range(100)))
+    pool.seq_lens[0] = 100
+    pool.fork(_i32([0, 0]), _i32([1, 2]))
+    assert rb.rtp_check_status(pool.ctx, pool.status) == rb.RTP_OK
+    before = [x.clone() for x in arrays]
+    graph = torch.cuda.CUDAGraph()                     # the step of a server: room, then the rows
+    seqs, one = _i32([0, 1, 2]), _i32([1, 1, 1])
+    rows = torch.ones((3, 1, 128), dtype=torch.bfloat16, device="cuda") * 3
+    w_k, pos = torch.ones((1, 128, 16), dtype=torch.bfloat16, device="cuda"), _i32([100, 100, 100])
+    with torch.cuda.graph(graph):
+        pool.reserve(seqs, one)
+        rb.rtp_kv_append(pool.ctx, pool.params, pool.cache, rows, -rows, seqs, pos, pool.status)
+        rb.rtp_index_keys(pool.ctx, pool.params, pool.cache, rows, w_k, seqs, pos)
+    graph.replay()
+    assert rb.rtp_check_status(pool.ctx, pool.status) == rb.RTP_ERR_CAPACITY
+    for x, b in zip(arrays, before):
+        assert torch.equal(x, b)
+    pool.status.zero_()
+    pool.free(_i32([2]))                               # one sample leaves: there is room for the others
+    rb.rtp_cache_reserve(pool.ctx, pool.params, pool.cache, pool.page_refs, _i32([0, 1]), _i32([1, 1]), pool.workspace, pool.status)
+    append([0, 1], [100, 100])
+    assert rb.rtp_check_status(pool.ctx, pool.status) == rb.RTP_OK
+    table = pool.block_table.tolist()
+    assert table[0][0] == table[1][0] and table[0][1] != table[1][1]
+    for x, b in zip(arrays, before):
+        assert torch.equal(x[table[0][0]], b[table[0][0]])
+        own = [x[table[s][1], :, 36] for s in (0, 1)]
+        assert own[0].any() and own[1].any()
+        assert x.shape[-1] == 64 or not torch.equal(own[0], own[1])      # (rows of ones and twos have the same 4-bit codes)
+        for s in (0, 1):
+            assert torch.equal(x[table[s][1], :, :36], b[1, :, :36])
+
+
+def test_appends_only_go_to_pages_that_one_sequence_holds():
+    """Counts of zero (not mapped by a reserve), one and two; a cache that does not name its counts is written as before."""
+    for kv4 in (False, True):
+        pool, append, arrays = _page_pool(4, 3, 2, kv4)
+        pool.block_table[:, 0] = _i32([0, 1, 2])
+        pool.page_refs.copy_(_i32([0, 1, 2, 0]))
+        before = [x.clone() for x in arrays]
+        append([0, 1, 2], [5, 5, 5])
+        assert rb.rtp_check_status(pool.ctx, pool.status) == rb.RTP_ERR_INVALID
+        for x, b in zip(arrays, before):
+            assert torch.equal(x[[0, 2, 3]], b[[0, 2, 3]]) and x[1, :, 5].any()
+        plain = rb.make_cache(arrays[0], arrays[1], None, pool.block_table, pool.seq_lens, kv_scales=arrays[2] if kv4 else None)
+        rows = torch.ones((3, 1, 128), dtype=torch.bfloat16, device="cuda")
+        pool.status.zero_()
+        rb.rtp_kv_append(pool.ctx, pool.params, plain, rows, rows, _i32([0, 1, 2]), _i32([6, 6, 6]), pool.status)
+        assert rb.rtp_check_status(pool.ctx, pool.status) == rb.RTP_OK
+        assert all(arrays[0][p, :, 6].any() for p in range(3))
+        other = torch.zeros_like(pool.page_refs)
+        with pytest.raises(rb.RtpError) as e:
+            rb.rtp_cache_free(pool.ctx, pool.params, pool.cache, other, _i32([0]), pool.status)
+        assert e.value.code == rb.RTP_ERR_INVALID and pool.block_table[0, 0] == 0
