@@ -218,6 +218,9 @@ class PagePool:
     ``status`` collects what only the device can see (a full pool: RTP_ERR_CAPACITY)."""
 
     def __init__(self, params: rb.Params, num_pages: int, batch: int, max_pages: int, device="cuda:0"):
+        dev = torch.device(device)
+        if dev.type == "cuda" and dev.index is not None and dev.index != torch.cuda.current_device():
+            raise rb.RtpError(rb.RTP_ERR_INVALID, "PagePool", f"{dev} is not the current device, on which the calls run")
         i32 = dict(dtype=torch.int32, device=device)
         self.ctx, self.params = rb.Context(), params
         self.block_table = torch.full((batch, max_pages), -1, **i32)
@@ -228,6 +231,17 @@ class PagePool:
         self.cache = self.workspace = None
 
     def cache_of(self, k_pages, v_pages, ikey_pages=None, kv_scales=None) -> rb.RtpCache:
+        """Arrays [num_pages, heads, 64, ..] on the pool's device: K and V with the parameter block's KV heads, index keys with
+        its index heads; None for what the cache does not hold."""
+        for name, x, heads in (("k_pages", k_pages, self.params.c.n_kv_heads), ("v_pages", v_pages, self.params.c.n_kv_heads),
+                               ("ikey_pages", ikey_pages, self.params.c.n_index_heads),
+                               ("kv_scales", kv_scales, self.params.c.n_kv_heads)):
+            if x is None:
+                continue
+            want = (self.page_refs.numel(), heads)
+            if tuple(x.shape[:2]) != want or x.device != self.page_refs.device or not x.is_contiguous():
+                raise rb.RtpError(rb.RTP_ERR_INVALID, "PagePool.cache_of",
+                                  f"{name} has to be a contiguous array of {want[0]} pages of {want[1]} heads on {self.page_refs.device}")
         self.cache = rb.make_cache(k_pages, v_pages, ikey_pages, self.block_table, self.seq_lens, kv_scales=kv_scales,
                                    page_refs=self.page_refs)
         self.workspace = torch.empty(rb.rtp_cache_workspace_bytes(self.cache, min(4096, int(self.seq_lens.shape[0]))),
