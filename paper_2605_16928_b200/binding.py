@@ -224,6 +224,16 @@ def make_cache(k_pages, v_pages, ikey_pages, block_table, seq_lens, k_local_page
     num_pages = int((k_pages if k_pages is not None else ikey_pages).shape[0])
     if ikey_format is None:   # the tensor's element size says which: uint8 pages are E4M3 codes
         ikey_format = RTP_IKEY_E4M3 if (ikey_pages is not None and ikey_pages.element_size() == 1) else RTP_IKEY_BF16
+    # the K/V pages' element size and kv_scales have to say the same: one format read as the other runs beyond the pages' end
+    wide = 2 if kv_scales is None else 1
+    for name, t in (("k_pages", k_pages), ("v_pages", v_pages), ("k_local_pages", k_local_pages), ("v_local_pages", v_local_pages)):
+        if hasattr(t, "element_size") and t.element_size() != wide:
+            raise RtpError(RTP_ERR_INVALID, "make_cache", f"{name} holds elements of {t.element_size()} bytes: " +
+                           ("4-bit codes (uint8) belong to kv_scales" if kv_scales is not None else "16-bit floats, or 4-bit codes with kv_scales"))
+    for name, t, n in (("kv_scales", kv_scales, num_pages),
+                       ("kv_local_scales", kv_local_scales, k_local_pages.shape[0] if k_local_pages is not None else 0)):
+        if hasattr(t, "element_size") and (t.element_size() != 1 or t.shape[0] < n):
+            raise RtpError(RTP_ERR_INVALID, "make_cache", f"{name} has to be uint8, one block for each of {n} pages")
     n_local, ring = 0, 0
     if k_local_pages is not None:
         n_local = k_local_pages.shape[0]
