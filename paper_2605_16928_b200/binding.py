@@ -174,6 +174,17 @@ def _i32_array(vals: Sequence[int]):
     return arr
 
 
+def _same_length(where: str, a, b):
+    """Arrays of which the library is told one length (None: not given)."""
+    if b is not None and a.shape[0] != b.shape[0]:
+        raise RtpError(RTP_ERR_INVALID, where, f"arrays that go together have {a.shape[0]} and {b.shape[0]} entries")
+
+
+def _enough_counts(where: str, cache, page_refs):
+    if hasattr(page_refs, "shape") and page_refs.shape[0] < cache.num_pages:
+        raise RtpError(RTP_ERR_INVALID, where, f"page_refs has {page_refs.shape[0]} counts for {cache.num_pages} pages")
+
+
 class Params:
     """Owns an ``rtp_params`` block and the host head-map arrays it points to."""
 
@@ -234,6 +245,8 @@ def make_cache(k_pages, v_pages, ikey_pages, block_table, seq_lens, k_local_page
                        ("kv_local_scales", kv_local_scales, k_local_pages.shape[0] if k_local_pages is not None else 0)):
         if hasattr(t, "element_size") and (t.element_size() != 1 or t.shape[0] < n):
             raise RtpError(RTP_ERR_INVALID, "make_cache", f"{name} has to be uint8, one block for each of {n} pages")
+    if hasattr(page_refs, "shape") and page_refs.shape[0] < num_pages:
+        raise RtpError(RTP_ERR_INVALID, "make_cache", f"page_refs has {page_refs.shape[0]} counts for {num_pages} pages")
     n_local, ring = 0, 0
     if k_local_pages is not None:
         n_local = k_local_pages.shape[0]
@@ -307,6 +320,8 @@ def rtp_kv_append(ctx, params, cache, k_new, v_new, tok_seq, tok_pos, status, st
 
 def rtp_kv_expand(ctx, params, cache, src_pages, dst_pages, k_out, v_out, status, stream=None):
     """src_pages, dst_pages (or None: page i): int32 [n]; k_out, v_out: bf16 [pages, KV heads of the main pool, 64, 128]."""
+    _same_length("rtp_kv_expand", src_pages, dst_pages)
+    _same_length("rtp_kv_expand", k_out, v_out)
     ctx._check(ctx.lib.rtp_kv_expand(ctx.h, params.ref(), C.byref(cache), _ptr(src_pages), _ptr(dst_pages),
                                      src_pages.shape[0], _ptr(k_out), _ptr(v_out), k_out.shape[0], _ptr(status),
                                      _stream(stream)), "rtp_kv_expand")
@@ -317,17 +332,22 @@ def rtp_cache_workspace_bytes(cache, n_seqs: int) -> int:
 
 
 def rtp_cache_copy_pages(ctx, params, cache, src_pages, dst_pages, status, stream=None):
+    _same_length("rtp_cache_copy_pages", src_pages, dst_pages)
     ctx._check(ctx.lib.rtp_cache_copy_pages(ctx.h, params.ref(), C.byref(cache), _ptr(src_pages), _ptr(dst_pages),
                                             src_pages.shape[0], _ptr(status), _stream(stream)), "rtp_cache_copy_pages")
 
 
 def rtp_cache_fork(ctx, params, cache, page_refs, src_seqs, dst_seqs, status, stream=None):
     """Writes page_refs and the block table and sequence lengths that ``cache`` describes (as the three calls below do)."""
+    _same_length("rtp_cache_fork", src_seqs, dst_seqs)
+    _enough_counts("rtp_cache_fork", cache, page_refs)
     ctx._check(ctx.lib.rtp_cache_fork(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(src_seqs), _ptr(dst_seqs),
                                       src_seqs.shape[0], _ptr(status), _stream(stream)), "rtp_cache_fork")
 
 
 def rtp_cache_reserve(ctx, params, cache, page_refs, seqs, n_tokens, workspace, status, stream=None):
+    _same_length("rtp_cache_reserve", seqs, n_tokens)
+    _enough_counts("rtp_cache_reserve", cache, page_refs)
     ctx._check(ctx.lib.rtp_cache_reserve(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(seqs), _ptr(n_tokens),
                                          seqs.shape[0], _ptr(workspace),
                                          workspace.nbytes, _ptr(status), _stream(stream)),
@@ -335,12 +355,14 @@ def rtp_cache_reserve(ctx, params, cache, page_refs, seqs, n_tokens, workspace, 
 
 
 def rtp_cache_free(ctx, params, cache, page_refs, seqs, status, stream=None):
+    _enough_counts("rtp_cache_free", cache, page_refs)
     ctx._check(ctx.lib.rtp_cache_free(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(seqs), seqs.shape[0],
                                       _ptr(status), _stream(stream)), "rtp_cache_free")
 
 
 def rtp_cache_compact(ctx, params, cache, page_refs, n_used, workspace, status, stream=None):
     """n_used: int32 [1] on the device, written."""
+    _enough_counts("rtp_cache_compact", cache, page_refs)
     ctx._check(ctx.lib.rtp_cache_compact(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(n_used), _ptr(workspace),
                                          workspace.nbytes, _ptr(status), _stream(stream)),
                "rtp_cache_compact")

@@ -36,3 +36,20 @@ def test_pages_and_scales_that_do_not_belong_together_are_refused(over):
     with pytest.raises(rb.RtpError) as e:
         _cache(**over)
     assert e.value.code == rb.RTP_ERR_INVALID
+
+
+def test_arrays_that_go_together_have_one_length():
+    """Calls that take the length of one array for another's: refused before the library is reached (there is no context here)."""
+    one, two, many = (torch.zeros(n, dtype=torch.int32) for n in (1, 2, 6))
+    c, ws = _cache(), torch.zeros(1 << 12, dtype=torch.uint8)
+    for call, args in ((rb.rtp_kv_expand, (two, None, _wide(6), _wide(5), one)), (rb.rtp_kv_expand, (two, None, _wide(5), _wide(6), one)),
+                       (rb.rtp_kv_expand, (two, one, _wide(), _wide(), one)), (rb.rtp_cache_copy_pages, (two, one, one)),
+                       (rb.rtp_cache_fork, (many, two, one, one)), (rb.rtp_cache_fork, (two, one, one, one)),
+                       (rb.rtp_cache_reserve, (many, two, one, ws, one)), (rb.rtp_cache_reserve, (two, one, one, ws, one)),
+                       (rb.rtp_cache_free, (two, one, one)), (rb.rtp_cache_compact, (two, one, ws, one))):
+        with pytest.raises(rb.RtpError) as e:
+            call(None, None, c, *args)
+        assert e.value.code == rb.RTP_ERR_INVALID
+    with pytest.raises(rb.RtpError):
+        _cache(page_refs=two)
+    assert _cache(page_refs=many).page_refs == many.data_ptr()
