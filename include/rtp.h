@@ -258,7 +258,8 @@ rtp_status rtp_kv_expand(rtp_ctx* ctx, const rtp_params* params, const rtp_cache
 
 /* ---- pages: copies, shared sequences, allocation, release, compaction (the paper has no counterpart) ----
  * The calls below manage the pages of the MAIN pool: every array that the cache names (k_pages, v_pages, kv_scales,
- * ikey_pages; NULL ones are left out) is treated alike.  Apart from rtp_cache_copy_pages they own
+ * ikey_pages; NULL ones are left out) is treated alike.  Their heads are those of the parameter block, which therefore has to be the one that
+ * the cache was laid out with (RTP_ERR_INVALID if there are ikey_pages and it has no index heads).  Apart from rtp_cache_copy_pages they own
  *   page_refs          DEVICE int32 [num_pages]: the number of block-table entries that name each page; 0 = free.  A caller
  *                      that starts with an empty cache sets it to 0, block_table to -1 and seq_lens to 0;
  *   cache->block_table and cache->seq_lens, which they WRITE: an unmapped entry is -1, and the mapped entries of a sequence

@@ -189,6 +189,7 @@ const char* check_rows(const int32_t* row_seq, const int32_t* row_pos, int32_t s
 const char* page_arrays(const rtp_cache* c, const CacheView& cv, PageArrays* pa) {
   if ((c->k_pages == nullptr) != (c->v_pages == nullptr)) return "k_pages and v_pages must both be given or both be NULL";
   if (c->k_pages && cv.kv_fp4 && !c->kv_scales) return "kv_scales is NULL";
+  if (c->ikey_pages && cv.n_ih == 0) return "ikey_pages, but no index heads in the parameter block: their size is not known";
   const int64_t kv = c->k_pages ? (int64_t)cv.n_kv * kPage * (cv.kv_fp4 ? kHeadDim / 2 : kHeadDim * 2) : 0;
   const int64_t sc = c->k_pages && cv.kv_fp4 ? (int64_t)cv.n_kv * kPage * (kHeadDim / 8) : 0;
   const int64_t ik = c->ikey_pages ? (int64_t)cv.n_ih * kPage * kIndexDim * (cv.ikey_fp8 ? 1 : 2) : 0;

@@ -133,3 +133,22 @@ def test_appends_only_go_to_pages_that_one_sequence_holds():
         with pytest.raises(rb.RtpError) as e:
             rb.rtp_cache_free(pool.ctx, pool.params, pool.cache, other, _i32([0]), pool.status)
         assert e.value.code == rb.RTP_ERR_INVALID and pool.block_table[0, 0] == 0
+
+
+def test_index_keys_are_not_left_behind():
+    """A parameter block without index heads does not say how large the index keys of a page are: refused by every page call."""
+    pool = Pool(10, 2, 4)
+    d = Device(pool, n_kv=2, n_ih=1)
+    none = rb.Params(2, 2, [], [], [], [])
+    one = _i32([0])
+    p = (d.ctx, none, d.cache)
+    for f, a in ((rb.rtp_cache_copy_pages, (one, _i32([1]), d.status)), (rb.rtp_cache_fork, (d.refs, one, _i32([1]), d.status)),
+                 (rb.rtp_cache_reserve, (d.refs, one, one, d.ws, d.status)), (rb.rtp_cache_free, (d.refs, one, d.status)),
+                 (rb.rtp_cache_compact, (d.refs, d.n_used, d.ws, d.status))):
+        with pytest.raises(rb.RtpError) as e:
+            f(*p, *a)
+        assert e.value.code == rb.RTP_ERR_INVALID
+        d.same()
+    d.cache = rb.make_cache(d.k, d.v, None, d.table, d.lens)
+    rb.rtp_cache_copy_pages(d.ctx, none, d.cache, one, _i32([1]), d.status)
+    assert d.code() == rb.RTP_OK and torch.equal(d.k[0].view(torch.uint8), d.k[1].view(torch.uint8))
