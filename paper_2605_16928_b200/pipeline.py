@@ -215,7 +215,7 @@ class PagePool:
     the pool the description that the other calls take; every method is one call in stream order, nothing is read back.  The
     description names the reference counts, so that appends leave pages alone that sequences share (after a reserve that found
     the pool full, for instance).
-    ``status`` collects what only the device can see (a full pool: RTP_ERR_CAPACITY)."""
+    ``status`` collects what only the device can see (a full pool: RTP_ERR_CAPACITY) until ``status_code`` reads it."""
 
     def __init__(self, params: rb.Params, num_pages: int, batch: int, max_pages: int, device="cuda:0"):
         dev = torch.device(device)
@@ -261,4 +261,8 @@ class PagePool:
         rb.rtp_cache_compact(self.ctx, self.params, self.cache, self.page_refs, self.n_used, self.workspace, self.status)
 
     def status_code(self) -> int:
-        return rb.rtp_check_status(self.ctx, self.status)
+        """The largest code recorded since the last call of this method, which clears it."""
+        code = rb.rtp_check_status(self.ctx, self.status)
+        if code != rb.RTP_OK:
+            self.status.zero_()
+        return code

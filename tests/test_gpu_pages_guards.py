@@ -152,3 +152,21 @@ def test_index_keys_are_not_left_behind():
     d.cache = rb.make_cache(d.k, d.v, None, d.table, d.lens)
     rb.rtp_cache_copy_pages(d.ctx, none, d.cache, one, _i32([1]), d.status)
     assert d.code() == rb.RTP_OK and torch.equal(d.k[0].view(torch.uint8), d.k[1].view(torch.uint8))
+
+
+def test_a_full_pool_is_reported_once():
+    """Evicting and trying again: the status of the calls since the last look, not of all calls ever."""
+    pool, append, _ = _page_pool(3, 3, 4, True)
+    pool.reserve(_i32([0]), _i32([128]))
+    assert pool.status_code() == rb.RTP_OK
+    pool.reserve(_i32([1]), _i32([128]))
+    assert pool.status_code() == rb.RTP_ERR_CAPACITY
+    assert pool.status_code() == rb.RTP_OK
+    pool.free(_i32([0]))
+    pool.reserve(_i32([1]), _i32([128]))
+    assert pool.status_code() == rb.RTP_OK and (pool.block_table[1, :2] >= 0).all()
+    pool.free(_i32([7]))
+    pool.reserve(_i32([2]), _i32([1]))
+    assert pool.status_code() == rb.RTP_ERR_INVALID
+    pool.reserve(_i32([0]), _i32([300]))
+    assert pool.status_code() == rb.RTP_ERR_CAPACITY
