@@ -524,7 +524,8 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
         }
       }
       if (g == 0 && (!kPairs || c < 2)) {
-        rw[kHeadDim] = empty[j] ? -INFINITY : base[j];
+        // (scores that are not numbers leave no reference behind, but a sum that is none either: that has to reach the output)
+        rw[kHeadDim] = l[j] != l[j] ? 0.f : empty[j] ? -INFINITY : base[j];
         rw[kHeadDim + 1] = l[j];
       }
     }
@@ -561,11 +562,11 @@ __global__ void __launch_bounds__(kThreads, 4) attn_rows4_kernel(
     }
     if (n_splits == 1) {
       const int64_t oh = (int64_t)r * d.n_q + qh0 + gg;
-      const float inv = lt > 0.f ? 1.f / lt : 0.f;
+      const float inv = lt == 0.f ? 0.f : 1.f / lt;   // (a sum that is not a number gives such an output)
       __nv_bfloat162* to = reinterpret_cast<__nv_bfloat162*>(out + oh * kHeadDim) + lane;
       to[0] = __floats2bfloat162_rn(a0.x * inv, a0.y * inv);
       to[32] = __floats2bfloat162_rn(a1.x * inv, a1.y * inv);
-      if (lse && lane == 0) lse[oh] = lt > 0.f ? (mt + log2f(lt)) * kLn2 : -INFINITY;
+      if (lse && lane == 0) lse[oh] = lt == 0.f ? -INFINITY : (mt + log2f(lt)) * kLn2;
     } else {
       float2* p = reinterpret_cast<float2*>(partial + (((int64_t)blockIdx.x * G + gg) * n_splits + split) * kPartial);
       p[lane] = a0;
@@ -659,8 +660,8 @@ __global__ void __launch_bounds__(32 * W) attn_merge4_kernel(
 #pragma unroll
   for (int k = 0; k < W; ++k) a += red[k][tid];
   const int64_t oh = r * d.n_q + qh;
-  out[oh * kHeadDim + tid] = __float2bfloat16_rn(lt > 0.f ? a / lt : 0.f);
-  if (lse && tid == 0) lse[oh] = lt > 0.f ? (mt + log2f(lt)) * kLn2 : -INFINITY;
+  out[oh * kHeadDim + tid] = __float2bfloat16_rn(lt == 0.f ? 0.f : a / lt);
+  if (lse && tid == 0) lse[oh] = lt == 0.f ? -INFINITY : (mt + log2f(lt)) * kLn2;
 }
 
 template <int G, int SET>
