@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(kUniThreads) blk_union_kernel(const CacheView 
   }
   const int nb = (n_keys + kPage - 1) >> kPageShift;
   const int nbw = (nb + 31) >> 5;
-  __shared__ int s_cnt[8];                 // list length of head g of the group (0: not a retrieval head)
+  __shared__ __align__(16) int s_cnt[8];   // list length of head g of the group (0: not a retrieval head)
   __shared__ const int32_t* s_lst[8];
   for (int i = tid; i < d.group * nbw_max; i += kUniThreads) uni_bits[i] = 0u;
   if (tid == 0) s_base = 0;
@@ -387,10 +387,14 @@ __global__ void __launch_bounds__(kUniThreads) blk_union_kernel(const CacheView 
     }
   }
   __syncthreads();
-  // the threads are dealt to the heads, so that the loads of all heads are in flight together (groups of 1, 2, 4 or 8)
-  {
-    const int per = kUniThreads / d.group, g = tid / per, t = tid % per;
-    const int cnt = s_cnt[g];
+  // the threads are dealt to the heads that have a list, so that the loads of all of them are in flight together
+  const int4 c0 = *reinterpret_cast<const int4*>(s_cnt), c1 = *reinterpret_cast<const int4*>(s_cnt + 4);
+  uint32_t act = (c0.x > 0 ? 1u : 0u) | (c0.y > 0 ? 2u : 0u) | (c0.z > 0 ? 4u : 0u) | (c0.w > 0 ? 8u : 0u) | (c1.x > 0 ? 16u : 0u) |
+                 (c1.y > 0 ? 32u : 0u) | (c1.z > 0 ? 64u : 0u) | (c1.w > 0 ? 128u : 0u);
+  const int per = kUniThreads / max(__popc(act), 1), t = tid % per;
+  for (int k = tid / per; k > 0; --k) act &= act - 1u;
+  if (act) {   // (none for the threads that the division leaves over)
+    const int g = __ffs(act) - 1, cnt = s_cnt[g];
     const int32_t* lst = s_lst[g];
     for (int j0 = t; j0 < cnt; j0 += per * kUniLoads) {
       int page[kUniLoads];
@@ -409,12 +413,15 @@ __global__ void __launch_bounds__(kUniThreads) blk_union_kernel(const CacheView 
   }
   __syncthreads();
   int32_t* out = uni_idx + (int64_t)blockIdx.x * uni_stride;
-  for (int w0 = 0; w0 < nbw; w0 += kUniThreads / 4) {   // (a thread writes the pages of a quarter of a word)
-    const int w = w0 + (tid >> 2);
+  // a thread writes the pages of a quarter or a half of a word, or of a word: as few as one round allows
+  const int cut = nbw <= kUniThreads / 4 ? 2 : nbw <= kUniThreads / 2 ? 1 : 0, bits = 32 >> cut;
+  const uint32_t part = (0xffffffffu >> (32 - bits)) << (bits * (tid & ((1 << cut) - 1)));
+  for (int w0 = 0; w0 < nbw; w0 += kUniThreads >> cut) {
+    const int w = w0 + (tid >> cut);
     uint32_t any = 0u;
     if (w < nbw)
       for (int g = 0; g < d.group; ++g) any |= uni_bits[g * nbw_max + w];
-    any &= 0xffu << (8 * (tid & 3));
+    any &= part;
     const int mine = __popc(any);
     int inc = mine;
 #pragma unroll

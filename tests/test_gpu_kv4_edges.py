@@ -60,3 +60,50 @@ def test_a_query_that_is_not_a_number(L, group, bad):
     c.out.fill_(-77), c.lse.fill_(-77)
     rb.rtp_sparse_attn_decode(*c.args(), tok, torch.zeros_like(cnt), c.out, c.lse, c.ws, c.status)
     assert not c.out[0, :group].any() and (c.lse[0, :group] == -np.inf).all()
+
+
+@pytest.mark.parametrize("ret", [[0], [7], [1, 6], [0, 3, 5], [0, 1, 2, 4, 7], list(range(8))])
+def test_page_lists_of_some_heads_of_a_group(ret):
+    """Any number of a group's eight heads with a list, lists of any length (none at all for one), pages of every word."""
+    h = _h()
+    L, W = 5000, 79
+    c = h.Cache4([L, 700], n_kv=1, group=8, k=[np.tile(np.random.default_rng(0).standard_normal((100, 1, 128)), (n // 100, 1, 1)) for n in (L, 700)])
+    c.params = rb.Params(8, 1, ret, [0] * len(ret), [0], [])
+    c.ret = ret
+    rng = np.random.default_rng(len(ret))
+    cnt = np.array([[[W, 0, 40, 1, 79, 13, 3, 64][i] for i in range(len(ret))], [min(11, 1 + 3 * i) for i in range(len(ret))]])
+    idx = np.stack([[rng.permutation(n)[np.arange(W) % n] for _ in ret] for n in (W, 11)])
+    sets = lambda r, hd: [t for p in idx[r, ret.index(hd), :cnt[r, ret.index(hd)]] for t in range(64 * p, min(64 * p + 64, c.lens[r]))]
+    rb.rtp_sparse_attn_decode_blocks(*c.args(), h.dev_i32(idx), h.dev_i32(cnt), c.out, c.lse, c.ws, c.status)
+    assert c.code() == rb.RTP_OK
+    c.check(ret, sets)
+
+
+@pytest.mark.parametrize("n_pages", [8191, 8193, 16384, 16400])
+def test_page_lists_of_long_tables(n_pages):
+    """Unions of up to 512 words of 32 pages and beyond: every listed page of a list without an order is attended to once per head
+    (a table that maps all pages of a sequence to one: the log-sum-exp counts the tokens)."""
+    h = _h()
+    c = h.Cache4([64], n_kv=1, group=4, k=[np.zeros((64, 1, 128))])
+    L = 64 * n_pages - 5
+    table = h.dev_i32(np.full((1, n_pages), c.bt[0, 0]))
+    lens = h.dev_i32([L])
+    cache = rb.make_cache(c.d_k, c.d_v, None, table, lens, kv_scales=c.d_s)
+    c.params = rb.Params(4, 1, [0, 2, 3], [0] * 3, [0], [])
+    cnt = np.array([[n_pages, 1000, 1]])
+    rng = np.random.default_rng(n_pages)
+    idx = np.stack([rng.permutation(n_pages) for _ in range(3)])[None]
+    idx[0, 2, 0] = n_pages - 1
+    ws = torch.empty(rb.rtp_workspace_bytes(c.params, 1, L), dtype=torch.uint8, device="cuda")
+    rb.rtp_sparse_attn_decode_blocks(c.ctx, c.params, cache, c.d_q, h.dev_i32([0]), h.dev_i32([L - 1]), h.dev_i32(idx), h.dev_i32(cnt),
+                                     c.out, c.lse, ws, c.status)
+    assert c.code() == rb.RTP_OK
+    tokens = [64 * n - 5 * bool((idx[0, i, :n] == n_pages - 1).any()) for i, n in enumerate(cnt[0])]
+    lse = c.lse[0, [0, 2, 3]].double().cpu().numpy()
+    # scores are zero: sums of ones (times 2^7), exact in fp32 up to 2^24; a logarithm and a product in fp32
+    assert (np.abs(lse - np.log(tokens)) <= 2.0 ** -22 * np.log(tokens)).all(), (lse, np.log(tokens))
+    v = c.v[0][:, 0]
+    want = v.mean(0)
+    got = c.out[0, 0].double().cpu().numpy()
+    # all heads but the tail of five tokens in one page: the mean moves by at most 5 |v| / L; fp16 probabilities are exact (2^7)
+    assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 20 * np.abs(v).max() / L + 2.0 ** -14).all()
