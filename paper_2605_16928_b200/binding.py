@@ -208,7 +208,6 @@ class Params:
                            C.cast(self._a, C.POINTER(C.c_int32)), C.cast(self._b, C.POINTER(C.c_int32)),
                            C.cast(self._c, C.POINTER(C.c_int32)), C.cast(self._d, C.POINTER(C.c_int32)),
                            top_k, force_sink, force_recent)
-        self._ref = C.byref(self.c)
 
     @classmethod
     def from_workload(cls, wl, **over) -> "Params":
@@ -221,7 +220,7 @@ class Params:
         return cls(**kw)
 
     def ref(self):
-        return self._ref
+        return C.byref(self.c)
 
 
 def make_cache(k_pages, v_pages, ikey_pages, block_table, seq_lens, k_local_pages=None, v_local_pages=None,

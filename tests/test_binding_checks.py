@@ -53,3 +53,13 @@ def test_arrays_that_go_together_have_one_length():
     with pytest.raises(rb.RtpError):
         _cache(page_refs=two)
     assert _cache(page_refs=many).page_refs == many.data_ptr()
+
+
+def test_a_replaced_parameter_block_is_the_one_that_calls_take():
+    from paper_2605_16928_b200 import build as rbuild
+    rbuild.build_library()
+    p = rb.Params(8, 2, [], [], [], [])
+    before = rb.rtp_workspace_bytes(p, 1, 4096)
+    other = rb.Params(8, 2, list(range(8)), [0] * 8, [0], [])
+    p.c = other.c
+    assert rb.rtp_workspace_bytes(p, 1, 4096) > before
