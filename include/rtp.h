@@ -156,7 +156,8 @@ typedef struct rtp_cache {
    * as 0, and RTP_ERR_UNSUPPORTED is recorded in the status word for either.  The decode calls (rtp_sparse_attn_decode,
    * rtp_sparse_attn_decode_static, rtp_sparse_attn_decode_blocks, rtp_dense_attn_decode, rtp_local_attn with row arrays)
    * and the list form of rtp_sparse_attn_prefill read such a cache; the other prefill calls need bf16 pages
-   * (RTP_ERR_UNSUPPORTED), which rtp_kv_expand makes of it.  A query head that holds a NaN, or an infinity that meets a key of
+   * (RTP_ERR_UNSUPPORTED), which rtp_kv_expand makes of the main pool's.  (A local pool is not expanded: its heads are served by
+   * rtp_local_attn with row arrays, a chunk's rows included.)  A query head that holds a NaN, or an infinity that meets a key of
    * zero, gives an output and a log-sum-exp that are not numbers. */
   int32_t kv_format;
   void* kv_scales;       /* DEVICE, RTP_KV_FP4 only */

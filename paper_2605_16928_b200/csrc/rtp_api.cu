@@ -743,7 +743,9 @@ rtp_status rtp_local_attn(rtp_ctx* ctx, const rtp_params* params, const rtp_cach
   if (R == 0 || params->n_local_kv_heads == 0) return RTP_OK;
   if (!q || !out) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
-  if (cv.kv_fp4 && !row_seq) return fail(ctx, RTP_ERR_UNSUPPORTED, "4-bit K/V cache: row arrays only (or rtp_kv_expand its pages)");
+  if (cv.kv_fp4 && !row_seq)
+    return fail(ctx, RTP_ERR_UNSUPPORTED, cache->k_local_pages ? "4-bit K/V cache with a local pool: row arrays only"
+                                                               : "4-bit K/V cache: row arrays only (or rtp_kv_expand its pages)");
   hm.n_kv_list = params->n_local_kv_heads;
   for (int i = 0; i < hm.n_kv_list; ++i) hm.kv_list[i] = (uint8_t)params->local_kv_heads[i];
   // a mixed group: its retrieval heads are written by the sparse call, not by this one

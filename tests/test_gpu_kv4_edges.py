@@ -107,3 +107,33 @@ def test_page_lists_of_long_tables(n_pages):
     got = c.out[0, 0].double().cpu().numpy()
     # all heads but the tail of five tokens in one page: the mean moves by at most 5 |v| / L; fp16 probabilities are exact (2^7)
     assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 20 * np.abs(v).max() / L + 2.0 ** -14).all()
+
+
+def test_a_chunk_over_a_4bit_local_pool():
+    """The chunk form is refused, without the advice to expand a pool that no call expands; the same rows as row arrays answer
+    like the rows over one pool, bit for bit."""
+    h = _h()
+    L, C, window = 400, 50, 100
+    rng = np.random.default_rng(3)
+    k, v = (rng.standard_normal((L, 2, 128)) for _ in range(2))
+    c = h.Cache4([L], n_kv=2, group=2, ret_kv=(0,), local_kv=(1,), window=window, n_sink=4, k=[k], v=[v])
+    c.set_rows(rng.standard_normal((C, 4, 128)), [0] * C, L - C + np.arange(C))
+    kl, vl = (torch.full((8, 1, 64, 64), 255, dtype=torch.uint8, device="cuda") for _ in range(2))
+    sl = torch.full((8, 1, 64, 16), 255, dtype=torch.uint8, device="cuda")
+    ring = 6
+    km, vm, sm = (x[:, :1].contiguous() for x in (c.d_k, c.d_v, c.d_s))
+    table = h.dev_i32(rng.permutation(8)[:1 + ring][None])
+    cache = rb.make_cache(km, vm, None, c.d_bt, c.d_lens, kl, vl, table, 1, kv_scales=sm, kv_local_scales=sl)
+    for lo in range(0, L, 100):
+        rb.rtp_kv_append(c.ctx, c.params, cache, h.dev_bf16(k[lo:lo + 100]), h.dev_bf16(v[lo:lo + 100]), h.dev_i32([0] * 100),
+                         h.dev_i32(range(lo, lo + 100)), c.status)
+    p = (c.ctx, c.params, cache)
+    with pytest.raises(rb.RtpError) as e:
+        rb.rtp_local_attn(*p, c.d_q, None, None, 0, L - C, C, c.out, c.lse, c.ws, c.status)
+    assert e.value.code == rb.RTP_ERR_UNSUPPORTED and "expand" not in str(e.value)
+    rb.rtp_local_attn(*c.args(), 0, 0, C, c.out, c.lse, c.ws, c.status)
+    want = c.out.clone(), c.lse.clone()
+    c.out.fill_(-77), c.lse.fill_(-77)
+    rb.rtp_local_attn(*p, *c.args()[3:], 0, 0, C, c.out, c.lse, c.ws, c.status)
+    assert c.code() == rb.RTP_OK and torch.equal(c.out, want[0]) and torch.equal(c.lse, want[1])
+    c.check([2, 3], lambda r, hd: [t for t in range(c.row_pos[r] + 1) if t < 4 or t > c.row_pos[r] - window])
