@@ -94,7 +94,7 @@ class PrefillPath(_Base):
         self.sel_tie = torch.empty((chunk, self.n_ret), dtype=torch.int32, device=self.dev)
         self.tok_seq = torch.zeros(chunk, dtype=torch.int32, device=self.dev)
         self.pos_all = torch.arange(L, dtype=torch.int32, device=self.dev)
-        self.launches_per_chunk = 6   # index_keys, 2 x query projection, select, sparse attention, local attention
+        self.launches_per_chunk = 6 + kv_fp4   # (expansion,) index_keys, 2 x query projection, select, sparse attention, local attention
         self.blk_mask = None          # block-wise path (Section 3.4): allocated on first use
 
     def _expand(self, n_tokens: int):

@@ -137,3 +137,22 @@ def test_a_chunk_over_a_4bit_local_pool():
     rb.rtp_local_attn(*p, *c.args()[3:], 0, 0, C, c.out, c.lse, c.ws, c.status)
     assert c.code() == rb.RTP_OK and torch.equal(c.out, want[0]) and torch.equal(c.lse, want[1])
     c.check([2, 3], lambda r, hd: [t for t in range(c.row_pos[r] + 1) if t < 4 or t > c.row_pos[r] - window])
+
+
+def test_launches_of_a_prefill_chunk_are_counted():
+    from torch.profiler import ProfilerActivity, profile
+
+    from paper_2605_16928_b200 import pipeline, synth_device
+    L = 300
+    data = synth_device.config_3_device(L=L, window=100)
+    for kv_fp4 in (False, True):
+        path = pipeline.PrefillPath(data, L, kv_fp4=kv_fp4)
+        out = torch.zeros((L, 32, 128), dtype=torch.bfloat16, device="cuda")
+        kp = data.k_pre_rows(0, 0, L)
+        path.run_chunk(0, L, data.q[:L], kp, out)
+        torch.cuda.synchronize()
+        with profile(activities=[ProfilerActivity.CUDA]) as p:
+            path.run_chunk(0, L, data.q[:L], kp, out)
+            torch.cuda.synchronize()
+        kernels = [e for e in p.events() if e.device_type == torch.autograd.DeviceType.CUDA and "rtp::" in e.name]
+        assert len(kernels) == path.launches_per_chunk, [e.name for e in kernels]
