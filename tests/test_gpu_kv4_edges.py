@@ -156,3 +156,55 @@ def test_launches_of_a_prefill_chunk_are_counted():
             torch.cuda.synchronize()
         kernels = [e for e in p.events() if e.device_type == torch.autograd.DeviceType.CUDA and "rtp::" in e.name]
         assert len(kernels) == path.launches_per_chunk, [e.name for e in kernels]
+
+
+@pytest.mark.parametrize("cols", [0, 70, 2048, 16384])
+def test_tables_wider_than_their_sequences(cols):
+    """A server's table is as wide as its longest context: splits are planned for that, the sequences are short."""
+    h = _h()
+    c = h.Cache4([4096, 1, 700], n_kv=2, group=4, ret_kv=(0,), local_kv=(1,), window=500, seed=7, table_cols=cols,
+                 k=[np.tile(np.random.default_rng(b).standard_normal((min(n, 128), 2, 128)), (max(1, n // 128), 1, 1))[:n] if n != 700 else
+                    np.random.default_rng(9).standard_normal((700, 2, 128)) for b, n in enumerate([4096, 1, 700])])
+    ws = torch.empty(max(c.ws.numel(), rb.rtp_workspace_bytes(c.params, 3, 64 * max(64, cols))), dtype=torch.uint8, device="cuda")
+    rb.rtp_dense_attn_decode(*c.args(), None, c.out, c.lse, ws, c.status)
+    c.check(range(8), lambda r, hd: range(c.lens[r]))
+    c.out.fill_(-77), c.lse.fill_(-77)
+    rb.rtp_local_attn(*c.args(), 0, 0, 3, c.out, c.lse, ws, c.status)
+    c.check(range(4, 8), lambda r, hd: [t for t in range(c.lens[r]) if t < 4 or t >= c.lens[r] - 500])
+    rng = np.random.default_rng(cols)
+    n_pages = [-(-n // 64) for n in c.lens]
+    cnt = np.array([[rng.integers(0, n + 1) for _ in range(4)] for n in n_pages])
+    idx = np.stack([[rng.permutation(n)[np.arange(64) % n] for _ in range(4)] for n in n_pages])
+    sets = lambda r, hd: [t for p in idx[r, hd, :cnt[r, hd]] for t in range(64 * p, min(64 * p + 64, c.lens[r]))]
+    for w in (ws, torch.empty(16, dtype=torch.uint8, device="cuda")):
+        c.out.fill_(-77), c.lse.fill_(-77)
+        rb.rtp_sparse_attn_decode_blocks(*c.args(), h.dev_i32(idx), h.dev_i32(cnt), c.out, c.lse, w, c.status)
+        c.check(range(4), sets)
+    cnt = np.array([[min(n, 900), 1, 0, n // 2] for n in c.lens])
+    idx = np.stack([[rng.permutation(n)[np.arange(900) % n] for _ in range(4)] for n in c.lens])
+    c.out.fill_(-77), c.lse.fill_(-77)
+    rb.rtp_sparse_attn_decode(*c.args(), h.dev_i32(idx), h.dev_i32(cnt), c.out, c.lse, ws, c.status)
+    cnt = np.minimum(cnt, 900)
+    c.check(range(4), lambda r, hd: idx[r, hd, :cnt[r, hd]])
+    assert c.code() == rb.RTP_OK
+
+
+@pytest.mark.parametrize("entry", [-1, 10 ** 6, 2 ** 31 - 1, -2 ** 31])
+def test_table_entries_that_name_no_page(entry):
+    """An unmapped entry inside a sequence, or one beyond the pool: reported; the rows of other sequences answer as ever."""
+    h = _h()
+    c = h.Cache4([300, 200], n_kv=2, group=2, ret_kv=(0,), local_kv=(1,), window=250, seed=3)
+    c.d_bt[0, 2] = entry
+    tok, cnt = h.dev_i32(np.tile(np.arange(200), (2, 2, 1))), h.dev_i32(np.full((2, 2), 200))
+    page, n_page = h.dev_i32(np.tile(np.arange(4), (2, 2, 1))), h.dev_i32(np.full((2, 2), 4))
+    local = lambda r, hd: [t for t in range(200) if t < 4 or t >= 200 - 250]
+    for call, heads, sets in (
+            (lambda: rb.rtp_dense_attn_decode(*c.args(), None, c.out, c.lse, c.ws, c.status), range(4), lambda r, hd: range(200)),
+            (lambda: rb.rtp_local_attn(*c.args(), 0, 0, 2, c.out, c.lse, c.ws, c.status), range(2, 4), local),
+            (lambda: rb.rtp_sparse_attn_decode(*c.args(), tok, cnt, c.out, c.lse, c.ws, c.status), range(2), lambda r, hd: range(200)),
+            (lambda: rb.rtp_sparse_attn_decode_blocks(*c.args(), page, n_page, c.out, c.lse, c.ws, c.status), range(2), lambda r, hd: range(200))):
+        c.status.zero_()
+        c.out.fill_(-77), c.lse.fill_(-77)
+        call()
+        assert c.code() == rb.RTP_ERR_INVALID
+        c.check(heads, sets, rows=[1])
