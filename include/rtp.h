@@ -215,7 +215,9 @@ rtp_status rtp_debug_select_path(rtp_ctx* ctx, int32_t path);
  * its cut on demand, sized at 32 KB per (row, head), rounded up to whole
  * tiles of 128 pairs (2 GB for 8192 rows x 8 heads).  A larger workspace is
  * used in full; a row that finds the pool empty narrows its candidates by one
- * more pass over the keys instead. */
+ * more pass over the keys instead.  The split scratch of the decode calls is sized for
+ * either K/V format: a 4-bit cache is cut into up to four times as many splits as
+ * a bf16 one where contexts are short.  A call with less takes fewer splits. */
 size_t rtp_workspace_bytes(const rtp_params* params, int64_t rows, int64_t max_seq_len);
 
 /* Synchronises `stream`, reads the DEVICE status word and returns it as an

@@ -25,8 +25,8 @@
 //
 // What bounds it: 484 warp instructions per 32 tokens and KV head (128 conversions, 128 products with scales, 32 MMAs, 32 shared
 // reads, 9 copies; an issue slot in two of three cycles) next to 4.6 KB.  4 x 512K tokens, 8 KV heads, groups of 4 (2.4 GB):
-// 367 us = 6.6 TB/s from a cold card, about 440 at its power limit; a tenth of the tokens in lists per head, random rows: 74 us,
-// bound by DRAM's 64-byte pieces (192 bytes a token instead of 144).
+// 367 to 390 us = 6.2 to 6.6 TB/s from a cold card, 430 to 470 at its power limit; a tenth of the tokens in lists per head, random rows:
+// 74 us, bound by DRAM's 64-byte pieces (192 bytes for each of 1.63 M list entries, 4.2 TB/s; a token that two heads list is gathered twice).
 #include "kv4.cuh"
 
 namespace rtp {
@@ -696,8 +696,9 @@ int max_splits4(int64_t units, int64_t max_set, int sm_count) {
 // Split count of a call.  Long sets get one round of the four resident CTAs per SM.  Shorter ones get one or two CTAs per SM:
 // they finish as early, with fewer partial results to merge (8 KV heads, us with 1 / 2 / 4 CTAs per SM: 4K tokens 5.8 / 6.7 /
 // 8.2, 8K 7.1 / 7.5 / 8.6, 32K 14.2 / 12.3 / 13.1, 64K and more best with 4), as long as a CTA has at most 512 tokens (four
-// tiles per warp) per resident CTA; a list, whose tokens come one by one, 128.  No CTA gets fewer than 128 tokens (a tile per
-// warp), and the four warps equally many tiles where the count is free.
+// tiles per warp) per resident CTA; a list, whose tokens come one by one, 128.  `max_set` is what the block table (or the
+// list's stride) has room for: a set of that size gives every CTA at least 128 tokens (a tile per warp), and the four warps equally
+// many tiles where the count is free.  A shorter one in a wide table is dealt out in pairs of tiles, over fewer of the CTAs.
 int plan_splits4(int64_t units, int64_t max_set, int sm_count, bool list) {
   if (units <= 0) return 1;
   const int64_t tiles = (max_set + kTileTok - 1) / kTileTok, cap = std::max<int64_t>(1, (tiles + kWarps - 1) / kWarps);

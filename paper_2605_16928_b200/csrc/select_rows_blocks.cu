@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(kUniThreads) blk_union_kernel(const CacheView 
   }
   __syncthreads();
   int32_t* out = uni_idx + (int64_t)blockIdx.x * uni_stride;
-  // a thread writes the pages of a quarter or a half of a word, or of a word: as few as one round allows
+  // a thread writes the pages of a quarter or a half of a word, or of a whole word: the smallest piece with which one pass of the loop does
   const int cut = nbw <= kUniThreads / 4 ? 2 : nbw <= kUniThreads / 2 ? 1 : 0, bits = 32 >> cut;
   const uint32_t part = (0xffffffffu >> (32 - bits)) << (bits * (tid & ((1 << cut) - 1)));
   for (int w0 = 0; w0 < nbw; w0 += kUniThreads >> cut) {
