@@ -79,7 +79,8 @@ class PrefillPath(_Base):
 
     def __init__(self, data, chunk: int, kv_fp4: bool = False):
         """kv_fp4: every run_* call expands the pages of the sequence so far to bf16 and attends to those (``attn_cache``);
-        the expansion of 128K tokens is about a hundredth of a chunk's dense attention over them."""
+        the expansion of 128K tokens is about a hundredth of a chunk's dense attention over them.  The bf16 pool stands beside the
+        4-bit one for as long as the path does: the saving is the decode's that follows."""
         L = int(data.seq_lens[0])
         super().__init__(data, chunk, L, kv_fp4=kv_fp4)
         self.L, self.chunk = L, chunk
@@ -232,7 +233,8 @@ class PagePool:
 
     def cache_of(self, k_pages, v_pages, ikey_pages=None, kv_scales=None) -> rb.RtpCache:
         """Arrays [num_pages, heads, 64, ..] on the pool's device: K and V with the parameter block's KV heads, index keys with
-        its index heads; None for what the cache does not hold."""
+        its index heads; None for what the cache does not hold.  A pool is one set of arrays: reserve and compact copy the pages of
+        those named last, so every layer has a pool of its own."""
         for name, x, heads in (("k_pages", k_pages, self.params.c.n_kv_heads), ("v_pages", v_pages, self.params.c.n_kv_heads),
                                ("ikey_pages", ikey_pages, self.params.c.n_index_heads),
                                ("kv_scales", kv_scales, self.params.c.n_kv_heads)):
