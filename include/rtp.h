@@ -56,6 +56,8 @@ extern "C" {
 #define RTP_MAX_Q_HEADS 128
 #define RTP_MAX_INDEX_HEADS 32
 #define RTP_MAX_HEADS_PER_INDEX_HEAD 16
+#define RTP_MAX_BEAMS 64
+#define RTP_MAX_BEAM_K 64
 
 typedef enum rtp_status {
   RTP_OK = 0,
@@ -249,6 +251,26 @@ rtp_status rtp_kv_append(rtp_ctx* ctx, const rtp_params* params, const rtp_cache
                          const void* k_new, const void* v_new, const int32_t* tok_seq,
                          const int32_t* tok_pos, int64_t T, int32_t* status, void* stream);
 
+/* ---- the same append for rows that are not rotated yet (rotary position embedding; the paper's keys and queries
+ *      are pre-RoPE for the indexer and post-RoPE for the attention, Section 3.2) --------------
+ * One launch takes what the projections of a layer made of T tokens: queries are rotated into q_out, keys rotated and put with
+ * their values into their pages (of either pool and format, as rtp_kv_append does it with rotated keys), and index keys are made of
+ * the UNROTATED keys (as rtp_index_keys makes them of k_pre, bit for bit).
+ * rope_freqs DEVICE double [rotary_dim / 2]: radians per position of each pair (any frequency scaling is the caller's); the
+ *   angle of position p is p * rope_freqs[i], formed in 64 bits.  (a, b) -> (a c - b s, b c + a s), c, s = rope_scale * cos, sin, rounded
+ *   once to bf16.  Pairs: channels i and i + rotary_dim / 2, or 2 i and 2 i + 1 if interleaved != 0; channels from rotary_dim (a
+ *   multiple of 16 up to 128) on pass through.
+ * q DEVICE bf16 [T, n_q_heads, 128] with token stride q_stride (elements, a multiple of 8: q, k and v may be slices of one
+ *   projection's output), q_out DEVICE bf16 [T, n_q_heads, 128] dense.  Both NULL: keys and values only.  q_out may be q itself if that is
+ *   dense; other overlaps are not allowed.  Queries are rotated whatever becomes of their token's append.
+ * k, v DEVICE bf16 [T, n_kv_heads, 128] with token strides k_stride, v_stride.
+ * w_k DEVICE bf16 [n_index_heads, 128, 16], or NULL: no index keys (index head j reads KV head index_head_kv[j]).
+ * tok_seq, tok_pos, skipped rows, page_refs, *status: as rtp_kv_append. */
+rtp_status rtp_rope_append(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, const double* rope_freqs,
+                           int32_t rotary_dim, int32_t interleaved, float rope_scale, const void* q, int64_t q_stride,
+                           const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out, const void* w_k,
+                           const int32_t* tok_seq, const int32_t* tok_pos, int64_t T, int32_t* status, void* stream);
+
 /* ---- pages of a 4-bit cache as bf16 pages (the paper has no counterpart) -----------
  * Page src_pages[i] of the cache's main pool, decoded, goes to page dst_pages[i] of a bf16 pool (dst_pages == NULL: to
  * page i); exact, every value of the format is a bf16 number.  A chunked prefill over a 4-bit cache appends its chunk,
@@ -284,6 +306,13 @@ rtp_status rtp_kv_expand(rtp_ctx* ctx, const rtp_params* params, const rtp_cache
  *   call, a src that is also a dst of the call, a dst that is not empty or a src with an unmapped page: skipped,
  *   RTP_ERR_INVALID.  DEVICE int32 [n]; n <= 65535.
  *
+ * rtp_cache_reorder: what sequence src_seqs[i] holds becomes what sequence dst_seqs[i] holds, for all i at once: entries, lengths
+ *   and references, while what the destinations held is given back.  Sources may be destinations and may be named several
+ *   times: after a step of a beam search, the surviving hypotheses' parents in the places of the beams (parent of rtp_beam_select).
+ *   Pages then have several holders; reserve copies the one page that several would write.  A dst named before in the same call
+ *   or an index out of range: skipped, RTP_ERR_INVALID (also recorded for entries at or beyond num_pages, which are carried over
+ *   as they are).  DEVICE int32 [n]; n <= 4096 (RTP_ERR_UNSUPPORTED).
+ *
  * rtp_cache_reserve: room for n_tokens[i] more tokens in sequence seqs[i] (positions seq_lens .. seq_lens + n_tokens - 1; seq_lens
  *   itself is left to the caller, as in rtp_kv_append).  Unmapped pages up to there are taken from the free ones, and a
  *   partly filled last page that other sequences share is replaced by a copy of its own, contents included, if at
@@ -308,6 +337,8 @@ rtp_status rtp_cache_copy_pages(rtp_ctx* ctx, const rtp_params* params, const rt
                                 const int32_t* dst_pages, int64_t n, int32_t* status, void* stream);
 rtp_status rtp_cache_fork(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
                           const int32_t* src_seqs, const int32_t* dst_seqs, int64_t n, int32_t* status, void* stream);
+rtp_status rtp_cache_reorder(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
+                             const int32_t* src_seqs, const int32_t* dst_seqs, int64_t n, int32_t* status, void* stream);
 rtp_status rtp_cache_reserve(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
                              const int32_t* seqs, const int32_t* n_tokens, int64_t n, void* workspace,
                              size_t workspace_bytes, int32_t* status, void* stream);
@@ -315,6 +346,28 @@ rtp_status rtp_cache_free(rtp_ctx* ctx, const rtp_params* params, const rtp_cach
                           const int32_t* seqs, int64_t n, int32_t* status, void* stream);
 rtp_status rtp_cache_compact(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
                              int32_t* n_used, void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/* ---- beam search: the next continuations (the paper has no counterpart) -----------
+ * Row g * n_beams + b of the logits belongs to beam b of group g (one prompt's hypotheses).  Per group, the k continuations (b, t)
+ * with the largest scores[b] + log_softmax(logits[b])[t]; equal scores: the lower (b, t) first.
+ * logits     DEVICE [n_groups * n_beams, vocab] fp32, bf16 or fp16 (logits_format), row_stride elements (>= vocab) from row to row
+ * scores     DEVICE fp32 [n_groups * n_beams] of the hypotheses so far, or NULL (all 0); -infinity: a beam that is not in use yet
+ * finished   DEVICE int32 [n_groups * n_beams] or NULL: a hypothesis with a value other than 0 has ended; its only continuation is
+ *            (b, pad_token) with its score unchanged
+ * parent     DEVICE int32 [n_groups, k]: ROW of the continued hypothesis (g * n_beams + b: what rtp_cache_reorder takes if
+ *            sequences are numbered like rows); token DEVICE int32 [n_groups, k]; scores_out DEVICE fp32 [n_groups, k]; best first.
+ *            Where a group has fewer than k continuations (ended ones): -1, -1, -infinity behind them.
+ * A logit of -infinity is ruled out: its score is -infinity, and it is taken behind all others only.  NaN and +infinity count as
+ * -infinity, RTP_ERR_INVALID is recorded (also for a score that is NaN or +infinity).  Scores are compared in 64 bits.
+ * n_beams <= 64, k <= 64, k <= n_beams * vocab.  workspace: rtp_beam_workspace_bytes(n_groups * n_beams, vocab, k). */
+#define RTP_LOGITS_F32 0
+#define RTP_LOGITS_BF16 1
+#define RTP_LOGITS_F16 2
+size_t rtp_beam_workspace_bytes(int64_t rows, int64_t vocab, int32_t k);
+rtp_status rtp_beam_select(rtp_ctx* ctx, const void* logits, int32_t logits_format, int64_t row_stride, int64_t n_groups,
+                           int32_t n_beams, int64_t vocab, const float* scores, const int32_t* finished, int32_t pad_token,
+                           int32_t k, int32_t* parent, int32_t* token, float* scores_out, void* workspace, size_t workspace_bytes,
+                           int32_t* status, void* stream);
 
 /* ---- S1: query projection (Eq. 4, the W^Q q_pre factor) --------------------
  * q_pre  DEVICE bf16 [R, n_q_heads, 128] pre-RoPE queries (all heads; only the

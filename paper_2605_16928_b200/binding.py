@@ -19,17 +19,21 @@ LIB_PATH = os.path.join(_PKG_DIR, "librtp.so")
 RTP_OK, RTP_ERR_INVALID, RTP_ERR_CAPACITY, RTP_ERR_UNSUPPORTED, RTP_ERR_CUDA, RTP_ERR_TIMEOUT = range(6)
 RTP_IKEY_BF16, RTP_IKEY_E4M3 = 0, 1
 RTP_KV_BF16, RTP_KV_FP4 = 0, 1
+RTP_LOGITS_F32, RTP_LOGITS_BF16, RTP_LOGITS_F16 = 0, 1, 2
 _STATUS_NAMES = ["RTP_OK", "RTP_ERR_INVALID", "RTP_ERR_CAPACITY", "RTP_ERR_UNSUPPORTED", "RTP_ERR_CUDA",
                  "RTP_ERR_TIMEOUT"]
 
 EXPORTS = [
     "rtp_version", "rtp_struct_bytes", "rtp_create", "rtp_destroy", "rtp_last_error", "rtp_debug_wait_test", "rtp_debug_select_path", "rtp_workspace_bytes", "rtp_check_status",
-    "rtp_kv_append", "rtp_kv_expand", "rtp_cache_workspace_bytes", "rtp_cache_copy_pages", "rtp_cache_fork", "rtp_cache_reserve",
+    "rtp_kv_append", "rtp_rope_append", "rtp_kv_expand", "rtp_cache_reorder", "rtp_beam_workspace_bytes", "rtp_beam_select", "rtp_cache_workspace_bytes", "rtp_cache_copy_pages", "rtp_cache_fork", "rtp_cache_reserve",
     "rtp_cache_free", "rtp_cache_compact", "rtp_index_keys", "rtp_index_queries", "rtp_index_score", "rtp_topp_select", "rtp_sparse_attn_decode", "rtp_sparse_attn_decode_static",
     "rtp_sparse_attn_prefill", "rtp_local_attn", "rtp_dense_attn_prefill", "rtp_dense_attn_decode",
     "rtp_block_workspace_bytes", "rtp_topp_select_blocks", "rtp_sparse_attn_prefill_blocks",
     "rtp_topp_select_blocks_rows", "rtp_sparse_attn_decode_blocks",
 ]
+
+
+_LOGITS = {"torch.float32": RTP_LOGITS_F32, "torch.bfloat16": RTP_LOGITS_BF16, "torch.float16": RTP_LOGITS_F16}
 
 
 class RtpError(RuntimeError):
@@ -101,6 +105,8 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.rtp_index_keys.argtypes = [vp, PP, PC, vp, vp, vp, vp, i64, vp]
     lib.rtp_kv_append.restype = i32
     lib.rtp_kv_append.argtypes = [vp, PP, PC, vp, vp, vp, vp, i64, vp, vp]
+    lib.rtp_rope_append.restype = i32
+    lib.rtp_rope_append.argtypes = [vp, PP, PC, vp, i32, i32, C.c_float, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp]
     lib.rtp_kv_expand.restype = i32
     lib.rtp_kv_expand.argtypes = [vp, PP, PC, vp, vp, i64, vp, vp, i32, vp, vp]
     lib.rtp_cache_workspace_bytes.restype = sz
@@ -109,12 +115,18 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.rtp_cache_copy_pages.argtypes = [vp, PP, PC, vp, vp, i64, vp, vp]
     lib.rtp_cache_fork.restype = i32
     lib.rtp_cache_fork.argtypes = [vp, PP, PC, vp, vp, vp, i64, vp, vp]
+    lib.rtp_cache_reorder.restype = i32
+    lib.rtp_cache_reorder.argtypes = [vp, PP, PC, vp, vp, vp, i64, vp, vp]
     lib.rtp_cache_reserve.restype = i32
     lib.rtp_cache_reserve.argtypes = [vp, PP, PC, vp, vp, vp, i64, vp, sz, vp, vp]
     lib.rtp_cache_free.restype = i32
     lib.rtp_cache_free.argtypes = [vp, PP, PC, vp, vp, i64, vp, vp]
     lib.rtp_cache_compact.restype = i32
     lib.rtp_cache_compact.argtypes = [vp, PP, PC, vp, vp, vp, sz, vp, vp]
+    lib.rtp_beam_workspace_bytes.restype = sz
+    lib.rtp_beam_workspace_bytes.argtypes = [i64, i64, i32]
+    lib.rtp_beam_select.restype = i32
+    lib.rtp_beam_select.argtypes = [vp, vp, i32, i64, i64, i32, i64, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp, vp]
     lib.rtp_index_queries.restype = i32
     lib.rtp_index_queries.argtypes = [vp, PP, vp, vp, i64, vp, vp]
     lib.rtp_index_score.restype = i32
@@ -183,6 +195,24 @@ def _same_length(where: str, a, b):
 def _enough_counts(where: str, cache, page_refs):
     if hasattr(page_refs, "shape") and page_refs.shape[0] < cache.num_pages:
         raise RtpError(RTP_ERR_INVALID, where, f"page_refs has {page_refs.shape[0]} counts for {cache.num_pages} pages")
+
+
+def _rows_of(where: str, name: str, x, heads: int) -> int:
+    """Token stride of rows [T, heads, 128] whose heads lie side by side (a slice of a projection's output, for instance)."""
+    if x.dim() != 3 or x.element_size() != 2 or x.shape[1] != heads or x.shape[2] != 128 or x.stride(2) != 1 or (heads > 1 and x.stride(1) != 128):
+        raise RtpError(RTP_ERR_INVALID, where, f"{name} has to be 16-bit [tokens, {heads}, 128], its heads side by side")
+    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), heads * 128) // 8 * 8
+
+
+class Rope:
+    """What the rotation of a layer is: radians per position of each pair (float64 [rotary_dim / 2] on the device), how channels
+    pair (halves, or neighbours if interleaved), and a factor on sine and cosine."""
+
+    def __init__(self, freqs, rotary_dim: int = 128, interleaved: bool = False, scale: float = 1.0):
+        if hasattr(freqs, "shape") and (freqs.element_size() != 8 or not freqs.is_floating_point() or not freqs.is_contiguous()
+                                        or freqs.numel() != rotary_dim // 2):
+            raise RtpError(RTP_ERR_INVALID, "Rope", f"freqs has to be float64 [{rotary_dim // 2}]")
+        self.freqs, self.rotary_dim, self.interleaved, self.scale = freqs, int(rotary_dim), bool(interleaved), float(scale)
 
 
 class Params:
@@ -317,6 +347,21 @@ def rtp_kv_append(ctx, params, cache, k_new, v_new, tok_seq, tok_pos, status, st
                "rtp_kv_append")
 
 
+def rtp_rope_append(ctx, params, cache, rope: Rope, q, k, v, q_out, w_k, tok_seq, tok_pos, status, stream=None):
+    """q [T, query heads, 128], k, v [T, KV heads, 128]: unrotated rows, dense or slices of one projection's output; q_out dense
+    (q and q_out None: keys and values only); w_k: index projections, or None."""
+    n_q, n_kv = params.c.n_q_heads, params.c.n_kv_heads
+    for x in (k, v, tok_pos, q, q_out):
+        _same_length("rtp_rope_append", tok_seq, x)
+    sq = _rows_of("rtp_rope_append", "q", q, n_q) if q is not None else 0
+    sk, sv = _rows_of("rtp_rope_append", "k", k, n_kv), _rows_of("rtp_rope_append", "v", v, n_kv)
+    if q_out is not None and (_rows_of("rtp_rope_append", "q_out", q_out, n_q) != n_q * 128):
+        raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", "q_out has to be dense")
+    ctx._check(ctx.lib.rtp_rope_append(ctx.h, params.ref(), C.byref(cache), _ptr(rope.freqs), rope.rotary_dim, rope.interleaved,
+                                       rope.scale, _ptr(q), sq, _ptr(k), sk, _ptr(v), sv, _ptr(q_out), _ptr(w_k), _ptr(tok_seq),
+                                       _ptr(tok_pos), tok_seq.shape[0], _ptr(status), _stream(stream)), "rtp_rope_append")
+
+
 def rtp_kv_expand(ctx, params, cache, src_pages, dst_pages, k_out, v_out, status, stream=None):
     """src_pages, dst_pages (or None: page i): int32 [n]; k_out, v_out: bf16 [pages, KV heads of the main pool, 64, 128]."""
     _same_length("rtp_kv_expand", src_pages, dst_pages)
@@ -344,6 +389,14 @@ def rtp_cache_fork(ctx, params, cache, page_refs, src_seqs, dst_seqs, status, st
                                       src_seqs.shape[0], _ptr(status), _stream(stream)), "rtp_cache_fork")
 
 
+def rtp_cache_reorder(ctx, params, cache, page_refs, src_seqs, dst_seqs, status, stream=None):
+    """Sequence dst_seqs[i] becomes what src_seqs[i] was, all at once (src may be dst, and may be named several times)."""
+    _same_length("rtp_cache_reorder", src_seqs, dst_seqs)
+    _enough_counts("rtp_cache_reorder", cache, page_refs)
+    ctx._check(ctx.lib.rtp_cache_reorder(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(src_seqs), _ptr(dst_seqs),
+                                         src_seqs.shape[0], _ptr(status), _stream(stream)), "rtp_cache_reorder")
+
+
 def rtp_cache_reserve(ctx, params, cache, page_refs, seqs, n_tokens, workspace, status, stream=None):
     _same_length("rtp_cache_reserve", seqs, n_tokens)
     _enough_counts("rtp_cache_reserve", cache, page_refs)
@@ -365,6 +418,34 @@ def rtp_cache_compact(ctx, params, cache, page_refs, n_used, workspace, status, 
     ctx._check(ctx.lib.rtp_cache_compact(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(n_used), _ptr(workspace),
                                          workspace.nbytes, _ptr(status), _stream(stream)),
                "rtp_cache_compact")
+
+
+def rtp_beam_workspace_bytes(rows: int, vocab: int, k: int) -> int:
+    return int(load_library().rtp_beam_workspace_bytes(int(rows), int(vocab), int(k)))
+
+
+def rtp_beam_select(ctx, logits, scores, finished, pad_token, parent, token, scores_out, workspace, status, stream=None):
+    """logits [rows, vocab] (fp32, bf16 or fp16; rows may be strided), rows = groups x beams; scores fp32 [rows] or None; finished int32
+    [rows] or None; parent, token int32 and scores_out fp32 [groups, k]: written."""
+    rows, vocab = logits.shape
+    groups, k = parent.shape
+    beams = rows // groups if groups else 1
+    if groups * beams != rows:
+        raise RtpError(RTP_ERR_INVALID, "rtp_beam_select", f"{rows} rows are not {groups} groups")
+    if (token.shape != parent.shape or scores_out.shape != parent.shape or (scores is not None and scores.numel() != rows)
+            or (finished is not None and finished.numel() != rows) or logits.stride(1) != 1
+            or not (parent.is_contiguous() and token.is_contiguous() and scores_out.is_contiguous())):
+        raise RtpError(RTP_ERR_INVALID, "rtp_beam_select", "arrays that go together have other shapes or strides")
+    for name, x, size in (("scores", scores, 4), ("finished", finished, 4), ("parent", parent, 4), ("token", token, 4), ("scores_out", scores_out, 4)):
+        if x is not None and x.element_size() != size:
+            raise RtpError(RTP_ERR_INVALID, "rtp_beam_select", f"{name} has to hold elements of {size} bytes")
+    fmt = _LOGITS.get(str(logits.dtype))
+    if fmt is None:
+        raise RtpError(RTP_ERR_INVALID, "rtp_beam_select", f"logits of {logits.dtype}")
+    ctx._check(ctx.lib.rtp_beam_select(ctx.h, _ptr(logits), fmt, logits.stride(0) if rows > 1 else vocab, groups, beams, vocab,
+                                       _ptr(scores), _ptr(finished), int(pad_token), k, _ptr(parent), _ptr(token),
+                                       _ptr(scores_out), _ptr(workspace), workspace.nbytes, _ptr(status), _stream(stream)),
+               "rtp_beam_select")
 
 
 def rtp_index_queries(ctx, params, q_pre, w_q, qt_out, stream=None):

@@ -448,6 +448,77 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
   if (tid == 0) head->n_pairs = s.n_pairs;
 }
 
+// ---- reorder -----------------------------------------------------------------------------------------
+// All requests at once: dst_i becomes what src_i was.  A sequence may be a source and a destination, so that every entry that
+// is read has to be read before any is written.  Columns of the table do not depend on one another: a CTA takes eight of them (a 32-byte
+// sector of every row), reads what all sources hold there into shared memory, and then writes.  Entries that do not change, those of
+// a prompt that all hypotheses share, cost a read only; counts move by one for each entry that does.
+constexpr int kReorderCols = 8;
+
+// The first request that names each destination: open addressing over twice as many places as there are requests.
+__device__ __forceinline__ unsigned place_of(int2* places, unsigned mask, int dst) {
+  unsigned h = ((unsigned)dst * 2654435761u) & mask;
+  for (;;) {   // (at most half of the places are taken: an empty one, or the one that holds dst, is met)
+    const int old = atomicCAS(&places[h].x, -1, dst);
+    if (old == -1 || old == dst) return h;
+    h = (h + 1) & mask;
+  }
+}
+
+__global__ void __launch_bounds__(kRowThreads) reorder_kernel(int32_t* __restrict__ table, int32_t* __restrict__ seq_lens,
+                                                              int32_t* __restrict__ refs, const int num_pages, const int batch,
+                                                              const int max_pages, const int32_t* __restrict__ src_seqs,
+                                                              const int32_t* __restrict__ dst_seqs, const int n,
+                                                              const unsigned mask, int32_t* status) {
+  chain_wait();
+  extern __shared__ __align__(16) unsigned char smem_reorder[];
+  int2* places = reinterpret_cast<int2*>(smem_reorder);            // [mask + 1]
+  int* dst_of = reinterpret_cast<int*>(places + mask + 1);         // [n], -1: nothing is done
+  int* held = dst_of + n;                                          // [n][8] entries of the sources, or [n] lengths
+  const int tid = threadIdx.x;
+  const bool lens = blockIdx.x == gridDim.x - 1;                   // the last CTA moves the lengths
+  const int col = blockIdx.x * kReorderCols + (tid & (kReorderCols - 1));
+  for (unsigned h = tid; h <= mask; h += kRowThreads) places[h] = make_int2(-1, 0x7fffffff);
+  __syncthreads();
+  for (int i = tid; i < n; i += kRowThreads) {
+    const int dst = dst_seqs[i];
+    const bool ok = (unsigned)dst < (unsigned)batch;
+    dst_of[i] = ok ? dst : -1;
+    if (ok) atomicMin(&places[place_of(places, mask, dst)].y, i);
+  }
+  bool bad = false;
+  for (int i = tid / kReorderCols; i < n; i += kRowThreads / kReorderCols) {
+    const int src = src_seqs[i];
+    const bool ok = (unsigned)src < (unsigned)batch;
+    if (lens) {
+      if ((tid & (kReorderCols - 1)) == 0) held[i] = ok ? seq_lens[src] : 0;
+    } else if (col < max_pages) {
+      held[i * kReorderCols + (tid & (kReorderCols - 1))] = ok ? table[(int64_t)src * max_pages + col] : -1;
+    }
+  }
+  __syncthreads();
+  for (int i = tid / kReorderCols; i < n; i += kRowThreads / kReorderCols) {
+    const int dst = dst_of[i];
+    if (dst < 0 || (unsigned)src_seqs[i] >= (unsigned)batch || places[place_of(places, mask, dst)].y != i) {
+      bad = true;
+      continue;
+    }
+    if (lens) {
+      if ((tid & (kReorderCols - 1)) == 0) seq_lens[dst] = held[i];
+    } else if (col < max_pages) {
+      int32_t* to = table + (int64_t)dst * max_pages + col;
+      const int old = *to, now = held[i * kReorderCols + (tid & (kReorderCols - 1))];
+      if (old != now) {
+        *to = now;
+        if (page_ok(old, num_pages)) atomicSub(refs + old, 1);
+        if (page_ok(now, num_pages)) atomicAdd(refs + now, 1);
+      }
+      bad = bad || now >= num_pages;
+    }
+  }
+  if (bad) set_status(status, RTP_ERR_INVALID);
+}
+
 // ---- compact -----------------------------------------------------------------------------------------
 // With n_used pages in use, the k-th used page at or above n_used goes to the k-th free page below it.  That is CTA 0's work;
 // the others look meanwhile for table entries that name a page without references (one below n_used would be filled with somebody
@@ -609,6 +680,23 @@ cudaError_t launch_reserve(const PageArrays& arrays, int32_t* table, const int32
   if (e != cudaSuccess || pa.total_pieces == 0) return e;
   (void)launch_chained(copy_pages_kernel, dim3(copy_grid(pa, n)), dim3(SmallCopy::kThreads), 0, st, pa, num_pages, src, dst, 0,
                        (const PlanHead*)head, status);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_reorder(int32_t* table, int32_t* seq_lens, int32_t* refs, int num_pages, int batch, int max_pages,
+                           const int32_t* src, const int32_t* dst, int n, int32_t* status, cudaStream_t st) {
+  if (n == 0) return cudaSuccess;
+  unsigned places = 64;
+  while (places < 2u * (unsigned)n) places *= 2;
+  constexpr size_t kMost = (size_t)2 * kReserveMax * sizeof(int2) + (size_t)kReserveMax * (1 + kReorderCols) * sizeof(int);
+  static_assert(kMost <= 227 * 1024, "the lists of a call lie in shared memory");
+  static PerDeviceOnce once;
+  cudaError_t e = set_dyn_smem_once(reorder_kernel, (int)kMost, once);
+  if (e != cudaSuccess) return e;
+  const size_t smem = places * sizeof(int2) + (size_t)n * (1 + kReorderCols) * sizeof(int);
+  const unsigned grid = (unsigned)((max_pages + kReorderCols - 1) / kReorderCols) + 1;
+  (void)launch_chained(reorder_kernel, dim3(grid), dim3(kRowThreads), smem, st, table, seq_lens, refs, num_pages, batch, max_pages,
+                       src, dst, n, places - 1, status);
   return cudaGetLastError();
 }
 

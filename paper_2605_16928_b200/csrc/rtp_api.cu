@@ -342,6 +342,35 @@ rtp_status rtp_kv_append(rtp_ctx* ctx, const rtp_params* params, const rtp_cache
   return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_kv_append");
 }
 
+rtp_status rtp_rope_append(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, const double* rope_freqs,
+                           int32_t rotary_dim, int32_t interleaved, float rope_scale, const void* q, int64_t q_stride,
+                           const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out, const void* w_k,
+                           const int32_t* tok_seq, const int32_t* tok_pos, int64_t T, int32_t* status, void* stream) {
+  RTP_COMMON_PROLOGUE(true, w_k != nullptr)
+  if (T < 0) return fail(ctx, RTP_ERR_INVALID, "T is negative");
+  if (T == 0) return RTP_OK;
+  if (!k || !v || !tok_seq || !tok_pos || !rope_freqs) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
+  if ((q == nullptr) != (q_out == nullptr)) return fail(ctx, RTP_ERR_INVALID, "q and q_out must both be given or both be NULL");
+  if (rotary_dim < 16 || rotary_dim > kHeadDim || rotary_dim % 16) return fail(ctx, RTP_ERR_INVALID, "rotary_dim must be a multiple of 16 up to 128");
+  if (!(rope_scale > -1e30f) || !(rope_scale < 1e30f)) return fail(ctx, RTP_ERR_INVALID, "rope_scale must be finite");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(w_k) || !aligned16(rope_freqs))
+    return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
+  if ((q && (q_stride % 8 || q_stride < (int64_t)d.n_q * kHeadDim)) || k_stride % 8 || v_stride % 8 ||
+      k_stride < (int64_t)d.n_kv * kHeadDim || v_stride < (int64_t)d.n_kv * kHeadDim)
+    return fail(ctx, RTP_ERR_INVALID, "token strides must be multiples of 8 that hold a token's heads");
+  if (q == q_out && q && q_stride != (int64_t)d.n_q * kHeadDim) return fail(ctx, RTP_ERR_INVALID, "queries in place must be dense");
+  if (w_k && d.n_ih == 0) return fail(ctx, RTP_ERR_INVALID, "no index heads");
+  if (T >= ((int64_t)1 << 31) / (d.n_q + 2 * d.n_kv + 1)) return fail(ctx, RTP_ERR_UNSUPPORTED, "2^31 or more (token, head) rows in one call");
+  CacheView lv = {};
+  if (cache->k_local_pages) lv = local_view(cv, cache, params);
+  cudaError_t e = launch_rope_append(cv, lv, d, hm, rope_freqs, rotary_dim, interleaved != 0, rope_scale,
+                                     reinterpret_cast<const __nv_bfloat16*>(q), q_stride, reinterpret_cast<const __nv_bfloat16*>(k),
+                                     k_stride, reinterpret_cast<const __nv_bfloat16*>(v), v_stride,
+                                     reinterpret_cast<__nv_bfloat16*>(q_out), reinterpret_cast<const __nv_bfloat16*>(w_k), tok_seq,
+                                     tok_pos, T, status, st);
+  return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_rope_append");
+}
+
 rtp_status rtp_kv_expand(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, const int32_t* src_pages,
                          const int32_t* dst_pages, int64_t n, void* k_out, void* v_out, int32_t n_out_pages,
                          int32_t* status, void* stream) {
@@ -401,6 +430,15 @@ rtp_status rtp_cache_fork(rtp_ctx* ctx, const rtp_params* params, const rtp_cach
   return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_cache_fork");
 }
 
+rtp_status rtp_cache_reorder(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
+                             const int32_t* src_seqs, const int32_t* dst_seqs, int64_t n, int32_t* status, void* stream) {
+  RTP_PAGES_PROLOGUE(kReserveMax)
+  if (n == 0) return RTP_OK;
+  if (!src_seqs || !dst_seqs) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
+  cudaError_t e = launch_reorder(table, lens, page_refs, cv.num_pages, cv.batch, cv.max_pages, src_seqs, dst_seqs, (int)n, status, st);
+  return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_cache_reorder");
+}
+
 rtp_status rtp_cache_reserve(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, int32_t* page_refs,
                              const int32_t* seqs, const int32_t* n_tokens, int64_t n, void* workspace,
                              size_t workspace_bytes, int32_t* status, void* stream) {
@@ -433,6 +471,39 @@ rtp_status rtp_cache_compact(rtp_ctx* ctx, const rtp_params* params, const rtp_c
   cudaError_t e = launch_compact(pa, table, (int64_t)cv.batch * cv.max_pages, page_refs, cv.num_pages, n_used, workspace, status, st);
   if (e == cudaErrorNotSupported) return fail(ctx, RTP_ERR_UNSUPPORTED, "too many pages in one call");
   return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_cache_compact");
+}
+
+static const char* check_beam(int64_t n_groups, int32_t n_beams, int64_t vocab, int32_t k) {
+  if (n_groups < 0 || n_beams < 1 || n_beams > RTP_MAX_BEAMS) return "bad group or beam count";
+  if (k < 1 || k > RTP_MAX_BEAM_K) return "k must be between 1 and 64";
+  if (vocab < 1 || vocab >= ((int64_t)1 << 31) / n_beams || vocab >= (int64_t)1 << 30) return "bad vocabulary size";
+  if (k > n_beams * vocab) return "k is more than there are continuations";
+  return nullptr;
+}
+
+size_t rtp_beam_workspace_bytes(int64_t rows, int64_t vocab, int32_t k) {
+  if (rows < 1 || check_beam(1, 1, vocab, 1) || k < 1 || k > RTP_MAX_BEAM_K) return 0;
+  return beam_workspace_bytes(rows, vocab, k, current_sm_count(kFallbackSm));
+}
+
+rtp_status rtp_beam_select(rtp_ctx* ctx, const void* logits, int32_t logits_format, int64_t row_stride, int64_t n_groups,
+                           int32_t n_beams, int64_t vocab, const float* scores, const int32_t* finished, int32_t pad_token,
+                           int32_t k, int32_t* parent, int32_t* token, float* scores_out, void* workspace, size_t workspace_bytes,
+                           int32_t* status, void* stream) {
+  if (!ctx) return RTP_ERR_INVALID;
+  if (logits_format != RTP_LOGITS_F32 && logits_format != RTP_LOGITS_BF16 && logits_format != RTP_LOGITS_F16)
+    return fail(ctx, RTP_ERR_INVALID, "unknown logits_format");
+  if (const char* m = check_beam(n_groups, n_beams, vocab, k)) return fail(ctx, RTP_ERR_INVALID, m);
+  if (row_stride < vocab) return fail(ctx, RTP_ERR_INVALID, "row_stride is less than the vocabulary");
+  if (n_groups == 0) return RTP_OK;
+  if (!logits || !parent || !token || !scores_out || !workspace) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
+  if (!aligned16(logits) || !aligned16(workspace)) return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
+  if (n_groups >= ((int64_t)1 << 31) / (n_beams * (int64_t)k)) return fail(ctx, RTP_ERR_UNSUPPORTED, "too many groups in one call");
+  if (workspace_bytes < beam_workspace_bytes(n_groups * n_beams, vocab, k, ctx->sm_count)) return fail(ctx, RTP_ERR_CAPACITY, "workspace too small");
+  cudaError_t e = launch_beam_select(logits, logits_format, row_stride, n_groups, n_beams, vocab, scores, finished, pad_token, k, parent,
+                                     token, scores_out, workspace, status, ctx->sm_count, reinterpret_cast<cudaStream_t>(stream));
+  if (e == cudaErrorNotSupported) return fail(ctx, RTP_ERR_UNSUPPORTED, "vocabulary times beams too large");
+  return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_beam_select");
 }
 
 rtp_status rtp_index_queries(rtp_ctx* ctx, const rtp_params* params, const void* q_pre, const void* w_q, int64_t R,

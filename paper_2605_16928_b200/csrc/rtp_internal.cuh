@@ -184,6 +184,18 @@ cudaError_t launch_kv4_append(const CacheView& cv, int n_src_heads, const __nv_b
 cudaError_t launch_kv4_expand(const CacheView& cv, const int32_t* src_pages, const int32_t* dst_pages, int64_t n, void* k_out,
                               void* v_out, int32_t n_out_pages, int32_t* status, cudaStream_t st);
 
+// lv: the local heads' pool (n_kv = 0 if there is none).
+cudaError_t launch_rope_append(const CacheView& cv, const CacheView& lv, const Dims& d, const HeadMaps& hm, const double* freqs,
+                               int rotary_dim, bool interleaved, float scale, const __nv_bfloat16* q, int64_t q_stride,
+                               const __nv_bfloat16* k, int64_t k_stride, const __nv_bfloat16* v, int64_t v_stride,
+                               __nv_bfloat16* q_out, const __nv_bfloat16* w_k, const int32_t* tok_seq, const int32_t* tok_pos,
+                               int64_t T, int32_t* status, cudaStream_t st);
+
+size_t beam_workspace_bytes(int64_t rows, int64_t vocab, int k, int sm_count);
+cudaError_t launch_beam_select(const void* logits, int format, int64_t row_stride, int64_t n_groups, int n_beams, int64_t vocab,
+                               const float* scores, const int32_t* finished, int pad_token, int k, int32_t* parent, int32_t* token,
+                               float* scores_out, void* ws, int32_t* status, int sm_count, cudaStream_t st);
+
 // Pages of the main pool: the arrays that a page consists of (keys, values, 4-bit scales, index keys; absent ones have no bytes).
 constexpr int kPageArrays = 4;
 constexpr int kReserveMax = 4096;   // sequences of one reserve call
@@ -202,6 +214,8 @@ cudaError_t launch_free(int32_t* table, int32_t* seq_lens, int32_t* refs, int nu
 cudaError_t launch_reserve(const PageArrays& pa, int32_t* table, const int32_t* seq_lens, int32_t* refs, int num_pages, int batch,
                            int max_pages, const int32_t* seqs, const int32_t* n_tokens, int n, void* ws, int32_t* status,
                            cudaStream_t st);
+cudaError_t launch_reorder(int32_t* table, int32_t* seq_lens, int32_t* refs, int num_pages, int batch, int max_pages,
+                           const int32_t* src, const int32_t* dst, int n, int32_t* status, cudaStream_t st);
 cudaError_t launch_compact(const PageArrays& pa, int32_t* table, int64_t n_entries, int32_t* refs, int num_pages,
                            int32_t* n_used, void* ws, int32_t* status, cudaStream_t st);
 

@@ -256,6 +256,10 @@ class PagePool:
     def fork(self, src_seqs, dst_seqs):
         rb.rtp_cache_fork(self.ctx, self.params, self.cache, self.page_refs, src_seqs, dst_seqs, self.status)
 
+    def reorder(self, src_seqs, dst_seqs):
+        """Sequence dst_seqs[i] becomes what src_seqs[i] was, all at once."""
+        rb.rtp_cache_reorder(self.ctx, self.params, self.cache, self.page_refs, src_seqs, dst_seqs, self.status)
+
     def free(self, seqs):
         rb.rtp_cache_free(self.ctx, self.params, self.cache, self.page_refs, seqs, self.status)
 
