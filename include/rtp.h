@@ -586,6 +586,34 @@ rtp_status rtp_dense_attn_decode(rtp_ctx* ctx, const rtp_params* params, const r
                                  float* lse, void* workspace, size_t workspace_bytes,
                                  int32_t* status, void* stream);
 
+/* ---- attention of chunks of several sequences: the ragged batch of a serving step (the paper has no counterpart; the sets are
+ *      those of S7 and S9) ------------------------------------------------------------
+ * Chunk c (any number of rows, 0 included) has rows row_offsets[c] .. row_offsets[c + 1] - 1 of q and out, at positions
+ * chunk_start[c], chunk_start[c] + 1, .. of sequence chunk_seq[c]: single decode rows, a few tokens to verify, pieces of prompts, in any
+ * mixture.  Their keys and values have been appended and counted in seq_lens; a row at position m sees keys n <= m.
+ * q DEVICE bf16 [R, n_q_heads, 128] post-RoPE; chunk_seq, chunk_start DEVICE int32 [n_chunks], row_offsets DEVICE int32
+ *   [n_chunks + 1], not decreasing, at most R; rows of no chunk (behind the last one, for instance) are left as they are.
+ * pattern: RTP_CHUNK_DENSE   every listed KV head over all keys n <= m;
+ *          RTP_CHUNK_LOCAL   the listed ones among local_kv_heads over sinks and window, as rtp_local_attn (retrieval query heads
+ *                            of a mixed group are not written), the others not at all;
+ *          RTP_CHUNK_BY_HEAD local heads over sinks and window, retrieval query heads of a mixed group and all other KV heads over
+ *                            all keys: a layer in the paper's prefill mode (Section 3.2) in one call.
+ * kv_heads HOST int32 [n_heads], each once, or NULL: all.  Any group size n_q_heads / n_kv_heads.
+ * out, lse as rtp_dense_attn_prefill (a row that sees no key: 0, -infinity).  A position beyond its sequence, a sequence or an offset out
+ * of range: RTP_ERR_INVALID in the status word; such rows see the keys that there are, chunks with wrong offsets are left out.
+ * K and V of all positions up to a chunk's last row are taken as finite: one that is not may reach every row of its tile of 128 keys.
+ * bf16 caches (RTP_ERR_UNSUPPORTED on a 4-bit one).  On a truncated cache a chunk of local heads needs ring_pages * 64 >= window +
+ * its rows + 64, unless its sequence has not outgrown the pool: else it is left out and RTP_ERR_CAPACITY recorded.  n_chunks <= 8192.
+ * workspace: rtp_chunk_workspace_bytes(params, n_chunks, R) (RTP_ERR_CAPACITY). */
+#define RTP_CHUNK_DENSE 0
+#define RTP_CHUNK_LOCAL 1
+#define RTP_CHUNK_BY_HEAD 2
+size_t rtp_chunk_workspace_bytes(const rtp_params* params, int64_t n_chunks, int64_t rows);
+rtp_status rtp_attn_chunks(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, const void* q, const int32_t* chunk_seq,
+                           const int32_t* chunk_start, const int32_t* row_offsets, int64_t n_chunks, int64_t R, int32_t pattern,
+                           const int32_t* kv_heads, int32_t n_heads, void* out, float* lse, void* workspace,
+                           size_t workspace_bytes, int32_t* status, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,13 +19,14 @@ LIB_PATH = os.path.join(_PKG_DIR, "librtp.so")
 RTP_OK, RTP_ERR_INVALID, RTP_ERR_CAPACITY, RTP_ERR_UNSUPPORTED, RTP_ERR_CUDA, RTP_ERR_TIMEOUT = range(6)
 RTP_IKEY_BF16, RTP_IKEY_E4M3 = 0, 1
 RTP_KV_BF16, RTP_KV_FP4 = 0, 1
+RTP_CHUNK_DENSE, RTP_CHUNK_LOCAL, RTP_CHUNK_BY_HEAD = 0, 1, 2
 RTP_LOGITS_F32, RTP_LOGITS_BF16, RTP_LOGITS_F16 = 0, 1, 2
 _STATUS_NAMES = ["RTP_OK", "RTP_ERR_INVALID", "RTP_ERR_CAPACITY", "RTP_ERR_UNSUPPORTED", "RTP_ERR_CUDA",
                  "RTP_ERR_TIMEOUT"]
 
 EXPORTS = [
     "rtp_version", "rtp_struct_bytes", "rtp_create", "rtp_destroy", "rtp_last_error", "rtp_debug_wait_test", "rtp_debug_select_path", "rtp_workspace_bytes", "rtp_check_status",
-    "rtp_kv_append", "rtp_rope_append", "rtp_kv_expand", "rtp_cache_reorder", "rtp_beam_workspace_bytes", "rtp_beam_select", "rtp_cache_workspace_bytes", "rtp_cache_copy_pages", "rtp_cache_fork", "rtp_cache_reserve",
+    "rtp_kv_append", "rtp_rope_append", "rtp_kv_expand", "rtp_cache_reorder", "rtp_beam_workspace_bytes", "rtp_beam_select", "rtp_chunk_workspace_bytes", "rtp_attn_chunks", "rtp_cache_workspace_bytes", "rtp_cache_copy_pages", "rtp_cache_fork", "rtp_cache_reserve",
     "rtp_cache_free", "rtp_cache_compact", "rtp_index_keys", "rtp_index_queries", "rtp_index_score", "rtp_topp_select", "rtp_sparse_attn_decode", "rtp_sparse_attn_decode_static",
     "rtp_sparse_attn_prefill", "rtp_local_attn", "rtp_dense_attn_prefill", "rtp_dense_attn_decode",
     "rtp_block_workspace_bytes", "rtp_topp_select_blocks", "rtp_sparse_attn_prefill_blocks",
@@ -156,6 +157,10 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.rtp_dense_attn_prefill.argtypes = [vp, PP, PC, vp, i32, i32, i64, vp, i32, vp, vp, vp, vp]
     lib.rtp_dense_attn_decode.restype = i32
     lib.rtp_dense_attn_decode.argtypes = [vp, PP, PC, vp, vp, vp, i64, vp, i32, vp, vp, vp, sz, vp, vp]
+    lib.rtp_chunk_workspace_bytes.restype = sz
+    lib.rtp_chunk_workspace_bytes.argtypes = [PP, i64, i64]
+    lib.rtp_attn_chunks.restype = i32
+    lib.rtp_attn_chunks.argtypes = [vp, PP, PC, vp, vp, vp, vp, i64, i64, i32, vp, i32, vp, vp, vp, sz, vp, vp]
     if path is None:
         _LIB = lib
     return lib
@@ -574,3 +579,23 @@ def rtp_dense_attn_decode(ctx, params, cache, q, row_seq, row_pos, kv_heads, out
                                              len(kv_heads) if kv_heads is not None else 0, _ptr(out), _ptr(lse),
                                              _ptr(workspace), workspace.nbytes,
                                              _ptr(status), _stream(stream)), "rtp_dense_attn_decode")
+
+
+def rtp_chunk_workspace_bytes(params: Params, n_chunks: int, rows: int) -> int:
+    return int(load_library().rtp_chunk_workspace_bytes(params.ref(), int(n_chunks), int(rows)))
+
+
+def rtp_attn_chunks(ctx, params, cache, q, chunk_seq, chunk_start, row_offsets, pattern, kv_heads, out, lse, workspace, status,
+                    stream=None):
+    """q, out: [rows, query heads, 128]; chunk c: rows row_offsets[c] .. row_offsets[c + 1] - 1 at positions chunk_start[c] .. of
+    sequence chunk_seq[c]; kv_heads: None (all) or the KV heads that are computed."""
+    _same_length("rtp_attn_chunks", chunk_seq, chunk_start)
+    for x in (out, lse):
+        _same_length("rtp_attn_chunks", q, x)
+    if row_offsets.shape[0] != chunk_seq.shape[0] + 1:
+        raise RtpError(RTP_ERR_INVALID, "rtp_attn_chunks", f"{chunk_seq.shape[0]} chunks with {row_offsets.shape[0]} offsets")
+    arr = _i32_array(kv_heads) if kv_heads is not None else None
+    ctx._check(ctx.lib.rtp_attn_chunks(ctx.h, params.ref(), C.byref(cache), _ptr(q), _ptr(chunk_seq), _ptr(chunk_start), _ptr(row_offsets),
+                                       chunk_seq.shape[0], q.shape[0], int(pattern), C.cast(arr, C.c_void_p) if arr is not None else None,
+                                       len(kv_heads) if kv_heads is not None else 0, _ptr(out), _ptr(lse), _ptr(workspace),
+                                       workspace.nbytes, _ptr(status), _stream(stream)), "rtp_attn_chunks")

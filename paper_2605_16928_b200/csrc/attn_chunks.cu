@@ -1,0 +1,776 @@
+// Attention of chunks of several sequences over the paged cache (rtp_attn_chunks): a chunk is any number of consecutive rows of a
+// sequence, one (a decode step), a few (tokens to verify) or thousands (a piece of a prompt), all in one call.
+//
+// Work.  A unit is a KV head with its query heads, over up to 2 x BMP consecutive positions of a chunk (BMP = 128 / G positions x G
+// heads fill the 128 rows of an MMA).  Its cost is the number of key tiles (128 keys) that its rows see, from one to thousands,
+// known on the device only.  plan_kernel counts it out: units are dealt round robin as long as there are two rounds and more of them
+// (CTAs that run at the same time then walk the same keys, which come from L2), and the last one or two rounds, or all of a small call,
+// are laid end to end and cut into equal pieces, one per CTA, at any key tile.  A piece that is not a whole unit leaves its rows'
+// maxima, sums and unnormalised outputs in the workspace; merge_kernel joins them by log-sum-exp.
+//
+// Tiles.  One CTA per SM (384 threads), persistent over its list of pieces:
+//   warp 9    Q (TMA, rows in the order [position][head]) and K tiles, warp 10 V tiles, into a ring of five 32 KB slots; table entries
+//             are looked up 16 tiles at a time.  Keys that no row may see are zeroed in V (their pages' tails may hold anything).
+//   warp 8    issues S = Q K^T (128 x 128 x 128) and O += P V on the 5th-generation tensor cores, S of a job before P V of the job
+//             before it, across pieces: the next piece's tiles are on their way while this one ends.
+//   warps 0-7 two groups of 128 threads, thread = row = TMEM lane: S to registers, mask, online softmax in 32 bits, P (bf16) back to
+//             TMEM over the first half of S, from where the MMA takes it: shared memory holds no P and serves the ring instead.
+// Jobs alternate between the groups.  A unit of more than BMP positions has two Q tiles, one per group, over the same K / V tiles
+// (half the traffic); a smaller one has one, and the groups take every other key tile and are joined at the end, straight from TMEM.
+// S and P of a group share 128 columns: S of its next job is issued behind the P V that reads P, and the tensor core runs them in order.
+#include "tc_common.cuh"
+
+namespace rtp {
+
+// 3-D tensor map of query rows [rows][n_heads][128] bf16 with a box of box_rows x box_heads x 64 (tensor_map.cu).
+cudaError_t make_heads_map(CUtensorMap* map, const void* base, int64_t rows, int n_heads, int box_heads, int box_rows, int swizzle);
+
+namespace {
+
+constexpr int kThreads = 384;
+constexpr int kTile = 128;                     // keys per tile
+constexpr int kBlk = 128 * 128;                // bytes of a [128 rows][64 elements] bf16 block
+constexpr int kSlot = 2 * kBlk;                // a Q, K or V tile
+constexpr int kRing = 5;
+constexpr int kRingOff = 2 * kSlot;            // behind two Q tiles
+constexpr int kBarOff = kRingOff + kRing * kSlot;
+constexpr int kXchOff = kBarOff + 256;         // float [2 groups][2][128 rows]
+constexpr int kSmem = kXchOff + 2048;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kMaxUnits = 64;                  // (KV head, pattern) pairs of a call
+constexpr int kPlanThreads = 1024;
+
+enum Bar { kQFull = 0, kQEmpty = 2, kFull = 4, kEmpty = kFull + kRing, kSFull = kEmpty + kRing, kPFull = kSFull + 2, kOFull = kPFull + 2,
+           kAux = kOFull + 2, kNumBars };
+static_assert(kNumBars * 8 + 16 <= 256, "barriers, TMEM address and abort flag");
+
+// A KV head of the call: sinks and window or everything before the row; which of its query heads are written.
+enum UnitFlags { kLocal = 1, kSkipRet = 2, kSkipOther = 4, kLocalPool = 8 };
+struct HeadUnits {
+  uint8_t head[kMaxUnits], flags[kMaxUnits];
+  int32_t n;
+  uint32_t ret_q[RTP_MAX_Q_HEADS / 32];        // retrieval query heads
+  __device__ bool writes(int unit, int qh) const {
+    const bool ret = (ret_q[qh >> 5] >> (qh & 31)) & 1u;
+    return !((flags[unit] & kSkipRet) && ret) && !((flags[unit] & kSkipOther) && !ret);
+  }
+};
+
+// A piece of a unit: key tiles tile_lo .. tile_hi - 1 of its n_tiles.
+struct __align__(16) Piece {
+  int32_t row0, pos0, n_pos, seq;              // rows row0 .. of q at positions pos0 ..
+  int32_t unit, kt_first, n_sink_tiles, n_keys;
+  int32_t tile_lo, tile_hi, slot, id;          // slot: of its partial result, or -1; id: number of the unit
+};
+struct __align__(16) MergeUnit {
+  int32_t row0, n_pos, unit, id;
+  int32_t first_cta, last_cta, pad0, pad1;
+};
+struct Plan {                                  // where things lie in the workspace
+  int32_t* n_merge;
+  int32_t* piece_begin;                        // [n_ctas + 1]
+  int32_t* part_id;                            // [2 n_ctas]: unit of the partial result in a slot, or -1
+  MergeUnit* merge;                            // [n_ctas]
+  Piece* pieces;                               // [max_pieces]
+  float* ml;                                   // [2 n_ctas][slot_rows][2]
+  float* o;                                    // [2 n_ctas][slot_rows][128]
+  int32_t n_ctas, max_units, slot_rows;
+};
+
+struct ChunkArgs {
+  const int32_t *seq, *start, *offsets;
+  int32_t n_chunks, G, bmp;
+  int64_t R;
+  int64_t ring_tokens, pool_tokens;            // of the local pool, 0 if no unit reads one
+};
+
+// ---- plan --------------------------------------------------------------------------------------------
+// Costs are in jobs (a key tile of a Q tile); a piece has a start and an end beside them.
+constexpr int kPieceCost = 3;
+constexpr int kMinJobs = 6;                    // a piece of its own (and a merge) has to be worth it
+constexpr int kSnap = 3;                       // key tiles that are not cut off
+
+struct PlanShared {
+  int64_t warp_sum[33];
+  int64_t total;
+  int32_t n_units;
+  int64_t load[1024];                          // jobs dealt to each CTA, then the cuts
+  int64_t before[1024 + 1];                    // jobs in front of each unit of the cut part
+  int32_t begin[1024 + 1];
+};
+
+__device__ __forceinline__ int64_t scan64(int64_t x, int64_t* warp_sum, int lane, int warp) {   // exclusive; warp_sum[32]: the total
+  int64_t s = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += y;
+  }
+  __syncthreads();
+  if (lane == 31) warp_sum[warp] = s;
+  __syncthreads();
+  if (warp == 0) {
+    const int64_t w = warp_sum[lane];
+    int64_t t = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, t, o);
+      if (lane >= o) t += y;
+    }
+    warp_sum[lane] = t - w;
+    if (lane == 31) warp_sum[32] = t;
+  }
+  __syncthreads();
+  return warp_sum[warp] + s - x;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ CacheView cv,
+                                                            const __grid_constant__ HeadUnits hu, const __grid_constant__ Plan plan,
+                                                            const int n_sink, const int window, int32_t* status) {
+  chain_wait();
+  extern __shared__ __align__(16) unsigned char smem_plan[];
+  PlanShared& s = *reinterpret_cast<PlanShared*>(smem_plan);
+  int4* chunk = reinterpret_cast<int4*>(smem_plan + ((sizeof(PlanShared) + 15) & ~15));   // [n_chunks]: units before, rows, start, keys
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int N = plan.n_ctas, H = hu.n, span = 2 * a.bmp;
+  // chunks, with what is wrong in them
+  int64_t mine = 0;
+  const int per = (a.n_chunks + kPlanThreads - 1) / kPlanThreads, c0 = min(tid * per, a.n_chunks), c1 = min(c0 + per, a.n_chunks);
+  bool bad = false;
+  for (int c = c0; c < c1; ++c) {
+    const int64_t lo = a.offsets[c], hi = a.offsets[c + 1];
+    int rows = (int)(hi - lo);
+    if (lo < 0 || hi < lo || hi > a.R) {       // no rows of the call
+      rows = 0;
+      bad = true;
+    }
+    const int seq = a.seq[c], start = a.start[c];
+    int keys = (unsigned)seq < (unsigned)cv.batch ? max(0, min(cv.seq_lens[seq], cv.cap_tokens)) : 0;
+    if (start < 0) keys = 0;
+    if (rows > 0 && (int64_t)start + rows > keys) bad = true;
+    // a ring has to hold the window of the chunk's first row when the last one has been appended
+    if (rows > 0 && a.ring_tokens && a.ring_tokens < (int64_t)window + rows + kPage && (int64_t)start + rows > a.pool_tokens) {
+      rows = 0;
+      set_status(status, RTP_ERR_CAPACITY);
+    }
+    chunk[c] = make_int4(0, rows, start, keys);
+    mine += (int64_t)((rows + span - 1) / span) * H;
+  }
+  int64_t at = scan64(mine, s.warp_sum, lane, warp);
+  const int64_t total_units = s.warp_sum[32];
+  for (int c = c0; c < c1; ++c) {
+    chunk[c].x = (int)min(at, (int64_t)0x7fffffff);
+    at += (int64_t)((chunk[c].y + span - 1) / span) * H;
+  }
+  for (int i = tid; i < 2 * N; i += kPlanThreads) plan.part_id[i] = -1;
+  for (int i = tid; i < N; i += kPlanThreads) s.load[i] = 0;
+  if (tid == 0) *plan.n_merge = 0;
+  if (bad) set_status(status, RTP_ERR_INVALID);
+  __syncthreads();
+  if (total_units > plan.max_units) {          // offsets that run back and forth: nothing is done
+    if (tid == 0) set_status(status, RTP_ERR_INVALID);
+    for (int i = tid; i <= N; i += kPlanThreads) plan.piece_begin[i] = 0;
+    return;
+  }
+  const int U = (int)total_units;
+  // unit u: chunk by chunk, head by head, the last positions first
+  auto describe = [&](int u, Piece& p) -> int {   // returns its key tiles
+    int lo = 0, hi = a.n_chunks;               // the last chunk with units before <= u that has any: the last one with x <= u
+    while (lo + 1 < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (chunk[mid].x <= u) lo = mid; else hi = mid;
+    }
+    const int4 c = chunk[lo];
+    const int nt = (c.y + span - 1) / span, r = u - c.x, h = r / nt, t = nt - 1 - (r - h * nt);
+    p.pos0 = c.z + t * span;
+    p.n_pos = min(span, c.y - t * span);
+    p.row0 = a.offsets[lo] + t * span;
+    p.seq = a.seq[lo];
+    p.unit = h;
+    p.n_keys = min(c.w, p.pos0 + p.n_pos);
+    p.id = u;
+    const int n_all = p.n_keys > 0 ? (p.n_keys - 1) / kTile + 1 : 0;
+    p.kt_first = p.n_sink_tiles = 0;
+    if (hu.flags[h] & kLocal) {
+      p.kt_first = min(max(0, p.pos0 - window + 1) / kTile, n_all);
+      p.n_sink_tiles = min(min((n_sink + kTile - 1) / kTile, p.kt_first), n_all);
+    }
+    return p.n_sink_tiles + n_all - p.kt_first;
+  };
+  auto jobs_per_tile = [&](const Piece& p) { return p.n_pos > a.bmp ? 2 : 1; };
+  auto cost = [&](int u) -> int64_t {
+    Piece p;
+    const int n = describe(u, p);
+    return kPieceCost + (int64_t)n * jobs_per_tile(p);
+  };
+  const int rounds = U >= 2 * N ? U / N - 1 : 0, D = rounds * N, M = U - D;   // M < 2 N
+  int64_t dealt = 0;
+  for (int u = tid; u < D; u += kPlanThreads) {
+    const int64_t w = cost(u);
+    dealt += w;
+    atomicAdd(reinterpret_cast<unsigned long long*>(&s.load[u % N]), (unsigned long long)w);
+  }
+  const int64_t w_mine = tid < M ? cost(D + tid) : 0;
+  scan64(dealt, s.warp_sum, lane, warp);
+  const int64_t W_dealt = s.warp_sum[32];
+  const int64_t before = scan64(w_mine, s.warp_sum, lane, warp);
+  const int64_t W_cut = s.warp_sum[32];
+  if (tid < M) s.before[tid] = before;
+  if (tid == 0) s.before[M] = W_cut;
+  // What each CTA takes of the cut part: with nothing dealt, equal shares for as many as are worth it; else up to the mean.
+  int64_t room = 0;
+  const int takers = rounds ? N : (int)max((int64_t)1, min((int64_t)N, W_cut / (kMinJobs + kPieceCost)));
+  if (tid < N) room = rounds ? max((int64_t)0, (W_dealt + W_cut) / N + 1 - s.load[tid]) : (tid < takers ? 1 : 0);
+  const int64_t room_before = scan64(room, s.warp_sum, lane, warp), rooms = s.warp_sum[32];
+  __syncthreads();
+  if (tid < N) s.load[tid] = rooms > 0 ? (int64_t)((double)W_cut * (double)room_before / (double)rooms) : (tid ? W_cut : 0);
+  __syncthreads();
+  // the pieces of CTA tid: units that meet [from, to)
+  const int64_t from = tid < N ? s.load[tid] : 0, to = tid + 1 < N ? s.load[tid + 1] : W_cut;
+  auto cut_at = [&](int64_t x, int64_t u0, int n, int per_tile) -> int {   // the key tile of a unit (u0 < x < its end) at which a cut at x falls
+    const int t = x <= u0 + kPieceCost ? 0 : (int)((x - u0 - kPieceCost + per_tile - 1) / per_tile);
+    return t < kSnap ? 0 : n - t < kSnap ? n : t;
+  };
+  auto walk = [&](auto&& emit) {
+    if (tid >= N || from >= to) return;
+    int lo = 0, hi = M;                        // the last unit with before <= from
+    while (lo + 1 < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (s.before[mid] <= from) lo = mid; else hi = mid;
+    }
+    for (int j = lo; j < M && s.before[j] < to; ++j) {
+      Piece p;
+      const int64_t u0 = s.before[j];
+      const int n = describe(D + j, p);
+      p.tile_lo = from <= u0 ? 0 : cut_at(from, u0, n, jobs_per_tile(p));
+      p.tile_hi = to >= s.before[j + 1] ? n : cut_at(to, u0, n, jobs_per_tile(p));
+      if (p.tile_lo < p.tile_hi || (n == 0 && u0 >= from)) emit(p, n, j);
+    }
+  };
+  int n_cut = 0;
+  walk([&](const Piece&, int, int) { ++n_cut; });
+  const int cut_before = (int)scan64(n_cut, s.warp_sum, lane, warp);
+  if (tid < N) s.begin[tid] = tid * rounds + cut_before;
+  if (tid == 0) s.begin[N] = N * rounds + (int)s.warp_sum[32];
+  __syncthreads();
+  for (int i = tid; i <= N; i += kPlanThreads) plan.piece_begin[i] = s.begin[i];
+  for (int u = tid; u < D; u += kPlanThreads) {
+    Piece p;
+    p.tile_hi = describe(u, p);
+    p.tile_lo = 0;
+    p.slot = -1;
+    plan.pieces[s.begin[u % N] + u / N] = p;
+  }
+  int k = tid < N ? s.begin[tid] + rounds : 0;
+  walk([&](Piece& p, int n, int j) {
+    p.slot = -1;
+    if (p.tile_lo > 0 || p.tile_hi < n) {
+      p.slot = 2 * tid + (p.tile_lo == 0);     // (a CTA has one piece that begins inside a unit, and one that only ends there)
+      plan.part_id[p.slot] = p.id;
+      if (p.tile_lo == 0) {
+        int lo = tid, hi = N - 1;              // the last CTA whose share begins before the unit's end
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) >> 1;
+          if (s.load[mid] < s.before[j + 1]) lo = mid; else hi = mid - 1;
+        }
+        plan.merge[atomicAdd(plan.n_merge, 1)] = MergeUnit{p.row0, p.n_pos, p.unit, p.id, tid, lo, 0, 0};
+      }
+    }
+    plan.pieces[k++] = p;
+  });
+}
+
+// ---- attention ----------------------------------------------------------------------------------------
+__device__ __forceinline__ uint64_t desc128(uint32_t saddr, uint32_t lbo) { return smem_desc_sw(saddr, lbo, 1024, 2); }
+// D (TMEM) += A (TMEM: two bf16 per column, lane = row) B (shared memory)
+__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+
+struct __align__(64) Maps {
+  CUtensorMap q, k, v, lk, lv;                 // queries; pages of the main and of the local pool
+};
+
+__global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_constant__ Maps maps, const __grid_constant__ CacheView cv,
+                                                                  const __grid_constant__ CacheView lv, const __grid_constant__ HeadUnits hu,
+                                                                  const __grid_constant__ Plan plan, const __grid_constant__ Dims d,
+                                                                  const int bmp, __nv_bfloat16* __restrict__ out,
+                                                                  float* __restrict__ lse, int32_t* status) {
+  chain_wait();
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const uint32_t sbase = s_u32(smem);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kBarOff + kNumBars * 8);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kBarOff + kNumBars * 8 + 8);
+  auto bar = [&](int i) { return sbase + kBarOff + i * 8; };
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int G = d.group;
+  const int p_lo = __ldcg(plan.piece_begin + blockIdx.x), p_hi = __ldcg(plan.piece_begin + blockIdx.x + 1);
+  if (p_lo >= p_hi) return;
+
+  if (tid == 0) {
+    for (int i = 0; i < kNumBars; ++i) mbar_init(bar(i), i >= kPFull && i < kPFull + 2 ? 128 : 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s_u32(tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;            // S / P of the groups: columns 0, 128; their O: 256, 384
+
+  auto load_piece = [&](int i) -> Piece {
+    Piece p;
+    const int4* src = reinterpret_cast<const int4*>(plan.pieces + i);
+    int4* dst = reinterpret_cast<int4*>(&p);
+#pragma unroll
+    for (int x = 0; x < 3; ++x) dst[x] = __ldcg(src + x);
+    return p;
+  };
+
+  // 256 x 232 + 128 x 40 = 384 x 168 registers
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp == 9 || warp == 10) {
+      // ================================ loaders: Q and K, V ================================
+      const bool is_v = warp == 10;
+      unsigned fill = 0, item = is_v ? 1 : 0, n_aux = 0;
+      for (int i = p_lo; i < p_hi; ++i) {
+        const Piece p = load_piece(i);
+        const int flags = hu.flags[p.unit], kvh = hu.head[p.unit];
+        const bool local_pool = flags & kLocalPool;
+        const CacheView& view = local_pool ? lv : cv;
+        const CUtensorMap* map = is_v ? (local_pool ? &maps.lv : &maps.v) : (local_pool ? &maps.lk : &maps.k);
+        const int kslot = view.kv_slot[kvh];
+        const int64_t bt_base = (int64_t)p.seq * view.max_pages;
+        if (!is_v && p.tile_lo < p.tile_hi) {
+          for (int t = 0; t < (p.n_pos > bmp ? 2 : 1); ++t, ++fill) {
+            const int b = fill & 1;
+            if (fill >= 2) mbar_wait(bar(kQEmpty + b), ((fill >> 1) - 1) & 1, abort_flag, status, d.wait_ns);
+            if (lane == 0) {
+              mbar_expect_tx(bar(kQFull + b), (uint32_t)(G * bmp) * 256u);
+              tma_load_3d(sbase + b * kSlot, &maps.q, 0, kvh * G, p.row0 + t * bmp, bar(kQFull + b));
+              tma_load_3d(sbase + b * kSlot + kBlk, &maps.q, 64, kvh * G, p.row0 + t * bmp, bar(kQFull + b));
+            }
+            __syncwarp();
+          }
+        }
+        int entry = 0;                         // lane: page of tile base + lane / 2
+        for (int x = p.tile_lo; x < p.tile_hi; ++x, item += 2) {
+          const int rel = (x - p.tile_lo) & 15;
+          if (rel == 0) {
+            const int y = x + (lane >> 1);
+            const int page = 2 * (y < p.n_sink_tiles ? y : p.kt_first + (y - p.n_sink_tiles)) + (lane & 1);
+            entry = -1;
+            if (y < p.tile_hi && page * kPage < p.n_keys) entry = safe_phys(view, bt_base + page_entry(view, page), status);
+          }
+          const int ph0 = __shfl_sync(0xffffffffu, entry, 2 * rel), ph1 = __shfl_sync(0xffffffffu, entry, 2 * rel + 1);
+          const int kt = x < p.n_sink_tiles ? x : p.kt_first + (x - p.n_sink_tiles);
+          const int slot = item % kRing;
+          const unsigned use = item / kRing;
+          if (use >= 1) mbar_wait(bar(kEmpty + slot), (use - 1) & 1, abort_flag, status, d.wait_ns);
+          const uint32_t dst = sbase + kRingOff + slot * kSlot;
+          const int n_ok = p.n_keys - kt * kTile;   // keys of the tile that rows may see
+          const bool part = is_v && n_ok < kTile;
+          const uint32_t fb = part ? bar(kAux) : bar(kFull + slot);
+          if (lane == 0 && !(d.wait_test && !is_v && item == 0)) {   // (the test hook drops one signal)
+            mbar_expect_tx(fb, ph1 >= 0 ? 2 * kBlk : kBlk);
+            const int y0 = (ph0 * view.n_kv + kslot) * kPage, y1 = (ph1 * view.n_kv + kslot) * kPage;
+            tma_load_2d(dst, map, 0, y0, fb);
+            tma_load_2d(dst + kBlk, map, 64, y0, fb);
+            if (ph1 >= 0) {
+              tma_load_2d(dst + kPage * 128, map, 0, y1, fb);
+              tma_load_2d(dst + kBlk + kPage * 128, map, 64, y1, fb);
+            }
+          }
+          __syncwarp();
+          if (part) {                          // what lies behind the last key is not read: 0 x NaN is no 0
+            mbar_wait(bar(kAux), n_aux & 1, abort_flag, status, d.wait_ns);
+            ++n_aux;
+            unsigned char* v = smem + kRingOff + slot * kSlot;
+            for (int z = n_ok * 8 + lane; z < kTile * 8; z += 32) {
+              *reinterpret_cast<uint4*>(v + z * 16) = make_uint4(0, 0, 0, 0);
+              *reinterpret_cast<uint4*>(v + kBlk + z * 16) = make_uint4(0, 0, 0, 0);
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kFull + slot));
+          }
+        }
+      }
+    } else if (warp == 8) {
+      // ================================ MMA issuer ================================
+      const uint32_t idesc_s = instr_desc_mn(128, 128, false), idesc_o = instr_desc_mn(128, 128, true);
+      unsigned job = 0, tile = 0, fill = 0, n_p[2] = {0, 0};
+      // the P V that is still to be issued
+      bool wait_pv = false, pv_first = false, pv_free = false, pv_last = false;
+      int pv_g = 0;
+      unsigned pv_item = 0;
+      auto issue_pv = [&]() {
+        const int slot = pv_item % kRing;
+        mbar_wait(bar(kFull + slot), (pv_item / kRing) & 1, abort_flag, status, d.wait_ns);
+        mbar_wait(bar(kPFull + pv_g), (pv_g ? n_p[1] : n_p[0]) & 1, abort_flag, status, d.wait_ns);
+        if (pv_g) ++n_p[1]; else ++n_p[0];
+        tc_fence_after();
+        if (lane == 0) {
+          const uint32_t v = sbase + kRingOff + slot * kSlot;
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks)       // 16 keys per step: 8 columns of P
+            tc_mma_ts(tmem + 256u + pv_g * 128u, tmem + pv_g * 128u + ks * 8u, desc128(v + ks * 2048, kBlk), idesc_o, (!pv_first || ks) ? 1u : 0u);
+          if (pv_free) tc_commit(bar(kEmpty + slot));
+          if (pv_last) tc_commit(bar(kOFull + pv_g));
+        }
+        __syncwarp();
+      };
+      for (int i = p_lo; i < p_hi; ++i) {
+        const Piece p = load_piece(i);
+        const int n = p.tile_hi - p.tile_lo, nq = p.n_pos > bmp ? 2 : 1, jobs = n * nq;
+        for (int x = 0; x < jobs; ++x, ++job) {
+          const int g = job & 1, qt = nq == 2 ? (x & 1) : 0, t = nq == 2 ? x >> 1 : x;
+          const unsigned k_item = 2 * (tile + t), qf = fill + qt;
+          const int slot = k_item % kRing, qb = qf & 1;
+          if (t == 0) mbar_wait(bar(kQFull + qb), (qf >> 1) & 1, abort_flag, status, d.wait_ns);
+          mbar_wait(bar(kFull + slot), (k_item / kRing) & 1, abort_flag, status, d.wait_ns);
+          tc_fence_after();
+          if (lane == 0) {
+            const uint32_t q = sbase + qb * kSlot, k = sbase + kRingOff + slot * kSlot;
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+              tc_mma(tmem + g * 128u, desc128(q + (ks >> 2) * kBlk + (ks & 3) * 32, 16), desc128(k + (ks >> 2) * kBlk + (ks & 3) * 32, 16), idesc_s,
+                     ks ? 1u : 0u);
+            tc_commit(bar(kSFull + g));
+            if (qt == nq - 1) tc_commit(bar(kEmpty + slot));
+            if (t == n - 1) tc_commit(bar(kQEmpty + qb));
+          }
+          __syncwarp();
+          if (wait_pv) issue_pv();
+          wait_pv = true;
+          pv_g = g;
+          pv_item = k_item + 1;
+          pv_first = x < 2;
+          pv_free = qt == nq - 1;
+          pv_last = x + 2 >= jobs;
+        }
+        tile += n;
+        if (n > 0) fill += nq;
+      }
+      if (wait_pv) issue_pv();
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    // ================================ softmax (thread = row) ================================
+    const int grp = tid >> 7, row = tid & 127, po = row / G, hs = row - po * G;
+    const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t tmem_s = tmem + grp * 128u + lane_addr, tmem_o = tmem + 256u + grp * 128u + lane_addr;
+    const uint32_t tmem_o2 = tmem + 256u + (grp ^ 1) * 128u + lane_addr;
+    float* xch = reinterpret_cast<float*>(smem + kXchOff);
+    const float sc2 = d.sm_scale * kLog2e;
+    unsigned job0 = 0, n_s = 0, n_o = 0;
+    for (int i = p_lo; i < p_hi; ++i) {
+      const Piece p = load_piece(i);
+      const int n = p.tile_hi - p.tile_lo, nq = p.n_pos > bmp ? 2 : 1, jobs = n * nq;
+      const int x0 = jobs ? (int)((grp ^ job0) & 1) : grp;          // this group's first job; without keys, group = Q tile
+      job0 += jobs;
+      const int qt = nq == 2 ? x0 : 0;
+      const bool row_ok = po < bmp && qt * bmp + po < p.n_pos;
+      const int pos = p.pos0 + qt * bmp + po, lim = min(pos, p.n_keys - 1);
+      const bool local = hu.flags[p.unit] & kLocal;
+      const bool warp_on = __any_sync(0xffffffffu, row_ok);
+      float m_ref = -INFINITY, l_run = 0.f;
+      for (int x = x0; x < jobs; x += 2, ++n_s) {
+        const int tt = p.tile_lo + (nq == 2 ? x >> 1 : x);
+        const int n_base = (tt < p.n_sink_tiles ? tt : p.kt_first + (tt - p.n_sink_tiles)) * kTile;
+        mbar_wait(bar(kSFull + grp), n_s & 1, abort_flag, status, d.wait_ns);
+        if (warp_on) {
+          tc_fence_after();
+          float s[kTile];
+          {
+            uint32_t* r0p = reinterpret_cast<uint32_t*>(s);
+            uint32_t* r1p = r0p + 64;
+            RTP_TMEM_LD64(r0p, tmem_s);
+            RTP_TMEM_LD64(r1p, tmem_s + 64);
+            tc_wait_ld();
+          }
+          if (n_base + kTile - 1 > lim || (local && n_base <= pos - d.window)) {
+            const int hi = lim - n_base, lo = local ? pos - d.window - n_base : -1, sink = local ? d.n_sink - n_base : 0;
+#pragma unroll
+            for (int e = 0; e < kTile; ++e)
+              if (!(e <= hi && (e > lo || e < sink))) s[e] = -INFINITY;
+          }
+          float tmax;
+          {
+            float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
+#pragma unroll
+            for (int e = 4; e < kTile; e += 4) {
+              t0 = fmaxf(t0, s[e]); t1 = fmaxf(t1, s[e + 1]); t2 = fmaxf(t2, s[e + 2]); t3 = fmaxf(t3, s[e + 3]);
+            }
+            tmax = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * sc2;
+          }
+          // the reference is raised, and O and l scaled, only when a maximum exceeds it by more than 2^8 (any reference gives the same
+          // quotient); the group's P V of before is complete, since S was issued behind it
+          const bool raise = tmax > m_ref + 8.0f;
+          if (x >= 2 && __any_sync(0xffffffffu, raise)) {
+            const float f = raise ? ((m_ref == -INFINITY) ? 0.f : fast_ex2(m_ref - tmax)) : 1.f;
+#pragma unroll
+            for (int c4 = 0; c4 < 4; ++c4) {
+              uint32_t r[32];
+              RTP_TMEM_LD32(r, tmem_o + c4 * 32);
+              tc_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
+              RTP_TMEM_ST32(tmem_o + c4 * 32, r);
+            }
+            l_run *= f;
+          }
+          if (raise) m_ref = tmax;
+          const float mb = (m_ref == -INFINITY) ? 0.f : m_ref;
+          float rs[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {        // P is rounded to bf16 for the MMA; the sum is of the 32-bit values
+            uint32_t pk[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const float p0 = fast_ex2(fmaf(s[h * 64 + 2 * e], sc2, -mb)), p1 = fast_ex2(fmaf(s[h * 64 + 2 * e + 1], sc2, -mb));
+              rs[e & 3] += p0 + p1;
+              const __nv_bfloat162 v = __floats2bfloat162_rn(p0, p1);
+              pk[e] = *reinterpret_cast<const uint32_t*>(&v);
+            }
+            RTP_TMEM_ST32(tmem_s + h * 32, pk);
+          }
+          l_run += (rs[0] + rs[1]) + (rs[2] + rs[3]);
+          tc_wait_st();
+          tc_fence_before();
+        }
+        mbar_arrive(bar(kPFull + grp));
+      }
+      // ---- end of the piece ----
+      const bool mine = x0 < jobs;             // this group has an accumulator
+      const bool joined = nq == 1 && jobs >= 2;
+      if (mine) {
+        mbar_wait(bar(kOFull + grp), n_o & 1, abort_flag, status, d.wait_ns);
+        ++n_o;
+        tc_fence_after();
+      }
+      float m_tot = m_ref, l_tot = l_run, w_me = 1.f, w_ot = 0.f;
+      if (joined) {                            // both groups have seen this row: each takes half of the channels
+        xch[(grp * 2 + 0) * 128 + row] = m_ref;
+        xch[(grp * 2 + 1) * 128 + row] = l_run;
+        tc_fence_before();
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        tc_fence_after();
+        const float m_ot = xch[((grp ^ 1) * 2 + 0) * 128 + row], l_ot = xch[((grp ^ 1) * 2 + 1) * 128 + row];
+        m_tot = fmaxf(m_ref, m_ot);
+        w_me = (m_ref == -INFINITY) ? (l_run == 0.f ? 0.f : l_run) : fast_ex2(m_ref - m_tot);
+        w_ot = (m_ot == -INFINITY) ? (l_ot == 0.f ? 0.f : l_ot) : fast_ex2(m_ot - m_tot);
+        l_tot = l_run * w_me + l_ot * w_ot;
+      }
+      const bool writer = joined || mine || (jobs == 0 && grp < nq);
+      if (writer && warp_on) {
+        const int c_lo = joined ? grp * 2 : 0, c_hi = joined ? c_lo + 2 : 4;   // pieces of 32 channels
+        const int64_t r_out = p.row0 + qt * bmp + po;
+        const int qh = hu.head[p.unit] * G + hs;
+        const bool wr = row_ok && (p.slot >= 0 || hu.writes(p.unit, row_ok ? qh : 0));
+        // (a sum that is no number stays one: only a row that saw nothing is 0)
+        const float inv = p.slot >= 0 ? 1.f : l_tot == 0.f ? 0.f : 1.f / l_tot;
+        const float f_me = w_me * inv, f_ot = w_ot * inv;
+        const int64_t prow = ((int64_t)p.slot * plan.slot_rows + qt * 128 + row);
+        for (int c4 = c_lo; c4 < c_hi; ++c4) {
+          uint32_t r[32], r2[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) r[e] = 0u;
+          if (mine) RTP_TMEM_LD32(r, tmem_o + c4 * 32);
+          if (joined) RTP_TMEM_LD32(r2, tmem_o2 + c4 * 32);
+          tc_wait_ld();
+          float o[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(r[e]) * f_me;
+          if (joined) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = fmaf(__uint_as_float(r2[e]), f_ot, o[e]);
+          }
+          if (l_tot == 0.f) {                  // (accumulators of keys that were all masked, or none)
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = 0.f;
+          }
+          if (wr && p.slot >= 0) {
+            float4* dst = reinterpret_cast<float4*>(plan.o + prow * kHeadDim + c4 * 32);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+          } else if (wr) {
+            uint4* dst = reinterpret_cast<uint4*>(out + (r_out * d.n_q + qh) * kHeadDim + c4 * 32);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t w[4];
+#pragma unroll
+              for (int y = 0; y < 4; ++y) {
+                const __nv_bfloat162 v = __floats2bfloat162_rn(o[8 * e + 2 * y], o[8 * e + 2 * y + 1]);
+                w[y] = *reinterpret_cast<const uint32_t*>(&v);
+              }
+              dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+        }
+        if (wr && c_lo == 0) {
+          if (p.slot >= 0) {
+            *reinterpret_cast<float2*>(plan.ml + prow * 2) = make_float2(m_tot, l_tot);
+          } else if (lse) {
+            lse[r_out * d.n_q + qh] = l_tot == 0.f ? -INFINITY : (m_tot + log2f(l_tot)) * kLn2;
+          }
+        }
+      }
+      if (joined) {                            // the other group's accumulator is no longer read
+        tc_fence_before();
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        tc_fence_after();
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {                           // copies that are still under way land before the block's memory is given up
+    const unsigned long long t0 = global_ns();
+    while (global_ns() - t0 < 1000000ull) __nanosleep(1000);
+  }
+  if (warp == 8) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+// ---- merge: a warp per row of a cut unit ---------------------------------------------------------------
+constexpr int kMergeWarps = 8;
+__global__ void __launch_bounds__(kMergeWarps * 32) merge_kernel(const __grid_constant__ HeadUnits hu, const __grid_constant__ Plan plan,
+                                                                 const int G, const int bmp, const int n_q, __nv_bfloat16* __restrict__ out,
+                                                                 float* __restrict__ lse) {
+  chain_wait();
+  if ((int)blockIdx.x >= __ldcg(plan.n_merge)) return;
+  const int4* src = reinterpret_cast<const int4*>(plan.merge + blockIdx.x);
+  const int4 a = __ldcg(src), b = __ldcg(src + 1);   // row0, n_pos, unit, id; first and last CTA
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int R = a.y * G;
+  for (int y = blockIdx.y * kMergeWarps + warp; y < R; y += gridDim.y * kMergeWarps) {
+    const int po = y / G, hs = y - po * G, qt = po / bmp, row = qt * 128 + (po - qt * bmp) * G + hs;
+    const int qh = hu.head[a.z] * G + hs;
+    if (!hu.writes(a.z, qh)) continue;
+    // parts in the order of their CTAs: the first one's last piece, the others' first
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c0 = b.x; c0 <= b.y; c0 += 32) {
+      const int c = c0 + lane, slot = 2 * c + (c == b.x);
+      const bool there = c <= b.y && __ldcg(plan.part_id + slot) == a.w;
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (there) ml = __ldcg(reinterpret_cast<const float2*>(plan.ml) + (int64_t)slot * plan.slot_rows + row);
+      const float m_new = fmaxf(m, warp_max(ml.x));
+      const float mb = m_new == -INFINITY ? 0.f : m_new;
+      const float f = m == -INFINITY ? 1.f : fast_ex2(m - mb), w = ml.x == -INFINITY && ml.y == 0.f ? 0.f : ml.x == -INFINITY ? ml.y : fast_ex2(ml.x - mb);
+      m = m_new;
+      l = l * f + warp_sum(ml.y * w);
+      o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+      uint32_t todo = __ballot_sync(0xffffffffu, there);
+      while (todo) {
+        const int j = __ffs(todo) - 1;
+        todo &= todo - 1;
+        const float wj = __shfl_sync(0xffffffffu, w, j);
+        const int sl = __shfl_sync(0xffffffffu, slot, j);
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(plan.o + ((int64_t)sl * plan.slot_rows + row) * kHeadDim) + lane);
+        o.x = fmaf(v.x, wj, o.x); o.y = fmaf(v.y, wj, o.y); o.z = fmaf(v.z, wj, o.z); o.w = fmaf(v.w, wj, o.w);
+      }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const __nv_bfloat162 u = __floats2bfloat162_rn(o.x * inv, o.y * inv), v = __floats2bfloat162_rn(o.z * inv, o.w * inv);
+    const int64_t at = (int64_t)(a.x + po) * n_q + qh;
+    reinterpret_cast<uint2*>(out + at * kHeadDim)[lane] = make_uint2(*reinterpret_cast<const uint32_t*>(&u), *reinterpret_cast<const uint32_t*>(&v));
+    if (lse && lane == 0) lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  }
+}
+
+Plan carve(void* ws, int G, int n_units, int64_t n_chunks, int64_t R, int sm_count, size_t* bytes) {
+  Plan p = {};
+  p.n_ctas = std::min(sm_count, 1024);
+  const int bmp = kTile / G;
+  const int64_t units = (R / (2 * bmp) + n_chunks) * n_units;
+  p.max_units = (int)std::min<int64_t>(units, 0x7fffffff);
+  p.slot_rows = R > bmp ? 256 : (int)(R * G);
+  char* base = reinterpret_cast<char*>(ws);
+  size_t off = 0;
+  auto take = [&](size_t n) {
+    char* r = base + off;
+    off += (n + 255) & ~(size_t)255;
+    return r;
+  };
+  p.n_merge = reinterpret_cast<int32_t*>(take(4));
+  p.piece_begin = reinterpret_cast<int32_t*>(take((size_t)(p.n_ctas + 1) * 4));
+  p.part_id = reinterpret_cast<int32_t*>(take((size_t)p.n_ctas * 8));
+  p.merge = reinterpret_cast<MergeUnit*>(take((size_t)p.n_ctas * sizeof(MergeUnit)));
+  p.pieces = reinterpret_cast<Piece*>(take((size_t)(units + p.n_ctas) * sizeof(Piece)));
+  p.ml = reinterpret_cast<float*>(take((size_t)2 * p.n_ctas * p.slot_rows * 8));
+  p.o = reinterpret_cast<float*>(take((size_t)2 * p.n_ctas * p.slot_rows * kHeadDim * 4));
+  *bytes = off;
+  return p;
+}
+
+size_t plan_smem(int64_t n_chunks) { return ((sizeof(PlanShared) + 15) & ~(size_t)15) + (size_t)n_chunks * sizeof(int4); }
+
+}  // namespace
+
+size_t attn_chunks_workspace_bytes(const Dims& d, int64_t n_chunks, int64_t R, int sm_count) {
+  size_t bytes = 0;
+  carve(nullptr, d.group, std::min(2 * d.n_kv, kMaxUnits), n_chunks, R, sm_count, &bytes);
+  return bytes;
+}
+
+cudaError_t launch_attn_chunks(const CacheView& cv, const CacheView& lv, const Dims& d, const ChunkHeads& ch, const __nv_bfloat16* q,
+                               const int32_t* chunk_seq, const int32_t* chunk_start, const int32_t* row_offsets, int64_t n_chunks,
+                               int64_t R, __nv_bfloat16* out, float* lse, void* ws, size_t ws_bytes, int32_t* status, int sm_count,
+                               cudaStream_t st) {
+  if (n_chunks == 0 || R == 0 || ch.n == 0) return cudaSuccess;
+  HeadUnits hu = {};
+  for (int i = 0; i < RTP_MAX_Q_HEADS / 32; ++i) hu.ret_q[i] = ch.ret_q[i];
+  for (int i = 0; i < ch.n; ++i) {
+    hu.head[i] = ch.head[i];
+    hu.flags[i] = (uint8_t)((ch.local[i] ? kLocal : 0) | (ch.skip_ret[i] ? kSkipRet : 0) | (ch.skip_other[i] ? kSkipOther : 0) |
+                            (ch.local[i] && lv.n_kv > 0 ? kLocalPool : 0));
+  }
+  hu.n = ch.n;
+  const int bmp = kTile / d.group;
+  size_t need = 0;
+  Plan plan = carve(ws, d.group, ch.n, n_chunks, R, sm_count, &need);
+  if (need > ws_bytes) return cudaErrorMemoryAllocation;
+  if ((int64_t)plan.max_units + plan.n_ctas >= ((int64_t)1 << 31) - 1) return cudaErrorNotSupported;
+  Maps maps = {};
+  const int swz = (int)CU_TENSOR_MAP_SWIZZLE_128B;
+  cudaError_t e = make_heads_map(&maps.q, q, R, d.n_q, d.group, bmp, swz);
+  if (e == cudaSuccess && cv.n_kv > 0) e = make_rows_map(&maps.k, cv.k, (int64_t)cv.num_pages * cv.n_kv * kPage, kHeadDim, 64, kPage, swz);
+  if (e == cudaSuccess && cv.n_kv > 0) e = make_rows_map(&maps.v, cv.v, (int64_t)cv.num_pages * cv.n_kv * kPage, kHeadDim, 64, kPage, swz);
+  if (e == cudaSuccess && lv.n_kv > 0) e = make_rows_map(&maps.lk, lv.k, (int64_t)lv.num_pages * lv.n_kv * kPage, kHeadDim, 64, kPage, swz);
+  if (e == cudaSuccess && lv.n_kv > 0) e = make_rows_map(&maps.lv, lv.v, (int64_t)lv.num_pages * lv.n_kv * kPage, kHeadDim, 64, kPage, swz);
+  if (e != cudaSuccess) return e;
+  static PerDeviceOnce once_plan, once_attn;
+  e = set_dyn_smem_once(plan_kernel, (int)plan_smem(kMaxChunks), once_plan);
+  if (e == cudaSuccess) e = set_dyn_smem_once(attn_chunks_kernel, kSmem, once_attn);
+  if (e != cudaSuccess) return e;
+  bool ring = false;
+  for (int i = 0; i < ch.n; ++i) ring = ring || (hu.flags[i] & kLocalPool);
+  const ChunkArgs a = {chunk_seq, chunk_start, row_offsets, (int32_t)n_chunks, d.group, bmp, R,
+                       ring ? (int64_t)lv.ring_pages * kPage : 0, ring ? (int64_t)lv.max_pages * kPage : 0};
+  (void)launch_chained(plan_kernel, dim3(1), dim3(kPlanThreads), plan_smem(n_chunks), st, a, cv, hu, plan, d.n_sink, d.window, status);
+  (void)launch_chained(attn_chunks_kernel, dim3(plan.n_ctas), dim3(kThreads), (size_t)kSmem, st, maps, cv, lv, hu, plan, d, bmp, out, lse, status);
+  const int merge_rows = (int)std::min<int64_t>(R, 2 * bmp) * d.group;
+  (void)launch_chained(merge_kernel, dim3(plan.n_ctas, (unsigned)std::min(8, (merge_rows + kMergeWarps - 1) / kMergeWarps)), dim3(kMergeWarps * 32), 0, st,
+                       hu, plan, d.group, bmp, d.n_q, out, lse);
+  return cudaGetLastError();
+}
+
+}  // namespace rtp

@@ -905,4 +905,60 @@ rtp_status rtp_dense_attn_decode(rtp_ctx* ctx, const rtp_params* params, const r
   return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_dense_attn_decode");
 }
 
+size_t rtp_chunk_workspace_bytes(const rtp_params* params, int64_t n_chunks, int64_t rows) {
+  Dims d;
+  HeadMaps hm;
+  if (check_params(params, &d, &hm) || n_chunks <= 0 || n_chunks > kMaxChunks || rows <= 0 || rows >= (int64_t)1 << 31) return 0;
+  return attn_chunks_workspace_bytes(d, n_chunks, rows, current_sm_count(kFallbackSm));
+}
+
+rtp_status rtp_attn_chunks(rtp_ctx* ctx, const rtp_params* params, const rtp_cache* cache, const void* q, const int32_t* chunk_seq,
+                           const int32_t* chunk_start, const int32_t* row_offsets, int64_t n_chunks, int64_t R, int32_t pattern,
+                           const int32_t* kv_heads, int32_t n_heads, void* out, float* lse, void* workspace,
+                           size_t workspace_bytes, int32_t* status, void* stream) {
+  RTP_COMMON_PROLOGUE(true, false)
+  if (pattern != RTP_CHUNK_DENSE && pattern != RTP_CHUNK_LOCAL && pattern != RTP_CHUNK_BY_HEAD) return fail(ctx, RTP_ERR_INVALID, "unknown pattern");
+  if (n_chunks < 0 || R < 0) return fail(ctx, RTP_ERR_INVALID, "chunk or row count is negative");
+  if (n_chunks > kMaxChunks) return fail(ctx, RTP_ERR_UNSUPPORTED, "more than 8192 chunks in one call");
+  if (R >= ((int64_t)1 << 31) / d.n_q) return fail(ctx, RTP_ERR_UNSUPPORTED, "2^31 or more (row, head) pairs in one call");
+  if (const char* m = fill_kv_list(params, kv_heads, n_heads, &hm)) return fail(ctx, RTP_ERR_INVALID, m);
+  if (n_chunks == 0 || R == 0) return RTP_OK;
+  if (cv.kv_fp4) return fail(ctx, RTP_ERR_UNSUPPORTED, "4-bit K/V cache: decode calls only (or rtp_kv_expand its pages)");
+  if (!q || !out || !chunk_seq || !chunk_start || !row_offsets || !workspace) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
+  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
+  bool is_local[32] = {}, named[32] = {};
+  for (int i = 0; i < params->n_local_kv_heads; ++i) is_local[params->local_kv_heads[i]] = true;
+  ChunkHeads ch = {};
+  for (int i = 0; i < d.n_ret; ++i) ch.ret_q[hm.ret_q_head[i] >> 5] |= 1u << (hm.ret_q_head[i] & 31);
+  auto add = [&](int head, bool local, bool skip_ret, bool skip_other) {
+    ch.head[ch.n] = (uint8_t)head;
+    ch.local[ch.n] = local;
+    ch.skip_ret[ch.n] = skip_ret;
+    ch.skip_other[ch.n++] = skip_other;
+  };
+  for (int i = 0; i < hm.n_kv_list; ++i) {
+    const int h = hm.kv_list[i];
+    if (named[h]) return fail(ctx, RTP_ERR_INVALID, "a KV head is named twice");
+    named[h] = true;
+    int n_ret = 0;   // retrieval heads in its group
+    for (int g = 0; g < d.group; ++g) n_ret += (ch.ret_q[(h * d.group + g) >> 5] >> ((h * d.group + g) & 31)) & 1u;
+    const bool local = pattern != RTP_CHUNK_DENSE && is_local[h];
+    if (local) add(h, true, true, false);
+    if (pattern == RTP_CHUNK_DENSE || (pattern == RTP_CHUNK_BY_HEAD && !is_local[h])) add(h, false, false, false);
+    // a mixed group: its retrieval heads attend to everything
+    if (pattern == RTP_CHUNK_BY_HEAD && is_local[h] && n_ret > 0) add(h, false, false, true);
+  }
+  for (int i = 0; i < ch.n; ++i)
+    if (!ch.local[i] && cv.kv_slot[ch.head[i]] == 0xff)
+      return fail(ctx, RTP_ERR_UNSUPPORTED, "the cache is truncated for local heads: a dense call may only name the other KV heads");
+  if (ch.n == 0) return RTP_OK;
+  CacheView lv = {};
+  if (cache->k_local_pages) lv = local_view(cv, cache, params);   // (whether its rings suffice is seen on the device)
+  cudaError_t e = launch_attn_chunks(cv, lv, d, ch, reinterpret_cast<const __nv_bfloat16*>(q), chunk_seq, chunk_start, row_offsets, n_chunks, R,
+                                     reinterpret_cast<__nv_bfloat16*>(out), lse, workspace, workspace_bytes, status, ctx->sm_count, st);
+  if (e == cudaErrorMemoryAllocation) return fail(ctx, RTP_ERR_CAPACITY, "workspace too small");
+  if (e == cudaErrorNotSupported) return fail(ctx, RTP_ERR_UNSUPPORTED, "too many rows in one call");
+  return e == cudaSuccess ? RTP_OK : cuda_fail(ctx, e, "rtp_attn_chunks");
+}
+
 }  // extern "C"

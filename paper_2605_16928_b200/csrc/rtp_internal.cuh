@@ -278,6 +278,21 @@ cudaError_t launch_attn_prefill_tc(const CacheView& cv, const Dims& d, const Hea
                                    __nv_bfloat16* out, float* lse, int32_t* status, cudaStream_t st,
                                    const uint32_t* blk_mask, int64_t mask_words);
 
+// Chunks of several sequences: KV heads of the call, each with its pattern and the query heads of its group that are left out.
+constexpr int kMaxChunks = 8192;
+struct ChunkHeads {
+  uint8_t head[64];
+  bool local[64], skip_ret[64], skip_other[64];
+  int32_t n;
+  uint32_t ret_q[RTP_MAX_Q_HEADS / 32];   // retrieval query heads
+};
+size_t attn_chunks_workspace_bytes(const Dims& d, int64_t n_chunks, int64_t R, int sm_count);
+// lv: the local heads' pool (n_kv = 0 if there is none).  cudaErrorMemoryAllocation: the workspace is too small.
+cudaError_t launch_attn_chunks(const CacheView& cv, const CacheView& lv, const Dims& d, const ChunkHeads& ch, const __nv_bfloat16* q,
+                               const int32_t* chunk_seq, const int32_t* chunk_start, const int32_t* row_offsets, int64_t n_chunks,
+                               int64_t R, __nv_bfloat16* out, float* lse, void* ws, size_t ws_bytes, int32_t* status, int sm_count,
+                               cudaStream_t st);
+
 // Block-wise top-p of a prefill chunk (Section 3.4): one bit per (row, retrieval head, page).
 size_t select_blocks_workspace_bytes(const Dims& d, const HeadMaps& hm, int64_t R, int64_t max_len, int sm_count);
 size_t select_rows_blocks_workspace_bytes(const Dims& d, int64_t R, int64_t max_len);

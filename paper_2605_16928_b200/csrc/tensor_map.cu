@@ -81,4 +81,19 @@ cudaError_t make_rows_map(CUtensorMap* map, const void* base, int64_t rows, int 
   return cudaSuccess;
 }
 
+// Query rows as [rows][n_heads][128] (encoded for every call: a program's activations move).
+cudaError_t make_heads_map(CUtensorMap* map, const void* base, int64_t rows, int n_heads, int box_heads, int box_rows, int swizzle) {
+  cudaError_t e = cudaSuccess;
+  EncodeTiledFn encode = encode_fn(&e);
+  if (!encode) return e;
+  const cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)n_heads, (cuuint64_t)rows};
+  const cuuint64_t strides[2] = {(cuuint64_t)kHeadDim * 2, (cuuint64_t)n_heads * kHeadDim * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, (CUtensorMapSwizzle)swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 }  // namespace rtp
