@@ -40,8 +40,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMaxUnits = 64;                  // (KV head, pattern) pairs of a call
 constexpr int kPlanThreads = 1024;
 
-enum Bar { kQFull = 0, kQEmpty = 2, kFull = 4, kEmpty = kFull + kRing, kSFull = kEmpty + kRing, kPFull = kSFull + 2, kOFull = kPFull + 2,
-           kAux = kOFull + 2, kNumBars };
+enum Bar { kQFull = 0, kQEmpty = 2, kFull = 4, kEmpty = kFull + kRing, kSFull = kEmpty + kRing, kPFull = kSFull + 2, kOFull = kPFull + 4,
+           kAux = kOFull + 2, kNumBars };   // (P: first and second half of each group's)
 static_assert(kNumBars * 8 + 16 <= 256, "barriers, TMEM address and abort flag");
 
 // A KV head of the call: sinks and window or everything before the row; which of its query heads are written.
@@ -68,10 +68,11 @@ struct __align__(16) MergeUnit {
 };
 struct Plan {                                  // where things lie in the workspace
   int32_t* n_merge;
-  int32_t* piece_begin;                        // [n_ctas + 1]
+  int32_t *piece_begin, *piece_end;            // [n_ctas]
   int32_t* part_id;                            // [2 n_ctas]: unit of the partial result in a slot, or -1
   MergeUnit* merge;                            // [n_ctas]
-  Piece* pieces;                               // [max_pieces]
+  Piece* pieces;
+  int64_t* before;                             // [max_units + 1], of calls with many units of different costs
   float* ml;                                   // [2 n_ctas][slot_rows][2]
   float* o;                                    // [2 n_ctas][slot_rows][128]
   int32_t n_ctas, max_units, slot_rows;
@@ -89,62 +90,73 @@ struct ChunkArgs {
 constexpr int kPieceCost = 3;
 constexpr int kMinJobs = 6;                    // a piece of its own (and a merge) has to be worth it
 constexpr int kSnap = 3;                       // key tiles that are not cut off
+constexpr int kPlanUnits = 1024;               // units whose costs lie in shared memory
 
 struct PlanShared {
   int64_t warp_sum[33];
-  int64_t total;
-  int32_t n_units;
-  int64_t load[1024];                          // jobs dealt to each CTA, then the cuts
-  int64_t before[1024 + 1];                    // jobs in front of each unit of the cut part
+  int64_t load[1024 + 1];                      // jobs dealt to each CTA, then the cuts
+  int64_t before[kPlanUnits + 1];
   int32_t begin[1024 + 1];
 };
 
-__device__ __forceinline__ int64_t scan64(int64_t x, int64_t* warp_sum, int lane, int warp) {   // exclusive; warp_sum[32]: the total
+// Exclusive sum over the block; warp_sum[32]: the total.
+__device__ __forceinline__ int64_t scan64(int64_t x, int64_t* warp_sum) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   int64_t s = x;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int64_t y = __shfl_up_sync(0xffffffffu, s, o);
     if (lane >= o) s += y;
   }
-  __syncthreads();
+  __syncthreads();                             // (the last sum's readers are through)
   if (lane == 31) warp_sum[warp] = s;
   __syncthreads();
-  if (warp == 0) {
-    const int64_t w = warp_sum[lane];
-    int64_t t = w;
+  const int64_t w = lane < warps ? warp_sum[lane] : 0;
+  int64_t t = w;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(0xffffffffu, t, o);
-      if (lane >= o) t += y;
-    }
-    warp_sum[lane] = t - w;
-    if (lane == 31) warp_sum[32] = t;
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, t, o);
+    if (lane >= o) t += y;
   }
+  if (warp == 0 && lane == 31) warp_sum[32] = t;
+  const int64_t mine = __shfl_sync(0xffffffffu, t - w, warp) + s - x;
   __syncthreads();
-  return warp_sum[warp] + s - x;
+  return mine;
+}
+// The last i in [0, n) with v[i] <= x (v[0] <= x).
+template <class V>
+__device__ __forceinline__ int last_at(int n, int64_t x, V v) {
+  int lo = 0, hi = n;
+  while (lo + 1 < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (v(mid) <= x) lo = mid; else hi = mid;
+  }
+  return lo;
 }
 
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constant__ ChunkArgs a, const __grid_constant__ CacheView cv,
                                                             const __grid_constant__ HeadUnits hu, const __grid_constant__ Plan plan,
                                                             const int n_sink, const int window, int32_t* status) {
   chain_wait();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // (the attention kernel sets itself up and waits for this one)
   extern __shared__ __align__(16) unsigned char smem_plan[];
   PlanShared& s = *reinterpret_cast<PlanShared*>(smem_plan);
   int4* chunk = reinterpret_cast<int4*>(smem_plan + ((sizeof(PlanShared) + 15) & ~15));   // [n_chunks]: units before, rows, start, keys
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int2* where = reinterpret_cast<int2*>(chunk + a.n_chunks);                              // [n_chunks]: row in q, sequence
+  const int tid = threadIdx.x, nt = blockDim.x;
   const int N = plan.n_ctas, H = hu.n, span = 2 * a.bmp;
   // chunks, with what is wrong in them
   int64_t mine = 0;
-  const int per = (a.n_chunks + kPlanThreads - 1) / kPlanThreads, c0 = min(tid * per, a.n_chunks), c1 = min(c0 + per, a.n_chunks);
+  const int per = (a.n_chunks + nt - 1) / nt, c0 = min(tid * per, a.n_chunks), c1 = min(c0 + per, a.n_chunks);
   bool bad = false;
   for (int c = c0; c < c1; ++c) {
     const int64_t lo = a.offsets[c], hi = a.offsets[c + 1];
+    const int seq = a.seq[c], start = a.start[c];
     int rows = (int)(hi - lo);
     if (lo < 0 || hi < lo || hi > a.R) {       // no rows of the call
       rows = 0;
       bad = true;
     }
-    const int seq = a.seq[c], start = a.start[c];
     int keys = (unsigned)seq < (unsigned)cv.batch ? max(0, min(cv.seq_lens[seq], cv.cap_tokens)) : 0;
     if (start < 0) keys = 0;
     if (rows > 0 && (int64_t)start + rows > keys) bad = true;
@@ -154,38 +166,36 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
       set_status(status, RTP_ERR_CAPACITY);
     }
     chunk[c] = make_int4(0, rows, start, keys);
+    where[c] = make_int2((int)lo, seq);
     mine += (int64_t)((rows + span - 1) / span) * H;
   }
-  int64_t at = scan64(mine, s.warp_sum, lane, warp);
-  const int64_t total_units = s.warp_sum[32];
-  for (int c = c0; c < c1; ++c) {
-    chunk[c].x = (int)min(at, (int64_t)0x7fffffff);
-    at += (int64_t)((chunk[c].y + span - 1) / span) * H;
-  }
-  for (int i = tid; i < 2 * N; i += kPlanThreads) plan.part_id[i] = -1;
-  for (int i = tid; i < N; i += kPlanThreads) s.load[i] = 0;
-  if (tid == 0) *plan.n_merge = 0;
   if (bad) set_status(status, RTP_ERR_INVALID);
-  __syncthreads();
+  for (int i = tid; i < 2 * N; i += nt) plan.part_id[i] = -1;
+  for (int i = tid; i < N; i += nt) s.load[i] = 0;
+  if (tid == 0) *plan.n_merge = 0;
+  int64_t at = scan64(mine, s.warp_sum);
+  const int64_t total_units = s.warp_sum[32];
   if (total_units > plan.max_units) {          // offsets that run back and forth: nothing is done
     if (tid == 0) set_status(status, RTP_ERR_INVALID);
-    for (int i = tid; i <= N; i += kPlanThreads) plan.piece_begin[i] = 0;
+    for (int i = tid; i < N; i += nt) plan.piece_begin[i] = plan.piece_end[i] = 0;
     return;
   }
+  for (int c = c0; c < c1; ++c) {
+    chunk[c].x = (int)at;
+    at += (int64_t)((chunk[c].y + span - 1) / span) * H;
+  }
+  __syncthreads();
   const int U = (int)total_units;
-  // unit u: chunk by chunk, head by head, the last positions first
-  auto describe = [&](int u, Piece& p) -> int {   // returns its key tiles
-    int lo = 0, hi = a.n_chunks;               // the last chunk with units before <= u that has any: the last one with x <= u
-    while (lo + 1 < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (chunk[mid].x <= u) lo = mid; else hi = mid;
-    }
-    const int4 c = chunk[lo];
-    const int nt = (c.y + span - 1) / span, r = u - c.x, h = r / nt, t = nt - 1 - (r - h * nt);
+  // unit u: chunk by chunk, head by head, the last positions first; returns its key tiles
+  auto describe = [&](int u, Piece& p) -> int {
+    const int i = last_at(a.n_chunks, u, [&](int j) { return chunk[j].x; });
+    const int4 c = chunk[i];
+    const int2 w = where[i];
+    const int nq = (c.y + span - 1) / span, r = u - c.x, h = r / nq, t = nq - 1 - (r - h * nq);
     p.pos0 = c.z + t * span;
     p.n_pos = min(span, c.y - t * span);
-    p.row0 = a.offsets[lo] + t * span;
-    p.seq = a.seq[lo];
+    p.row0 = w.x + t * span;
+    p.seq = w.y;
     p.unit = h;
     p.n_keys = min(c.w, p.pos0 + p.n_pos);
     p.id = u;
@@ -197,97 +207,133 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     }
     return p.n_sink_tiles + n_all - p.kt_first;
   };
-  auto jobs_per_tile = [&](const Piece& p) { return p.n_pos > a.bmp ? 2 : 1; };
-  auto cost = [&](int u) -> int64_t {
-    Piece p;
-    const int n = describe(u, p);
-    return kPieceCost + (int64_t)n * jobs_per_tile(p);
-  };
-  const int rounds = U >= 2 * N ? U / N - 1 : 0, D = rounds * N, M = U - D;   // M < 2 N
-  int64_t dealt = 0;
-  for (int u = tid; u < D; u += kPlanThreads) {
-    const int64_t w = cost(u);
-    dealt += w;
-    atomicAdd(reinterpret_cast<unsigned long long*>(&s.load[u % N]), (unsigned long long)w);
-  }
-  const int64_t w_mine = tid < M ? cost(D + tid) : 0;
-  scan64(dealt, s.warp_sum, lane, warp);
-  const int64_t W_dealt = s.warp_sum[32];
-  const int64_t before = scan64(w_mine, s.warp_sum, lane, warp);
-  const int64_t W_cut = s.warp_sum[32];
-  if (tid < M) s.before[tid] = before;
-  if (tid == 0) s.before[M] = W_cut;
-  // What each CTA takes of the cut part: with nothing dealt, equal shares for as many as are worth it; else up to the mean.
-  int64_t room = 0;
-  const int takers = rounds ? N : (int)max((int64_t)1, min((int64_t)N, W_cut / (kMinJobs + kPieceCost)));
-  if (tid < N) room = rounds ? max((int64_t)0, (W_dealt + W_cut) / N + 1 - s.load[tid]) : (tid < takers ? 1 : 0);
-  const int64_t room_before = scan64(room, s.warp_sum, lane, warp), rooms = s.warp_sum[32];
-  __syncthreads();
-  if (tid < N) s.load[tid] = rooms > 0 ? (int64_t)((double)W_cut * (double)room_before / (double)rooms) : (tid ? W_cut : 0);
-  __syncthreads();
-  // the pieces of CTA tid: units that meet [from, to)
-  const int64_t from = tid < N ? s.load[tid] : 0, to = tid + 1 < N ? s.load[tid + 1] : W_cut;
-  auto cut_at = [&](int64_t x, int64_t u0, int n, int per_tile) -> int {   // the key tile of a unit (u0 < x < its end) at which a cut at x falls
-    const int t = x <= u0 + kPieceCost ? 0 : (int)((x - u0 - kPieceCost + per_tile - 1) / per_tile);
-    return t < kSnap ? 0 : n - t < kSnap ? n : t;
-  };
-  auto walk = [&](auto&& emit) {
-    if (tid >= N || from >= to) return;
-    int lo = 0, hi = M;                        // the last unit with before <= from
-    while (lo + 1 < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (s.before[mid] <= from) lo = mid; else hi = mid;
-    }
-    for (int j = lo; j < M && s.before[j] < to; ++j) {
+  // Costs: the dealt units' go to their CTAs, the others' into a list.
+  int rounds = U >= 2 * N ? U / N - 1 : 0;
+  int64_t* before = s.before;
+  int64_t W_dealt = 0, W_cut = 0;
+  for (;;) {
+    const int D = rounds * N, M = U - D;
+    before = M <= kPlanUnits ? s.before : plan.before;
+    for (int u = tid; u < U; u += nt) {
       Piece p;
-      const int64_t u0 = s.before[j];
-      const int n = describe(D + j, p);
-      p.tile_lo = from <= u0 ? 0 : cut_at(from, u0, n, jobs_per_tile(p));
-      p.tile_hi = to >= s.before[j + 1] ? n : cut_at(to, u0, n, jobs_per_tile(p));
-      if (p.tile_lo < p.tile_hi || (n == 0 && u0 >= from)) emit(p, n, j);
+      const int n = describe(u, p);
+      const int64_t w = kPieceCost + (int64_t)n * (p.n_pos > a.bmp ? 2 : 1);
+      if (u < D) atomicAdd(reinterpret_cast<unsigned long long*>(&s.load[u % N]), (unsigned long long)w);
+      else before[u - D] = w;
     }
-  };
-  int n_cut = 0;
-  walk([&](const Piece&, int, int) { ++n_cut; });
-  const int cut_before = (int)scan64(n_cut, s.warp_sum, lane, warp);
-  if (tid < N) s.begin[tid] = tid * rounds + cut_before;
-  if (tid == 0) s.begin[N] = N * rounds + (int)s.warp_sum[32];
+    __syncthreads();
+    const int each = (M + nt - 1) / nt, j0 = min(tid * each, M), j1 = min(j0 + each, M);
+    int64_t sum = 0;
+    for (int j = j0; j < j1; ++j) sum += before[j];
+    int64_t run = scan64(sum, s.warp_sum);
+    W_cut = s.warp_sum[32];
+    for (int j = j0; j < j1; ++j) {
+      const int64_t w = before[j];
+      before[j] = run;
+      run += w;
+    }
+    if (tid == 0) before[M] = W_cut;
+    if (rounds == 0) break;
+    // Whole units only where no CTA gets more than its share of them: a few that cost more than the others are cut instead.
+    scan64(tid < N ? s.load[tid] : 0, s.warp_sum);
+    W_dealt = s.warp_sum[32];
+    if (!__syncthreads_or(tid < N && s.load[tid] * N > W_dealt + W_cut)) break;
+    rounds = 0;
+  }
   __syncthreads();
-  for (int i = tid; i <= N; i += kPlanThreads) plan.piece_begin[i] = s.begin[i];
-  for (int u = tid; u < D; u += kPlanThreads) {
+  const int D = rounds * N, M = U - D;
+  // What each CTA takes of the cut part: up to the mean; with nothing dealt, equal shares for as many as are worth it.
+  if (rounds) {
+    const int64_t room = tid < N ? max((int64_t)0, (W_dealt + W_cut) / N + 1 - s.load[tid]) : 0;
+    const int64_t room_before = scan64(room, s.warp_sum), rooms = s.warp_sum[32];
+    if (tid < N) s.load[tid] = (int64_t)((double)W_cut * (double)room_before / (double)rooms);
+  } else {
+    const int64_t takers = max((int64_t)1, min((int64_t)N, W_cut / (kMinJobs + kPieceCost)));
+    if (tid < N) s.load[tid] = W_cut * min((int64_t)tid, takers) / takers;
+  }
+  if (tid == 0) s.load[N] = W_cut;
+  __syncthreads();
+  // CTA tid takes the units that meet [from, to); its list has room for all of them
+  const bool taker = tid < N && s.load[tid] < s.load[tid + 1];
+  const int64_t from = taker ? s.load[tid] : 0, to = taker ? s.load[tid + 1] : 0;
+  auto at_unit = [&](int j) { return before[j]; };
+  const int j_first = taker ? last_at(M, from, at_unit) : 0, j_end = taker ? last_at(M, to - 1, at_unit) + 1 : 0;
+  const int cut_before = (int)scan64(j_end - j_first, s.warp_sum);
+  if (tid < N) s.begin[tid] = tid * rounds + cut_before;
+  __syncthreads();
+  for (int u = tid; u < D; u += nt) {
     Piece p;
     p.tile_hi = describe(u, p);
     p.tile_lo = 0;
     p.slot = -1;
     plan.pieces[s.begin[u % N] + u / N] = p;
   }
-  int k = tid < N ? s.begin[tid] + rounds : 0;
-  walk([&](Piece& p, int n, int j) {
+  if (tid >= N) return;
+  auto cut_at = [&](int64_t x, int64_t u0, int n, int per_tile) -> int {   // the key tile of a unit (u0 < x < its end) at which a cut at x falls
+    const int t = x <= u0 + kPieceCost ? 0 : (int)((x - u0 - kPieceCost + per_tile - 1) / per_tile);
+    return t < kSnap ? 0 : n - t < kSnap ? n : t;
+  };
+  int k = s.begin[tid] + rounds;
+  for (int j = j_first; j < j_end; ++j) {
+    Piece p;
+    const int64_t u0 = before[j], u1 = before[j + 1];
+    const int n = describe(D + j, p), per_tile = p.n_pos > a.bmp ? 2 : 1;
+    p.tile_lo = from <= u0 ? 0 : cut_at(from, u0, n, per_tile);
+    p.tile_hi = to >= u1 ? n : cut_at(to, u0, n, per_tile);
+    if (!(p.tile_lo < p.tile_hi || (n == 0 && u0 >= from))) continue;
     p.slot = -1;
     if (p.tile_lo > 0 || p.tile_hi < n) {
       p.slot = 2 * tid + (p.tile_lo == 0);     // (a CTA has one piece that begins inside a unit, and one that only ends there)
       plan.part_id[p.slot] = p.id;
-      if (p.tile_lo == 0) {
-        int lo = tid, hi = N - 1;              // the last CTA whose share begins before the unit's end
-        while (lo < hi) {
-          const int mid = (lo + hi + 1) >> 1;
-          if (s.load[mid] < s.before[j + 1]) lo = mid; else hi = mid - 1;
-        }
-        plan.merge[atomicAdd(plan.n_merge, 1)] = MergeUnit{p.row0, p.n_pos, p.unit, p.id, tid, lo, 0, 0};
+      if (p.tile_lo == 0) {                    // up to the last CTA whose share begins before the unit's end
+        const int last = last_at(N, u1 - 1, [&](int i) { return s.load[i]; });
+        plan.merge[atomicAdd(plan.n_merge, 1)] = MergeUnit{p.row0, p.n_pos, p.unit, p.id, tid, last, 0, 0};
       }
     }
     plan.pieces[k++] = p;
-  });
+  }
+  plan.piece_begin[tid] = s.begin[tid];
+  plan.piece_end[tid] = k;
 }
 
 // ---- attention ----------------------------------------------------------------------------------------
-__device__ __forceinline__ uint64_t desc128(uint32_t saddr, uint32_t lbo) { return smem_desc_sw(saddr, lbo, 1024, 2); }
-// D (TMEM) += A (TMEM: two bf16 per column, lane = row) B (shared memory)
-__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// Descriptors in two words: between the steps of a product only the address in the lower one moves.
+__device__ __forceinline__ uint2 desc128(uint32_t saddr, uint32_t lbo) {
+  const uint64_t d = smem_desc_sw(saddr, lbo, 1024, 2);
+  return make_uint2((uint32_t)d, (uint32_t)(d >> 32));
+}
+// D (TMEM) += A B, both from shared memory; and with A from TMEM (two bf16 per column, lane = row)
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint2 a, uint2 b, uint32_t a_off, uint32_t b_off, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      "{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %6, 0;\nmov.b64 a, {%1, %2};\nmov.b64 b, {%3, %4};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n}" ::"r"(d_tmem),
+      "r"(a.x + (a_off >> 4)), "r"(a.y), "r"(b.x + (b_off >> 4)), "r"(b.y), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint2 b, uint32_t b_off, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p;\n.reg .b64 b;\nsetp.ne.b32 p, %5, 0;\nmov.b64 b, {%2, %3};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n}" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b.x + (b_off >> 4)), "r"(b.y), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+  return p != 0;
+}
+// a * b + c on two numbers at a time
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
 }
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile(
@@ -305,7 +351,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
                                                                   const __grid_constant__ Plan plan, const __grid_constant__ Dims d,
                                                                   const int bmp, __nv_bfloat16* __restrict__ out,
                                                                   float* __restrict__ lse, int32_t* status) {
-  chain_wait();
   extern __shared__ __align__(1024) unsigned char smem[];
   const uint32_t sbase = s_u32(smem);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kBarOff + kNumBars * 8);
@@ -313,11 +358,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
   auto bar = [&](int i) { return sbase + kBarOff + i * 8; };
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int G = d.group;
-  const int p_lo = __ldcg(plan.piece_begin + blockIdx.x), p_hi = __ldcg(plan.piece_begin + blockIdx.x + 1);
-  if (p_lo >= p_hi) return;
-
   if (tid == 0) {
-    for (int i = 0; i < kNumBars; ++i) mbar_init(bar(i), i >= kPFull && i < kPFull + 2 ? 128 : 1);
+    for (int i = 0; i < kNumBars; ++i) mbar_init(bar(i), i >= kPFull && i < kPFull + 4 ? 128 : 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -328,6 +370,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  chain_wait();                                // (what is above touches nothing but the block's own memory)
+  const int p_lo = __ldcg(plan.piece_begin + blockIdx.x), p_hi = __ldcg(plan.piece_end + blockIdx.x);
   const uint32_t tmem = *tmem_slot;            // S / P of the groups: columns 0, 128; their O: 256, 384
 
   auto load_piece = [&](int i) -> Piece {
@@ -412,6 +456,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
     } else if (warp == 8) {
       // ================================ MMA issuer ================================
       const uint32_t idesc_s = instr_desc_mn(128, 128, false), idesc_o = instr_desc_mn(128, 128, true);
+      const uint2 q_desc = desc128(sbase, 16), k_desc = desc128(sbase + kRingOff, 16), v_desc = desc128(sbase + kRingOff, kBlk);
       unsigned job = 0, tile = 0, fill = 0, n_p[2] = {0, 0};
       // the P V that is still to be issued
       bool wait_pv = false, pv_first = false, pv_free = false, pv_last = false;
@@ -420,18 +465,27 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
       auto issue_pv = [&]() {
         const int slot = pv_item % kRing;
         mbar_wait(bar(kFull + slot), (pv_item / kRing) & 1, abort_flag, status, d.wait_ns);
-        mbar_wait(bar(kPFull + pv_g), (pv_g ? n_p[1] : n_p[0]) & 1, abort_flag, status, d.wait_ns);
+        const unsigned phase = (pv_g ? n_p[1] : n_p[0]) & 1;
         if (pv_g) ++n_p[1]; else ++n_p[0];
-        tc_fence_after();
-        if (lane == 0) {
-          const uint32_t v = sbase + kRingOff + slot * kSlot;
+        const uint2 v = make_uint2(v_desc.x + slot * (kSlot >> 4), v_desc.y);
+        const uint32_t d_o = tmem + 256u + pv_g * 128u, a_p = tmem + pv_g * 128u;
 #pragma unroll
-          for (int ks = 0; ks < 8; ++ks)       // 16 keys per step: 8 columns of P
-            tc_mma_ts(tmem + 256u + pv_g * 128u, tmem + pv_g * 128u + ks * 8u, desc128(v + ks * 2048, kBlk), idesc_o, (!pv_first || ks) ? 1u : 0u);
-          if (pv_free) tc_commit(bar(kEmpty + slot));
-          if (pv_last) tc_commit(bar(kOFull + pv_g));
+        for (int h = 0; h < 2; ++h) {
+          mbar_wait(bar(kPFull + 2 * pv_g + h), phase, abort_flag, status, d.wait_ns);
+          tc_fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {      // 16 keys per step: 8 columns of P
+              const int ks = 4 * h + k;
+              mma_ts(d_o, a_p + ks * 8u, v, ks * 2048, idesc_o, ks ? 1u : pv_first ? 0u : 1u);
+            }
+            if (h == 1) {
+              if (pv_free) tc_commit(bar(kEmpty + slot));
+              if (pv_last) tc_commit(bar(kOFull + pv_g));
+            }
+          }
+          __syncwarp();
         }
-        __syncwarp();
       };
       for (int i = p_lo; i < p_hi; ++i) {
         const Piece p = load_piece(i);
@@ -443,12 +497,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
           if (t == 0) mbar_wait(bar(kQFull + qb), (qf >> 1) & 1, abort_flag, status, d.wait_ns);
           mbar_wait(bar(kFull + slot), (k_item / kRing) & 1, abort_flag, status, d.wait_ns);
           tc_fence_after();
-          if (lane == 0) {
-            const uint32_t q = sbase + qb * kSlot, k = sbase + kRingOff + slot * kSlot;
+          if (elect_one()) {
+            const uint2 q = make_uint2(q_desc.x + qb * (kSlot >> 4), q_desc.y), k = make_uint2(k_desc.x + slot * (kSlot >> 4), k_desc.y);
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks)
-              tc_mma(tmem + g * 128u, desc128(q + (ks >> 2) * kBlk + (ks & 3) * 32, 16), desc128(k + (ks >> 2) * kBlk + (ks & 3) * 32, 16), idesc_s,
-                     ks ? 1u : 0u);
+              mma_ss(tmem + g * 128u, q, k, (ks >> 2) * kBlk + (ks & 3) * 32, (ks >> 2) * kBlk + (ks & 3) * 32, idesc_s, ks ? 1u : 0u);
             tc_commit(bar(kSFull + g));
             if (qt == nq - 1) tc_commit(bar(kEmpty + slot));
             if (t == n - 1) tc_commit(bar(kQEmpty + qb));
@@ -495,64 +548,80 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
         if (warp_on) {
           tc_fence_after();
           float s[kTile];
-          {
-            uint32_t* r0p = reinterpret_cast<uint32_t*>(s);
-            uint32_t* r1p = r0p + 64;
-            RTP_TMEM_LD64(r0p, tmem_s);
-            RTP_TMEM_LD64(r1p, tmem_s + 64);
-            tc_wait_ld();
-          }
-          if (n_base + kTile - 1 > lim || (local && n_base <= pos - d.window)) {
-            const int hi = lim - n_base, lo = local ? pos - d.window - n_base : -1, sink = local ? d.n_sink - n_base : 0;
+          uint32_t* s_lo = reinterpret_cast<uint32_t*>(s);
+          uint32_t* s_hi = s_lo + 64;
+          RTP_TMEM_LD64(s_lo, tmem_s);
+          tc_wait_ld();
+          RTP_TMEM_LD64(s_hi, tmem_s + 64);
+          const bool masked = n_base + kTile - 1 > lim || (local && n_base <= pos - d.window);
+          const int hi = lim - n_base, lo = local ? pos - d.window - n_base : -1, sink = local ? d.n_sink - n_base : 0;
+          if (masked) {
 #pragma unroll
-            for (int e = 0; e < kTile; ++e)
+            for (int e = 0; e < 64; ++e)
               if (!(e <= hi && (e > lo || e < sink))) s[e] = -INFINITY;
           }
-          float tmax;
-          {
-            float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
+          float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
 #pragma unroll
-            for (int e = 4; e < kTile; e += 4) {
-              t0 = fmaxf(t0, s[e]); t1 = fmaxf(t1, s[e + 1]); t2 = fmaxf(t2, s[e + 2]); t3 = fmaxf(t3, s[e + 3]);
-            }
-            tmax = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * sc2;
+          for (int e = 4; e + 8 <= 64; e += 8) {
+            t0 = fmaxf(fmaxf(t0, s[e]), s[e + 1]); t1 = fmaxf(fmaxf(t1, s[e + 2]), s[e + 3]);
+            t2 = fmaxf(fmaxf(t2, s[e + 4]), s[e + 5]); t3 = fmaxf(fmaxf(t3, s[e + 6]), s[e + 7]);
           }
+          t0 = fmaxf(fmaxf(t0, s[60]), s[61]); t1 = fmaxf(fmaxf(t1, s[62]), s[63]);
+          tc_wait_ld();
+          if (masked) {
+#pragma unroll
+            for (int e = 64; e < kTile; ++e)
+              if (!(e <= hi && (e > lo || e < sink))) s[e] = -INFINITY;
+          }
+#pragma unroll
+          for (int e = 64; e < kTile; e += 8) {
+            t0 = fmaxf(fmaxf(t0, s[e]), s[e + 1]); t1 = fmaxf(fmaxf(t1, s[e + 2]), s[e + 3]);
+            t2 = fmaxf(fmaxf(t2, s[e + 4]), s[e + 5]); t3 = fmaxf(fmaxf(t3, s[e + 6]), s[e + 7]);
+          }
+          const float tmax = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * sc2;
           // the reference is raised, and O and l scaled, only when a maximum exceeds it by more than 2^8 (any reference gives the same
           // quotient); the group's P V of before is complete, since S was issued behind it
           const bool raise = tmax > m_ref + 8.0f;
-          if (x >= 2 && __any_sync(0xffffffffu, raise)) {
-            const float f = raise ? ((m_ref == -INFINITY) ? 0.f : fast_ex2(m_ref - tmax)) : 1.f;
+          if (__any_sync(0xffffffffu, raise)) {
+            if (x >= 2) {
+              const float f = raise ? ((m_ref == -INFINITY) ? 0.f : fast_ex2(m_ref - tmax)) : 1.f;
+#pragma unroll 1
+              for (int c4 = 0; c4 < 4; ++c4) {
+                uint32_t r[32];
+                RTP_TMEM_LD32(r, tmem_o + c4 * 32);
+                tc_wait_ld();
 #pragma unroll
-            for (int c4 = 0; c4 < 4; ++c4) {
-              uint32_t r[32];
-              RTP_TMEM_LD32(r, tmem_o + c4 * 32);
-              tc_wait_ld();
-#pragma unroll
-              for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
-              RTP_TMEM_ST32(tmem_o + c4 * 32, r);
+                for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
+                RTP_TMEM_ST32(tmem_o + c4 * 32, r);
+              }
+              l_run *= f;
             }
-            l_run *= f;
+            if (raise) m_ref = tmax;
           }
-          if (raise) m_ref = tmax;
           const float mb = (m_ref == -INFINITY) ? 0.f : m_ref;
-          float rs[4] = {0.f, 0.f, 0.f, 0.f};
+          const float2 sc22 = make_float2(sc2, sc2), mb2 = make_float2(-mb, -mb);
+          float2 rs0 = make_float2(0.f, 0.f), rs1 = rs0;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {        // P is rounded to bf16 for the MMA; the sum is of the 32-bit values
             uint32_t pk[32];
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-              const float p0 = fast_ex2(fmaf(s[h * 64 + 2 * e], sc2, -mb)), p1 = fast_ex2(fmaf(s[h * 64 + 2 * e + 1], sc2, -mb));
-              rs[e & 3] += p0 + p1;
-              const __nv_bfloat162 v = __floats2bfloat162_rn(p0, p1);
+              const float2 z = fma2(make_float2(s[h * 64 + 2 * e], s[h * 64 + 2 * e + 1]), sc22, mb2);
+              const float2 pr = make_float2(fast_ex2(z.x), fast_ex2(z.y));
+              if (e & 1) rs1 = add2(rs1, pr); else rs0 = add2(rs0, pr);
+              const __nv_bfloat162 v = __floats2bfloat162_rn(pr.x, pr.y);
               pk[e] = *reinterpret_cast<const uint32_t*>(&v);
             }
             RTP_TMEM_ST32(tmem_s + h * 32, pk);
+            tc_wait_st();
+            tc_fence_before();
+            mbar_arrive(bar(kPFull + 2 * grp + h));
           }
-          l_run += (rs[0] + rs[1]) + (rs[2] + rs[3]);
-          tc_wait_st();
-          tc_fence_before();
+          l_run += (rs0.x + rs0.y) + (rs1.x + rs1.y);
+        } else {
+          mbar_arrive(bar(kPFull + 2 * grp));
+          mbar_arrive(bar(kPFull + 2 * grp + 1));
         }
-        mbar_arrive(bar(kPFull + grp));
       }
       // ---- end of the piece ----
       const bool mine = x0 < jobs;             // this group has an accumulator
@@ -711,17 +780,19 @@ Plan carve(void* ws, int G, int n_units, int64_t n_chunks, int64_t R, int sm_cou
     return r;
   };
   p.n_merge = reinterpret_cast<int32_t*>(take(4));
-  p.piece_begin = reinterpret_cast<int32_t*>(take((size_t)(p.n_ctas + 1) * 4));
+  p.piece_begin = reinterpret_cast<int32_t*>(take((size_t)p.n_ctas * 4));
+  p.piece_end = reinterpret_cast<int32_t*>(take((size_t)p.n_ctas * 4));
   p.part_id = reinterpret_cast<int32_t*>(take((size_t)p.n_ctas * 8));
   p.merge = reinterpret_cast<MergeUnit*>(take((size_t)p.n_ctas * sizeof(MergeUnit)));
   p.pieces = reinterpret_cast<Piece*>(take((size_t)(units + p.n_ctas) * sizeof(Piece)));
+  p.before = reinterpret_cast<int64_t*>(take((size_t)(units + 1) * 8));
   p.ml = reinterpret_cast<float*>(take((size_t)2 * p.n_ctas * p.slot_rows * 8));
   p.o = reinterpret_cast<float*>(take((size_t)2 * p.n_ctas * p.slot_rows * kHeadDim * 4));
   *bytes = off;
   return p;
 }
 
-size_t plan_smem(int64_t n_chunks) { return ((sizeof(PlanShared) + 15) & ~(size_t)15) + (size_t)n_chunks * sizeof(int4); }
+size_t plan_smem(int64_t n_chunks) { return ((sizeof(PlanShared) + 15) & ~(size_t)15) + (size_t)n_chunks * (sizeof(int4) + sizeof(int2)); }
 
 }  // namespace
 
@@ -765,7 +836,7 @@ cudaError_t launch_attn_chunks(const CacheView& cv, const CacheView& lv, const D
   for (int i = 0; i < ch.n; ++i) ring = ring || (hu.flags[i] & kLocalPool);
   const ChunkArgs a = {chunk_seq, chunk_start, row_offsets, (int32_t)n_chunks, d.group, bmp, R,
                        ring ? (int64_t)lv.ring_pages * kPage : 0, ring ? (int64_t)lv.max_pages * kPage : 0};
-  (void)launch_chained(plan_kernel, dim3(1), dim3(kPlanThreads), plan_smem(n_chunks), st, a, cv, hu, plan, d.n_sink, d.window, status);
+  (void)launch_chained(plan_kernel, dim3(1), dim3(plan.n_ctas <= 512 ? 512 : kPlanThreads), plan_smem(n_chunks), st, a, cv, hu, plan, d.n_sink, d.window, status);
   (void)launch_chained(attn_chunks_kernel, dim3(plan.n_ctas), dim3(kThreads), (size_t)kSmem, st, maps, cv, lv, hu, plan, d, bmp, out, lse, status);
   const int merge_rows = (int)std::min<int64_t>(R, 2 * bmp) * d.group;
   (void)launch_chained(merge_kernel, dim3(plan.n_ctas, (unsigned)std::min(8, (merge_rows + kMergeWarps - 1) / kMergeWarps)), dim3(kMergeWarps * 32), 0, st,
