@@ -60,15 +60,16 @@ struct HeadUnits {
 struct __align__(16) Piece {
   int32_t row0, pos0, n_pos, seq;              // rows row0 .. of q at positions pos0 ..
   int32_t unit, kt_first, n_sink_tiles, n_keys;
-  int32_t tile_lo, tile_hi, slot, id;          // slot: of its partial result, or -1; id: number of the unit
+  int32_t tile_lo, tile_hi, slot, id;          // slot: of its partial result, or one of the two below; id: number of the unit
 };
+constexpr int kWhole = -1, kNothing = -2;
 struct __align__(16) MergeUnit {
   int32_t row0, n_pos, unit, id;
   int32_t first_cta, last_cta, pad0, pad1;
 };
 struct Plan {                                  // where things lie in the workspace
   int32_t* n_merge;
-  int32_t *piece_begin, *piece_end;            // [n_ctas]
+  int32_t* piece_begin;                        // [n_ctas + 1]
   int32_t* part_id;                            // [2 n_ctas]: unit of the partial result in a slot, or -1
   MergeUnit* merge;                            // [n_ctas]
   Piece* pieces;
@@ -89,6 +90,7 @@ struct ChunkArgs {
 // Costs are in jobs (a key tile of a Q tile); a piece has a start and an end beside them.
 constexpr int kPieceCost = 3;
 constexpr int kMinJobs = 6;                    // a piece of its own (and a merge) has to be worth it
+constexpr int kMinShare = 24;                  // jobs of a CTA's share of what is not dealt
 constexpr int kSnap = 3;                       // key tiles that are not cut off
 constexpr int kPlanUnits = 1024;               // units whose costs lie in shared memory
 
@@ -96,7 +98,7 @@ struct PlanShared {
   int64_t warp_sum[33];
   int64_t load[1024 + 1];                      // jobs dealt to each CTA, then the cuts
   int64_t before[kPlanUnits + 1];
-  int32_t begin[1024 + 1];
+  int32_t begin[1024], first[1024];            // of each CTA: pairs in front of its own, its first unit
 };
 
 // Exclusive sum over the block; warp_sum[32]: the total.
@@ -177,7 +179,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
   const int64_t total_units = s.warp_sum[32];
   if (total_units > plan.max_units) {          // offsets that run back and forth: nothing is done
     if (tid == 0) set_status(status, RTP_ERR_INVALID);
-    for (int i = tid; i < N; i += nt) plan.piece_begin[i] = plan.piece_end[i] = 0;
+    for (int i = tid; i <= N; i += nt) plan.piece_begin[i] = 0;
     return;
   }
   for (int c = c0; c < c1; ++c) {
@@ -208,7 +210,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     return p.n_sink_tiles + n_all - p.kt_first;
   };
   // Costs: the dealt units' go to their CTAs, the others' into a list.
-  int rounds = U >= 2 * N ? U / N - 1 : 0;
+  int rounds = U / N;
   int64_t* before = s.before;
   int64_t W_dealt = 0, W_cut = 0;
   for (;;) {
@@ -234,11 +236,17 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     }
     if (tid == 0) before[M] = W_cut;
     if (rounds == 0) break;
-    // Whole units only where no CTA gets more than its share of them: a few that cost more than the others are cut instead.
+    // Whole units only where no CTA gets more than its share of them (a few that cost more than the others are cut instead), and one
+    // round less where the rest would be cut into crumbs.
     scan64(tid < N ? s.load[tid] : 0, s.warp_sum);
     W_dealt = s.warp_sum[32];
-    if (!__syncthreads_or(tid < N && s.load[tid] * N > W_dealt + W_cut)) break;
-    rounds = 0;
+    const bool uneven = __syncthreads_or(tid < N && s.load[tid] * N > W_dealt + W_cut);
+    const bool crumbs = W_cut > 0 && W_cut < (int64_t)N * kMinShare;
+    if (!uneven && !(crumbs && rounds == U / N)) break;
+    rounds = uneven ? 0 : rounds - 1;
+    __syncthreads();
+    for (int i = tid; i < N; i += nt) s.load[i] = 0;
+    __syncthreads();
   }
   __syncthreads();
   const int D = rounds * N, M = U - D;
@@ -248,52 +256,55 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     const int64_t room_before = scan64(room, s.warp_sum), rooms = s.warp_sum[32];
     if (tid < N) s.load[tid] = (int64_t)((double)W_cut * (double)room_before / (double)rooms);
   } else {
-    const int64_t takers = max((int64_t)1, min((int64_t)N, W_cut / (kMinJobs + kPieceCost)));
-    if (tid < N) s.load[tid] = W_cut * min((int64_t)tid, takers) / takers;
+    const int takers = max(1, (int)min((int64_t)N, W_cut / (kMinJobs + kPieceCost)));
+    if (tid < N) s.load[tid] = tid < takers ? (int64_t)((double)W_cut * tid / takers) : W_cut;
   }
   if (tid == 0) s.load[N] = W_cut;
   __syncthreads();
-  // CTA tid takes the units that meet [from, to); its list has room for all of them
+  // CTA i takes the units j that meet [load[i], load[i + 1])
   const bool taker = tid < N && s.load[tid] < s.load[tid + 1];
-  const int64_t from = taker ? s.load[tid] : 0, to = taker ? s.load[tid + 1] : 0;
   auto at_unit = [&](int j) { return before[j]; };
-  const int j_first = taker ? last_at(M, from, at_unit) : 0, j_end = taker ? last_at(M, to - 1, at_unit) + 1 : 0;
-  const int cut_before = (int)scan64(j_end - j_first, s.warp_sum);
-  if (tid < N) s.begin[tid] = tid * rounds + cut_before;
+  const int j_first = taker ? last_at(M, s.load[tid], at_unit) : 0, j_end = taker ? last_at(M, s.load[tid + 1] - 1, at_unit) + 1 : 0;
+  const int cut_before = (int)scan64(j_end - j_first, s.warp_sum), pairs = (int)s.warp_sum[32];
+  if (tid < N) {
+    s.begin[tid] = cut_before;
+    s.first[tid] = j_first;
+    plan.piece_begin[tid] = tid * rounds + cut_before;
+  }
+  if (tid == 0) plan.piece_begin[N] = N * rounds + pairs;
   __syncthreads();
   for (int u = tid; u < D; u += nt) {
     Piece p;
     p.tile_hi = describe(u, p);
     p.tile_lo = 0;
-    p.slot = -1;
-    plan.pieces[s.begin[u % N] + u / N] = p;
+    p.slot = kWhole;
+    plan.pieces[(u % N) * rounds + s.begin[u % N] + u / N] = p;
   }
-  if (tid >= N) return;
-  auto cut_at = [&](int64_t x, int64_t u0, int n, int per_tile) -> int {   // the key tile of a unit (u0 < x < its end) at which a cut at x falls
-    const int t = x <= u0 + kPieceCost ? 0 : (int)((x - u0 - kPieceCost + per_tile - 1) / per_tile);
+  // the key tile of a unit (u0 < x < its end) at which a cut at x falls
+  auto cut_at = [&](int64_t x, int64_t u0, int n, int per_tile) -> int {
+    const int t = x <= u0 + kPieceCost ? 0 : (int)((x - u0 - kPieceCost + per_tile - 1) >> (per_tile - 1));
     return t < kSnap ? 0 : n - t < kSnap ? n : t;
   };
-  int k = s.begin[tid] + rounds;
-  for (int j = j_first; j < j_end; ++j) {
+  for (int q = tid; q < pairs; q += nt) {      // a thread per (CTA, unit) pair
+    const int i = last_at(N, q, [&](int c) { return s.begin[c]; }), j = s.first[i] + q - s.begin[i];
     Piece p;
-    const int64_t u0 = before[j], u1 = before[j + 1];
+    const int64_t from = s.load[i], to = s.load[i + 1], u0 = before[j], u1 = before[j + 1];
     const int n = describe(D + j, p), per_tile = p.n_pos > a.bmp ? 2 : 1;
     p.tile_lo = from <= u0 ? 0 : cut_at(from, u0, n, per_tile);
     p.tile_hi = to >= u1 ? n : cut_at(to, u0, n, per_tile);
-    if (!(p.tile_lo < p.tile_hi || (n == 0 && u0 >= from))) continue;
-    p.slot = -1;
-    if (p.tile_lo > 0 || p.tile_hi < n) {
-      p.slot = 2 * tid + (p.tile_lo == 0);     // (a CTA has one piece that begins inside a unit, and one that only ends there)
+    p.slot = kWhole;
+    if (p.tile_lo >= p.tile_hi && !(n == 0 && u0 >= from)) {
+      p.slot = kNothing;                       // (less than is cut off of a unit: its neighbours have it)
+    } else if (p.tile_lo > 0 || p.tile_hi < n) {
+      p.slot = 2 * i + (p.tile_lo == 0);       // (a CTA has one piece that begins inside a unit, and one that only ends there)
       plan.part_id[p.slot] = p.id;
       if (p.tile_lo == 0) {                    // up to the last CTA whose share begins before the unit's end
-        const int last = last_at(N, u1 - 1, [&](int i) { return s.load[i]; });
-        plan.merge[atomicAdd(plan.n_merge, 1)] = MergeUnit{p.row0, p.n_pos, p.unit, p.id, tid, last, 0, 0};
+        const int last = last_at(N, u1 - 1, [&](int c) { return s.load[c]; });
+        plan.merge[atomicAdd(plan.n_merge, 1)] = MergeUnit{p.row0, p.n_pos, p.unit, p.id, i, last, 0, 0};
       }
     }
-    plan.pieces[k++] = p;
+    plan.pieces[(i + 1) * rounds + q] = p;
   }
-  plan.piece_begin[tid] = s.begin[tid];
-  plan.piece_end[tid] = k;
 }
 
 // ---- attention ----------------------------------------------------------------------------------------
@@ -316,6 +327,12 @@ __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint2 b
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n}" ::"r"(d_tmem),
       "r"(a_tmem), "r"(b.x + (b_off >> 4)), "r"(b.y), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+// A wait that is usually over already: asked once without parking the thread.
+__device__ __forceinline__ void wait_for(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status, unsigned long long limit_ns) {
+  uint32_t ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  if (!ok) mbar_wait(bar, parity, abort_flag, status, limit_ns);
 }
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
@@ -371,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
   __syncthreads();
   tc_fence_after();
   chain_wait();                                // (what is above touches nothing but the block's own memory)
-  const int p_lo = __ldcg(plan.piece_begin + blockIdx.x), p_hi = __ldcg(plan.piece_end + blockIdx.x);
+  const int p_lo = __ldcg(plan.piece_begin + blockIdx.x), p_hi = __ldcg(plan.piece_begin + blockIdx.x + 1);
   const uint32_t tmem = *tmem_slot;            // S / P of the groups: columns 0, 128; their O: 256, 384
 
   auto load_piece = [&](int i) -> Piece {
@@ -389,20 +406,31 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
     if (warp == 9 || warp == 10) {
       // ================================ loaders: Q and K, V ================================
       const bool is_v = warp == 10;
-      unsigned fill = 0, item = is_v ? 1 : 0, n_aux = 0;
+      unsigned fill = 0, n_aux = 0;
+      int slot = is_v ? 1 : 0, phase = 1;      // (a wait for the phase before the first passes at once)
+      bool drop = d.wait_test && !is_v;        // (the test hook drops the first signal)
       for (int i = p_lo; i < p_hi; ++i) {
         const Piece p = load_piece(i);
+        if (p.slot == kNothing) continue;
         const int flags = hu.flags[p.unit], kvh = hu.head[p.unit];
         const bool local_pool = flags & kLocalPool;
         const CacheView& view = local_pool ? lv : cv;
         const CUtensorMap* map = is_v ? (local_pool ? &maps.lv : &maps.v) : (local_pool ? &maps.lk : &maps.k);
-        const int kslot = view.kv_slot[kvh];
+        const int kslot = view.kv_slot[kvh], n_kv = view.n_kv;
         const int64_t bt_base = (int64_t)p.seq * view.max_pages;
+        // Row in the pool of the pages of 16 tiles (lane: tile base + lane / 2, first or second page; -1: no key there), looked up while
+        // the tiles before them are loaded.
+        auto tile_of = [&](int x) { return x < p.n_sink_tiles ? x : p.kt_first + (x - p.n_sink_tiles); };
+        auto look_up = [&](int base) {
+          const int y = base + (lane >> 1), page = 2 * tile_of(y) + (lane & 1);
+          return y < p.tile_hi && page * kPage < p.n_keys ? (safe_phys(view, bt_base + page_entry(view, page), status) * n_kv + kslot) * kPage : -1;
+        };
+        int next = look_up(p.tile_lo), rows = 0;
         if (!is_v && p.tile_lo < p.tile_hi) {
           for (int t = 0; t < (p.n_pos > bmp ? 2 : 1); ++t, ++fill) {
             const int b = fill & 1;
-            if (fill >= 2) mbar_wait(bar(kQEmpty + b), ((fill >> 1) - 1) & 1, abort_flag, status, d.wait_ns);
-            if (lane == 0) {
+            if (fill >= 2) wait_for(bar(kQEmpty + b), ((fill >> 1) - 1) & 1, abort_flag, status, d.wait_ns);
+            if (elect_one()) {
               mbar_expect_tx(bar(kQFull + b), (uint32_t)(G * bmp) * 256u);
               tma_load_3d(sbase + b * kSlot, &maps.q, 0, kvh * G, p.row0 + t * bmp, bar(kQFull + b));
               tma_load_3d(sbase + b * kSlot + kBlk, &maps.q, 64, kvh * G, p.row0 + t * bmp, bar(kQFull + b));
@@ -410,37 +438,31 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
             __syncwarp();
           }
         }
-        int entry = 0;                         // lane: page of tile base + lane / 2
-        for (int x = p.tile_lo; x < p.tile_hi; ++x, item += 2) {
+        for (int x = p.tile_lo; x < p.tile_hi; ++x) {
           const int rel = (x - p.tile_lo) & 15;
           if (rel == 0) {
-            const int y = x + (lane >> 1);
-            const int page = 2 * (y < p.n_sink_tiles ? y : p.kt_first + (y - p.n_sink_tiles)) + (lane & 1);
-            entry = -1;
-            if (y < p.tile_hi && page * kPage < p.n_keys) entry = safe_phys(view, bt_base + page_entry(view, page), status);
+            rows = next;
+            next = look_up(x + 16);
           }
-          const int ph0 = __shfl_sync(0xffffffffu, entry, 2 * rel), ph1 = __shfl_sync(0xffffffffu, entry, 2 * rel + 1);
-          const int kt = x < p.n_sink_tiles ? x : p.kt_first + (x - p.n_sink_tiles);
-          const int slot = item % kRing;
-          const unsigned use = item / kRing;
-          if (use >= 1) mbar_wait(bar(kEmpty + slot), (use - 1) & 1, abort_flag, status, d.wait_ns);
+          const int y0 = __shfl_sync(0xffffffffu, rows, 2 * rel), y1 = __shfl_sync(0xffffffffu, rows, 2 * rel + 1);
+          wait_for(bar(kEmpty + slot), phase, abort_flag, status, d.wait_ns);
           const uint32_t dst = sbase + kRingOff + slot * kSlot;
-          const int n_ok = p.n_keys - kt * kTile;   // keys of the tile that rows may see
+          const int n_ok = p.n_keys - tile_of(x) * kTile;   // keys of the tile that rows may see
           const bool part = is_v && n_ok < kTile;
           const uint32_t fb = part ? bar(kAux) : bar(kFull + slot);
-          if (lane == 0 && !(d.wait_test && !is_v && item == 0)) {   // (the test hook drops one signal)
-            mbar_expect_tx(fb, ph1 >= 0 ? 2 * kBlk : kBlk);
-            const int y0 = (ph0 * view.n_kv + kslot) * kPage, y1 = (ph1 * view.n_kv + kslot) * kPage;
+          if (elect_one() && !drop) {
+            mbar_expect_tx(fb, y1 >= 0 ? 2 * kBlk : kBlk);
             tma_load_2d(dst, map, 0, y0, fb);
             tma_load_2d(dst + kBlk, map, 64, y0, fb);
-            if (ph1 >= 0) {
+            if (y1 >= 0) {
               tma_load_2d(dst + kPage * 128, map, 0, y1, fb);
               tma_load_2d(dst + kBlk + kPage * 128, map, 64, y1, fb);
             }
           }
           __syncwarp();
+          drop = false;
           if (part) {                          // what lies behind the last key is not read: 0 x NaN is no 0
-            mbar_wait(bar(kAux), n_aux & 1, abort_flag, status, d.wait_ns);
+            wait_for(bar(kAux), n_aux & 1, abort_flag, status, d.wait_ns);
             ++n_aux;
             unsigned char* v = smem + kRingOff + slot * kSlot;
             for (int z = n_ok * 8 + lane; z < kTile * 8; z += 32) {
@@ -451,27 +473,31 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(kFull + slot));
           }
+          slot += 2;
+          if (slot >= kRing) {
+            slot -= kRing;
+            phase ^= 1;
+          }
         }
       }
     } else if (warp == 8) {
       // ================================ MMA issuer ================================
       const uint32_t idesc_s = instr_desc_mn(128, 128, false), idesc_o = instr_desc_mn(128, 128, true);
       const uint2 q_desc = desc128(sbase, 16), k_desc = desc128(sbase + kRingOff, 16), v_desc = desc128(sbase + kRingOff, kBlk);
-      unsigned job = 0, tile = 0, fill = 0, n_p[2] = {0, 0};
+      unsigned job = 0, fill = 0, n_p = 0;     // n_p: phase bit of each group's P
+      int slot = 0, phase = 0;                 // of the next tile's K; its V is in the slot behind
       // the P V that is still to be issued
-      bool wait_pv = false, pv_first = false, pv_free = false, pv_last = false;
-      int pv_g = 0;
-      unsigned pv_item = 0;
+      bool wait_pv = false, pv_first = false, pv_new = false, pv_free = false, pv_last = false;
+      int pv_g = 0, pv_slot = 0, pv_phase = 0;
       auto issue_pv = [&]() {
-        const int slot = pv_item % kRing;
-        mbar_wait(bar(kFull + slot), (pv_item / kRing) & 1, abort_flag, status, d.wait_ns);
-        const unsigned phase = (pv_g ? n_p[1] : n_p[0]) & 1;
-        if (pv_g) ++n_p[1]; else ++n_p[0];
-        const uint2 v = make_uint2(v_desc.x + slot * (kSlot >> 4), v_desc.y);
+        if (pv_new) wait_for(bar(kFull + pv_slot), pv_phase, abort_flag, status, d.wait_ns);
+        const unsigned par = (n_p >> pv_g) & 1u;
+        n_p ^= 1u << pv_g;
+        const uint2 v = make_uint2(v_desc.x + pv_slot * (kSlot >> 4), v_desc.y);
         const uint32_t d_o = tmem + 256u + pv_g * 128u, a_p = tmem + pv_g * 128u;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          mbar_wait(bar(kPFull + 2 * pv_g + h), phase, abort_flag, status, d.wait_ns);
+          wait_for(bar(kPFull + 2 * pv_g + h), par, abort_flag, status, d.wait_ns);
           tc_fence_after();
           if (elect_one()) {
 #pragma unroll
@@ -480,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
               mma_ts(d_o, a_p + ks * 8u, v, ks * 2048, idesc_o, ks ? 1u : pv_first ? 0u : 1u);
             }
             if (h == 1) {
-              if (pv_free) tc_commit(bar(kEmpty + slot));
+              if (pv_free) tc_commit(bar(kEmpty + pv_slot));
               if (pv_last) tc_commit(bar(kOFull + pv_g));
             }
           }
@@ -489,13 +515,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
       };
       for (int i = p_lo; i < p_hi; ++i) {
         const Piece p = load_piece(i);
+        if (p.slot == kNothing) continue;
         const int n = p.tile_hi - p.tile_lo, nq = p.n_pos > bmp ? 2 : 1, jobs = n * nq;
         for (int x = 0; x < jobs; ++x, ++job) {
           const int g = job & 1, qt = nq == 2 ? (x & 1) : 0, t = nq == 2 ? x >> 1 : x;
-          const unsigned k_item = 2 * (tile + t), qf = fill + qt;
-          const int slot = k_item % kRing, qb = qf & 1;
-          if (t == 0) mbar_wait(bar(kQFull + qb), (qf >> 1) & 1, abort_flag, status, d.wait_ns);
-          mbar_wait(bar(kFull + slot), (k_item / kRing) & 1, abort_flag, status, d.wait_ns);
+          const unsigned qf = fill + qt;
+          const int qb = qf & 1;
+          if (t == 0) wait_for(bar(kQFull + qb), (qf >> 1) & 1, abort_flag, status, d.wait_ns);
+          if (qt == 0) wait_for(bar(kFull + slot), phase, abort_flag, status, d.wait_ns);
           tc_fence_after();
           if (elect_one()) {
             const uint2 q = make_uint2(q_desc.x + qb * (kSlot >> 4), q_desc.y), k = make_uint2(k_desc.x + slot * (kSlot >> 4), k_desc.y);
@@ -510,12 +537,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
           if (wait_pv) issue_pv();
           wait_pv = true;
           pv_g = g;
-          pv_item = k_item + 1;
           pv_first = x < 2;
+          pv_new = qt == 0;
           pv_free = qt == nq - 1;
           pv_last = x + 2 >= jobs;
+          pv_slot = slot + 1 == kRing ? 0 : slot + 1;
+          pv_phase = phase ^ (slot + 1 == kRing);
+          if (qt == nq - 1) {                  // two slots on
+            slot += 2;
+            if (slot >= kRing) {
+              slot -= kRing;
+              phase ^= 1;
+            }
+          }
         }
-        tile += n;
         if (n > 0) fill += nq;
       }
       if (wait_pv) issue_pv();
@@ -532,6 +567,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
     unsigned job0 = 0, n_s = 0, n_o = 0;
     for (int i = p_lo; i < p_hi; ++i) {
       const Piece p = load_piece(i);
+      if (p.slot == kNothing) continue;
       const int n = p.tile_hi - p.tile_lo, nq = p.n_pos > bmp ? 2 : 1, jobs = n * nq;
       const int x0 = jobs ? (int)((grp ^ job0) & 1) : grp;          // this group's first job; without keys, group = Q tile
       job0 += jobs;
@@ -544,7 +580,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
       for (int x = x0; x < jobs; x += 2, ++n_s) {
         const int tt = p.tile_lo + (nq == 2 ? x >> 1 : x);
         const int n_base = (tt < p.n_sink_tiles ? tt : p.kt_first + (tt - p.n_sink_tiles)) * kTile;
-        mbar_wait(bar(kSFull + grp), n_s & 1, abort_flag, status, d.wait_ns);
+        wait_for(bar(kSFull + grp), n_s & 1, abort_flag, status, d.wait_ns);
         if (warp_on) {
           tc_fence_after();
           float s[kTile];
@@ -719,31 +755,39 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
 }
 
 // ---- merge: a warp per row of a cut unit ---------------------------------------------------------------
+// The first CTA's last piece and the others' first ones, in their order.  What the first two left is requested before it is known
+// how much it counts: most units are cut once.
 constexpr int kMergeWarps = 8;
 __global__ void __launch_bounds__(kMergeWarps * 32) merge_kernel(const __grid_constant__ HeadUnits hu, const __grid_constant__ Plan plan,
-                                                                 const int G, const int bmp, const int n_q, __nv_bfloat16* __restrict__ out,
-                                                                 float* __restrict__ lse) {
+                                                                 const int G, const int bmp, const int n_q, const int rows,
+                                                                 __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
   chain_wait();
-  if ((int)blockIdx.x >= __ldcg(plan.n_merge)) return;
-  const int4* src = reinterpret_cast<const int4*>(plan.merge + blockIdx.x);
-  const int4 a = __ldcg(src), b = __ldcg(src + 1);   // row0, n_pos, unit, id; first and last CTA
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int R = a.y * G;
-  for (int y = blockIdx.y * kMergeWarps + warp; y < R; y += gridDim.y * kMergeWarps) {
+  const int lane = threadIdx.x & 31, n = __ldcg(plan.n_merge) * rows;
+  for (int item = (int)(blockIdx.x * kMergeWarps + (threadIdx.x >> 5)); item < n; item += (int)gridDim.x * kMergeWarps) {
+    const int u = item / rows, y = item - u * rows;
+    const int4* src = reinterpret_cast<const int4*>(plan.merge + u);
+    const int4 a = __ldcg(src), b = __ldcg(src + 1);   // row0, n_pos, unit, id; first and last CTA
     const int po = y / G, hs = y - po * G, qt = po / bmp, row = qt * 128 + (po - qt * bmp) * G + hs;
     const int qh = hu.head[a.z] * G + hs;
-    if (!hu.writes(a.z, qh)) continue;
-    // parts in the order of their CTAs: the first one's last piece, the others' first
+    if (po >= a.y || !hu.writes(a.z, qh)) continue;
+    auto part = [&](int slot) { return __ldcg(reinterpret_cast<const float4*>(plan.o + ((int64_t)slot * plan.slot_rows + row) * kHeadDim) + lane); };
+    const float4 o0 = part(2 * b.x + 1), o1 = part(2 * min(b.x + 1, plan.n_ctas - 1));
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int c0 = b.x; c0 <= b.y; c0 += 32) {
       const int c = c0 + lane, slot = 2 * c + (c == b.x);
-      const bool there = c <= b.y && __ldcg(plan.part_id + slot) == a.w;
       float2 ml = make_float2(-INFINITY, 0.f);
-      if (there) ml = __ldcg(reinterpret_cast<const float2*>(plan.ml) + (int64_t)slot * plan.slot_rows + row);
+      int id = -1;
+      if (c <= b.y) {
+        id = __ldcg(plan.part_id + slot);
+        ml = __ldcg(reinterpret_cast<const float2*>(plan.ml) + (int64_t)slot * plan.slot_rows + row);
+      }
+      const bool there = id == a.w;
+      if (!there) ml = make_float2(-INFINITY, 0.f);
       const float m_new = fmaxf(m, warp_max(ml.x));
       const float mb = m_new == -INFINITY ? 0.f : m_new;
-      const float f = m == -INFINITY ? 1.f : fast_ex2(m - mb), w = ml.x == -INFINITY && ml.y == 0.f ? 0.f : ml.x == -INFINITY ? ml.y : fast_ex2(ml.x - mb);
+      // (a sum without a maximum is 0, or no number, which it has to stay)
+      const float f = m == -INFINITY ? 1.f : fast_ex2(m - mb), w = ml.x == -INFINITY ? ml.y : fast_ex2(ml.x - mb);
       m = m_new;
       l = l * f + warp_sum(ml.y * w);
       o.x *= f; o.y *= f; o.z *= f; o.w *= f;
@@ -752,15 +796,15 @@ __global__ void __launch_bounds__(kMergeWarps * 32) merge_kernel(const __grid_co
         const int j = __ffs(todo) - 1;
         todo &= todo - 1;
         const float wj = __shfl_sync(0xffffffffu, w, j);
-        const int sl = __shfl_sync(0xffffffffu, slot, j);
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(plan.o + ((int64_t)sl * plan.slot_rows + row) * kHeadDim) + lane);
+        const int at = c0 + j;
+        const float4 v = at == b.x ? o0 : at == b.x + 1 ? o1 : part(2 * at);
         o.x = fmaf(v.x, wj, o.x); o.y = fmaf(v.y, wj, o.y); o.z = fmaf(v.z, wj, o.z); o.w = fmaf(v.w, wj, o.w);
       }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const __nv_bfloat162 u = __floats2bfloat162_rn(o.x * inv, o.y * inv), v = __floats2bfloat162_rn(o.z * inv, o.w * inv);
+    const __nv_bfloat162 p = __floats2bfloat162_rn(o.x * inv, o.y * inv), q = __floats2bfloat162_rn(o.z * inv, o.w * inv);
     const int64_t at = (int64_t)(a.x + po) * n_q + qh;
-    reinterpret_cast<uint2*>(out + at * kHeadDim)[lane] = make_uint2(*reinterpret_cast<const uint32_t*>(&u), *reinterpret_cast<const uint32_t*>(&v));
+    reinterpret_cast<uint2*>(out + at * kHeadDim)[lane] = make_uint2(*reinterpret_cast<const uint32_t*>(&p), *reinterpret_cast<const uint32_t*>(&q));
     if (lse && lane == 0) lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
   }
 }
@@ -780,8 +824,7 @@ Plan carve(void* ws, int G, int n_units, int64_t n_chunks, int64_t R, int sm_cou
     return r;
   };
   p.n_merge = reinterpret_cast<int32_t*>(take(4));
-  p.piece_begin = reinterpret_cast<int32_t*>(take((size_t)p.n_ctas * 4));
-  p.piece_end = reinterpret_cast<int32_t*>(take((size_t)p.n_ctas * 4));
+  p.piece_begin = reinterpret_cast<int32_t*>(take((size_t)(p.n_ctas + 1) * 4));
   p.part_id = reinterpret_cast<int32_t*>(take((size_t)p.n_ctas * 8));
   p.merge = reinterpret_cast<MergeUnit*>(take((size_t)p.n_ctas * sizeof(MergeUnit)));
   p.pieces = reinterpret_cast<Piece*>(take((size_t)(units + p.n_ctas) * sizeof(Piece)));
@@ -838,9 +881,12 @@ cudaError_t launch_attn_chunks(const CacheView& cv, const CacheView& lv, const D
                        ring ? (int64_t)lv.ring_pages * kPage : 0, ring ? (int64_t)lv.max_pages * kPage : 0};
   (void)launch_chained(plan_kernel, dim3(1), dim3(plan.n_ctas <= 512 ? 512 : kPlanThreads), plan_smem(n_chunks), st, a, cv, hu, plan, d.n_sink, d.window, status);
   (void)launch_chained(attn_chunks_kernel, dim3(plan.n_ctas), dim3(kThreads), (size_t)kSmem, st, maps, cv, lv, hu, plan, d, bmp, out, lse, status);
-  const int merge_rows = (int)std::min<int64_t>(R, 2 * bmp) * d.group;
-  (void)launch_chained(merge_kernel, dim3(plan.n_ctas, (unsigned)std::min(8, (merge_rows + kMergeWarps - 1) / kMergeWarps)), dim3(kMergeWarps * 32), 0, st,
-                       hu, plan, d.group, bmp, d.n_q, out, lse);
+  // sequences that are too short to be cut need no merge
+  if (((int64_t)std::max(cv.max_pages, lv.max_pages) * kPage + kTile - 1) / kTile >= 2 * kSnap) {
+    const int rows = (int)std::min<int64_t>(R, 2 * bmp) * d.group;
+    const int64_t blocks = std::min<int64_t>(((int64_t)plan.n_ctas * rows + kMergeWarps - 1) / kMergeWarps, (int64_t)8 * sm_count);
+    (void)launch_chained(merge_kernel, dim3((unsigned)blocks), dim3(kMergeWarps * 32), 0, st, hu, plan, d.group, bmp, d.n_q, rows, out, lse);
+  }
   return cudaGetLastError();
 }
 
