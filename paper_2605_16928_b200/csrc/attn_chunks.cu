@@ -308,24 +308,34 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
 }
 
 // ---- attention ----------------------------------------------------------------------------------------
-// Descriptors in two words: between the steps of a product only the address in the lower one moves.
-__device__ __forceinline__ uint2 desc128(uint32_t saddr, uint32_t lbo) {
-  const uint64_t d = smem_desc_sw(saddr, lbo, 1024, 2);
-  return make_uint2((uint32_t)d, (uint32_t)(d >> 32));
-}
-// D (TMEM) += A B, both from shared memory; and with A from TMEM (two bf16 per column, lane = row)
-__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint2 a, uint2 b, uint32_t a_off, uint32_t b_off, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ uint64_t desc128(uint32_t saddr, uint32_t lbo) { return smem_desc_sw(saddr, lbo, 1024, 2); }
+// The products are single statements of few instructions: the issuing thread shares its scheduler with two softmax warps that seldom
+// leave it a slot.  (A probe: an issuer of twice the instructions next to two warps of FMAs took 1.5 to 5 times as long.)
+// D (TMEM) = A B^T over 128 channels, both from shared memory: eight steps of 16 channels, 32 bytes each, four to a block.
+__device__ __forceinline__ void mma_ss8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc) {
   asm volatile(
-      "{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %6, 0;\nmov.b64 a, {%1, %2};\nmov.b64 b, {%3, %4};\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n}" ::"r"(d_tmem),
-      "r"(a.x + (a_off >> 4)), "r"(a.y), "r"(b.x + (b_off >> 4)), "r"(b.y), "r"(idesc), "r"(accumulate)
+      "{\n.reg .pred t, f;\n.reg .b64 a, b;\nsetp.ne.b32 t, 1, 0;\nsetp.ne.b32 f, 0, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, f;\n"
+      "add.s64 a, %1, 2;\nadd.s64 b, %2, 2;\ntcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n"
+      "add.s64 a, %1, 4;\nadd.s64 b, %2, 4;\ntcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n"
+      "add.s64 a, %1, 6;\nadd.s64 b, %2, 6;\ntcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n"
+      "add.s64 a, %1, 1024;\nadd.s64 b, %2, 1024;\ntcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n"
+      "add.s64 a, %1, 1026;\nadd.s64 b, %2, 1026;\ntcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n"
+      "add.s64 a, %1, 1028;\nadd.s64 b, %2, 1028;\ntcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n"
+      "add.s64 a, %1, 1030;\nadd.s64 b, %2, 1030;\ntcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint2 b, uint32_t b_off, uint32_t idesc, uint32_t accumulate) {
+static_assert(kBlk >> 4 == 1024, "the distance of two blocks in a descriptor");
+// D (TMEM) += A (TMEM: two bf16 per column, lane = row) B over 64 keys: four steps of 16 keys, 8 columns of A and 2 KB of B each.
+__device__ __forceinline__ void mma_ts4(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n.reg .pred p;\n.reg .b64 b;\nsetp.ne.b32 p, %5, 0;\nmov.b64 b, {%2, %3};\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n}" ::"r"(d_tmem),
-      "r"(a_tmem), "r"(b.x + (b_off >> 4)), "r"(b.y), "r"(idesc), "r"(accumulate)
+      "{\n.reg .pred t, p;\n.reg .b64 b;\n.reg .b32 a;\nsetp.ne.b32 t, 1, 0;\nsetp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      "add.u32 a, %1, 8;\nadd.s64 b, %2, 128;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n"
+      "add.u32 a, %1, 16;\nadd.s64 b, %2, 256;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n"
+      "add.u32 a, %1, 24;\nadd.s64 b, %2, 384;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 // A wait that is usually over already: asked once without parking the thread.
@@ -389,7 +399,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
   tc_fence_after();
   chain_wait();                                // (what is above touches nothing but the block's own memory)
   const int p_lo = __ldcg(plan.piece_begin + blockIdx.x), p_hi = __ldcg(plan.piece_begin + blockIdx.x + 1);
-  const uint32_t tmem = *tmem_slot;            // S / P of the groups: columns 0, 128; their O: 256, 384
+  // All 512 columns are this block's, from address 0 on: S / P of the groups at columns 0, 128; their O at 256, 384.
+  constexpr uint32_t tmem = 0;
 
   auto load_piece = [&](int i) -> Piece {
     Piece p;
@@ -482,78 +493,69 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
       }
     } else if (warp == 8) {
       // ================================ MMA issuer ================================
-      const uint32_t idesc_s = instr_desc_mn(128, 128, false), idesc_o = instr_desc_mn(128, 128, true);
-      const uint2 q_desc = desc128(sbase, 16), k_desc = desc128(sbase + kRingOff, 16), v_desc = desc128(sbase + kRingOff, kBlk);
-      unsigned job = 0, fill = 0, n_p = 0;     // n_p: phase bit of each group's P
-      int slot = 0, phase = 0;                 // of the next tile's K; its V is in the slot behind
-      // the P V that is still to be issued
-      bool wait_pv = false, pv_first = false, pv_new = false, pv_free = false, pv_last = false;
-      int pv_g = 0, pv_slot = 0, pv_phase = 0;
-      auto issue_pv = [&]() {
-        if (pv_new) wait_for(bar(kFull + pv_slot), pv_phase, abort_flag, status, d.wait_ns);
-        const unsigned par = (n_p >> pv_g) & 1u;
-        n_p ^= 1u << pv_g;
-        const uint2 v = make_uint2(v_desc.x + pv_slot * (kSlot >> 4), v_desc.y);
-        const uint32_t d_o = tmem + 256u + pv_g * 128u, a_p = tmem + pv_g * 128u;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          wait_for(bar(kPFull + 2 * pv_g + h), par, abort_flag, status, d.wait_ns);
+      // One thread.  The tensor core holds about four products that are issued and not done: as long as the thread is back within their
+      // time (256 cycles) it does not run dry, which would cost 400 cycles.
+      if (elect_one()) {
+        const uint32_t idesc_s = instr_desc_mn(128, 128, false), idesc_o = instr_desc_mn(128, 128, true);
+        const uint64_t q_desc = desc128(sbase, 16), k_desc = desc128(sbase + kRingOff, 16), v_desc = desc128(sbase + kRingOff, kBlk);
+        unsigned fill = 0, p_phase = 0;        // p_phase: a bit for each group
+        int g = 0, slot = 0, phase = 0;        // group of the next job; ring slot of the next tile's K (its V is in the one behind)
+        // the P V that is still to be issued, of group g ^ 1: bits 0 there, 1 its tile's first, 2 its piece's first, 3 its tile's last,
+        // 4 its piece's last, 5 phase of its V's slot
+        unsigned pv = 0;
+        int pv_slot = 0;
+        auto issue_pv = [&]() {
+          if (!(pv & 1u)) return;
+          const int pg = g ^ 1;
+          const uint32_t p_bar = bar(kPFull) + pg * 16, v_bar = pv_slot * 8, par = (p_phase >> pg) & 1u;
+          const uint64_t v = v_desc + (uint32_t)(pv_slot * (kSlot >> 4));
+          p_phase ^= 1u << pg;
+          if (pv & 2u) wait_for(bar(kFull) + v_bar, (pv >> 5) & 1u, abort_flag, status, d.wait_ns);
+          wait_for(p_bar, par, abort_flag, status, d.wait_ns);
           tc_fence_after();
-          if (elect_one()) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {      // 16 keys per step: 8 columns of P
-              const int ks = 4 * h + k;
-              mma_ts(d_o, a_p + ks * 8u, v, ks * 2048, idesc_o, ks ? 1u : pv_first ? 0u : 1u);
-            }
-            if (h == 1) {
-              if (pv_free) tc_commit(bar(kEmpty + pv_slot));
-              if (pv_last) tc_commit(bar(kOFull + pv_g));
-            }
-          }
-          __syncwarp();
-        }
-      };
-      for (int i = p_lo; i < p_hi; ++i) {
-        const Piece p = load_piece(i);
-        if (p.slot == kNothing) continue;
-        const int n = p.tile_hi - p.tile_lo, nq = p.n_pos > bmp ? 2 : 1, jobs = n * nq;
-        for (int x = 0; x < jobs; ++x, ++job) {
-          const int g = job & 1, qt = nq == 2 ? (x & 1) : 0, t = nq == 2 ? x >> 1 : x;
-          const unsigned qf = fill + qt;
-          const int qb = qf & 1;
-          if (t == 0) wait_for(bar(kQFull + qb), (qf >> 1) & 1, abort_flag, status, d.wait_ns);
-          if (qt == 0) wait_for(bar(kFull + slot), phase, abort_flag, status, d.wait_ns);
+          mma_ts4(256u + pg * 128u, pg * 128u, v, idesc_o, ~pv & 4u);
+          wait_for(p_bar + 8, par, abort_flag, status, d.wait_ns);
           tc_fence_after();
-          if (elect_one()) {
-            const uint2 q = make_uint2(q_desc.x + qb * (kSlot >> 4), q_desc.y), k = make_uint2(k_desc.x + slot * (kSlot >> 4), k_desc.y);
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-              mma_ss(tmem + g * 128u, q, k, (ks >> 2) * kBlk + (ks & 3) * 32, (ks >> 2) * kBlk + (ks & 3) * 32, idesc_s, ks ? 1u : 0u);
-            tc_commit(bar(kSFull + g));
-            if (qt == nq - 1) tc_commit(bar(kEmpty + slot));
-            if (t == n - 1) tc_commit(bar(kQEmpty + qb));
-          }
-          __syncwarp();
-          if (wait_pv) issue_pv();
-          wait_pv = true;
-          pv_g = g;
-          pv_first = x < 2;
-          pv_new = qt == 0;
-          pv_free = qt == nq - 1;
-          pv_last = x + 2 >= jobs;
-          pv_slot = slot + 1 == kRing ? 0 : slot + 1;
-          pv_phase = phase ^ (slot + 1 == kRing);
-          if (qt == nq - 1) {                  // two slots on
-            slot += 2;
-            if (slot >= kRing) {
-              slot -= kRing;
-              phase ^= 1;
+          mma_ts4(256u + pg * 128u, pg * 128u + 32u, v + (4 * 2048 >> 4), idesc_o, 1u);
+          if (pv & 8u) tc_commit(bar(kEmpty) + v_bar);
+          if (pv & 16u) tc_commit(bar(kOFull) + pg * 8);
+        };
+        for (int i = p_lo; i < p_hi; ++i) {
+          const Piece p = load_piece(i);
+          const int n = p.tile_hi - p.tile_lo;
+          const bool two = p.n_pos > bmp;
+          if (p.slot == kNothing || n == 0) continue;
+          const int b0 = fill & 1, b1 = b0 ^ 1, jobs = two ? 2 * n : n;
+          wait_for(bar(kQFull + b0), (fill >> 1) & 1, abort_flag, status, d.wait_ns);
+          if (two) wait_for(bar(kQFull + b1), ((fill + 1) >> 1) & 1, abort_flag, status, d.wait_ns);
+          fill += two ? 2 : 1;
+#pragma unroll 1
+          for (int x = 0; x < jobs; ++x) {
+            const int second = two ? x & 1 : 0;
+            if (!second) wait_for(bar(kFull) + slot * 8, phase, abort_flag, status, d.wait_ns);
+            tc_fence_after();
+            mma_ss8(g * 128u, q_desc + (uint32_t)((b0 ^ second) * (kSlot >> 4)), k_desc + (uint32_t)(slot * (kSlot >> 4)), idesc_s);
+            tc_commit(bar(kSFull) + g * 8);
+            const bool done = !two || second;  // with this tile
+            if (done) tc_commit(bar(kEmpty) + slot * 8);
+            if (x + (two ? 2 : 1) >= jobs) tc_commit(bar(kQEmpty) + (b0 ^ second) * 8);
+            issue_pv();
+            g ^= 1;
+            const bool wrap = slot + 1 == kRing;
+            pv_slot = wrap ? 0 : slot + 1;
+            pv = 1u | (second ? 0u : 2u) | (x < 2 ? 4u : 0u) | (done ? 8u : 0u) | (x + 2 >= jobs ? 16u : 0u) | ((unsigned)(phase ^ (int)wrap) << 5);
+            if (done) {
+              slot += 2;
+              if (slot >= kRing) {
+                slot -= kRing;
+                phase ^= 1;
+              }
             }
           }
         }
-        if (n > 0) fill += nq;
+        issue_pv();
       }
-      if (wait_pv) issue_pv();
+      __syncwarp();
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
@@ -750,7 +752,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
   }
   if (warp == 8) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(*tmem_slot), "r"(512) : "memory");
   }
 }
 

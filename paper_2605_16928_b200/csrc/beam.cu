@@ -16,6 +16,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxEl = 32;               // logits per thread
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kSlack = 8;                // the search for the bound stops when that many threads too many reach it
 // Threads whose maximum is above the bound: fewer than k + slack.  Each may have all of its logits above it.
 constexpr int kList = (RTP_MAX_BEAM_K + kSlack) * kMaxEl + RTP_MAX_BEAM_K;
@@ -55,8 +56,8 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const __grid_const
   constexpr int VN = Vec<T>::n, NV = EL / VN;
   static_assert(EL % VN == 0 && EL <= kMaxEl, "");
   __shared__ __align__(8) uint2 s_list[kList];     // ordered key, token
-  __shared__ uint32_t s_red[kWarps];
-  __shared__ float s_sum[kWarps];
+  __shared__ float s_max[kWarps], s_sum[kWarps];
+  __shared__ uint32_t s_min[kWarps];
   __shared__ int s_n, s_scan[kWarps];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t row = blockIdx.x / a.n_slices;
@@ -68,69 +69,93 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const __grid_const
   }
   const T* base = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
   const int skew = (int)((reinterpret_cast<uintptr_t>(base) & 15u) / sizeof(T));
-  const int first = slice * (kThreads * EL) - skew;   // token of the slice's first element (may be negative)
+  const int first = slice * (kThreads * EL) - skew + tid * VN;   // token of the thread's first logit (may be negative)
   float x[EL];
+  bool odd = false;                                // the thread has logits that are not there, or that are no numbers
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int t0 = first + (v * kThreads + tid) * VN;
+    const int t0 = first + v * kThreads * VN;
     if (t0 >= 0 && t0 + VN <= a.vocab) {
       const uint4 w = ld_stream_v4(base + t0);
       const T* e = reinterpret_cast<const T*>(&w);
 #pragma unroll
       for (int i = 0; i < VN; ++i) x[v * VN + i] = to_f(e[i]);
     } else {
+      odd = true;
 #pragma unroll
-      for (int i = 0; i < VN; ++i) x[v * VN + i] = t0 + i >= 0 && t0 + i < a.vocab ? to_f(base[t0 + i]) : __int_as_float(0x7fffffff);
+      for (int i = 0; i < VN; ++i) x[v * VN + i] = t0 + i >= 0 && t0 + i < a.vocab ? to_f(base[t0 + i]) : -INFINITY;
     }
   }
-  // keys that order like the logits; 0: there is no such token.  A logit that is NaN or +infinity is none that can be chosen.
-  uint32_t mine = 0, bad = 0;
-#pragma unroll
-  for (int i = 0; i < EL; ++i) {
-    const int t = first + ((i / VN) * kThreads + tid) * VN + i % VN;
-    const bool there = t >= 0 && t < a.vocab;
-    if (!(x[i] < INFINITY)) {
-      bad |= there;
-      x[i] = -INFINITY;
-    }
-    mine = max(mine, there ? okey(x[i]) : 0u);
-  }
-  if (bad) set_status(a.status, RTP_ERR_INVALID);
   if (tid == 0) s_n = 0;
+  // A logit that is NaN or +infinity is none that can be chosen: as -infinity.
+  float mine = x[0];
+#pragma unroll
+  for (int i = 1; i < EL; ++i) mine = fmaxf(mine, x[i]);   // (NaN is passed over)
   {
-    const uint32_t w = __reduce_max_sync(0xffffffffu, mine);
-    if (lane == 0) s_red[warp] = w;
+    float nan = 0.f;
+#pragma unroll
+    for (int i = 0; i < EL; ++i) nan += x[i];              // not a number, or +infinity, if one of them is (or -infinity)
+    if (!(nan < INFINITY) || mine == INFINITY) {
+      bool bad = false;
+#pragma unroll
+      for (int i = 0; i < EL; ++i)
+        if (!(x[i] < INFINITY)) {
+          x[i] = -INFINITY;
+          bad = true;
+        }
+      if (bad) set_status(a.status, RTP_ERR_INVALID);
+      mine = x[0];
+#pragma unroll
+      for (int i = 1; i < EL; ++i) mine = fmaxf(mine, x[i]);
+    }
+  }
+  // whether the thread has any token at all (-infinity is one that is ruled out; a place behind the row's end is none)
+  bool some = true;
+  if (odd) {
+    some = false;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) some = some || (first + v * kThreads * VN + VN > 0 && first + v * kThreads * VN < a.vocab);
+  }
+  const uint32_t key = some ? okey(mine) : 0u;
+  const float w_max = warp_max(mine);
+  const uint32_t w_min = __reduce_min_sync(0xffffffffu, key);
+  if (lane == 0) {
+    s_max[warp] = w_max;
+    s_min[warp] = w_min;
   }
   __syncthreads();
-  uint32_t top = 0;
+  float m = s_max[0];
+  uint32_t lo = s_min[0];
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) top = max(top, s_red[w]);
-  const float m = top ? okey_to_float(top) : -INFINITY, mb = m == -INFINITY ? 0.f : m;
-  float sum = 0.f;
+  for (int w = 1; w < kWarps; ++w) {
+    m = fmaxf(m, s_max[w]);
+    lo = min(lo, s_min[w]);
+  }
+  // sum of exponentials relative to the slice's maximum: four chains
+  const float mb = m == -INFINITY ? 0.f : m;   // (taken off first: the type's largest values times log2(e) are no numbers)
+  float sum4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < EL; ++i) sum += expf(x[i] - mb);
-  sum = warp_sum(sum);
+  for (int i = 0; i < EL; ++i) sum4[i & 3] += fast_ex2((x[i] - mb) * kLog2e);
+  const float sum = warp_sum((sum4[0] + sum4[1]) + (sum4[2] + sum4[3]));
   if (lane == 0) s_sum[warp] = sum;
-  // the largest bound that k threads' maxima reach (or that a few more do)
-  uint32_t lo = 0, hi = top;
+  // the largest bound that k threads' maxima reach (or that a few more do), between the smallest and the largest of them
+  uint32_t hi = okey(m);
   while (lo < hi) {
     const uint32_t mid = lo + (hi - lo) / 2 + 1;
-    const int n = __syncthreads_count(mine >= mid);
+    const int n = __syncthreads_count(key >= mid);
     if (n >= a.k) lo = mid; else hi = mid - 1;
     if (n >= a.k && n <= a.k + kSlack) break;
   }
   const uint32_t bound = max(lo, 1u);
-  auto key_of = [&](int i, int& t) -> uint32_t {
-    t = first + ((i / VN) * kThreads + tid) * VN + i % VN;
-    return t >= 0 && t < a.vocab ? okey(x[i]) : 0u;
-  };
-  int reach = 0, t;
-  if (mine >= bound) {
+  auto token_of = [&](int i) { return first + (i / VN) * kThreads * VN + i % VN; };
+  auto there = [&](int i) { return !odd || (token_of(i) >= 0 && token_of(i) < a.vocab); };
+  int reach = 0;
+  if (key >= bound) {
+    const float at = bound <= okey(-INFINITY) ? -INFINITY : okey_to_float(bound);
 #pragma unroll
-    for (int i = 0; i < EL; ++i) reach += key_of(i, t) >= bound;
+    for (int i = 0; i < EL; ++i) reach += x[i] >= at && there(i);
   }
   const int w_reach = __reduce_add_sync(0xffffffffu, reach);
-  __syncthreads();
   if (lane == 0 && w_reach) atomicAdd(&s_n, w_reach);
   __syncthreads();
   const bool all = s_n <= kList;                    // else too many equal the bound: the first of them are taken in order
@@ -140,8 +165,8 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const __grid_const
   if (reach) {
 #pragma unroll
     for (int i = 0; i < EL; ++i) {
-      const uint32_t key = key_of(i, t);
-      if (key > bound || (all && key == bound)) s_list[atomicAdd(&s_n, 1)] = make_uint2(key, (uint32_t)t);
+      const uint32_t ki = there(i) ? okey(x[i]) : 0u;
+      if (ki > bound || (all && ki == bound)) s_list[atomicAdd(&s_n, 1)] = make_uint2(ki, (uint32_t)token_of(i));
     }
   }
   __syncthreads();
@@ -153,10 +178,8 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const __grid_const
     for (int v = 0; v < NV; ++v) {
       uint32_t eq = 0;
 #pragma unroll
-      for (int i = 0; i < EL; ++i) {
-        const uint32_t key = key_of(i, t);
-        if (i / VN == v && key == bound) eq |= 1u << (i % VN);
-      }
+      for (int i = 0; i < EL; ++i)
+        if (i / VN == v && there(i) && okey(x[i]) == bound) eq |= 1u << (i % VN);
       const int c = __popc(eq);
       int s = c;
 #pragma unroll
@@ -175,7 +198,7 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const __grid_const
       }
       for (int i = 0; i < VN; ++i)
         if ((eq >> i) & 1u) {
-          if (at < need) s_list[n + at] = make_uint2(bound, (uint32_t)(first + (v * kThreads + tid) * VN + i));
+          if (at < need) s_list[n + at] = make_uint2(bound, (uint32_t)(first + v * kThreads * VN + i));
           ++at;
         }
       before += total;
