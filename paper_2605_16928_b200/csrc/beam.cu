@@ -1,10 +1,11 @@
 // Selection of a beam search step: the k best continuations of every group of beams, score = scores[beam] + log_softmax(logits)[token],
 // equal scores going to the lower (beam, token).
 //
-// Bound by the one read of the logits.  A row is cut into slices, one CTA each, that hold their logits in registers: maximum and
-// sum of exponentials, and the slice's k best tokens.  Those need no sort: the k-th largest of the 256 threads' maxima is a
-// lower bound of the k-th largest logit that only a few more than k logits reach; they go to a list, which is ordered by
-// counting.  A second kernel, one CTA per group, joins the rows' sums and takes the k best of the sorted lists one by one.
+// Bound by the one read of the logits.  A row is cut into slices of whole chunks, one CTA each, whose threads hold the logits of a
+// chunk in registers while the next ones are on their way; every thread keeps a running maximum and sum of exponentials of its own.
+// The slice's k best tokens need no sort of the chunks: in the first one, the k-th largest of the 256 threads' maxima is a lower bound
+// of the k-th largest logit that only a few more than k logits reach.  Those go to a list, and of the later chunks only what lies
+// above the list's bound.  A second kernel, one CTA per group, joins the rows' sums and takes the k best of the sorted lists one by one.
 // Tokens of one row are ordered by their logits alone; where rows meet, scores are 64-bit (sums of exponentials are 32-bit
 // within a slice, 64-bit across slices), so that neighbours are not swapped by the rounding of a normaliser.
 #include "rtp_device.cuh"
@@ -15,11 +16,16 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kMaxEl = 32;               // logits per thread
+constexpr int kMaxEl = 16;               // logits of a chunk per thread
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kSlack = 8;                // the search for the bound stops when that many threads too many reach it
-// Threads whose maximum is above the bound: fewer than k + slack.  Each may have all of its logits above it.
-constexpr int kList = (RTP_MAX_BEAM_K + kSlack) * kMaxEl + RTP_MAX_BEAM_K;
+// Threads whose maximum is above the bound: fewer than k + slack, and each may have all of its logits above it.
+constexpr int kAdd = (RTP_MAX_BEAM_K + kSlack) * kMaxEl + RTP_MAX_BEAM_K;
+constexpr int kKeep = 512;               // a list that is longer is cut to its k best before more is added
+constexpr int kList = kKeep + kAdd;
+constexpr int kShort = 64;               // lists that are ordered without a bound
+constexpr int kSelect = 256;
+constexpr int kGroup = 8;                // chunks between two barriers
 
 struct Cand {
   float x;
@@ -29,7 +35,7 @@ struct Cand {
 struct BeamArgs {
   const void* logits;
   int64_t row_stride;
-  int32_t n_beams, vocab, k, n_slices, pad_token;
+  int32_t n_beams, vocab, k, n_slices, chunks, pad_token;   // chunks: of a slice
   const float* scores;
   const int32_t* finished;
   Cand* cand;        // [rows, slices, k], best first
@@ -48,17 +54,71 @@ __device__ __forceinline__ float to_f(float x) { return x; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
 
-// Slices are counted from the 16-byte boundary at or below the row's first logit, so that whole pieces are single loads whatever
+// Pieces to 32 bits.
+__device__ __forceinline__ void unpack(const uint4& w, float* x, float) {
+  x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+}
+__device__ __forceinline__ void unpack(const uint4& w, float* x, __nv_bfloat16) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(u[i] << 16);
+    x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void unpack(const uint4& w, float* x, __half) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+  }
+}
+// Two numbers at a time.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+// m becomes the maximum of m and mine; returns the sum of exp(x - m).  Not below +infinity if one of x is NaN or +infinity.
+// (The maximum is taken off first: the largest logit's term is 1 and nothing else, so that rows with one certain token each are equal,
+// and the type's largest values times log2(e) would be no numbers.)
+template <int EL>
+__device__ __forceinline__ float weigh(const float (&x)[EL], float mine, float& m) {
+  m = fmaxf(m, mine);
+  const float off = m == -INFINITY ? 0.f : -m;
+  const float2 o2 = make_float2(off, off), l2 = make_float2(kLog2e, kLog2e);
+  float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+#pragma unroll
+  for (int i = 0; i < EL; i += 4) {
+    const float2 u = mul2(add2(make_float2(x[i], x[i + 1]), o2), l2), v = mul2(add2(make_float2(x[i + 2], x[i + 3]), o2), l2);
+    s0 = add2(s0, make_float2(fast_ex2(u.x), fast_ex2(u.y)));
+    s1 = add2(s1, make_float2(fast_ex2(v.x), fast_ex2(v.y)));
+  }
+  s0 = add2(s0, s1);
+  return s0.x + s0.y;
+}
+
+// Chunks are counted from the 16-byte boundary at or below the row's first logit, so that whole pieces are single loads whatever
 // the row's alignment; pieces that reach over an end of the row are loaded one by one.
 template <class T, int EL>
-__global__ void __launch_bounds__(kThreads) beam_slice_kernel(const __grid_constant__ BeamArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_constant__ BeamArgs a) {
   chain_wait();
-  constexpr int VN = Vec<T>::n, NV = EL / VN;
+  constexpr int VN = Vec<T>::n, NV = EL / VN, kChunk = kThreads * EL;
   static_assert(EL % VN == 0 && EL <= kMaxEl, "");
-  __shared__ __align__(8) uint2 s_list[kList];     // ordered key, token
+  __shared__ __align__(16) uint2 s_list[kList];    // ordered key, token
+  __shared__ __align__(16) uint2 s_sel[kSelect];
+  __shared__ uint2 s_best[RTP_MAX_BEAM_K];
   __shared__ float s_max[kWarps], s_sum[kWarps];
-  __shared__ uint32_t s_min[kWarps];
-  __shared__ int s_n, s_scan[kWarps];
+  __shared__ int s_n, s_sel_n, s_scan[kWarps];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t row = blockIdx.x / a.n_slices;
   const int slice = (int)(blockIdx.x - row * a.n_slices);
@@ -69,171 +129,303 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const __grid_const
   }
   const T* base = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
   const int skew = (int)((reinterpret_cast<uintptr_t>(base) & 15u) / sizeof(T));
-  const int first = slice * (kThreads * EL) - skew + tid * VN;   // token of the thread's first logit (may be negative)
-  float x[EL];
-  bool odd = false;                                // the thread has logits that are not there, or that are no numbers
+  const int c_lo = slice * a.chunks, c_hi = min(c_lo + a.chunks, (a.vocab + skew + kChunk - 1) / kChunk);
+  // the chunk lies within the row
+  auto whole = [&](int c) { return c > 0 && (c + 1) * kChunk - skew <= a.vocab; };
+  auto load = [&](int c, uint4 (&w)[NV]) {          // the thread's pieces of chunk c
+    const int first = c * kChunk - skew + tid * VN;
+    if (whole(c)) {
+      const T* p = base + first;
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int t0 = first + v * kThreads * VN;
-    if (t0 >= 0 && t0 + VN <= a.vocab) {
-      const uint4 w = ld_stream_v4(base + t0);
-      const T* e = reinterpret_cast<const T*>(&w);
-#pragma unroll
-      for (int i = 0; i < VN; ++i) x[v * VN + i] = to_f(e[i]);
-    } else {
-      odd = true;
-#pragma unroll
-      for (int i = 0; i < VN; ++i) x[v * VN + i] = t0 + i >= 0 && t0 + i < a.vocab ? to_f(base[t0 + i]) : -INFINITY;
+      for (int v = 0; v < NV; ++v) w[v] = ld_stream_v4(p + v * kThreads * VN);
+      return;
     }
-  }
-  if (tid == 0) s_n = 0;
-  // A logit that is NaN or +infinity is none that can be chosen: as -infinity.
-  float mine = x[0];
-#pragma unroll
-  for (int i = 1; i < EL; ++i) mine = fmaxf(mine, x[i]);   // (NaN is passed over)
-  {
-    float nan = 0.f;
-#pragma unroll
-    for (int i = 0; i < EL; ++i) nan += x[i];              // not a number, or +infinity, if one of them is (or -infinity)
-    if (!(nan < INFINITY) || mine == INFINITY) {
-      bool bad = false;
-#pragma unroll
-      for (int i = 0; i < EL; ++i)
-        if (!(x[i] < INFINITY)) {
-          x[i] = -INFINITY;
-          bad = true;
-        }
-      if (bad) set_status(a.status, RTP_ERR_INVALID);
-      mine = x[0];
-#pragma unroll
-      for (int i = 1; i < EL; ++i) mine = fmaxf(mine, x[i]);
-    }
-  }
-  // whether the thread has any token at all (-infinity is one that is ruled out; a place behind the row's end is none)
-  bool some = true;
-  if (odd) {
-    some = false;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) some = some || (first + v * kThreads * VN + VN > 0 && first + v * kThreads * VN < a.vocab);
-  }
-  const uint32_t key = some ? okey(mine) : 0u;
-  const float w_max = warp_max(mine);
-  const uint32_t w_min = __reduce_min_sync(0xffffffffu, key);
-  if (lane == 0) {
-    s_max[warp] = w_max;
-    s_min[warp] = w_min;
-  }
-  __syncthreads();
-  float m = s_max[0];
-  uint32_t lo = s_min[0];
-#pragma unroll
-  for (int w = 1; w < kWarps; ++w) {
-    m = fmaxf(m, s_max[w]);
-    lo = min(lo, s_min[w]);
-  }
-  // sum of exponentials relative to the slice's maximum: four chains
-  const float mb = m == -INFINITY ? 0.f : m;   // (taken off first: the type's largest values times log2(e) are no numbers)
-  float sum4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < EL; ++i) sum4[i & 3] += fast_ex2((x[i] - mb) * kLog2e);
-  const float sum = warp_sum((sum4[0] + sum4[1]) + (sum4[2] + sum4[3]));
-  if (lane == 0) s_sum[warp] = sum;
-  // the largest bound that k threads' maxima reach (or that a few more do), between the smallest and the largest of them
-  uint32_t hi = okey(m);
-  while (lo < hi) {
-    const uint32_t mid = lo + (hi - lo) / 2 + 1;
-    const int n = __syncthreads_count(key >= mid);
-    if (n >= a.k) lo = mid; else hi = mid - 1;
-    if (n >= a.k && n <= a.k + kSlack) break;
-  }
-  const uint32_t bound = max(lo, 1u);
-  auto token_of = [&](int i) { return first + (i / VN) * kThreads * VN + i % VN; };
-  auto there = [&](int i) { return !odd || (token_of(i) >= 0 && token_of(i) < a.vocab); };
-  int reach = 0;
-  if (key >= bound) {
-    const float at = bound <= okey(-INFINITY) ? -INFINITY : okey_to_float(bound);
-#pragma unroll
-    for (int i = 0; i < EL; ++i) reach += x[i] >= at && there(i);
-  }
-  const int w_reach = __reduce_add_sync(0xffffffffu, reach);
-  if (lane == 0 && w_reach) atomicAdd(&s_n, w_reach);
-  __syncthreads();
-  const bool all = s_n <= kList;                    // else too many equal the bound: the first of them are taken in order
-  __syncthreads();
-  if (tid == 0) s_n = 0;
-  __syncthreads();
-  if (reach) {
-#pragma unroll
-    for (int i = 0; i < EL; ++i) {
-      const uint32_t ki = there(i) ? okey(x[i]) : 0u;
-      if (ki > bound || (all && ki == bound)) s_list[atomicAdd(&s_n, 1)] = make_uint2(ki, (uint32_t)token_of(i));
-    }
-  }
-  __syncthreads();
-  int n = s_n;
-  if (!all && n < a.k) {
-    const int need = a.k - n;
-    int before = 0;                                 // equal ones in front of this piece
 #pragma unroll 1
     for (int v = 0; v < NV; ++v) {
-      uint32_t eq = 0;
+      const int t0 = first + v * kThreads * VN;
+      uint4 u;
+      if (t0 >= 0 && t0 + VN <= a.vocab) {
+        u = ld_stream_v4(base + t0);
+      } else {
+        T e[VN];
 #pragma unroll
-      for (int i = 0; i < EL; ++i)
-        if (i / VN == v && there(i) && okey(x[i]) == bound) eq |= 1u << (i % VN);
-      const int c = __popc(eq);
-      int s = c;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, s, o);
-        if (lane >= o) s += y;
+        for (int i = 0; i < VN; ++i) e[i] = t0 + i >= 0 && t0 + i < a.vocab ? base[t0 + i] : T(-INFINITY);
+        u = *reinterpret_cast<const uint4*>(e);
       }
-      __syncthreads();
-      if (lane == 31) s_scan[warp] = s;
-      __syncthreads();
-      int at = before + s - c, total = 0;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        at += w < warp ? s_scan[w] : 0;
-        total += s_scan[w];
-      }
-      for (int i = 0; i < VN; ++i)
-        if ((eq >> i) & 1u) {
-          if (at < need) s_list[n + at] = make_uint2(bound, (uint32_t)(first + v * kThreads * VN + i));
-          ++at;
-        }
-      before += total;
-      if (before >= need) break;                    // (the same in all threads)
+      for (int y = 0; y < NV; ++y)
+        if (y == v) w[y] = u;
     }
-    n += min(before, need);
+  };
+  if (tid == 0) s_n = 0;
+  int n = 0;                                       // entries of the list (the same in all threads, like what follows)
+  uint32_t least = 0;                              // a key that k entries of the list reach, once there are as many
+  float m = -INFINITY, sum = 0.f;                  // this thread's
+  // The largest bound that k threads' keys reach (or that a few more do), at least lo.
+  auto search = [&](uint32_t key, uint32_t lo) -> uint32_t {
+    const uint32_t w = __reduce_max_sync(0xffffffffu, key);
     __syncthreads();
-  }
-  // ordered by counting
-  for (int i = tid; i < n; i += kThreads) {
-    const uint2 me = s_list[i];
-    int rank = 0;
-    for (int o = 0; o < n; ++o) {
-      const uint2 y = s_list[o];
-      rank += y.x > me.x || (y.x == me.x && y.y < me.y);
+    if (lane == 0) s_scan[warp] = (int)w;
+    __syncthreads();
+    uint32_t hi = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) hi = max(hi, (uint32_t)s_scan[i]);
+    while (lo < hi) {
+      const uint32_t mid = lo + (hi - lo) / 2 + 1;
+      const int r = __syncthreads_count(key >= mid);
+      if (r >= a.k) lo = mid; else hi = mid - 1;
+      if (r >= a.k && r <= a.k + kSlack) break;
     }
-    if (rank < a.k) a.cand[out * a.k + rank] = Cand{okey_to_float(me.x), (int32_t)me.y};
+    return lo;
+  };
+  // The list's k best in their order, counted out; of a long list only those that reach a bound of its threads' best.
+  auto rank_of = [&](const uint2* v, int count, uint2 me) {
+    const uint64_t mk = ((uint64_t)me.x << 32) | ~me.y;     // (larger key first, then lower token)
+    int rank = 0, o = 0;
+    for (; o + 1 < count; o += 2) {
+      const uint4 y = *reinterpret_cast<const uint4*>(v + o);
+      rank += (((uint64_t)y.x << 32) | ~y.y) > mk;
+      rank += (((uint64_t)y.z << 32) | ~y.w) > mk;
+    }
+    if (o < count) rank += (((uint64_t)v[o].x << 32) | ~v[o].y) > mk;
+    return rank;
+  };
+  auto order = [&]() {
+    __syncthreads();
+    const uint2* v = s_list;
+    int count = n;
+    if (n > kShort) {
+      uint32_t best = 0;
+      for (int i = tid; i < n; i += kThreads) best = max(best, s_list[i].x);
+      const uint32_t bound = search(best, 0u);
+      if (tid == 0) s_sel_n = 0;
+      __syncthreads();
+      for (int i = tid; i < n; i += kThreads)
+        if (s_list[i].x >= bound) {
+          const int to = atomicAdd(&s_sel_n, 1);
+          if (to < kSelect) s_sel[to] = s_list[i];
+        }
+      __syncthreads();
+      if (s_sel_n <= kSelect) {                             // (else many are equal: all of them are looked at)
+        v = s_sel;
+        count = s_sel_n;
+      }
+    }
+    for (int i = tid; i < count; i += kThreads) {
+      const uint2 me = v[i];
+      const int rank = rank_of(v, count, me);
+      if (rank < a.k) s_best[rank] = me;
+    }
+    __syncthreads();
+  };
+  auto cut = [&]() {
+    order();
+    n = min(n, a.k);
+    for (int i = tid; i < n; i += kThreads) s_list[i] = s_best[i];
+    if (tid == 0) s_n = n;
+    if (n == a.k) least = max(least, s_best[a.k - 1].x);
+    __syncthreads();
+  };
+  // Once the list has k entries, chunks go by in groups without a barrier: what is above the bound is added, up to the list's end.  A group
+  // that would add more than there is room for (logits that rise along the row) is gone through again, chunk by chunk.
+  constexpr int kAhead = 2;
+  uint4 ahead[kAhead][NV];
+  bool again = false;                              // the same in all threads, like c
+  int again_end = c_lo;
+  int c = c_lo, group_end = c_lo;                  // chunks before group_end go by without a barrier
+  float m_group = m, sum_group = sum;              // as they were where the group began
+  auto fetch = [&]() {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (c + j < c_hi) load(c + j, ahead[j]);
+  };
+  fetch();
+#pragma unroll 1
+  while (c < c_hi) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j, ++c) {
+      if (c >= c_hi) break;
+      float x[EL];
+#pragma unroll
+      for (int v = 0; v < NV; ++v) unpack(ahead[j][v], x + v * VN, T());
+      if (c + kAhead < c_hi) load(c + kAhead, ahead[j]);
+      const int first = c * kChunk - skew + tid * VN;   // token of the thread's first logit (may be negative)
+      float mine = x[0];
+#pragma unroll
+      for (int i = 1; i < EL; ++i) mine = fmaxf(mine, x[i]);   // (NaN is passed over)
+      // running maximum and sum
+      const float m_was = m;
+      float part = weigh(x, mine, m);
+      if (!(part < INFINITY)) {
+        // a logit that is NaN or +infinity is none that can be chosen: as -infinity
+        set_status(a.status, RTP_ERR_INVALID);
+        mine = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < EL; ++i) {
+          if (!(x[i] < INFINITY)) x[i] = -INFINITY;
+          mine = fmaxf(mine, x[i]);
+        }
+        m = m_was;
+        part = weigh(x, mine, m);
+      }
+      if (m != m_was) sum *= m_was == -INFINITY ? 0.f : fast_ex2((m_was - m) * kLog2e);
+      sum += part;
+      // keys order like the logits; 0: the thread has no token here (-infinity is a token that is ruled out)
+      auto token_of = [&](int i) { return first + (i / VN) * kThreads * VN + i % VN; };
+      uint32_t valid = (1u << EL) - 1u;            // a bit for each of the thread's logits; pieces may reach over the row's ends
+      if (!whole(c)) {
+#pragma unroll
+        for (int i = 0; i < EL; ++i)
+          if (token_of(i) < 0 || token_of(i) >= a.vocab) valid &= ~(1u << i);
+      }
+      const uint32_t key = valid ? okey(mine) : 0u;
+      // the thread's logits of key `bound` and above; those above it
+      auto from = [&](uint32_t bound) {
+        const float at = bound <= okey(-INFINITY) ? -INFINITY : okey_to_float(bound);
+        uint32_t mask = 0;
+#pragma unroll
+        for (int i = 0; i < EL; ++i)
+          if (x[i] >= at) mask |= 1u << i;
+        return mask & valid;
+      };
+      auto above = [&](uint32_t bound) {
+        const float at = bound < okey(-INFINITY) ? -INFINITY : okey_to_float(bound);
+        uint32_t mask = 0;
+#pragma unroll
+        for (int i = 0; i < EL; ++i)
+          if (x[i] > at) mask |= 1u << i;
+        return bound < okey(-INFINITY) ? valid : mask & valid;
+      };
+      // few are added: they are read again, so that one short loop does for all places
+      auto add = [&](uint32_t mask) {
+        while (mask) {
+          const int t = token_of(__ffs(mask) - 1);
+          mask &= mask - 1;
+          const float v = to_f(base[t]);
+          const int to = atomicAdd(&s_n, 1);
+          if (to < kList) s_list[to] = make_uint2(v < INFINITY ? okey(v) : okey(-INFINITY), (uint32_t)t);
+        }
+      };
+      if (c < group_end) {
+        if (key > least) add(above(least));
+        continue;
+      }
+      if (n > kKeep) cut();
+      const uint32_t bound = max(search(key, 0u), 1u);
+      const uint32_t reach = key >= bound ? from(bound) : 0u, over = key >= bound ? above(bound) : 0u;
+      const int w_reach = __reduce_add_sync(0xffffffffu, __popc(reach));
+      __syncthreads();
+      if (lane == 0) s_scan[warp] = w_reach;
+      __syncthreads();
+      int reached = 0;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) reached += s_scan[w];
+      const bool all = reached <= kAdd;            // else too many equal the bound: the first of them are taken in order
+      add(all ? reach : over);
+      __syncthreads();
+      const int added = s_n - n;
+      n = s_n;
+      if (!all && added < a.k) {
+        const int need = a.k - added;
+        int before = 0;                            // equal ones in front of this piece
+#pragma unroll 1
+        for (int v = 0; v < NV; ++v) {
+          uint32_t eq = ((reach & ~over) >> (v * VN)) & ((1u << VN) - 1u);
+          const int cnt = __popc(eq);
+          int s = cnt;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, s, o);
+            if (lane >= o) s += y;
+          }
+          __syncthreads();
+          if (lane == 31) s_scan[warp] = s;
+          __syncthreads();
+          int at = before + s - cnt, total = 0;
+#pragma unroll
+          for (int w = 0; w < kWarps; ++w) {
+            at += w < warp ? s_scan[w] : 0;
+            total += s_scan[w];
+          }
+          for (; eq; eq &= eq - 1, ++at)
+            if (at < need) s_list[n + at] = make_uint2(bound, (uint32_t)(first + v * kThreads * VN + __ffs(eq) - 1));
+          before += total;
+          if (before >= need) break;               // (the same in all threads)
+        }
+        n += min(before, need);
+        __syncthreads();
+        if (tid == 0) s_n = n;
+      }
+      if (reached >= a.k) least = max(least, bound);
+      else if (n >= a.k) cut();                    // (short chunks: their entries' k-th best)
+      __syncthreads();
+    }
+    if (c < group_end && c < c_hi) continue;
+    if (group_end > c_lo && !again) {              // the end of a group
+      __syncthreads();
+      const int have = s_n;
+      __syncthreads();
+      if (have > kList) {
+        again = true;
+        c = group_end - kGroup;
+        m = m_group;
+        sum = sum_group;
+        if (tid == 0) s_n = n;
+        fetch();
+        again_end = group_end;
+        group_end = c_lo;
+        __syncthreads();
+        continue;
+      }
+      n = have;
+      if (n > 2 * a.k + 16) cut();
+    }
+    if (again && c >= again_end) again = false;
+    if (!again && n >= a.k && c < c_hi) {
+      group_end = c + kGroup;
+      m_group = m;
+      sum_group = sum;
+    }
   }
+  __syncthreads();
+  order();
+  const int kept = min(n, a.k);
+  for (int i = tid; i < kept; i += kThreads) a.cand[out * a.k + i] = Cand{okey_to_float(s_best[i].x), (int32_t)s_best[i].y};
+  // the slice's maximum and sum
+  const float w_max = warp_max(m);
+  if (lane == 0) s_max[warp] = w_max;
+  __syncthreads();
+  float top = s_max[0];
+#pragma unroll
+  for (int w = 1; w < kWarps; ++w) top = fmaxf(top, s_max[w]);
+  const float part = warp_sum(m == -INFINITY ? 0.f : sum * fast_ex2((m - top) * kLog2e));
+  if (lane == 0) s_sum[warp] = part;
+  __syncthreads();
   if (tid == 0) {
-    a.count[out] = min(n, a.k);
     float z = 0.f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) z += s_sum[w];
-    a.stat[out] = make_float2(m, z);
+    a.count[out] = kept;
+    a.stat[out] = make_float2(top, z);
   }
 }
 
-// One CTA per group.  Every thread watches the heads of the lists list = thread, thread + 256, ... and knows the best of them.
-__global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_constant__ BeamArgs a) {
+// One CTA per group.  The rows' normalisers, then all lists as 64-bit scores in shared memory where they fit, then k rounds in which every
+// lane knows the best of the lists list = thread, thread + threads, ...; a single warp does the rounds where 32 lanes have few lists each.
+// Lists are in the order of (beam, token): the slices of a row hold disjoint, ascending ranges of tokens, and a list is sorted.  So of
+// equal scores the lower list goes first.
+constexpr int kPickCached = 3400;                  // entries in shared memory
+__global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_constant__ BeamArgs a, const int cached) {
   chain_wait();
-  extern __shared__ __align__(16) unsigned char s_at[];   // uint8 [lists]: entries taken of each list
+  extern __shared__ __align__(16) unsigned char smem_pick[];
+  uint64_t* s_key = reinterpret_cast<uint64_t*>(smem_pick);              // [lists * k] if cached
+  int32_t* s_tok = reinterpret_cast<int32_t*>(s_key + cached);           // [lists * k] if cached
+  uint8_t* s_at = reinterpret_cast<uint8_t*>(s_tok + cached);            // [lists]: entries taken of each
+  uint8_t* s_cnt = s_at + a.n_beams * a.n_slices;                        // [lists]: entries of each
   __shared__ double s_off[RTP_MAX_BEAMS];                  // score of a token with the row's largest logit
   __shared__ float s_max[RTP_MAX_BEAMS];                   // that logit
   __shared__ int s_state[RTP_MAX_BEAMS];                   // 1: ended, 2: no token has a probability
-  __shared__ uint4 s_best[2][kWarps];                      // score (ordered, 64 bits), list, place of the winner in its list
+  __shared__ uint4 s_best[2][kWarps];                      // score (ordered, 64 bits), list, token of each warp's best
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t row0 = (int64_t)blockIdx.x * a.n_beams;
   const int lists = a.n_beams * a.n_slices;
@@ -262,95 +454,115 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_consta
       s_max[b] = m;
     }
   }
-  for (int l = tid; l < lists; l += kThreads) s_at[l] = 0;
+  for (int l = tid; l < lists; l += kThreads) {
+    const int b = l / a.n_slices;
+    s_at[l] = 0;
+    s_cnt[l] = a.finished && a.finished[row0 + b] != 0 ? (l == b * a.n_slices) : (uint8_t)a.count[row0 * a.n_slices + l];
+  }
   __syncthreads();
-  auto head_of = [&](int l, uint64_t& key, int& token) -> bool {   // the next candidate of a list; keys order like scores
-    const int b = l / a.n_slices, at = s_at[l];
-    const int64_t li = (row0 + b) * a.n_slices + (l - b * a.n_slices);
-    double score;
+  const Cand* cand = a.cand + row0 * a.n_slices * a.k;
+  auto entry = [&](int l, int i, int& token) -> uint64_t {   // an entry of a list; keys order like scores
+    const int b = l / a.n_slices;
+    double score = s_off[b];
     if (s_state[b] == 1) {
-      if (l != b * a.n_slices || at > 0) return false;
-      score = s_off[b];
       token = a.pad_token;
     } else {
-      if (at >= a.count[li]) return false;
-      const Cand c = a.cand[li * a.k + at];
+      const Cand c = cand[l * a.k + i];
       token = c.token;
-      score = s_state[b] == 2 ? -(double)INFINITY : s_off[b] + ((double)c.x - (double)s_max[b]);
+      score = s_state[b] == 2 ? -(double)INFINITY : score + ((double)c.x - (double)s_max[b]);
     }
     const uint64_t u = (uint64_t)__double_as_longlong(score + 0.0);
-    key = (u >> 63) ? ~u : u | 0x8000000000000000ull;
-    return true;
+    return (u >> 63) ? ~u : u | 0x8000000000000000ull;
   };
-  // Lists are in the order of (beam, token), so that among equal scores the lower list goes first; within a list it is sorted so.
-  // (Two slices of a row hold disjoint, ascending ranges of tokens.)
-  uint64_t best = 0;
+  if (cached) {
+    for (int e = tid; e < lists * a.k; e += kThreads) {
+      const int l = e / a.k, i = e - l * a.k;
+      if (i < s_cnt[l]) s_key[e] = entry(l, i, s_tok[e]);
+    }
+    __syncthreads();
+  }
+  const int threads = lists <= 128 ? 32 : kThreads;        // that do the rounds
+  if (tid >= threads) return;
+  uint64_t best = 0;                                       // (no score has key 0)
   int best_l = 0x7fffffff, best_tok = 0;
   auto look = [&]() {
     best = 0;
     best_l = 0x7fffffff;
-    for (int l = tid; l < lists; l += kThreads) {
-      uint64_t key;
-      int token;
-      if (head_of(l, key, token) && key > best) {
+    for (int l = tid; l < lists; l += threads) {
+      const int i = s_at[l];
+      if (i >= s_cnt[l]) continue;
+      int token = 0;
+      const uint64_t key = cached ? s_key[l * a.k + i] : entry(l, i, token);
+      if (key > best) {
         best = key;
         best_l = l;
-        best_tok = token;
+        best_tok = cached ? s_tok[l * a.k + i] : token;
       }
     }
   };
   look();
+  uint4 won = make_uint4(0, 0, 0, 0);                      // lane i: what round i, i + 32, .. chose
   for (int i = 0; i < a.k; ++i) {
     const uint32_t h = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32));
     const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32) == h ? (uint32_t)best : 0u);
-    const bool tie = best == (((uint64_t)h << 32) | lo);
-    const int l = __reduce_min_sync(0xffffffffu, tie ? best_l : 0x7fffffff);
+    const int l = __reduce_min_sync(0xffffffffu, best == (((uint64_t)h << 32) | lo) ? best_l : 0x7fffffff);
     const int tok = __shfl_sync(0xffffffffu, best_tok, l & 31);
-    if (lane == 0) s_best[i & 1][warp] = make_uint4(h, lo, (uint32_t)l, (uint32_t)tok);
-    __syncthreads();
-    uint4 win = s_best[i & 1][0];
+    uint4 win = make_uint4(h, lo, (uint32_t)l, (uint32_t)tok);
+    if (threads > 32) {
+      if (lane == 0) s_best[i & 1][warp] = win;
+      __syncthreads();
+      win = s_best[i & 1][0];
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) {
-      const uint4 o = s_best[i & 1][w];
-      const uint64_t ko = ((uint64_t)o.x << 32) | o.y, kw = ((uint64_t)win.x << 32) | win.y;
-      if (ko > kw || (ko == kw && o.z < win.z)) win = o;
+      for (int w = 1; w < kWarps; ++w) {
+        const uint4 o = s_best[i & 1][w];
+        const uint64_t ko = ((uint64_t)o.x << 32) | o.y, kw = ((uint64_t)win.x << 32) | win.y;
+        if (ko > kw || (ko == kw && o.z < win.z)) win = o;
+      }
     }
     const bool some = (win.x | win.y) != 0u;
-    if (tid == 0) {
-      const int64_t at = (int64_t)blockIdx.x * a.k + i;
-      const uint64_t u = ((uint64_t)win.x << 32) | win.y;
+    if (lane == (i & 31)) won = win;
+    if (warp == 0 && ((i & 31) == 31 || i + 1 == a.k) && (i & ~31) + lane <= i) {
+      const int64_t at = (int64_t)blockIdx.x * a.k + (i & ~31) + lane;
+      const bool any = (won.x | won.y) != 0u;
+      const uint64_t u = ((uint64_t)won.x << 32) | won.y;
       const double score = __longlong_as_double((long long)((u >> 63) ? u & 0x7fffffffffffffffull : ~u));
-      a.parent[at] = some ? (int32_t)(row0 + win.z / a.n_slices) : -1;
-      a.token[at] = some ? (int32_t)win.w : -1;
-      a.scores_out[at] = some ? (float)score : -INFINITY;
+      a.parent[at] = any ? (int32_t)(row0 + won.z / a.n_slices) : -1;
+      a.token[at] = any ? (int32_t)won.w : -1;
+      a.scores_out[at] = any ? (float)score : -INFINITY;
     }
-    if (some && (int)(win.z % kThreads) == tid) {
+    if (some && (int)(win.z % threads) == tid) {
       s_at[win.z] += 1;
       look();
     }
   }
 }
 
-// Logits per thread: as many CTAs as fill the device twice, within what a slice can hold.
-int beam_el(int64_t rows, int64_t vocab, int sm_count) {
-  const int64_t want = rows * vocab / ((int64_t)2 * sm_count * kThreads);
-  return want >= 32 ? 32 : want >= 16 ? 16 : 8;
+// How a row is cut: chunks of 4096 logits, of 2048 in calls that would leave SMs idle; and as many slices as make one wave of four CTAs
+// per SM, each of whole chunks.
+struct BeamCut {
+  int el, chunks, slices;                          // logits per thread and chunk, chunks per slice, slices per row
+};
+BeamCut beam_cut(int64_t rows, int64_t vocab, int sm_count) {
+  BeamCut c;
+  c.el = rows * vocab >= (int64_t)sm_count * kThreads * 32 ? 16 : 8;
+  const int64_t chunks = (vocab + 7 + (int64_t)kThreads * c.el - 1) / ((int64_t)kThreads * c.el);   // (7: a row's skew)
+  const int64_t want = std::max<int64_t>(1, std::min(chunks, (int64_t)4 * sm_count / rows));
+  c.chunks = (int)((chunks + want - 1) / want);
+  c.slices = (int)((chunks + c.chunks - 1) / c.chunks);
+  return c;
 }
-int beam_slices(int64_t vocab, int el) { return (int)((vocab + 7 + (int64_t)kThreads * el - 1) / ((int64_t)kThreads * el)); }   // (7: a row's skew)
 
 template <class T>
 cudaError_t launch_slices(const BeamArgs& a, int el, int64_t rows, cudaStream_t st) {
   const dim3 grid((unsigned)(rows * a.n_slices)), block(kThreads);
-  if (el == 32) (void)launch_chained(beam_slice_kernel<T, 32>, grid, block, 0, st, a);
-  else if (el == 16) (void)launch_chained(beam_slice_kernel<T, 16>, grid, block, 0, st, a);
-  else (void)launch_chained(beam_slice_kernel<T, 8>, grid, block, 0, st, a);
+  (void)launch_chained(el == 16 ? beam_slice_kernel<T, 16> : beam_slice_kernel<T, 8>, grid, block, 0, st, a);
   return cudaGetLastError();
 }
 
 }  // namespace
 
 size_t beam_workspace_bytes(int64_t rows, int64_t vocab, int k, int sm_count) {
-  const int64_t lists = rows * beam_slices(vocab, beam_el(rows, vocab, sm_count));
+  const int64_t lists = rows * beam_cut(rows, vocab, sm_count).slices;
   return (size_t)lists * (k * sizeof(Cand) + sizeof(float2) + sizeof(int32_t)) + 2 * 256;
 }
 
@@ -358,21 +570,22 @@ cudaError_t launch_beam_select(const void* logits, int format, int64_t row_strid
                                const float* scores, const int32_t* finished, int pad_token, int k, int32_t* parent, int32_t* token,
                                float* scores_out, void* ws, int32_t* status, int sm_count, cudaStream_t st) {
   const int64_t rows = n_groups * n_beams;
-  const int el = beam_el(rows, vocab, sm_count);
-  BeamArgs a = {logits, row_stride, n_beams, (int32_t)vocab, k, beam_slices(vocab, el), pad_token, scores, finished,
+  const BeamCut cut = beam_cut(rows, vocab, sm_count);
+  BeamArgs a = {logits, row_stride, n_beams, (int32_t)vocab, k, cut.slices, cut.chunks, pad_token, scores, finished,
                 nullptr, nullptr, nullptr, parent, token, scores_out, status};
-  const int64_t lists = rows * a.n_slices;
-  if (lists >= (int64_t)1 << 31 || (int64_t)n_beams * a.n_slices > 40000) return cudaErrorNotSupported;
+  const int64_t lists = rows * a.n_slices, group_lists = (int64_t)n_beams * a.n_slices;
+  if (lists >= (int64_t)1 << 31 || group_lists > 20000) return cudaErrorNotSupported;
   char* p = reinterpret_cast<char*>(ws);
   a.cand = reinterpret_cast<Cand*>(p);
   p += ((size_t)lists * k * sizeof(Cand) + 255) & ~(size_t)255;
   a.stat = reinterpret_cast<float2*>(p);
   p += (size_t)lists * sizeof(float2);
   a.count = reinterpret_cast<int32_t*>(p);
-  cudaError_t e = format == RTP_LOGITS_F32 ? launch_slices<float>(a, el, rows, st)
-                  : format == RTP_LOGITS_BF16 ? launch_slices<__nv_bfloat16>(a, el, rows, st) : launch_slices<__half>(a, el, rows, st);
+  cudaError_t e = format == RTP_LOGITS_F32 ? launch_slices<float>(a, cut.el, rows, st)
+                  : format == RTP_LOGITS_BF16 ? launch_slices<__nv_bfloat16>(a, cut.el, rows, st) : launch_slices<__half>(a, cut.el, rows, st);
   if (e != cudaSuccess) return e;
-  (void)launch_chained(beam_pick_kernel, dim3((unsigned)n_groups), dim3(kThreads), (size_t)n_beams * a.n_slices, st, a);
+  const int cached = group_lists * k <= kPickCached ? (int)(group_lists * k) : 0;
+  (void)launch_chained(beam_pick_kernel, dim3((unsigned)n_groups), dim3(kThreads), (size_t)cached * 12 + 2 * group_lists, st, a, cached);
   return cudaGetLastError();
 }
 
