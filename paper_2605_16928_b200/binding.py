@@ -34,7 +34,7 @@ EXPORTS = [
 ]
 
 
-_LOGITS = {"torch.float32": RTP_LOGITS_F32, "torch.bfloat16": RTP_LOGITS_BF16, "torch.float16": RTP_LOGITS_F16}
+_LOGITS = {}   # dtype -> logits_format (torch is not imported here)
 
 
 class RtpError(RuntimeError):
@@ -202,11 +202,12 @@ def _enough_counts(where: str, cache, page_refs):
         raise RtpError(RTP_ERR_INVALID, where, f"page_refs has {page_refs.shape[0]} counts for {cache.num_pages} pages")
 
 
-def _rows_of(where: str, name: str, x, heads: int) -> int:
-    """Token stride of rows [T, heads, 128] whose heads lie side by side (a slice of a projection's output, for instance)."""
-    if x.dim() != 3 or x.element_size() != 2 or x.shape[1] != heads or x.shape[2] != 128 or x.stride(2) != 1 or (heads > 1 and x.stride(1) != 128):
-        raise RtpError(RTP_ERR_INVALID, where, f"{name} has to be 16-bit [tokens, {heads}, 128], its heads side by side")
-    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), heads * 128) // 8 * 8
+def _rows_of(where: str, name: str, x, n: int, heads: int) -> int:
+    """Token stride of rows [n, heads, 128] whose heads lie side by side (a slice of a projection's output, for instance)."""
+    s = x.stride()
+    if x.shape != (n, heads, 128) or s[2] != 1 or (s[1] != 128 and heads > 1) or x.element_size() != 2:
+        raise RtpError(RTP_ERR_INVALID, where, f"{name} has to be 16-bit [{n} tokens, {heads}, 128], its heads side by side")
+    return s[0] if n > 1 else heads * 128
 
 
 class Rope:
@@ -355,16 +356,23 @@ def rtp_kv_append(ctx, params, cache, k_new, v_new, tok_seq, tok_pos, status, st
 def rtp_rope_append(ctx, params, cache, rope: Rope, q, k, v, q_out, w_k, tok_seq, tok_pos, status, stream=None):
     """q [T, query heads, 128], k, v [T, KV heads, 128]: unrotated rows, dense or slices of one projection's output; q_out dense
     (q and q_out None: keys and values only); w_k: index projections, or None."""
-    n_q, n_kv = params.c.n_q_heads, params.c.n_kv_heads
-    for x in (k, v, tok_pos, q, q_out):
-        _same_length("rtp_rope_append", tok_seq, x)
-    sq = _rows_of("rtp_rope_append", "q", q, n_q) if q is not None else 0
-    sk, sv = _rows_of("rtp_rope_append", "k", k, n_kv), _rows_of("rtp_rope_append", "v", v, n_kv)
-    if q_out is not None and (_rows_of("rtp_rope_append", "q_out", q_out, n_q) != n_q * 128):
-        raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", "q_out has to be dense")
-    ctx._check(ctx.lib.rtp_rope_append(ctx.h, params.ref(), C.byref(cache), _ptr(rope.freqs), rope.rotary_dim, rope.interleaved,
-                                       rope.scale, _ptr(q), sq, _ptr(k), sk, _ptr(v), sv, _ptr(q_out), _ptr(w_k), _ptr(tok_seq),
-                                       _ptr(tok_pos), tok_seq.shape[0], _ptr(status), _stream(stream)), "rtp_rope_append")
+    c = params.c
+    n, n_q, n_kv = tok_seq.shape[0], c.n_q_heads, c.n_kv_heads
+    sq, pq, po = 0, None, None
+    if q is not None and q_out is not None:
+        sq, pq, po = _rows_of("rtp_rope_append", "q", q, n, n_q), q.data_ptr(), q_out.data_ptr()
+        if _rows_of("rtp_rope_append", "q_out", q_out, n, n_q) != n_q * 128:
+            raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", "q_out has to be dense")
+    elif q is not None or q_out is not None:
+        raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", "q and q_out go together")
+    sk, sv = _rows_of("rtp_rope_append", "k", k, n, n_kv), _rows_of("rtp_rope_append", "v", v, n, n_kv)
+    if tok_pos.shape[0] != n:
+        _same_length("rtp_rope_append", tok_seq, tok_pos)
+    rc = ctx.lib.rtp_rope_append(ctx.h, C.byref(c), C.byref(cache), _ptr(rope.freqs), rope.rotary_dim, rope.interleaved, rope.scale, pq,
+                                 sq, k.data_ptr(), sk, v.data_ptr(), sv, po, _ptr(w_k), tok_seq.data_ptr(), tok_pos.data_ptr(), n,
+                                 _ptr(status), _stream(stream))
+    if rc:
+        ctx._check(rc, "rtp_rope_append")
 
 
 def rtp_kv_expand(ctx, params, cache, src_pages, dst_pages, k_out, v_out, status, stream=None):
@@ -433,24 +441,25 @@ def rtp_beam_select(ctx, logits, scores, finished, pad_token, parent, token, sco
     """logits [rows, vocab] (fp32, bf16 or fp16; rows may be strided), rows = groups x beams; scores fp32 [rows] or None; finished int32
     [rows] or None; parent, token int32 and scores_out fp32 [groups, k]: written."""
     rows, vocab = logits.shape
-    groups, k = parent.shape
+    shape = parent.shape
+    groups, k = shape
     beams = rows // groups if groups else 1
-    if groups * beams != rows:
-        raise RtpError(RTP_ERR_INVALID, "rtp_beam_select", f"{rows} rows are not {groups} groups")
-    if (token.shape != parent.shape or scores_out.shape != parent.shape or (scores is not None and scores.numel() != rows)
-            or (finished is not None and finished.numel() != rows) or logits.stride(1) != 1
-            or not (parent.is_contiguous() and token.is_contiguous() and scores_out.is_contiguous())):
-        raise RtpError(RTP_ERR_INVALID, "rtp_beam_select", "arrays that go together have other shapes or strides")
-    for name, x, size in (("scores", scores, 4), ("finished", finished, 4), ("parent", parent, 4), ("token", token, 4), ("scores_out", scores_out, 4)):
-        if x is not None and x.element_size() != size:
-            raise RtpError(RTP_ERR_INVALID, "rtp_beam_select", f"{name} has to hold elements of {size} bytes")
-    fmt = _LOGITS.get(str(logits.dtype))
+    fmt, st = _LOGITS.get(logits.dtype), logits.stride()
     if fmt is None:
-        raise RtpError(RTP_ERR_INVALID, "rtp_beam_select", f"logits of {logits.dtype}")
-    ctx._check(ctx.lib.rtp_beam_select(ctx.h, _ptr(logits), fmt, logits.stride(0) if rows > 1 else vocab, groups, beams, vocab,
-                                       _ptr(scores), _ptr(finished), int(pad_token), k, _ptr(parent), _ptr(token),
-                                       _ptr(scores_out), _ptr(workspace), workspace.nbytes, _ptr(status), _stream(stream)),
-               "rtp_beam_select")
+        fmt = _LOGITS.setdefault(logits.dtype, {"torch.float32": RTP_LOGITS_F32, "torch.bfloat16": RTP_LOGITS_BF16,
+                                                "torch.float16": RTP_LOGITS_F16}.get(str(logits.dtype), -1))
+    if (groups * beams != rows or token.shape != shape or scores_out.shape != shape or st[1] != 1 or fmt < 0
+            or not (parent.is_contiguous() and token.is_contiguous() and scores_out.is_contiguous())
+            or parent.element_size() != 4 or token.element_size() != 4 or scores_out.element_size() != 4
+            or (scores is not None and (scores.numel() != rows or scores.element_size() != 4))
+            or (finished is not None and (finished.numel() != rows or finished.element_size() != 4))):
+        raise RtpError(RTP_ERR_INVALID, "rtp_beam_select", "logits [groups x beams, vocabulary] in 32 or 16 bits, scores and finished one 32-bit "
+                       "value a row, parent, token and scores_out contiguous 32-bit [groups, k]")
+    rc = ctx.lib.rtp_beam_select(ctx.h, logits.data_ptr(), fmt, st[0] if rows > 1 else vocab, groups, beams, vocab, _ptr(scores),
+                                 _ptr(finished), pad_token, k, parent.data_ptr(), token.data_ptr(), scores_out.data_ptr(),
+                                 workspace.data_ptr(), workspace.nbytes, _ptr(status), _stream(stream))
+    if rc:
+        ctx._check(rc, "rtp_beam_select")
 
 
 def rtp_index_queries(ctx, params, q_pre, w_q, qt_out, stream=None):
@@ -589,13 +598,15 @@ def rtp_attn_chunks(ctx, params, cache, q, chunk_seq, chunk_start, row_offsets, 
                     stream=None):
     """q, out: [rows, query heads, 128]; chunk c: rows row_offsets[c] .. row_offsets[c + 1] - 1 at positions chunk_start[c] .. of
     sequence chunk_seq[c]; kv_heads: None (all) or the KV heads that are computed."""
-    _same_length("rtp_attn_chunks", chunk_seq, chunk_start)
-    for x in (out, lse):
-        _same_length("rtp_attn_chunks", q, x)
-    if row_offsets.shape[0] != chunk_seq.shape[0] + 1:
-        raise RtpError(RTP_ERR_INVALID, "rtp_attn_chunks", f"{chunk_seq.shape[0]} chunks with {row_offsets.shape[0]} offsets")
-    arr = _i32_array(kv_heads) if kv_heads is not None else None
-    ctx._check(ctx.lib.rtp_attn_chunks(ctx.h, params.ref(), C.byref(cache), _ptr(q), _ptr(chunk_seq), _ptr(chunk_start), _ptr(row_offsets),
-                                       chunk_seq.shape[0], q.shape[0], int(pattern), C.cast(arr, C.c_void_p) if arr is not None else None,
-                                       len(kv_heads) if kv_heads is not None else 0, _ptr(out), _ptr(lse), _ptr(workspace),
-                                       workspace.nbytes, _ptr(status), _stream(stream)), "rtp_attn_chunks")
+    n, rows = chunk_seq.shape[0], q.shape[0]
+    if chunk_start.shape[0] != n or row_offsets.shape[0] != n + 1 or out.shape[0] != rows or (lse is not None and lse.shape[0] != rows):
+        raise RtpError(RTP_ERR_INVALID, "rtp_attn_chunks", f"{n} chunks and {rows} rows: chunk_start, row_offsets (one more), out or lse are of other lengths")
+    arr, n_heads = None, 0
+    if kv_heads is not None:
+        n_heads = len(kv_heads)
+        arr = C.cast(_i32_array(kv_heads), C.c_void_p)
+    rc = ctx.lib.rtp_attn_chunks(ctx.h, C.byref(params.c), C.byref(cache), q.data_ptr(), chunk_seq.data_ptr(), chunk_start.data_ptr(),
+                                 row_offsets.data_ptr(), n, rows, pattern, arr, n_heads, out.data_ptr(), _ptr(lse),
+                                 workspace.data_ptr(), workspace.nbytes, _ptr(status), _stream(stream))
+    if rc:
+        ctx._check(rc, "rtp_attn_chunks")
