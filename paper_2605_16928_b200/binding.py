@@ -21,6 +21,7 @@ RTP_IKEY_BF16, RTP_IKEY_E4M3 = 0, 1
 RTP_KV_BF16, RTP_KV_FP4 = 0, 1
 RTP_CHUNK_DENSE, RTP_CHUNK_LOCAL, RTP_CHUNK_BY_HEAD = 0, 1, 2
 RTP_LOGITS_F32, RTP_LOGITS_BF16, RTP_LOGITS_F16 = 0, 1, 2
+RTP_MAX_BEAMS = RTP_MAX_BEAM_K = 64
 _STATUS_NAMES = ["RTP_OK", "RTP_ERR_INVALID", "RTP_ERR_CAPACITY", "RTP_ERR_UNSUPPORTED", "RTP_ERR_CUDA",
                  "RTP_ERR_TIMEOUT"]
 
@@ -210,6 +211,11 @@ def _rows_of(where: str, name: str, x, n: int, heads: int) -> int:
     return s[0] if n > 1 else heads * 128
 
 
+def _is_i32(x) -> bool:
+    """A dense array of 32-bit values."""
+    return x.element_size() == 4 and x.is_contiguous()
+
+
 class Rope:
     """What the rotation of a layer is: radians per position of each pair (float64 [rotary_dim / 2] on the device), how channels
     pair (halves, or neighbours if interleaved), and a factor on sine and cosine."""
@@ -366,8 +372,8 @@ def rtp_rope_append(ctx, params, cache, rope: Rope, q, k, v, q_out, w_k, tok_seq
     elif q is not None or q_out is not None:
         raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", "q and q_out go together")
     sk, sv = _rows_of("rtp_rope_append", "k", k, n, n_kv), _rows_of("rtp_rope_append", "v", v, n, n_kv)
-    if tok_pos.shape[0] != n:
-        _same_length("rtp_rope_append", tok_seq, tok_pos)
+    if tok_pos.shape[0] != n or not (_is_i32(tok_seq) and _is_i32(tok_pos)):
+        raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", f"tok_seq and tok_pos have to be contiguous int32 [{n}]")
     rc = ctx.lib.rtp_rope_append(ctx.h, C.byref(c), C.byref(cache), _ptr(rope.freqs), rope.rotary_dim, rope.interleaved, rope.scale, pq,
                                  sq, k.data_ptr(), sk, v.data_ptr(), sv, po, _ptr(w_k), tok_seq.data_ptr(), tok_pos.data_ptr(), n,
                                  _ptr(status), _stream(stream))
@@ -405,6 +411,8 @@ def rtp_cache_fork(ctx, params, cache, page_refs, src_seqs, dst_seqs, status, st
 def rtp_cache_reorder(ctx, params, cache, page_refs, src_seqs, dst_seqs, status, stream=None):
     """Sequence dst_seqs[i] becomes what src_seqs[i] was, all at once (src may be dst, and may be named several times)."""
     _same_length("rtp_cache_reorder", src_seqs, dst_seqs)
+    if not (_is_i32(src_seqs) and _is_i32(dst_seqs) and _is_i32(page_refs)):
+        raise RtpError(RTP_ERR_INVALID, "rtp_cache_reorder", "src_seqs, dst_seqs and page_refs have to be contiguous int32")
     _enough_counts("rtp_cache_reorder", cache, page_refs)
     ctx._check(ctx.lib.rtp_cache_reorder(ctx.h, params.ref(), C.byref(cache), _ptr(page_refs), _ptr(src_seqs), _ptr(dst_seqs),
                                          src_seqs.shape[0], _ptr(status), _stream(stream)), "rtp_cache_reorder")
@@ -449,12 +457,11 @@ def rtp_beam_select(ctx, logits, scores, finished, pad_token, parent, token, sco
         fmt = _LOGITS.setdefault(logits.dtype, {"torch.float32": RTP_LOGITS_F32, "torch.bfloat16": RTP_LOGITS_BF16,
                                                 "torch.float16": RTP_LOGITS_F16}.get(str(logits.dtype), -1))
     if (groups * beams != rows or token.shape != shape or scores_out.shape != shape or st[1] != 1 or fmt < 0
-            or not (parent.is_contiguous() and token.is_contiguous() and scores_out.is_contiguous())
-            or parent.element_size() != 4 or token.element_size() != 4 or scores_out.element_size() != 4
-            or (scores is not None and (scores.numel() != rows or scores.element_size() != 4))
-            or (finished is not None and (finished.numel() != rows or finished.element_size() != 4))):
+            or not (_is_i32(parent) and _is_i32(token) and _is_i32(scores_out))
+            or (scores is not None and (scores.numel() != rows or not _is_i32(scores)))
+            or (finished is not None and (finished.numel() != rows or not _is_i32(finished)))):
         raise RtpError(RTP_ERR_INVALID, "rtp_beam_select", "logits [groups x beams, vocabulary] in 32 or 16 bits, scores and finished one 32-bit "
-                       "value a row, parent, token and scores_out contiguous 32-bit [groups, k]")
+                       "value a row, parent, token and scores_out 32-bit [groups, k], contiguous but for the logits' rows")
     rc = ctx.lib.rtp_beam_select(ctx.h, logits.data_ptr(), fmt, st[0] if rows > 1 else vocab, groups, beams, vocab, _ptr(scores),
                                  _ptr(finished), pad_token, k, parent.data_ptr(), token.data_ptr(), scores_out.data_ptr(),
                                  workspace.data_ptr(), workspace.nbytes, _ptr(status), _stream(stream))
@@ -601,6 +608,12 @@ def rtp_attn_chunks(ctx, params, cache, q, chunk_seq, chunk_start, row_offsets, 
     n, rows = chunk_seq.shape[0], q.shape[0]
     if chunk_start.shape[0] != n or row_offsets.shape[0] != n + 1 or out.shape[0] != rows or (lse is not None and lse.shape[0] != rows):
         raise RtpError(RTP_ERR_INVALID, "rtp_attn_chunks", f"{n} chunks and {rows} rows: chunk_start, row_offsets (one more), out or lse are of other lengths")
+    n_q = params.c.n_q_heads
+    if not (_rows_of("rtp_attn_chunks", "q", q, rows, n_q) == _rows_of("rtp_attn_chunks", "out", out, rows, n_q) == n_q * 128
+            and _is_i32(chunk_seq) and _is_i32(chunk_start) and _is_i32(row_offsets)
+            and (lse is None or (lse.shape == (rows, n_q) and _is_i32(lse)))):
+        raise RtpError(RTP_ERR_INVALID, "rtp_attn_chunks", "q and out have to be dense [rows, query heads, 128], lse [rows, query heads] in 32 bits, and the "
+                       "chunks' arrays contiguous int32")
     arr, n_heads = None, 0
     if kv_heads is not None:
         n_heads = len(kv_heads)

@@ -9,8 +9,13 @@ prefill chunk runs on its pages expanded to bf16.
 
 ``PagePool`` is the device-side bookkeeping of a pool that sequences come to and leave: table, lengths and
 reference counts, and the calls that change them.
+
+``BeamPath`` is beam search over such pools: rotated appends, attention over ragged chunks, selection of the
+continuations, and the sequences' places after it.
 """
 from __future__ import annotations
+
+import itertools
 
 import torch
 
@@ -272,3 +277,99 @@ class PagePool:
         if code != rb.RTP_OK:
             self.status.zero_()
         return code
+
+
+class BeamPath:
+    """Beam search over page pools, one per layer: sequence g * n_beams + b of every pool is hypothesis b of group g.
+
+        path.prompts(lengths); out = path.attend(layer, q, k, v) for every layer; path.begin(logits of each prompt's last row)
+        path.advance();        out = path.attend(layer, q, k, v) for every layer; path.choose(logits of the hypotheses)      (a step)
+
+    ``tokens`` [groups x beams] are the tokens to go on with, ``parents`` the rows that they continue (None of a first choice),
+    ``scores`` the sums of log-probabilities and ``finished`` what has ended with ``end_token``.  Nothing is read back; a step writes to
+    the same arrays every time and may be captured into a graph.  ``status`` as in PagePool."""
+
+    def __init__(self, pools, rope: rb.Rope, n_groups: int, n_beams: int, vocab: int, max_rows: int, pattern: int = rb.RTP_CHUNK_BY_HEAD,
+                 pad_token: int = 0, end_token: int = -1):
+        """max_rows: of all prompts together."""
+        B, first = n_groups * n_beams, pools[0]
+        if any(p.seq_lens.shape[0] < B or p.cache is None for p in pools) or not 1 <= n_beams <= min(vocab, rb.RTP_MAX_BEAMS) or n_groups < 1:
+            raise rb.RtpError(rb.RTP_ERR_INVALID, "BeamPath", f"pools of {B} sequences with their arrays, 1 <= beams <= {rb.RTP_MAX_BEAMS} and the vocabulary")
+        self.pools, self.rope, self.pattern, self.pad_token, self.end_token = list(pools), rope, pattern, pad_token, end_token
+        self.ctx, self.n_groups, self.n_beams, self.vocab, self.max_rows = rb.Context(), n_groups, n_beams, vocab, max(max_rows, B)
+        dev = first.seq_lens.device
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.dev, self.status = dev, torch.zeros(1, **i32)
+        self.seqs, self.ones = torch.arange(B, **i32), torch.ones(B, **i32)
+        self.positions, self.offsets = torch.zeros(B, **i32), torch.arange(B + 1, **i32)
+        self.tokens, self.parents, self.finished = (torch.zeros((n_groups, n_beams), **i32) for _ in range(3))
+        self.scores, self._scores = (torch.zeros((n_groups, n_beams), dtype=torch.float32, device=dev) for _ in range(2))
+        heads = max(p.params.c.n_q_heads for p in pools)
+        self.q = torch.empty((self.max_rows, heads, 128), dtype=torch.bfloat16, device=dev)
+        ws = max([rb.rtp_chunk_workspace_bytes(p.params, B, self.max_rows) for p in pools] + [rb.rtp_beam_workspace_bytes(B, vocab, n_beams)])
+        self.workspace = torch.empty(ws, dtype=torch.uint8, device=dev)
+        self.batch = None
+
+    def prompts(self, lengths):
+        """One prompt a group, by its number of tokens: pages for them in every pool.  The sequences have to be empty."""
+        if len(lengths) != self.n_groups or min(lengths) < 1 or sum(lengths) > self.max_rows:
+            raise rb.RtpError(rb.RTP_ERR_INVALID, "BeamPath.prompts", f"{self.n_groups} lengths of at least one, at most {self.max_rows} in all")
+        i32 = dict(dtype=torch.int32, device=self.dev)
+        seqs, n = self.seqs[::self.n_beams].contiguous(), torch.tensor(lengths, **i32)
+        for p in self.pools:
+            p.reserve(seqs, n)
+        self.batch = (seqs, torch.zeros(self.n_groups, **i32), torch.tensor([0, *itertools.accumulate(lengths)], **i32),
+                      torch.repeat_interleave(seqs, n), torch.cat([torch.arange(x, **i32) for x in lengths]))
+
+    def advance(self):
+        """Room for one token of every hypothesis, behind its last one."""
+        self.positions.copy_(self.pools[0].seq_lens[:self.seqs.shape[0]])
+        for p in self.pools:
+            p.reserve(self.seqs, self.ones)
+        self.batch = (self.seqs, self.positions, self.offsets, self.seqs, self.positions)
+
+    def attend(self, layer: int, q, k, v, out=None, lse=None, w_k=None):
+        """The batch's rows of one layer as the projections leave them: rotated and appended, then attended over their sequences."""
+        pool = self.pools[layer]
+        seq, start, offsets, tok_seq, tok_pos = self.batch
+        q_rot = self.q.view(-1)[:q.shape[0] * q.shape[1] * 128].view(q.shape[0], q.shape[1], 128)
+        out = torch.empty_like(q_rot) if out is None else out
+        rb.rtp_rope_append(self.ctx, pool.params, pool.cache, self.rope, q, k, v, q_rot, w_k, tok_seq, tok_pos, self.status)
+        rb.rtp_attn_chunks(self.ctx, pool.params, pool.cache, q_rot, seq, start, offsets, self.pattern, None, out, lse, self.workspace, self.status)
+        return out
+
+    def _select(self, logits, scores, finished):
+        if logits.shape[1] != self.vocab:
+            raise rb.RtpError(rb.RTP_ERR_INVALID, "BeamPath", f"logits over {logits.shape[1]} tokens, not {self.vocab}")
+        rb.rtp_beam_select(self.ctx, logits, scores, finished, self.pad_token, self.parents, self.tokens, self._scores, self.workspace, self.status)
+        self.scores.copy_(self._scores)
+
+    def begin(self, logits):
+        """logits [groups, vocabulary] behind the prompts: the best tokens begin the hypotheses, which share their prompt's pages."""
+        if logits.shape[0] != self.n_groups:
+            raise rb.RtpError(rb.RTP_ERR_INVALID, "BeamPath.begin", f"logits of {logits.shape[0]} rows, not of {self.n_groups}")
+        self._select(logits, None, None)
+        if self.n_beams > 1:
+            src = self.seqs.view(self.n_groups, self.n_beams)[:, :1].expand(-1, self.n_beams - 1).reshape(-1)
+            dst = self.seqs.view(self.n_groups, self.n_beams)[:, 1:].reshape(-1)
+            for p in self.pools:
+                p.fork(src, dst)
+        self.finished.copy_(self.tokens == self.end_token)
+
+    def choose(self, logits):
+        """logits [groups x beams, vocabulary]: the best continuations take the hypotheses' places, with their sequences."""
+        if logits.shape[0] != self.seqs.shape[0]:
+            raise rb.RtpError(rb.RTP_ERR_INVALID, "BeamPath.choose", f"logits of {logits.shape[0]} rows, not of {self.seqs.shape[0]}")
+        self._select(logits, self.scores, self.finished)
+        parents = self.parents.view(-1)
+        for p in self.pools:
+            p.reorder(parents, self.seqs)
+        ended = self.finished.view(-1)[parents.clamp(min=0)].view_as(self.finished)
+        torch.maximum(ended, (self.tokens == self.end_token).int(), out=self.finished)
+
+    def status_code(self) -> int:
+        """The largest code that its own calls and its pools' have recorded since the last call of this method."""
+        code = rb.rtp_check_status(self.ctx, self.status)
+        if code != rb.RTP_OK:
+            self.status.zero_()
+        return max([code] + [p.status_code() for p in self.pools])
