@@ -318,6 +318,7 @@ class BeamPath:
         seqs, n = self.seqs[::self.n_beams].contiguous(), torch.tensor(lengths, **i32)
         for p in self.pools:
             p.reserve(seqs, n)
+            p.seq_lens[:self.seqs.shape[0]:self.n_beams] = n
         self.batch = (seqs, torch.zeros(self.n_groups, **i32), torch.tensor([0, *itertools.accumulate(lengths)], **i32),
                       torch.repeat_interleave(seqs, n), torch.cat([torch.arange(x, **i32) for x in lengths]))
 
@@ -326,6 +327,7 @@ class BeamPath:
         self.positions.copy_(self.pools[0].seq_lens[:self.seqs.shape[0]])
         for p in self.pools:
             p.reserve(self.seqs, self.ones)
+            p.seq_lens[:self.seqs.shape[0]] += 1
         self.batch = (self.seqs, self.positions, self.offsets, self.seqs, self.positions)
 
     def attend(self, layer: int, q, k, v, out=None, lse=None, w_k=None):
@@ -350,8 +352,8 @@ class BeamPath:
             raise rb.RtpError(rb.RTP_ERR_INVALID, "BeamPath.begin", f"logits of {logits.shape[0]} rows, not of {self.n_groups}")
         self._select(logits, None, None)
         if self.n_beams > 1:
-            src = self.seqs.view(self.n_groups, self.n_beams)[:, :1].expand(-1, self.n_beams - 1).reshape(-1)
-            dst = self.seqs.view(self.n_groups, self.n_beams)[:, 1:].reshape(-1)
+            src = self.seqs.view(self.n_groups, self.n_beams)[:, :1].expand(-1, self.n_beams - 1).contiguous().view(-1)
+            dst = self.seqs.view(self.n_groups, self.n_beams)[:, 1:].contiguous().view(-1)
             for p in self.pools:
                 p.fork(src, dst)
         self.finished.copy_(self.tokens == self.end_token)
