@@ -75,6 +75,40 @@ __device__ __forceinline__ void unpack(const uint4& w, float* x, __half) {
     x[2 * i + 1] = f.y;
   }
 }
+// The thread's largest logit; NaN is passed over (-infinity or NaN if there is nothing else).
+template <int NV>
+__device__ __forceinline__ float max_of(const uint4 (&w)[NV], float) {
+  float m = __uint_as_float(w[0].x);
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const float a = fmaxf(__uint_as_float(w[v].x), __uint_as_float(w[v].y)), b = fmaxf(__uint_as_float(w[v].z), __uint_as_float(w[v].w));
+    m = fmaxf(m, fmaxf(a, b));
+  }
+  return m;
+}
+template <class P, int NV>
+__device__ __forceinline__ P max_pair(const uint4 (&w)[NV]) {
+  P m = *reinterpret_cast<const P*>(&w[0].x);
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const P* p = reinterpret_cast<const P*>(&w[v]);
+    m = __hmax2(m, __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3])));
+  }
+  return m;
+}
+template <int NV>
+__device__ __forceinline__ float max_of(const uint4 (&w)[NV], __nv_bfloat16) {
+  const float2 f = __bfloat1622float2(max_pair<__nv_bfloat162>(w));
+  return fmaxf(f.x, f.y);
+}
+template <int NV>
+__device__ __forceinline__ float max_of(const uint4 (&w)[NV], __half) {
+  const float2 f = __half22float2(max_pair<__half2>(w));
+  return fmaxf(f.x, f.y);
+}
+// A thread's i-th logit, counted from its first one.
+template <int EL, int VN>
+__device__ __forceinline__ int token_of(int i) { return (i / VN) * kThreads * VN + i % VN; }
 // Two numbers at a time.
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   float2 r;
@@ -107,8 +141,27 @@ __device__ __forceinline__ float weigh(const float (&x)[EL], float mine, float& 
   return s0.x + s0.y;
 }
 
-// Chunks are counted from the 16-byte boundary at or below the row's first logit, so that whole pieces are single loads whatever
-// the row's alignment; pieces that reach over an end of the row are loaded one by one.
+// Which token is whose is the same whatever the row's alignment, so that rows of equal logits have equal normalisers.  A row that does not
+// begin at a 16-byte boundary is read in aligned pieces all the same: a thread's eight or four logits lie in two of them, which a shift joins
+// (twice the loads, most of them from L1).  Pieces that reach over an end of the row are loaded one by one.
+template <class T>
+__device__ __forceinline__ uint4 join(const uint4& lo, const uint4& hi, int s) {   // the 16 bytes from element s of lo on
+  uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  const int bytes = s * (int)sizeof(T);
+  if (bytes & 8) {
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+  }
+  if (bytes & 4) {
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+  }
+  const int bits = 8 * (bytes & 3);
+  return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                    __funnelshift_r(w[3], w[4], bits));
+}
+__device__ __forceinline__ uint4 ld_piece(const void* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+
 template <class T, int EL>
 __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_constant__ BeamArgs a) {
   chain_wait();
@@ -129,32 +182,59 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
   }
   const T* base = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
   const int skew = (int)((reinterpret_cast<uintptr_t>(base) & 15u) / sizeof(T));
-  const int c_lo = slice * a.chunks, c_hi = min(c_lo + a.chunks, (a.vocab + skew + kChunk - 1) / kChunk);
-  // the chunk lies within the row
-  auto whole = [&](int c) { return c > 0 && (c + 1) * kChunk - skew <= a.vocab; };
-  auto load = [&](int c, uint4 (&w)[NV]) {          // the thread's pieces of chunk c
-    const int first = c * kChunk - skew + tid * VN;
+  const int c_lo = slice * a.chunks, c_hi = min(c_lo + a.chunks, (a.vocab + kChunk - 1) / kChunk);
+  // no piece of the chunk reaches over an end of the row
+  auto whole = [&](int c) { return skew ? c > 0 && (c + 1) * kChunk + VN <= a.vocab : (c + 1) * kChunk <= a.vocab; };
+  auto load = [&](int c, uint4 (&w)[NV]) {          // the thread's pieces of chunk c of a row without skew
+    const T* p = base + c * kChunk + tid * VN;
     if (whole(c)) {
-      const T* p = base + first;
 #pragma unroll
       for (int v = 0; v < NV; ++v) w[v] = ld_stream_v4(p + v * kThreads * VN);
       return;
     }
-#pragma unroll 1
+#pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int t0 = first + v * kThreads * VN;
-      uint4 u;
-      if (t0 >= 0 && t0 + VN <= a.vocab) {
-        u = ld_stream_v4(base + t0);
+      const int t0 = c * kChunk + tid * VN + v * kThreads * VN;
+      if (t0 + VN <= a.vocab) {
+        w[v] = ld_stream_v4(base + t0);
       } else {
         T e[VN];
 #pragma unroll
-        for (int i = 0; i < VN; ++i) e[i] = t0 + i >= 0 && t0 + i < a.vocab ? base[t0 + i] : T(-INFINITY);
-        u = *reinterpret_cast<const uint4*>(e);
+        for (int i = 0; i < VN; ++i) e[i] = t0 + i < a.vocab ? base[t0 + i] : T(-INFINITY);
+        w[v] = *reinterpret_cast<const uint4*>(e);
+      }
+    }
+  };
+  auto load_two = [&](int c, uint4 (&lo)[NV], uint4 (&hi)[NV]) {   // and of one with
+    const T* p = base + c * kChunk + tid * VN - skew;
+    if (whole(c)) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        lo[v] = ld_piece(p + v * kThreads * VN);
+        hi[v] = ld_piece(p + v * kThreads * VN + VN);
+      }
+      return;
+    }
+#pragma unroll 1
+    for (int v = 0; v < NV; ++v) {
+      const int t0 = c * kChunk + tid * VN + v * kThreads * VN, first = t0 - skew;
+      uint4 u[2];
+      if (first >= 0 && first + 2 * VN <= a.vocab) {
+        u[0] = ld_piece(base + first);
+        u[1] = ld_piece(base + first + VN);
+      } else {
+        T e[2 * VN];
+#pragma unroll
+        for (int i = 0; i < 2 * VN; ++i) e[i] = first + i >= t0 && first + i < min(t0 + VN, a.vocab) ? base[first + i] : T(-INFINITY);
+        u[0] = reinterpret_cast<const uint4*>(e)[0];
+        u[1] = reinterpret_cast<const uint4*>(e)[1];
       }
 #pragma unroll
       for (int y = 0; y < NV; ++y)
-        if (y == v) w[y] = u;
+        if (y == v) {
+          lo[y] = u[0];
+          hi[y] = u[1];
+        }
     }
   };
   if (tid == 0) s_n = 0;
@@ -228,57 +308,142 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
   };
   // Once the list has k entries, chunks go by in groups without a barrier: what is above the bound is added, up to the list's end.  A group
   // that would add more than there is room for (logits that rise along the row) is gone through again, chunk by chunk.
-  constexpr int kAhead = 2;
-  uint4 ahead[kAhead][NV];
-  bool again = false;                              // the same in all threads, like c
-  int again_end = c_lo;
-  int c = c_lo, group_end = c_lo;                  // chunks before group_end go by without a barrier
-  float m_group = m, sum_group = sum;              // as they were where the group began
+  uint4 w0[NV], w1[NV];                            // chunks c and c + 1; of a row with skew the two pieces of chunk c
+  int c = c_lo, again_end = c_lo;                  // (the same in all threads, like n and least)
   auto fetch = [&]() {
+    if (skew) {
+      if (c < c_hi) load_two(c, w0, w1);
+    } else {
+      if (c < c_hi) load(c, w0);
+      if (c + 1 < c_hi) load(c + 1, w1);
+    }
+  };
+  // the chunk's logits out of their registers, and loads into those; returns the largest
+  auto unpack_all = [&](float (&x)[EL], const uint4 (&u)[NV]) -> float {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      if (c + j < c_hi) load(c + j, ahead[j]);
+    for (int v = 0; v < NV; ++v) unpack(u[v], x + v * VN, T());
+    return max_of(u, T());
+  };
+  auto take_straight = [&](float (&x)[EL], uint4 (&w)[NV], int at_c) -> float {
+    const float top = unpack_all(x, w);
+    if (at_c + 2 < c_hi) load(at_c + 2, w);
+    return top;
+  };
+  auto take_skewed = [&](float (&x)[EL], int at_c) -> float {
+    uint4 u[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) u[v] = join<T>(w0[v], w1[v], skew);
+    const float top = unpack_all(x, u);
+    if (at_c + 1 < c_hi) load_two(at_c + 1, w0, w1);
+    return top;
+  };
+  // few are added: they are read again, so that one short loop does for all places
+  auto add = [&](int first, uint32_t mask) {
+    while (mask) {
+      const int t = first + token_of<EL, VN>(__ffs(mask) - 1);
+      mask &= mask - 1;
+      const float v = to_f(base[t]);
+      const int to = atomicAdd(&s_n, 1);
+      if (to < kList) s_list[to] = make_uint2(v < INFINITY ? okey(v + 0.f) : okey(-INFINITY), (uint32_t)t);
+    }
+  };
+  // the thread's logits into its maximum and sum; returns the largest of them
+  auto account = [&](float (&x)[EL], float mine) -> float {
+    const float m_was = m;
+    float part = weigh(x, mine, m);
+    if (!(part < INFINITY)) {
+      // a logit that is NaN or +infinity is none that can be chosen: as -infinity
+      set_status(a.status, RTP_ERR_INVALID);
+      mine = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < EL; ++i) {
+        if (!(x[i] < INFINITY)) x[i] = -INFINITY;
+        mine = fmaxf(mine, x[i]);
+      }
+      m = m_was;
+      part = weigh(x, mine, m);
+    }
+    if (m != m_was) sum *= m_was == -INFINITY ? 0.f : fast_ex2((m_was - m) * kLog2e);
+    sum += part;
+    return mine;
+  };
+  // a chunk of a group (logits behind the row's end are -infinity: not above any bound)
+  auto stream = [&](float (&x)[EL], float top, int at_c, float at) {
+    if (account(x, top) > at) {
+      uint32_t mask = 0;
+#pragma unroll
+      for (int i = 0; i < EL; ++i)
+        if (x[i] > at) mask |= 1u << i;
+      add(at_c * kChunk + tid * VN, mask);
+    }
   };
   fetch();
 #pragma unroll 1
   while (c < c_hi) {
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j, ++c) {
-      if (c >= c_hi) break;
-      float x[EL];
-#pragma unroll
-      for (int v = 0; v < NV; ++v) unpack(ahead[j][v], x + v * VN, T());
-      if (c + kAhead < c_hi) load(c + kAhead, ahead[j]);
-      const int first = c * kChunk - skew + tid * VN;   // token of the thread's first logit (may be negative)
-      float mine = x[0];
-#pragma unroll
-      for (int i = 1; i < EL; ++i) mine = fmaxf(mine, x[i]);   // (NaN is passed over)
-      // running maximum and sum
-      const float m_was = m;
-      float part = weigh(x, mine, m);
-      if (!(part < INFINITY)) {
-        // a logit that is NaN or +infinity is none that can be chosen: as -infinity
-        set_status(a.status, RTP_ERR_INVALID);
-        mine = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < EL; ++i) {
-          if (!(x[i] < INFINITY)) x[i] = -INFINITY;
-          mine = fmaxf(mine, x[i]);
+    if (n >= a.k && c >= again_end) {
+      const int begin = c, end = min(c + kGroup, c_hi);
+      const float m_was = m, sum_was = sum, at = okey_to_float(max(least, okey(-INFINITY)));
+      if (skew) {
+#pragma unroll 1
+        for (; c < end; ++c) {
+          float x[EL];
+          const float top = take_skewed(x, c);
+          stream(x, top, c, at);
         }
-        m = m_was;
-        part = weigh(x, mine, m);
+      } else {
+#pragma unroll 1
+        for (; c < end; c += 2) {
+          float x[EL];
+          const float top = take_straight(x, w0, c);
+          stream(x, top, c, at);
+          if (c + 1 < end) {                       // (an odd group is the last one)
+            float y[EL];
+            const float top1 = take_straight(y, w1, c + 1);
+            stream(y, top1, c + 1, at);
+          }
+        }
+        c = end;
       }
-      if (m != m_was) sum *= m_was == -INFINITY ? 0.f : fast_ex2((m_was - m) * kLog2e);
-      sum += part;
+      __syncthreads();
+      const int have = s_n;
+      __syncthreads();
+      if (have > kList) {
+        again_end = end;
+        c = begin;
+        m = m_was;
+        sum = sum_was;
+        if (tid == 0) s_n = n;
+        fetch();
+        __syncthreads();
+        continue;
+      }
+      n = have;
+      if (n > 2 * a.k + 16) cut();
+      continue;
+    }
+    {
+      float x[EL], mine;
+      if (skew) {
+        mine = take_skewed(x, c);
+      } else {
+        mine = take_straight(x, w0, c);        // (chunk c + 2 into w0, which then change places)
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          const uint4 u = w0[v];
+          w0[v] = w1[v];
+          w1[v] = u;
+        }
+      }
+      const int first = c * kChunk + tid * VN;     // token of the thread's first logit
+      mine = account(x, mine);
       // keys order like the logits; 0: the thread has no token here (-infinity is a token that is ruled out)
-      auto token_of = [&](int i) { return first + (i / VN) * kThreads * VN + i % VN; };
       uint32_t valid = (1u << EL) - 1u;            // a bit for each of the thread's logits; pieces may reach over the row's ends
       if (!whole(c)) {
 #pragma unroll
         for (int i = 0; i < EL; ++i)
-          if (token_of(i) < 0 || token_of(i) >= a.vocab) valid &= ~(1u << i);
+          if (first + token_of<EL, VN>(i) >= a.vocab) valid &= ~(1u << i);
       }
-      const uint32_t key = valid ? okey(mine) : 0u;
+      const uint32_t key = valid ? okey(mine + 0.f) : 0u;   // (-0 is 0)
       // the thread's logits of key `bound` and above; those above it
       auto from = [&](uint32_t bound) {
         const float at = bound <= okey(-INFINITY) ? -INFINITY : okey_to_float(bound);
@@ -296,20 +461,6 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
           if (x[i] > at) mask |= 1u << i;
         return bound < okey(-INFINITY) ? valid : mask & valid;
       };
-      // few are added: they are read again, so that one short loop does for all places
-      auto add = [&](uint32_t mask) {
-        while (mask) {
-          const int t = token_of(__ffs(mask) - 1);
-          mask &= mask - 1;
-          const float v = to_f(base[t]);
-          const int to = atomicAdd(&s_n, 1);
-          if (to < kList) s_list[to] = make_uint2(v < INFINITY ? okey(v) : okey(-INFINITY), (uint32_t)t);
-        }
-      };
-      if (c < group_end) {
-        if (key > least) add(above(least));
-        continue;
-      }
       if (n > kKeep) cut();
       const uint32_t bound = max(search(key, 0u), 1u);
       const uint32_t reach = key >= bound ? from(bound) : 0u, over = key >= bound ? above(bound) : 0u;
@@ -321,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) reached += s_scan[w];
       const bool all = reached <= kAdd;            // else too many equal the bound: the first of them are taken in order
-      add(all ? reach : over);
+      add(first, all ? reach : over);
       __syncthreads();
       const int added = s_n - n;
       n = s_n;
@@ -360,32 +511,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
       else if (n >= a.k) cut();                    // (short chunks: their entries' k-th best)
       __syncthreads();
     }
-    if (c < group_end && c < c_hi) continue;
-    if (group_end > c_lo && !again) {              // the end of a group
-      __syncthreads();
-      const int have = s_n;
-      __syncthreads();
-      if (have > kList) {
-        again = true;
-        c = group_end - kGroup;
-        m = m_group;
-        sum = sum_group;
-        if (tid == 0) s_n = n;
-        fetch();
-        again_end = group_end;
-        group_end = c_lo;
-        __syncthreads();
-        continue;
-      }
-      n = have;
-      if (n > 2 * a.k + 16) cut();
-    }
-    if (again && c >= again_end) again = false;
-    if (!again && n >= a.k && c < c_hi) {
-      group_end = c + kGroup;
-      m_group = m;
-      sum_group = sum;
-    }
+    ++c;
   }
   __syncthreads();
   order();
@@ -537,15 +663,15 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_consta
   }
 }
 
-// How a row is cut: chunks of 4096 logits, of 2048 in calls that would leave SMs idle; and as many slices as make one wave of four CTAs
+// How a row is cut: chunks of 4096 logits, of 2048 if they are 32-bit or in calls that would leave SMs idle; and as many slices as make one wave of four CTAs
 // per SM, each of whole chunks.
 struct BeamCut {
   int el, chunks, slices;                          // logits per thread and chunk, chunks per slice, slices per row
 };
-BeamCut beam_cut(int64_t rows, int64_t vocab, int sm_count) {
+BeamCut beam_cut(int64_t rows, int64_t vocab, bool wide, int sm_count) {
   BeamCut c;
-  c.el = rows * vocab >= (int64_t)sm_count * kThreads * 32 ? 16 : 8;
-  const int64_t chunks = (vocab + 7 + (int64_t)kThreads * c.el - 1) / ((int64_t)kThreads * c.el);   // (7: a row's skew)
+  c.el = !wide && rows * vocab >= (int64_t)sm_count * kThreads * 32 ? 16 : 8;
+  const int64_t chunks = (vocab + (int64_t)kThreads * c.el - 1) / ((int64_t)kThreads * c.el);
   const int64_t want = std::max<int64_t>(1, std::min(chunks, (int64_t)4 * sm_count / rows));
   c.chunks = (int)((chunks + want - 1) / want);
   c.slices = (int)((chunks + c.chunks - 1) / c.chunks);
@@ -555,14 +681,17 @@ BeamCut beam_cut(int64_t rows, int64_t vocab, int sm_count) {
 template <class T>
 cudaError_t launch_slices(const BeamArgs& a, int el, int64_t rows, cudaStream_t st) {
   const dim3 grid((unsigned)(rows * a.n_slices)), block(kThreads);
-  (void)launch_chained(el == 16 ? beam_slice_kernel<T, 16> : beam_slice_kernel<T, 8>, grid, block, 0, st, a);
+  auto kernel = beam_slice_kernel<T, 8>;
+  if constexpr (sizeof(T) == 2)
+    if (el == 16) kernel = beam_slice_kernel<T, 16>;
+  (void)launch_chained(kernel, grid, block, 0, st, a);
   return cudaGetLastError();
 }
 
 }  // namespace
 
 size_t beam_workspace_bytes(int64_t rows, int64_t vocab, int k, int sm_count) {
-  const int64_t lists = rows * beam_cut(rows, vocab, sm_count).slices;
+  const int64_t lists = rows * std::max(beam_cut(rows, vocab, false, sm_count).slices, beam_cut(rows, vocab, true, sm_count).slices);
   return (size_t)lists * (k * sizeof(Cand) + sizeof(float2) + sizeof(int32_t)) + 2 * 256;
 }
 
@@ -570,11 +699,11 @@ cudaError_t launch_beam_select(const void* logits, int format, int64_t row_strid
                                const float* scores, const int32_t* finished, int pad_token, int k, int32_t* parent, int32_t* token,
                                float* scores_out, void* ws, int32_t* status, int sm_count, cudaStream_t st) {
   const int64_t rows = n_groups * n_beams;
-  const BeamCut cut = beam_cut(rows, vocab, sm_count);
+  const BeamCut cut = beam_cut(rows, vocab, format == RTP_LOGITS_F32, sm_count);
   BeamArgs a = {logits, row_stride, n_beams, (int32_t)vocab, k, cut.slices, cut.chunks, pad_token, scores, finished,
                 nullptr, nullptr, nullptr, parent, token, scores_out, status};
   const int64_t lists = rows * a.n_slices, group_lists = (int64_t)n_beams * a.n_slices;
-  if (lists >= (int64_t)1 << 31 || group_lists > 20000) return cudaErrorNotSupported;
+  if (lists >= (int64_t)1 << 31) return cudaErrorNotSupported;
   char* p = reinterpret_cast<char*>(ws);
   a.cand = reinterpret_cast<Cand*>(p);
   p += ((size_t)lists * k * sizeof(Cand) + 255) & ~(size_t)255;

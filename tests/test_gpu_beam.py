@@ -90,6 +90,26 @@ def test_ended_hypotheses_keep_their_score():
     assert check(x[:1], s[:1], i32([1]), 1, 2) == rb.RTP_OK
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("V", [50, 9001, 70000])
+def test_zeros_of_either_sign_are_equal(V, dtype):
+    x = torch.full((4, V), -0.0, device=DEV)
+    x[:, 1::3] = 0.0
+    x[2:, ::5] = -1.0
+    x[:, V // 2:] *= -1.0
+    x[1, V - 5:] = 2.0
+    assert check(x.to(dtype), None, None, 2, 40) == rb.RTP_OK
+
+
+def test_logits_that_rise_along_the_row():
+    """Every group of chunks has more above the bound than a list holds."""
+    V = 300000
+    x = torch.arange(2 * V, device=DEV).remainder(V).reshape(2, V).float() / 1024
+    assert check(x, None, None, 2, 64) == rb.RTP_OK
+    x[1] = x[1].flip(0)
+    assert check(x, None, None, 1, 3) == rb.RTP_OK
+
+
 def test_peaked_rows_and_large_magnitudes():
     x = torch.zeros((4, 9000), device=DEV)
     x[0, 8999], x[1, 0], x[2] = 80.0, 1e4, -1e4
