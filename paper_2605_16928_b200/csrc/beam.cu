@@ -25,6 +25,8 @@ constexpr int kKeep = 512;               // a list that is longer is cut to its 
 constexpr int kList = kKeep + kAdd;
 constexpr int kShort = 64;               // lists that are ordered without a bound
 constexpr int kSelect = 256;
+constexpr int kTops = kThreads / 4;
+static_assert(kTops >= RTP_MAX_BEAM_K, "a bound is the k-th of them");
 constexpr int kGroup = 8;                // chunks between two barriers
 
 struct Cand {
@@ -170,6 +172,8 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
   __shared__ __align__(16) uint2 s_list[kList];    // ordered key, token
   __shared__ __align__(16) uint2 s_sel[kSelect];
   __shared__ uint2 s_best[RTP_MAX_BEAM_K];
+  __shared__ __align__(16) uint32_t s_top[kTops];
+  __shared__ uint32_t s_range[2];
   __shared__ float s_max[kWarps], s_sum[kWarps];
   __shared__ int s_n, s_sel_n, s_scan[kWarps];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -241,22 +245,38 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
   int n = 0;                                       // entries of the list (the same in all threads, like what follows)
   uint32_t least = 0;                              // a key that k entries of the list reach, once there are as many
   float m = -INFINITY, sum = 0.f;                  // this thread's
-  // The largest bound that k threads' keys reach (or that a few more do), at least lo.
-  auto search = [&](uint32_t key, uint32_t lo) -> uint32_t {
-    const uint32_t w = __reduce_max_sync(0xffffffffu, key);
+  // The largest bound that k threads' keys reach (or that a few more do), or 0.  The k-th largest of 64 keys, each the largest of four
+  // threads', is one that k threads reach, and few more do unless k is near 64: from there the search goes on by halves.
+  auto search = [&](uint32_t key) -> uint32_t {
+    uint32_t four = max(key, __shfl_xor_sync(0xffffffffu, key, 1));
+    four = max(four, __shfl_xor_sync(0xffffffffu, four, 2));
     __syncthreads();
-    if (lane == 0) s_scan[warp] = (int)w;
+    if ((lane & 3) == 0) s_top[tid >> 2] = four;
+    if (tid == 0) {
+      s_range[0] = 0xffffffffu;
+      s_range[1] = 0u;
+    }
     __syncthreads();
-    uint32_t hi = 0;
+    int more = 0;                                  // keys above this one, a quarter of them in each of its threads
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i) hi = max(hi, (uint32_t)s_scan[i]);
-    while (lo < hi) {
-      const uint32_t mid = lo + (hi - lo) / 2 + 1;
+    for (int i = 0; i < kTops / 4; i += 4) {
+      const uint4 o = *reinterpret_cast<const uint4*>(s_top + (lane & 3) * (kTops / 4) + i);
+      more += (o.x > four) + (o.y > four) + (o.z > four) + (o.w > four);
+    }
+    more += __shfl_xor_sync(0xffffffffu, more, 1);
+    more += __shfl_xor_sync(0xffffffffu, more, 2);
+    const uint32_t w_lo = __reduce_min_sync(0xffffffffu, more < a.k ? four : 0xffffffffu), w_hi = __reduce_max_sync(0xffffffffu, four);
+    if (lane == 0) {
+      atomicMin(&s_range[0], w_lo);                // (the k-th largest is the least that fewer than k are above)
+      atomicMax(&s_range[1], w_hi);
+    }
+    __syncthreads();
+    uint32_t lo = s_range[0], hi = s_range[1];
+    for (uint32_t mid = lo; ; mid = lo + (hi - lo) / 2 + 1) {
       const int r = __syncthreads_count(key >= mid);
       if (r >= a.k) lo = mid; else hi = mid - 1;
-      if (r >= a.k && r <= a.k + kSlack) break;
+      if (lo >= hi || (r >= a.k && r <= a.k + kSlack)) return lo;
     }
-    return lo;
   };
   // The list's k best in their order, counted out; of a long list only those that reach a bound of its threads' best.
   auto rank_of = [&](const uint2* v, int count, uint2 me) {
@@ -277,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
     if (n > kShort) {
       uint32_t best = 0;
       for (int i = tid; i < n; i += kThreads) best = max(best, s_list[i].x);
-      const uint32_t bound = search(best, 0u);
+      const uint32_t bound = search(best);
       if (tid == 0) s_sel_n = 0;
       __syncthreads();
       for (int i = tid; i < n; i += kThreads)
@@ -462,7 +482,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
         return bound < okey(-INFINITY) ? valid : mask & valid;
       };
       if (n > kKeep) cut();
-      const uint32_t bound = max(search(key, 0u), 1u);
+      const uint32_t bound = max(search(key), 1u);
       const uint32_t reach = key >= bound ? from(bound) : 0u, over = key >= bound ? above(bound) : 0u;
       const int w_reach = __reduce_add_sync(0xffffffffu, __popc(reach));
       __syncthreads();
@@ -555,21 +575,38 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_consta
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t row0 = (int64_t)blockIdx.x * a.n_beams;
   const int lists = a.n_beams * a.n_slices;
+  // The lists are on their way while the normalisers are made.
+  constexpr int kEarly = 4;
+  const Cand* cand = a.cand + row0 * a.n_slices * a.k;
+  Cand early[kEarly];
+#pragma unroll
+  for (int j = 0; j < kEarly; ++j) {
+    const int e = tid + j * kThreads;
+    early[j] = e < cached ? cand[e] : Cand{0.f, 0};
+  }
+  for (int l = tid; l < lists; l += kThreads) {
+    const int b = l / a.n_slices, count = a.count[row0 * a.n_slices + l];
+    s_at[l] = 0;
+    s_cnt[l] = a.finished && a.finished[row0 + b] != 0 ? (l == b * a.n_slices) : (uint8_t)count;
+  }
   for (int b = warp; b < a.n_beams; b += kWarps) {
     const int64_t row = row0 + b;
-    float m = -INFINITY;
     const float2* st = a.stat + row * a.n_slices;
+    const float2 first = lane < a.n_slices ? st[lane] : make_float2(-INFINITY, 0.f);   // (nothing of a row that has ended is used)
+    double off = a.scores ? (double)a.scores[row] : 0.0;
     const bool ended = a.finished && a.finished[row] != 0;
-    if (!ended)
-      for (int s = lane; s < a.n_slices; s += 32) m = fmaxf(m, st[s].x);
-    m = warp_max(m);
+    float m = first.x;
+    for (int s = lane + 32; s < a.n_slices; s += 32) m = fmaxf(m, st[s].x);
+    m = ended ? -INFINITY : warp_max(m);
     double z = 0.0;
-    if (m != -INFINITY)
-      for (int s = lane; s < a.n_slices; s += 32) z += (double)st[s].y * exp((double)st[s].x - (double)m);
+    if (m != -INFINITY) {
+      // (a term's error is 2^-22 of it, the difference's rounding included where the term counts)
+      z = (double)first.y * (double)expf(first.x - m);
+      for (int s = lane + 32; s < a.n_slices; s += 32) z += (double)st[s].y * (double)expf(st[s].x - m);
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
     if (lane == 0) {
-      double off = a.scores ? (double)a.scores[row] : 0.0;
       if (!(off < (double)INFINITY)) {
         set_status(a.status, RTP_ERR_INVALID);
         off = -(double)INFINITY;
@@ -580,20 +617,13 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_consta
       s_max[b] = m;
     }
   }
-  for (int l = tid; l < lists; l += kThreads) {
-    const int b = l / a.n_slices;
-    s_at[l] = 0;
-    s_cnt[l] = a.finished && a.finished[row0 + b] != 0 ? (l == b * a.n_slices) : (uint8_t)a.count[row0 * a.n_slices + l];
-  }
   __syncthreads();
-  const Cand* cand = a.cand + row0 * a.n_slices * a.k;
-  auto entry = [&](int l, int i, int& token) -> uint64_t {   // an entry of a list; keys order like scores
+  auto entry = [&](int l, const Cand& c, int& token) -> uint64_t {   // of a list; keys order like scores
     const int b = l / a.n_slices;
     double score = s_off[b];
     if (s_state[b] == 1) {
       token = a.pad_token;
     } else {
-      const Cand c = cand[l * a.k + i];
       token = c.token;
       score = s_state[b] == 2 ? -(double)INFINITY : score + ((double)c.x - (double)s_max[b]);
     }
@@ -601,10 +631,14 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_consta
     return (u >> 63) ? ~u : u | 0x8000000000000000ull;
   };
   if (cached) {
-    for (int e = tid; e < lists * a.k; e += kThreads) {
-      const int l = e / a.k, i = e - l * a.k;
-      if (i < s_cnt[l]) s_key[e] = entry(l, i, s_tok[e]);
-    }
+    auto keep = [&](int e, const Cand& c) {
+      const int l = e / a.k;
+      if (e - l * a.k < s_cnt[l]) s_key[e] = entry(l, c, s_tok[e]);
+    };
+#pragma unroll
+    for (int j = 0; j < kEarly; ++j)
+      if (tid + j * kThreads < cached) keep(tid + j * kThreads, early[j]);
+    for (int e = tid + kEarly * kThreads; e < cached; e += kThreads) keep(e, cand[e]);
     __syncthreads();
   }
   const int threads = lists <= 128 ? 32 : kThreads;        // that do the rounds
@@ -618,7 +652,7 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_consta
       const int i = s_at[l];
       if (i >= s_cnt[l]) continue;
       int token = 0;
-      const uint64_t key = cached ? s_key[l * a.k + i] : entry(l, i, token);
+      const uint64_t key = cached ? s_key[l * a.k + i] : entry(l, s_state[l / a.n_slices] == 1 ? Cand{0.f, 0} : cand[l * a.k + i], token);
       if (key > best) {
         best = key;
         best_l = l;
