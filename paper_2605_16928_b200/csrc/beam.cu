@@ -383,18 +383,23 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
       m = m_was;
       part = weigh(x, mine, m);
     }
-    if (m != m_was) sum *= m_was == -INFINITY ? 0.f : fast_ex2((m_was - m) * kLog2e);
-    sum += part;
+    sum = sum * fast_ex2((m_was - (m == -INFINITY ? 0.f : m)) * kLog2e) + part;   // (nothing yet: 0 * 0)
     return mine;
   };
   // a chunk of a group (logits behind the row's end are -infinity: not above any bound)
   auto stream = [&](float (&x)[EL], float top, int at_c, float at) {
-    if (account(x, top) > at) {
+    const float mine = account(x, top);
+    if (mine > at) {
       uint32_t mask = 0;
 #pragma unroll
       for (int i = 0; i < EL; ++i)
         if (x[i] > at) mask |= 1u << i;
-      add(at_c * kChunk + tid * VN, mask);
+      if ((mask & (mask - 1)) == 0) {              // mostly one: the largest
+        const int to = atomicAdd(&s_n, 1);
+        if (to < kList) s_list[to] = make_uint2(okey(mine + 0.f), (uint32_t)(at_c * kChunk + tid * VN + token_of<EL, VN>(__ffs(mask) - 1)));
+      } else {
+        add(at_c * kChunk + tid * VN, mask);
+      }
     }
   };
   fetch();
