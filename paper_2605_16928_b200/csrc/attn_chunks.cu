@@ -209,6 +209,21 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     }
     return p.n_sink_tiles + n_all - p.kt_first;
   };
+  // A CTA each for few and short units: a cut of less than two shares each would not end sooner, and nothing has to be summed up (7 rows over
+  // 200 keys: 10 us against 17 by the general way below, over 1000 keys 17 against 24, over 1500 with 12 tiles 25 either way).
+  if (U <= N) {
+    Piece p;
+    if (tid < U) {
+      p.tile_hi = describe(tid, p);
+      p.tile_lo = 0;
+      p.slot = kWhole;
+    }
+    if (!__syncthreads_or(tid < U && (int64_t)p.tile_hi * (p.n_pos > a.bmp ? 2 : 1) > 2 * kMinJobs)) {
+      if (tid < U) plan.pieces[tid] = p;
+      for (int i = tid; i <= N; i += nt) plan.piece_begin[i] = min(i, U);
+      return;
+    }
+  }
   // Costs: the dealt units' go to their CTAs, the others' into a list.
   int rounds = U / N;
   int64_t* before = s.before;
