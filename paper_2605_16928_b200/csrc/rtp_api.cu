@@ -217,7 +217,7 @@ constexpr int kFallbackSm = 148;
 
 extern "C" {
 
-int32_t rtp_version(void) { return 201; }
+int32_t rtp_version(void) { return 202; }
 
 size_t rtp_struct_bytes(int32_t what) { return what == 0 ? sizeof(rtp_params) : (what == 1 ? sizeof(rtp_cache) : 0); }
 
