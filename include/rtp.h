@@ -358,7 +358,8 @@ rtp_status rtp_cache_compact(rtp_ctx* ctx, const rtp_params* params, const rtp_c
  *            sequences are numbered like rows); token DEVICE int32 [n_groups, k]; scores_out DEVICE fp32 [n_groups, k]; best first.
  *            Where a group has fewer than k continuations (ended ones): -1, -1, -infinity behind them.
  * A logit of -infinity is ruled out: its score is -infinity, and it is taken behind all others only.  NaN and +infinity count as
- * -infinity, RTP_ERR_INVALID is recorded (also for a score that is NaN or +infinity).  Scores are compared in 64 bits.
+ * -infinity, RTP_ERR_INVALID is recorded (also for a score that is NaN or +infinity).  Scores are compared in 64 bits; a row's
+ * normaliser is right to 2^-18 and the same for rows of equal logits, zeros of either sign being equal.
  * n_beams <= 64, k <= 64, k <= n_beams * vocab.  workspace: rtp_beam_workspace_bytes(n_groups * n_beams, vocab, k). */
 #define RTP_LOGITS_F32 0
 #define RTP_LOGITS_BF16 1
@@ -599,7 +600,7 @@ rtp_status rtp_dense_attn_decode(rtp_ctx* ctx, const rtp_params* params, const r
  *          RTP_CHUNK_BY_HEAD local heads over sinks and window, retrieval query heads of a mixed group and all other KV heads over
  *                            all keys: a layer in the paper's prefill mode (Section 3.2) in one call.
  * kv_heads HOST int32 [n_heads], each once, or NULL: all.  Any group size n_q_heads / n_kv_heads.
- * out, lse as rtp_dense_attn_prefill (a row that sees no key: 0, -infinity).  A position beyond its sequence, a sequence or an offset out
+ * out, lse as rtp_dense_attn_prefill (a row that sees no key: 0, -infinity); out must not overlap q.  A position beyond its sequence, a sequence or an offset out
  * of range: RTP_ERR_INVALID in the status word; such rows see the keys that there are, chunks with wrong offsets are left out.
  * K and V of all positions up to a chunk's last row are taken as finite: one that is not may reach every row of its tile of 128 keys.
  * bf16 caches (RTP_ERR_UNSUPPORTED on a 4-bit one).  On a truncated cache a chunk of local heads needs ring_pages * 64 >= window +

@@ -24,6 +24,7 @@ namespace rtp {
 
 // 3-D tensor map of query rows [rows][n_heads][128] bf16 with a box of box_rows x box_heads x 64 (tensor_map.cu).
 cudaError_t make_heads_map(CUtensorMap* map, const void* base, int64_t rows, int n_heads, int box_heads, int box_rows, int swizzle);
+cudaError_t encode_rows_map(CUtensorMap* map, const void* base, int64_t rows, int row_elems, int box_cols, int box_rows, int swizzle);
 
 namespace {
 
@@ -883,10 +884,10 @@ cudaError_t launch_attn_chunks(const CacheView& cv, const CacheView& lv, const D
   Maps maps = {};
   const int swz = (int)CU_TENSOR_MAP_SWIZZLE_128B;
   cudaError_t e = make_heads_map(&maps.q, q, R, d.n_q, d.group, bmp, swz);
-  if (e == cudaSuccess && cv.n_kv > 0) e = make_rows_map(&maps.k, cv.k, (int64_t)cv.num_pages * cv.n_kv * kPage, kHeadDim, 64, kPage, swz);
-  if (e == cudaSuccess && cv.n_kv > 0) e = make_rows_map(&maps.v, cv.v, (int64_t)cv.num_pages * cv.n_kv * kPage, kHeadDim, 64, kPage, swz);
-  if (e == cudaSuccess && lv.n_kv > 0) e = make_rows_map(&maps.lk, lv.k, (int64_t)lv.num_pages * lv.n_kv * kPage, kHeadDim, 64, kPage, swz);
-  if (e == cudaSuccess && lv.n_kv > 0) e = make_rows_map(&maps.lv, lv.v, (int64_t)lv.num_pages * lv.n_kv * kPage, kHeadDim, 64, kPage, swz);
+  if (e == cudaSuccess && cv.n_kv > 0) e = encode_rows_map(&maps.k, cv.k, (int64_t)cv.num_pages * cv.n_kv * kPage, kHeadDim, 64, kPage, swz);
+  if (e == cudaSuccess && cv.n_kv > 0) e = encode_rows_map(&maps.v, cv.v, (int64_t)cv.num_pages * cv.n_kv * kPage, kHeadDim, 64, kPage, swz);
+  if (e == cudaSuccess && lv.n_kv > 0) e = encode_rows_map(&maps.lk, lv.k, (int64_t)lv.num_pages * lv.n_kv * kPage, kHeadDim, 64, kPage, swz);
+  if (e == cudaSuccess && lv.n_kv > 0) e = encode_rows_map(&maps.lv, lv.v, (int64_t)lv.num_pages * lv.n_kv * kPage, kHeadDim, 64, kPage, swz);
   if (e != cudaSuccess) return e;
   static PerDeviceOnce once_plan, once_attn;
   e = set_dyn_smem_once(plan_kernel, (int)plan_smem(kMaxChunks), once_plan);

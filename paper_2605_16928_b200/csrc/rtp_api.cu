@@ -926,6 +926,7 @@ rtp_status rtp_attn_chunks(rtp_ctx* ctx, const rtp_params* params, const rtp_cac
   if (cv.kv_fp4) return fail(ctx, RTP_ERR_UNSUPPORTED, "4-bit K/V cache: decode calls only (or rtp_kv_expand its pages)");
   if (!q || !out || !chunk_seq || !chunk_start || !row_offsets || !workspace) return fail(ctx, RTP_ERR_INVALID, "NULL argument");
   if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return fail(ctx, RTP_ERR_INVALID, "misaligned pointer");
+  if (q == out) return fail(ctx, RTP_ERR_INVALID, "out cannot be q");   // (pieces of a unit read its queries at different times)
   bool is_local[32] = {}, named[32] = {};
   for (int i = 0; i < params->n_local_kv_heads; ++i) is_local[params->local_kv_heads[i]] = true;
   ChunkHeads ch = {};

@@ -28,6 +28,22 @@ EncodeTiledFn encode_fn(cudaError_t* err) {
 }
 }  // namespace
 
+cudaError_t encode_rows_map(CUtensorMap* map, const void* base, int64_t rows, int row_elems, int box_cols, int box_rows,
+                            int swizzle) {
+  cudaError_t e = cudaSuccess;
+  EncodeTiledFn encode = encode_fn(&e);
+  if (!encode) return e;
+  const cuuint64_t dims[2] = {(cuuint64_t)row_elems, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)row_elems * 2};
+  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, (CUtensorMapSwizzle)swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return cudaErrorInvalidValue;
+  return cudaSuccess;
+}
+
 // A descriptor depends only on (base, rows, row length, box, swizzle): the last few are kept, so a cache that does
 // not move is encoded once instead of once per launch.  (The descriptor holds a global address, which is the same
 // number on every device of the process only by accident: the device ordinal is part of the key.)
@@ -63,16 +79,8 @@ cudaError_t make_rows_map(CUtensorMap* map, const void* base, int64_t rows, int 
         return cudaSuccess;
       }
   }
-  EncodeTiledFn encode = encode_fn(&e);
-  if (!encode) return e;
-  const cuuint64_t dims[2] = {(cuuint64_t)row_elems, (cuuint64_t)rows};
-  const cuuint64_t strides[1] = {(cuuint64_t)row_elems * 2};
-  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
-  const cuuint32_t estr[2] = {1, 1};
-  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
-                            CU_TENSOR_MAP_INTERLEAVE_NONE, (CUtensorMapSwizzle)swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return cudaErrorInvalidValue;
+  e = encode_rows_map(map, base, rows, row_elems, box_cols, box_rows, swizzle);
+  if (e != cudaSuccess) return e;
   std::lock_guard<std::mutex> lock(g_map_mu);
   g_map_key[g_map_next] = key;
   g_map_val[g_map_next] = *map;

@@ -340,7 +340,7 @@ def test_refusals():
 
     assert call() == rb.RTP_OK and call(n=0) == rb.RTP_OK and call(R=0) == rb.RTP_OK
     for over in (dict(q=None), dict(s=None), dict(st=None), dict(o=None), dict(out=None), dict(ws=None), dict(n=-1), dict(R=-1), dict(pat=3), dict(pat=-1),
-                 dict(q=b.q.data_ptr() + 8), dict(kv=heads, nh=2), dict(kv=heads, nh=-1)):
+                 dict(q=b.q.data_ptr() + 8), dict(kv=heads, nh=2), dict(kv=heads, nh=-1), dict(out=b.q.data_ptr())):
         assert call(**over) == rb.RTP_ERR_INVALID, over
     assert call(n=8193) == call(R=1 << 30) == rb.RTP_ERR_UNSUPPORTED
     assert call(bytes=b.ws.nbytes // 2) == rb.RTP_ERR_CAPACITY
