@@ -18,6 +18,14 @@
 // Jobs alternate between the groups.  A unit of more than BMP positions has two Q tiles, one per group, over the same K / V tiles
 // (half the traffic); a smaller one has one, and the groups take every other key tile and are joined at the end, straight from TMEM.
 // S and P of a group share 128 columns: S of its next job is issued behind the P V that reads P, and the tensor core runs them in order.
+//
+// Bound and measured (8 KV heads, groups of 4, device time).  Long chunks: the tensor cores, 2048 rows over 32K keys 830 us = 1283 TFLOP/s
+// of 1694 that a library product reaches (1000 us by the prefill kernel of the other calls); what is missing is the chain S -> softmax ->
+// P -> next S of each group, of which two cover each other but not all of it, and the shared issue slots of the issuing warp and the softmax
+// warps.  Few rows: DRAM, 5 rows each of 32 sequences of 8K keys 120 us = 5.3 TB/s.  A mixture of pieces and single rows: both in turn,
+// 12 chunks up to 700 rows over up to 32K keys 272 us.  7 rows over 200 keys: two launches and one chain of loads and products, 10 us.
+// Tried and left: exponentials by polynomial on the FMA pipe (slower: one warp per scheduler is issue bound), P through shared memory,
+// a 56 / 224 register split, rolled loops, the merge launched ahead (no difference).
 #include "tc_common.cuh"
 
 namespace rtp {

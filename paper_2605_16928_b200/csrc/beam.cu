@@ -1,13 +1,19 @@
 // Selection of a beam search step: the k best continuations of every group of beams, score = scores[beam] + log_softmax(logits)[token],
 // equal scores going to the lower (beam, token).
 //
-// Bound by the one read of the logits.  A row is cut into slices of whole chunks, one CTA each, whose threads hold the logits of a
-// chunk in registers while the next ones are on their way; every thread keeps a running maximum and sum of exponentials of its own.
-// The slice's k best tokens need no sort of the chunks: in the first one, the k-th largest of the 256 threads' maxima is a lower bound
-// of the k-th largest logit that only a few more than k logits reach.  Those go to a list, and of the later chunks only what lies
-// above the list's bound.  A second kernel, one CTA per group, joins the rows' sums and takes the k best of the sorted lists one by one.
+// A row is cut into slices of whole chunks, one CTA each, whose threads hold the logits of a chunk in registers while the next ones are on
+// their way; every thread keeps a running maximum and sum of exponentials of its own.  The slice's k best tokens need no sort of the
+// chunks: in the first one, the k-th largest of the 256 threads' maxima is a lower bound of the k-th largest logit that only a few more
+// than k logits reach.  Those go to a list, and of the later chunks only what lies above the list's bound.  A second kernel, one CTA per
+// group, joins the rows' sums and takes the k best of the sorted lists one by one.
 // Tokens of one row are ordered by their logits alone; where rows meet, scores are 64-bit (sums of exponentials are 32-bit
 // within a slice, 64-bit across slices), so that neighbours are not swapped by the rounding of a normaliser.
+// Bound by the one read of the logits in principle (10 us for 32 x 8 beams over 128K in bf16); measured 32.5 us: the slices 25.6, of which 5
+// go by before the first list stands (loads of all CTAs at once, search, additions) and the rest is instruction issue and latency (210
+// warp instructions per 512 logits, of which 16 are exponentials and about 60 the additions to the lists), the second kernel 8.
+// 4 beams over 32K: 10 us, two launches of 4 and 7 us, chains of dependent loads, reductions and k rounds.
+// Tried and left: pairs of chunks per step (fewer instructions, more than the instruction cache holds: 31 us for the slices), one copy of
+// the chunk loop (27), groups that grow with the chunks seen (30), the second kernel launched ahead (no difference).
 #include "rtp_device.cuh"
 
 namespace rtp {
@@ -27,7 +33,7 @@ constexpr int kShort = 64;               // lists that are ordered without a bou
 constexpr int kSelect = 256;
 constexpr int kTops = kThreads / 4;
 static_assert(kTops >= RTP_MAX_BEAM_K, "a bound is the k-th of them");
-constexpr int kGroup = 8;                // chunks between two barriers
+constexpr int kGroup = 8;                // chunks between two barriers (the bound is that old)
 
 struct Cand {
   float x;
