@@ -22,18 +22,14 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kMaxEl = 16;               // logits of a chunk per thread
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kSlack = 8;                // the search for the bound stops when that many threads too many reach it
-// Threads whose maximum is above the bound: fewer than k + slack, and each may have all of its logits above it.
-constexpr int kAdd = (RTP_MAX_BEAM_K + kSlack) * kMaxEl + RTP_MAX_BEAM_K;
+constexpr int kSlack = 32;               // the search for the bound stops when that many threads too many reach it
 constexpr int kKeep = 512;               // a list that is longer is cut to its k best before more is added
-constexpr int kList = kKeep + kAdd;
+constexpr int kList = kKeep + kWarps * 32 * 8;   // (a warp adds at most a piece per lane at a time)
 constexpr int kShort = 64;               // lists that are ordered without a bound
 constexpr int kSelect = 256;
 constexpr int kTops = kThreads / 4;
 static_assert(kTops >= RTP_MAX_BEAM_K, "a bound is the k-th of them");
-constexpr int kGroup = 8;                // chunks between two barriers (the bound is that old)
 
 struct Cand {
   float x;
@@ -58,9 +54,6 @@ template <class T> struct Vec;           // 16 bytes of logits
 template <> struct Vec<float> { static constexpr int n = 4; };
 template <> struct Vec<__nv_bfloat16> { static constexpr int n = 8; };
 template <> struct Vec<__half> { static constexpr int n = 8; };
-__device__ __forceinline__ float to_f(float x) { return x; }
-__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
 
 // Pieces to 32 bits.
 __device__ __forceinline__ void unpack(const uint4& w, float* x, float) {
@@ -83,39 +76,59 @@ __device__ __forceinline__ void unpack(const uint4& w, float* x, __half) {
     x[2 * i + 1] = f.y;
   }
 }
-// The thread's largest logit; NaN is passed over (-infinity or NaN if there is nothing else).
-template <int NV>
-__device__ __forceinline__ float max_of(const uint4 (&w)[NV], float) {
+// The thread's largest logit, or NaN if one of them is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+  return m;
+}
+template <int N>
+__device__ __forceinline__ float max_of(const uint4 (&w)[N], float) {
   float m = __uint_as_float(w[0].x);
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const float a = fmaxf(__uint_as_float(w[v].x), __uint_as_float(w[v].y)), b = fmaxf(__uint_as_float(w[v].z), __uint_as_float(w[v].w));
-    m = fmaxf(m, fmaxf(a, b));
-  }
+  for (int v = 0; v < N; ++v)
+    m = max_nan(m, max_nan(max_nan(__uint_as_float(w[v].x), __uint_as_float(w[v].y)), max_nan(__uint_as_float(w[v].z), __uint_as_float(w[v].w))));
   return m;
 }
-template <class P, int NV>
-__device__ __forceinline__ P max_pair(const uint4 (&w)[NV]) {
+template <class P, int N>
+__device__ __forceinline__ P max_pair(const uint4 (&w)[N]) {
   P m = *reinterpret_cast<const P*>(&w[0].x);
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
+  for (int v = 0; v < N; ++v) {
     const P* p = reinterpret_cast<const P*>(&w[v]);
-    m = __hmax2(m, __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3])));
+    m = __hmax2_nan(m, __hmax2_nan(__hmax2_nan(p[0], p[1]), __hmax2_nan(p[2], p[3])));
   }
   return m;
 }
-template <int NV>
-__device__ __forceinline__ float max_of(const uint4 (&w)[NV], __nv_bfloat16) {
+template <int N>
+__device__ __forceinline__ float max_of(const uint4 (&w)[N], __nv_bfloat16) {
   const float2 f = __bfloat1622float2(max_pair<__nv_bfloat162>(w));
-  return fmaxf(f.x, f.y);
+  return max_nan(f.x, f.y);
 }
-template <int NV>
-__device__ __forceinline__ float max_of(const uint4 (&w)[NV], __half) {
+template <int N>
+__device__ __forceinline__ float max_of(const uint4 (&w)[N], __half) {
   const float2 f = __half22float2(max_pair<__half2>(w));
-  return fmaxf(f.x, f.y);
+  return max_nan(f.x, f.y);
 }
-// A thread's i-th logit, counted from its first one.
-template <int EL, int VN>
+// NaN and +infinity become -infinity.
+template <int N>
+__device__ __forceinline__ void rule_out(uint4 (&w)[N], float) {
+  auto f = [](uint32_t u) { return __uint_as_float(u) < INFINITY ? u : 0xff800000u; };
+#pragma unroll
+  for (int v = 0; v < N; ++v) w[v] = make_uint4(f(w[v].x), f(w[v].y), f(w[v].z), f(w[v].w));
+}
+template <int N, class H>
+__device__ __forceinline__ void rule_out(uint4 (&w)[N], H) {
+  const uint32_t none = std::is_same<H, __half>::value ? 0xfc00u : 0xff80u, top = none & 0x7fffu;
+  auto f = [=](uint32_t u) {                       // (a half-word is NaN or infinity from its type's infinity on)
+    const uint32_t lo = (u & 0x7fffu) >= top ? none : u & 0xffffu, hi = ((u >> 16) & 0x7fffu) >= top ? none : u >> 16;
+    return lo | hi << 16;
+  };
+#pragma unroll
+  for (int v = 0; v < N; ++v) w[v] = make_uint4(f(w[v].x), f(w[v].y), f(w[v].z), f(w[v].w));
+}
+// A thread's i-th logit, counted from its first one (in a chunk as in several that follow each other).
+template <int VN>
 __device__ __forceinline__ int token_of(int i) { return (i / VN) * kThreads * VN + i % VN; }
 // Two numbers at a time.
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
@@ -130,20 +143,21 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
       : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return r;
 }
-// m becomes the maximum of m and mine; returns the sum of exp(x - m).  Not below +infinity if one of x is NaN or +infinity.
-// (The maximum is taken off first: the largest logit's term is 1 and nothing else, so that rows with one certain token each are equal,
-// and the type's largest values times log2(e) would be no numbers.)
-template <int EL>
-__device__ __forceinline__ float weigh(const float (&x)[EL], float mine, float& m) {
-  m = fmaxf(m, mine);
-  const float off = m == -INFINITY ? 0.f : -m;
+// The sum of exp(x + off).
+template <class T, int N>
+__device__ __forceinline__ float weigh(const uint4 (&w)[N], float off) {
   const float2 o2 = make_float2(off, off), l2 = make_float2(kLog2e, kLog2e);
   float2 s0 = make_float2(0.f, 0.f), s1 = s0;
 #pragma unroll
-  for (int i = 0; i < EL; i += 4) {
-    const float2 u = mul2(add2(make_float2(x[i], x[i + 1]), o2), l2), v = mul2(add2(make_float2(x[i + 2], x[i + 3]), o2), l2);
-    s0 = add2(s0, make_float2(fast_ex2(u.x), fast_ex2(u.y)));
-    s1 = add2(s1, make_float2(fast_ex2(v.x), fast_ex2(v.y)));
+  for (int v = 0; v < N; ++v) {
+    float x[Vec<T>::n];
+    unpack(w[v], x, T());
+#pragma unroll
+    for (int i = 0; i < Vec<T>::n; i += 4) {
+      const float2 u = mul2(add2(make_float2(x[i], x[i + 1]), o2), l2), y = mul2(add2(make_float2(x[i + 2], x[i + 3]), o2), l2);
+      s0 = add2(s0, make_float2(fast_ex2(u.x), fast_ex2(u.y)));
+      s1 = add2(s1, make_float2(fast_ex2(y.x), fast_ex2(y.y)));
+    }
   }
   s0 = add2(s0, s1);
   return s0.x + s0.y;
@@ -168,20 +182,29 @@ __device__ __forceinline__ uint4 join(const uint4& lo, const uint4& hi, int s) {
   return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
                     __funnelshift_r(w[3], w[4], bits));
 }
+// A piece of which only the logits lo .. hi - 1 exist: the others are -infinity.
+template <class T>
+__device__ __noinline__ uint4 edge_piece(const T* base, int t0, int lo, int hi) {
+  T e[Vec<T>::n];
+#pragma unroll
+  for (int i = 0; i < Vec<T>::n; ++i) e[i] = t0 + i >= lo && t0 + i < hi ? base[t0 + i] : T(-INFINITY);
+  return *reinterpret_cast<const uint4*>(e);
+}
 __device__ __forceinline__ uint4 ld_piece(const void* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
 
 template <class T, int EL>
 __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_constant__ BeamArgs a) {
   chain_wait();
   constexpr int VN = Vec<T>::n, NV = EL / VN, kChunk = kThreads * EL;
-  static_assert(EL % VN == 0 && EL <= kMaxEl, "");
+  static_assert(EL % VN == 0, "");
   __shared__ __align__(16) uint2 s_list[kList];    // ordered key, token
   __shared__ __align__(16) uint2 s_sel[kSelect];
   __shared__ uint2 s_best[RTP_MAX_BEAM_K];
   __shared__ __align__(16) uint32_t s_top[kTops];
   __shared__ uint32_t s_range[2];
+  __shared__ uint8_t s_column[kThreads];
   __shared__ float s_max[kWarps], s_sum[kWarps];
-  __shared__ int s_n, s_sel_n, s_scan[kWarps];
+  __shared__ int s_n, s_sel_n, s_columns, s_scan[kWarps];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t row = blockIdx.x / a.n_slices;
   const int slice = (int)(blockIdx.x - row * a.n_slices);
@@ -193,64 +216,79 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
   const T* base = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
   const int skew = (int)((reinterpret_cast<uintptr_t>(base) & 15u) / sizeof(T));
   const int c_lo = slice * a.chunks, c_hi = min(c_lo + a.chunks, (a.vocab + kChunk - 1) / kChunk);
-  // no piece of the chunk reaches over an end of the row
-  auto whole = [&](int c) { return skew ? c > 0 && (c + 1) * kChunk + VN <= a.vocab : (c + 1) * kChunk <= a.vocab; };
-  auto load = [&](int c, uint4 (&w)[NV]) {          // the thread's pieces of chunk c of a row without skew
-    const T* p = base + c * kChunk + tid * VN;
-    if (whole(c)) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v) w[v] = ld_stream_v4(p + v * kThreads * VN);
-      return;
-    }
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int t0 = c * kChunk + tid * VN + v * kThreads * VN;
-      if (t0 + VN <= a.vocab) {
-        w[v] = ld_stream_v4(base + t0);
-      } else {
-        T e[VN];
-#pragma unroll
-        for (int i = 0; i < VN; ++i) e[i] = t0 + i < a.vocab ? base[t0 + i] : T(-INFINITY);
-        w[v] = *reinterpret_cast<const uint4*>(e);
-      }
+  const int stop = (int)min((int64_t)c_hi * kChunk, (int64_t)a.vocab);     // the slice's tokens end here
+  const uint32_t none = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;   // -infinity
+  // ---- the thread's maximum and sum, two chunks at a time; tokens behind the slice are -infinity
+  auto piece = [&](int t0) -> uint4 {              // of a row without skew
+    return t0 + VN <= stop ? ld_stream_v4(base + t0) : t0 < stop ? edge_piece(base, t0, t0, stop) : make_uint4(none, none, none, none);
+  };
+  auto two_pieces = [&](int t0, uint4& lo, uint4& hi) {   // that hold the logits from t0 on of a row with skew
+    const int first = t0 - skew;
+    if (first >= 0 && first + 2 * VN <= stop) {
+      lo = ld_piece(base + first);
+      hi = ld_piece(base + first + VN);
+    } else if (t0 < stop) {
+      lo = edge_piece(base, first, t0, min(t0 + VN, stop));
+      hi = edge_piece(base, first + VN, t0, min(t0 + VN, stop));
+    } else {
+      lo = hi = make_uint4(none, none, none, none);
     }
   };
-  auto load_two = [&](int c, uint4 (&lo)[NV], uint4 (&hi)[NV]) {   // and of one with
-    const T* p = base + c * kChunk + tid * VN - skew;
-    if (whole(c)) {
+  uint4 wa[2 * NV], wb[2 * NV];                    // chunks c and c + 1, c + 2 and c + 3; of a row with skew the pieces of two chunks
+  auto load_pair = [&](int c, uint4 (&w)[2 * NV]) {
+    const int t0 = c * kChunk + tid * VN;
+    if ((c + 2) * kChunk <= stop) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        lo[v] = ld_piece(p + v * kThreads * VN);
-        hi[v] = ld_piece(p + v * kThreads * VN + VN);
-      }
-      return;
+      for (int v = 0; v < 2 * NV; ++v) w[v] = ld_stream_v4(base + t0 + v * kThreads * VN);
+    } else {
+#pragma unroll
+      for (int v = 0; v < 2 * NV; ++v) w[v] = piece(t0 + v * kThreads * VN);
     }
+  };
+  auto load_pieces = [&](int c) {
+#pragma unroll
+    for (int v = 0; v < 2 * NV; ++v) two_pieces(c * kChunk + tid * VN + v * kThreads * VN, wa[v], wb[v]);
+  };
+  float m = -INFINITY, sum = 0.f;
+  // (The maximum is taken off first: the largest logit's term is 1 and nothing else, so that rows with one certain token each are equal, and
+  // the type's largest values times log2(e) would be no numbers.)
+  auto account = [&](uint4 (&w)[2 * NV]) {
+    float top = max_of(w, T());
+    if (!(top < INFINITY)) {                       // NaN and +infinity are none that can be chosen: as -infinity
+      set_status(a.status, RTP_ERR_INVALID);
+      rule_out(w, T());
+      top = max_of(w, T());
+    }
+    const float m_was = m;
+    m = fmaxf(m, top);
+    const float off = m == -INFINITY ? 0.f : -m;
+    sum = sum * fast_ex2((m_was + off) * kLog2e) + weigh<T>(w, off);   // (nothing yet: 0 * 0)
+  };
+  if (skew) {
+    load_pieces(c_lo);
 #pragma unroll 1
-    for (int v = 0; v < NV; ++v) {
-      const int t0 = c * kChunk + tid * VN + v * kThreads * VN, first = t0 - skew;
-      uint4 u[2];
-      if (first >= 0 && first + 2 * VN <= a.vocab) {
-        u[0] = ld_piece(base + first);
-        u[1] = ld_piece(base + first + VN);
-      } else {
-        T e[2 * VN];
+    for (int c = c_lo; c < c_hi; c += 2) {
+      uint4 u[2 * NV];
 #pragma unroll
-        for (int i = 0; i < 2 * VN; ++i) e[i] = first + i >= t0 && first + i < min(t0 + VN, a.vocab) ? base[first + i] : T(-INFINITY);
-        u[0] = reinterpret_cast<const uint4*>(e)[0];
-        u[1] = reinterpret_cast<const uint4*>(e)[1];
-      }
-#pragma unroll
-      for (int y = 0; y < NV; ++y)
-        if (y == v) {
-          lo[y] = u[0];
-          hi[y] = u[1];
-        }
+      for (int v = 0; v < 2 * NV; ++v) u[v] = join<T>(wa[v], wb[v], skew);
+      if (c + 2 < c_hi) load_pieces(c + 2);
+      account(u);
     }
-  };
-  if (tid == 0) s_n = 0;
+  } else {
+    load_pair(c_lo, wa);
+    load_pair(c_lo + 2, wb);
+#pragma unroll 1
+    for (int c = c_lo; c < c_hi; c += 4) {
+      account(wa);
+      if (c + 4 < c_hi) load_pair(c + 4, wa);
+      if (c + 2 >= c_hi) break;
+      account(wb);
+      if (c + 6 < c_hi) load_pair(c + 6, wb);
+    }
+  }
+  // ---- the slice's k best
   int n = 0;                                       // entries of the list (the same in all threads, like what follows)
-  uint32_t least = 0;                              // a key that k entries of the list reach, once there are as many
-  float m = -INFINITY, sum = 0.f;                  // this thread's
+  uint32_t least = 0;                              // the list takes keys from here on
   // The largest bound that k threads' keys reach (or that a few more do), or 0.  The k-th largest of 64 keys, each the largest of four
   // threads', is one that k threads reach, and few more do unless k is near 64: from there the search goes on by halves.
   auto search = [&](uint32_t key) -> uint32_t {
@@ -329,220 +367,101 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
     n = min(n, a.k);
     for (int i = tid; i < n; i += kThreads) s_list[i] = s_best[i];
     if (tid == 0) s_n = n;
-    if (n == a.k) least = max(least, s_best[a.k - 1].x);
+    least = max(least, s_best[a.k - 1].x);         // (n is k: there were more)
     __syncthreads();
   };
-  // Once the list has k entries, chunks go by in groups without a barrier: what is above the bound is added, up to the list's end.  A group
-  // that would add more than there is room for (logits that rise along the row) is gone through again, chunk by chunk.
-  uint4 w0[NV], w1[NV];                            // chunks c and c + 1; of a row with skew the two pieces of chunk c
-  int c = c_lo, again_end = c_lo;                  // (the same in all threads, like n and least)
-  auto fetch = [&]() {
+  // Threads whose maximum reaches the bound have what is to be looked at again: few of them, unless more equal the bound than that.  Then it is
+  // what lies above it, and of the equal ones the first in the order of their tokens.
+  const uint32_t key = c_lo * kChunk + tid * VN < stop ? okey(m + 0.f) : 0u;   // orders like the maximum (-0 is 0); 0: no token
+  const uint32_t bound = search(key);
+  const bool few = __syncthreads_count(key >= bound) <= a.k + kSlack;
+  least = few ? max(bound, 1u) : bound + 1;
+  if (tid == 0) s_n = s_columns = 0;
+  __syncthreads();
+  if (key >= least) s_column[atomicAdd(&s_columns, 1)] = (uint8_t)tid;
+  __syncthreads();
+  // A warp goes through a thread's logits, a piece per lane.
+  const int columns = s_columns, pieces = (c_hi - c_lo) * NV;
+  auto look = [&](int column, int p) {
+    const int t0 = c_lo * kChunk + p * kThreads * VN + s_column[column] * VN;
+    if (t0 >= stop) return;
+    uint4 w, hi;
     if (skew) {
-      if (c < c_hi) load_two(c, w0, w1);
+      two_pieces(t0, w, hi);
+      w = join<T>(w, hi, skew);
     } else {
-      if (c < c_hi) load(c, w0);
-      if (c + 1 < c_hi) load(c + 1, w1);
+      w = piece(t0);
     }
-  };
-  // the chunk's logits out of their registers, and loads into those; returns the largest
-  auto unpack_all = [&](float (&x)[EL], const uint4 (&u)[NV]) -> float {
+    float x[VN];
+    unpack(w, x, T());
 #pragma unroll
-    for (int v = 0; v < NV; ++v) unpack(u[v], x + v * VN, T());
-    return max_of(u, T());
-  };
-  auto take_straight = [&](float (&x)[EL], uint4 (&w)[NV], int at_c) -> float {
-    const float top = unpack_all(x, w);
-    if (at_c + 2 < c_hi) load(at_c + 2, w);
-    return top;
-  };
-  auto take_skewed = [&](float (&x)[EL], int at_c) -> float {
-    uint4 u[NV];
-#pragma unroll
-    for (int v = 0; v < NV; ++v) u[v] = join<T>(w0[v], w1[v], skew);
-    const float top = unpack_all(x, u);
-    if (at_c + 1 < c_hi) load_two(at_c + 1, w0, w1);
-    return top;
-  };
-  // few are added: they are read again, so that one short loop does for all places
-  auto add = [&](int first, uint32_t mask) {
-    while (mask) {
-      const int t = first + token_of<EL, VN>(__ffs(mask) - 1);
-      mask &= mask - 1;
-      const float v = to_f(base[t]);
-      const int to = atomicAdd(&s_n, 1);
-      if (to < kList) s_list[to] = make_uint2(v < INFINITY ? okey(v + 0.f) : okey(-INFINITY), (uint32_t)t);
-    }
-  };
-  // the thread's logits into its maximum and sum; returns the largest of them
-  auto account = [&](float (&x)[EL], float mine) -> float {
-    const float m_was = m;
-    float part = weigh(x, mine, m);
-    if (!(part < INFINITY)) {
-      // a logit that is NaN or +infinity is none that can be chosen: as -infinity
-      set_status(a.status, RTP_ERR_INVALID);
-      mine = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < EL; ++i) {
-        if (!(x[i] < INFINITY)) x[i] = -INFINITY;
-        mine = fmaxf(mine, x[i]);
-      }
-      m = m_was;
-      part = weigh(x, mine, m);
-    }
-    sum = sum * fast_ex2((m_was - (m == -INFINITY ? 0.f : m)) * kLog2e) + part;   // (nothing yet: 0 * 0)
-    return mine;
-  };
-  // a chunk of a group (logits behind the row's end are -infinity: not above any bound)
-  auto stream = [&](float (&x)[EL], float top, int at_c, float at) {
-    const float mine = account(x, top);
-    if (mine > at) {
-      uint32_t mask = 0;
-#pragma unroll
-      for (int i = 0; i < EL; ++i)
-        if (x[i] > at) mask |= 1u << i;
-      if ((mask & (mask - 1)) == 0) {              // mostly one: the largest
+    for (int i = 0; i < VN; ++i) {
+      const uint32_t u = x[i] < INFINITY ? okey(x[i] + 0.f) : okey(-INFINITY);
+      if (u >= least && t0 + i < stop) {
         const int to = atomicAdd(&s_n, 1);
-        if (to < kList) s_list[to] = make_uint2(okey(mine + 0.f), (uint32_t)(at_c * kChunk + tid * VN + token_of<EL, VN>(__ffs(mask) - 1)));
-      } else {
-        add(at_c * kChunk + tid * VN, mask);
+        if (to < kList) s_list[to] = make_uint2(u, (uint32_t)(t0 + i));
       }
     }
   };
-  fetch();
-#pragma unroll 1
-  while (c < c_hi) {
-    if (n >= a.k && c >= again_end) {
-      const int begin = c, end = min(c + kGroup, c_hi);
-      const float m_was = m, sum_was = sum, at = okey_to_float(max(least, okey(-INFINITY)));
-      if (skew) {
-#pragma unroll 1
-        for (; c < end; ++c) {
-          float x[EL];
-          const float top = take_skewed(x, c);
-          stream(x, top, c, at);
-        }
-      } else {
-#pragma unroll 1
-        for (; c < end; c += 2) {
-          float x[EL];
-          const float top = take_straight(x, w0, c);
-          stream(x, top, c, at);
-          if (c + 1 < end) {                       // (an odd group is the last one)
-            float y[EL];
-            const float top1 = take_straight(y, w1, c + 1);
-            stream(y, top1, c + 1, at);
-          }
-        }
-        c = end;
-      }
-      __syncthreads();
-      const int have = s_n;
-      __syncthreads();
-      if (have > kList) {
-        again_end = end;
-        c = begin;
-        m = m_was;
-        sum = sum_was;
-        if (tid == 0) s_n = n;
-        fetch();
+  for (int j = warp; j < columns; j += kWarps)
+    for (int p = lane; p < pieces; p += 32) look(j, p);
+  __syncthreads();
+  n = s_n;
+  if (n > kList) {                                 // so many in a few threads: again, with cuts in between that raise the bound
+    __syncthreads();
+    if (tid == 0) s_n = 0;
+    n = 0;
+    __syncthreads();
+    for (int j = 0; j < columns; j += kWarps)
+      for (int p = 0; p < pieces; p += 32) {
+        if (j + warp < columns && p + lane < pieces) look(j + warp, p + lane);
         __syncthreads();
-        continue;
-      }
-      n = have;
-      if (n > 2 * a.k + 16) cut();
-      continue;
-    }
-    {
-      float x[EL], mine;
-      if (skew) {
-        mine = take_skewed(x, c);
-      } else {
-        mine = take_straight(x, w0, c);        // (chunk c + 2 into w0, which then change places)
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          const uint4 u = w0[v];
-          w0[v] = w1[v];
-          w1[v] = u;
-        }
-      }
-      const int first = c * kChunk + tid * VN;     // token of the thread's first logit
-      mine = account(x, mine);
-      // keys order like the logits; 0: the thread has no token here (-infinity is a token that is ruled out)
-      uint32_t valid = (1u << EL) - 1u;            // a bit for each of the thread's logits; pieces may reach over the row's ends
-      if (!whole(c)) {
-#pragma unroll
-        for (int i = 0; i < EL; ++i)
-          if (first + token_of<EL, VN>(i) >= a.vocab) valid &= ~(1u << i);
-      }
-      const uint32_t key = valid ? okey(mine + 0.f) : 0u;   // (-0 is 0)
-      // the thread's logits of key `bound` and above; those above it
-      auto from = [&](uint32_t bound) {
-        const float at = bound <= okey(-INFINITY) ? -INFINITY : okey_to_float(bound);
-        uint32_t mask = 0;
-#pragma unroll
-        for (int i = 0; i < EL; ++i)
-          if (x[i] >= at) mask |= 1u << i;
-        return mask & valid;
-      };
-      auto above = [&](uint32_t bound) {
-        const float at = bound < okey(-INFINITY) ? -INFINITY : okey_to_float(bound);
-        uint32_t mask = 0;
-#pragma unroll
-        for (int i = 0; i < EL; ++i)
-          if (x[i] > at) mask |= 1u << i;
-        return bound < okey(-INFINITY) ? valid : mask & valid;
-      };
-      if (n > kKeep) cut();
-      const uint32_t bound = max(search(key), 1u);
-      const uint32_t reach = key >= bound ? from(bound) : 0u, over = key >= bound ? above(bound) : 0u;
-      const int w_reach = __reduce_add_sync(0xffffffffu, __popc(reach));
-      __syncthreads();
-      if (lane == 0) s_scan[warp] = w_reach;
-      __syncthreads();
-      int reached = 0;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) reached += s_scan[w];
-      const bool all = reached <= kAdd;            // else too many equal the bound: the first of them are taken in order
-      add(first, all ? reach : over);
-      __syncthreads();
-      const int added = s_n - n;
-      n = s_n;
-      if (!all && added < a.k) {
-        const int need = a.k - added;
-        int before = 0;                            // equal ones in front of this piece
-#pragma unroll 1
-        for (int v = 0; v < NV; ++v) {
-          uint32_t eq = ((reach & ~over) >> (v * VN)) & ((1u << VN) - 1u);
-          const int cnt = __popc(eq);
-          int s = cnt;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, s, o);
-            if (lane >= o) s += y;
-          }
-          __syncthreads();
-          if (lane == 31) s_scan[warp] = s;
-          __syncthreads();
-          int at = before + s - cnt, total = 0;
-#pragma unroll
-          for (int w = 0; w < kWarps; ++w) {
-            at += w < warp ? s_scan[w] : 0;
-            total += s_scan[w];
-          }
-          for (; eq; eq &= eq - 1, ++at)
-            if (at < need) s_list[n + at] = make_uint2(bound, (uint32_t)(first + v * kThreads * VN + __ffs(eq) - 1));
-          before += total;
-          if (before >= need) break;               // (the same in all threads)
-        }
-        n += min(before, need);
+        n = s_n;
         __syncthreads();
-        if (tid == 0) s_n = n;
+        if (n > kKeep) cut();
       }
-      if (reached >= a.k) least = max(least, bound);
-      else if (n >= a.k) cut();                    // (short chunks: their entries' k-th best)
+  }
+  if (!few && bound && n < a.k) {
+    int need = a.k - n;
+#pragma unroll 1
+    for (int p = 0; p < pieces && need > 0; ++p) {
+      const int t0 = c_lo * kChunk + p * kThreads * VN + tid * VN;
+      uint32_t eq = 0;                             // a bit for each of the thread's logits that is one
+      if (t0 < stop) {
+        uint4 w, hi;
+        if (skew) {
+          two_pieces(t0, w, hi);
+          w = join<T>(w, hi, skew);
+        } else {
+          w = piece(t0);
+        }
+        float x[VN];
+        unpack(w, x, T());
+#pragma unroll
+        for (int i = 0; i < VN; ++i)
+          if (t0 + i < stop && (x[i] < INFINITY ? okey(x[i] + 0.f) : okey(-INFINITY)) == bound) eq |= 1u << i;
+      }
+      const int cnt = __popc(eq);
+      int s = cnt;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += y;
+      }
       __syncthreads();
+      if (lane == 31) s_scan[warp] = s;
+      __syncthreads();
+      int at = s - cnt, total = 0;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        at += w < warp ? s_scan[w] : 0;
+        total += s_scan[w];
+      }
+      for (; eq; eq &= eq - 1, ++at)
+        if (at < need) s_list[n + at] = make_uint2(bound, (uint32_t)(t0 + __ffs(eq) - 1));
+      n += min(total, need);
+      need -= min(total, need);
     }
-    ++c;
   }
   __syncthreads();
   order();
