@@ -1,19 +1,21 @@
 // Selection of a beam search step: the k best continuations of every group of beams, score = scores[beam] + log_softmax(logits)[token],
 // equal scores going to the lower (beam, token).
 //
-// A row is cut into slices of whole chunks, one CTA each, whose threads hold the logits of a chunk in registers while the next ones are on
-// their way; every thread keeps a running maximum and sum of exponentials of its own.  The slice's k best tokens need no sort of the
-// chunks: in the first one, the k-th largest of the 256 threads' maxima is a lower bound of the k-th largest logit that only a few more
-// than k logits reach.  Those go to a list, and of the later chunks only what lies above the list's bound.  A second kernel, one CTA per
-// group, joins the rows' sums and takes the k best of the sorted lists one by one.
+// A row is cut into slices of whole chunks, one CTA each, whose threads hold the logits of two chunks in registers while the next ones are on
+// their way and keep a running maximum and sum of exponentials each.  The slice's k best tokens need no second pass: the k-th largest of
+// the 256 threads' maxima is a lower bound of the k-th largest logit, and only the threads that reach it, k and a few, have logits that
+// do.  Those are read again (from L2), go to a list, and the list's k best are put in order.  A second kernel, one CTA per group, joins the
+// rows' sums and takes the k best of the sorted lists one by one.
 // Tokens of one row are ordered by their logits alone; where rows meet, scores are 64-bit (sums of exponentials are 32-bit
 // within a slice, 64-bit across slices), so that neighbours are not swapped by the rounding of a normaliser.
-// Bound by the one read of the logits in principle (10 us for 32 x 8 beams over 128K in bf16); measured 32.5 us: the slices 25.6, of which 5
-// go by before the first list stands (loads of all CTAs at once, search, additions) and the rest is instruction issue and latency (210
-// warp instructions per 512 logits, of which 16 are exponentials and about 60 the additions to the lists), the second kernel 8.
-// 4 beams over 32K: 10 us, two launches of 4 and 7 us, chains of dependent loads, reductions and k rounds.
-// Tried and left: pairs of chunks per step (fewer instructions, more than the instruction cache holds: 31 us for the slices), one copy of
-// the chunk loop (27), groups that grow with the chunks seen (30), the second kernel launched ahead (no difference).
+// Bound by the one read of the logits in principle (10 us for 32 x 8 beams over 128K in bf16); measured 25 us: the slices 18, of which the
+// pass over the logits is about 11 (the special function unit's rate for one exponential per logit is 8), launch, first loads, bound and
+// lists the rest; the second kernel 8.  4 beams over 32K: 11 us, two launches of 4 and 7 us, chains of dependent loads, reductions
+// and k rounds.
+// Tried and left: a list that grows during the pass under a bound from its first chunk (the slices 26 us: additions were 40 % of the
+// instructions), logits of short slices kept in registers for the list and the second kernel launched ahead (no difference).
+#include <type_traits>
+
 #include "rtp_device.cuh"
 
 namespace rtp {
