@@ -110,6 +110,19 @@ def test_logits_that_rise_along_the_row():
     assert check(x, None, None, 1, 3) == rb.RTP_OK
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [20000, 20003])
+def test_large_logits_side_by_side_again_and_again(V, dtype):
+    """Large logits at a fixed distance from each other, so that few threads have thousands of them, in rows that are not cut."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(V)
+    x = torch.randn((600, V), device=DEV, generator=g)
+    t = torch.arange(V, device=DEV)
+    x[:, (t % 1024) < 300] += 50.0
+    x[::2, (t % 2048) >= 1400] += 60.0
+    assert check(x.to(dtype), None, None, 60, 64) == rb.RTP_OK
+
+
 def test_peaked_rows_and_large_magnitudes():
     x = torch.zeros((4, 9000), device=DEV)
     x[0, 8999], x[1, 0], x[2] = 80.0, 1e4, -1e4
