@@ -211,6 +211,11 @@ def _rows_of(where: str, name: str, x, n: int, heads: int) -> int:
     return s[0] if n > 1 else heads * 128
 
 
+def _is_rows(x, n: int, heads: int) -> bool:
+    """Dense 16-bit rows [n, heads, 128]."""
+    return x.is_contiguous() and x.numel() == n * heads * 128 and x.element_size() == 2 and x.dim() == 3
+
+
 def _is_i32(x) -> bool:
     """A dense array of 32-bit values."""
     return x.element_size() == 4 and x.is_contiguous()
@@ -363,20 +368,20 @@ def rtp_rope_append(ctx, params, cache, rope: Rope, q, k, v, q_out, w_k, tok_seq
     """q [T, query heads, 128], k, v [T, KV heads, 128]: unrotated rows, dense or slices of one projection's output; q_out dense
     (q and q_out None: keys and values only); w_k: index projections, or None."""
     c = params.c
-    n, n_q, n_kv = tok_seq.shape[0], c.n_q_heads, c.n_kv_heads
+    n, n_q, n_kv = tok_seq.numel(), c.n_q_heads, c.n_kv_heads
     sq, pq, po = 0, None, None
     if q is not None and q_out is not None:
         sq, pq, po = _rows_of("rtp_rope_append", "q", q, n, n_q), q.data_ptr(), q_out.data_ptr()
-        if _rows_of("rtp_rope_append", "q_out", q_out, n, n_q) != n_q * 128:
-            raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", "q_out has to be dense")
+        if not _is_rows(q_out, n, n_q):
+            raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", f"q_out has to be dense 16-bit [{n} tokens, {n_q}, 128]")
     elif q is not None or q_out is not None:
         raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", "q and q_out go together")
     sk, sv = _rows_of("rtp_rope_append", "k", k, n, n_kv), _rows_of("rtp_rope_append", "v", v, n, n_kv)
-    if tok_pos.shape[0] != n or not (_is_i32(tok_seq) and _is_i32(tok_pos)):
+    if tok_pos.numel() != n or not (_is_i32(tok_seq) and _is_i32(tok_pos)):
         raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", f"tok_seq and tok_pos have to be contiguous int32 [{n}]")
     rc = ctx.lib.rtp_rope_append(ctx.h, C.byref(c), C.byref(cache), _ptr(rope.freqs), rope.rotary_dim, rope.interleaved, rope.scale, pq,
-                                 sq, k.data_ptr(), sk, v.data_ptr(), sv, po, _ptr(w_k), tok_seq.data_ptr(), tok_pos.data_ptr(), n,
-                                 _ptr(status), _stream(stream))
+                                 sq, k.data_ptr(), sk, v.data_ptr(), sv, po, None if w_k is None else w_k.data_ptr(), tok_seq.data_ptr(),
+                                 tok_pos.data_ptr(), n, _ptr(status), _stream(stream))
     if rc:
         ctx._check(rc, "rtp_rope_append")
 
@@ -605,15 +610,12 @@ def rtp_attn_chunks(ctx, params, cache, q, chunk_seq, chunk_start, row_offsets, 
                     stream=None):
     """q, out: [rows, query heads, 128]; chunk c: rows row_offsets[c] .. row_offsets[c + 1] - 1 at positions chunk_start[c] .. of
     sequence chunk_seq[c]; kv_heads: None (all) or the KV heads that are computed."""
-    n, rows = chunk_seq.shape[0], q.shape[0]
-    if chunk_start.shape[0] != n or row_offsets.shape[0] != n + 1 or out.shape[0] != rows or (lse is not None and lse.shape[0] != rows):
-        raise RtpError(RTP_ERR_INVALID, "rtp_attn_chunks", f"{n} chunks and {rows} rows: chunk_start, row_offsets (one more), out or lse are of other lengths")
-    n_q = params.c.n_q_heads
-    if not (_rows_of("rtp_attn_chunks", "q", q, rows, n_q) == _rows_of("rtp_attn_chunks", "out", out, rows, n_q) == n_q * 128
-            and _is_i32(chunk_seq) and _is_i32(chunk_start) and _is_i32(row_offsets)
-            and (lse is None or (lse.shape == (rows, n_q) and _is_i32(lse)))):
-        raise RtpError(RTP_ERR_INVALID, "rtp_attn_chunks", "q and out have to be dense [rows, query heads, 128], lse [rows, query heads] in 32 bits, and the "
-                       "chunks' arrays contiguous int32")
+    n, rows, n_q = chunk_seq.numel(), q.shape[0], params.c.n_q_heads
+    if chunk_start.numel() != n or row_offsets.numel() != n + 1 or not (
+            _is_rows(q, rows, n_q) and _is_rows(out, rows, n_q) and _is_i32(chunk_seq) and _is_i32(chunk_start) and _is_i32(row_offsets)
+            and (lse is None or (lse.numel() == rows * n_q and _is_i32(lse)))) or q.shape != out.shape:
+        raise RtpError(RTP_ERR_INVALID, "rtp_attn_chunks", f"{n} chunks and {rows} rows: chunk_start [{n}] and row_offsets [{n + 1}] have to be contiguous int32, "
+                       f"q and out dense 16-bit [{rows}, {n_q}, 128], lse 32-bit [{rows}, {n_q}]")
     arr, n_heads = None, 0
     if kv_heads is not None:
         n_heads = len(kv_heads)
