@@ -104,14 +104,21 @@ constexpr int kSnap = 3;                       // key tiles that are not cut off
 constexpr int kPlanUnits = 1024;               // units whose costs lie in shared memory
 
 struct PlanShared {
-  int64_t warp_sum[33];
+  int64_t warp_sum[2][32];
   int64_t load[1024 + 1];                      // jobs dealt to each CTA, then the cuts
   int64_t before[kPlanUnits + 1];
   int32_t begin[1024], first[1024];            // of each CTA: pairs in front of its own, its first unit
+  int32_t n_merge;
 };
 
-// Exclusive sum over the block; warp_sum[32]: the total.
-__device__ __forceinline__ int64_t scan64(int64_t x, int64_t* warp_sum) {
+constexpr int kKeptUnits = 1024, kKeptChunks = 4096;   // units that are described once (their descriptions lie in shared memory)
+// Bytes in front of them: the above, and the chunks' lists.
+__host__ __device__ constexpr size_t plan_lists(int64_t n_chunks) {
+  return ((sizeof(PlanShared) + 15) & ~(size_t)15) + (((size_t)n_chunks * (sizeof(int4) + sizeof(int2)) + 15) & ~(size_t)15);
+}
+// Exclusive sum over the block, and the total.  The two rows of warp_sum are used in turn: who writes one again has passed the barrier of
+// the other, and so has everybody who read it.
+__device__ __forceinline__ int64_t scan64(int64_t x, int64_t (*warp_sum)[32], int& turn, int64_t& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   int64_t s = x;
 #pragma unroll
@@ -119,20 +126,18 @@ __device__ __forceinline__ int64_t scan64(int64_t x, int64_t* warp_sum) {
     const int64_t y = __shfl_up_sync(0xffffffffu, s, o);
     if (lane >= o) s += y;
   }
-  __syncthreads();                             // (the last sum's readers are through)
-  if (lane == 31) warp_sum[warp] = s;
+  if (lane == 31) warp_sum[turn][warp] = s;
   __syncthreads();
-  const int64_t w = lane < warps ? warp_sum[lane] : 0;
+  const int64_t w = lane < warps ? warp_sum[turn][lane] : 0;
+  turn ^= 1;
   int64_t t = w;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int64_t y = __shfl_up_sync(0xffffffffu, t, o);
     if (lane >= o) t += y;
   }
-  if (warp == 0 && lane == 31) warp_sum[32] = t;
-  const int64_t mine = __shfl_sync(0xffffffffu, t - w, warp) + s - x;
-  __syncthreads();
-  return mine;
+  total = __shfl_sync(0xffffffffu, t, 31);
+  return __shfl_sync(0xffffffffu, t - w, warp) + s - x;
 }
 // The last i in [0, n) with v[i] <= x (v[0] <= x).
 template <class V>
@@ -154,8 +159,10 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
   PlanShared& s = *reinterpret_cast<PlanShared*>(smem_plan);
   int4* chunk = reinterpret_cast<int4*>(smem_plan + ((sizeof(PlanShared) + 15) & ~15));   // [n_chunks]: units before, rows, start, keys
   int2* where = reinterpret_cast<int2*>(chunk + a.n_chunks);                              // [n_chunks]: row in q, sequence
+  Piece* kept = reinterpret_cast<Piece*>(smem_plan + plan_lists(a.n_chunks));                // [kKeptUnits] of calls with at most kKeptChunks chunks
   const int tid = threadIdx.x, nt = blockDim.x;
   const int N = plan.n_ctas, H = hu.n, span = 2 * a.bmp;
+  int turn = 0;
   // chunks, with what is wrong in them
   int64_t mine = 0;
   const int per = (a.n_chunks + nt - 1) / nt, c0 = min(tid * per, a.n_chunks), c1 = min(c0 + per, a.n_chunks);
@@ -183,9 +190,9 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
   if (bad) set_status(status, RTP_ERR_INVALID);
   for (int i = tid; i < 2 * N; i += nt) plan.part_id[i] = -1;
   for (int i = tid; i < N; i += nt) s.load[i] = 0;
-  if (tid == 0) *plan.n_merge = 0;
-  int64_t at = scan64(mine, s.warp_sum);
-  const int64_t total_units = s.warp_sum[32];
+  if (tid == 0) s.n_merge = *plan.n_merge = 0;
+  int64_t total_units;
+  int64_t at = scan64(mine, s.warp_sum, turn, total_units);
   if (total_units > plan.max_units) {          // offsets that run back and forth: nothing is done
     if (tid == 0) set_status(status, RTP_ERR_INVALID);
     for (int i = tid; i <= N; i += nt) plan.piece_begin[i] = 0;
@@ -198,7 +205,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
   __syncthreads();
   const int U = (int)total_units;
   // unit u: chunk by chunk, head by head, the last positions first; returns its key tiles
-  auto describe = [&](int u, Piece& p) -> int {
+  auto make = [&](int u, Piece& p) -> int {
     const int i = last_at(a.n_chunks, u, [&](int j) { return chunk[j].x; });
     const int4 c = chunk[i];
     const int2 w = where[i];
@@ -217,6 +224,20 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
       p.n_sink_tiles = min(min((n_sink + kTile - 1) / kTile, p.kt_first), n_all);
     }
     return p.n_sink_tiles + n_all - p.kt_first;
+  };
+  const bool keep = U <= kKeptUnits && a.n_chunks <= kKeptChunks;
+  if (keep) {
+    for (int u = tid; u < U; u += nt) {
+      Piece p;
+      p.tile_hi = make(u, p);
+      kept[u] = p;
+    }
+    __syncthreads();
+  }
+  auto describe = [&](int u, Piece& p) -> int {
+    if (!keep) return make(u, p);
+    p = kept[u];
+    return p.tile_hi;
   };
   // A CTA each for few and short units: a cut of less than two shares each would not end sooner, and nothing has to be summed up (7 rows over
   // 200 keys: 10 us against 17 by the general way below, over 1000 keys 17 against 24, over 1500 with 12 tiles 25 either way).
@@ -251,8 +272,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     const int each = (M + nt - 1) / nt, j0 = min(tid * each, M), j1 = min(j0 + each, M);
     int64_t sum = 0;
     for (int j = j0; j < j1; ++j) sum += before[j];
-    int64_t run = scan64(sum, s.warp_sum);
-    W_cut = s.warp_sum[32];
+    int64_t run = scan64(sum, s.warp_sum, turn, W_cut);
     for (int j = j0; j < j1; ++j) {
       const int64_t w = before[j];
       before[j] = run;
@@ -262,8 +282,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     if (rounds == 0) break;
     // Whole units only where no CTA gets more than its share of them (a few that cost more than the others are cut instead), and one
     // round less where the rest would be cut into crumbs.
-    scan64(tid < N ? s.load[tid] : 0, s.warp_sum);
-    W_dealt = s.warp_sum[32];
+    scan64(tid < N ? s.load[tid] : 0, s.warp_sum, turn, W_dealt);
     const bool uneven = __syncthreads_or(tid < N && s.load[tid] * N > W_dealt + W_cut);
     const bool crumbs = W_cut > 0 && W_cut < (int64_t)N * kMinShare;
     if (!uneven && !(crumbs && rounds == U / N)) break;
@@ -276,9 +295,11 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
   const int D = rounds * N, M = U - D;
   // What each CTA takes of the cut part: up to the mean; with nothing dealt, equal shares for as many as are worth it.
   if (rounds) {
-    const int64_t room = tid < N ? max((int64_t)0, (W_dealt + W_cut) / N + 1 - s.load[tid]) : 0;
-    const int64_t room_before = scan64(room, s.warp_sum), rooms = s.warp_sum[32];
-    if (tid < N) s.load[tid] = (int64_t)((double)W_cut * (double)room_before / (double)rooms);
+    // (the mean in double precision, and one more, so that there is room in any case)
+    const int64_t mean = (int64_t)((double)(W_dealt + W_cut) * (1.0 / N)) + 2, room = tid < N ? max((int64_t)0, mean - s.load[tid]) : 0;
+    int64_t rooms;
+    const int64_t room_before = scan64(room, s.warp_sum, turn, rooms);
+    if (tid < N) s.load[tid] = min(W_cut, (int64_t)((double)room_before * ((double)W_cut / (double)rooms)));
   } else {
     const int takers = max(1, (int)min((int64_t)N, W_cut / (kMinJobs + kPieceCost)));
     if (tid < N) s.load[tid] = tid < takers ? (int64_t)((double)W_cut * tid / takers) : W_cut;
@@ -289,7 +310,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
   const bool taker = tid < N && s.load[tid] < s.load[tid + 1];
   auto at_unit = [&](int j) { return before[j]; };
   const int j_first = taker ? last_at(M, s.load[tid], at_unit) : 0, j_end = taker ? last_at(M, s.load[tid + 1] - 1, at_unit) + 1 : 0;
-  const int cut_before = (int)scan64(j_end - j_first, s.warp_sum), pairs = (int)s.warp_sum[32];
+  int64_t pairs64;
+  const int cut_before = (int)scan64(j_end - j_first, s.warp_sum, turn, pairs64), pairs = (int)pairs64;
   if (tid < N) {
     s.begin[tid] = cut_before;
     s.first[tid] = j_first;
@@ -324,11 +346,13 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
       plan.part_id[p.slot] = p.id;
       if (p.tile_lo == 0) {                    // up to the last CTA whose share begins before the unit's end
         const int last = last_at(N, u1 - 1, [&](int c) { return s.load[c]; });
-        plan.merge[atomicAdd(plan.n_merge, 1)] = MergeUnit{p.row0, p.n_pos, p.unit, p.id, i, last, 0, 0};
+        plan.merge[atomicAdd(&s.n_merge, 1)] = MergeUnit{p.row0, p.n_pos, p.unit, p.id, i, last, 0, 0};
       }
     }
     plan.pieces[(i + 1) * rounds + q] = p;
   }
+  __syncthreads();
+  if (tid == 0) *plan.n_merge = s.n_merge;
 }
 
 // ---- attention ----------------------------------------------------------------------------------------
@@ -861,7 +885,7 @@ Plan carve(void* ws, int G, int n_units, int64_t n_chunks, int64_t R, int sm_cou
   return p;
 }
 
-size_t plan_smem(int64_t n_chunks) { return ((sizeof(PlanShared) + 15) & ~(size_t)15) + (size_t)n_chunks * (sizeof(int4) + sizeof(int2)); }
+size_t plan_smem(int64_t n_chunks) { return plan_lists(n_chunks) + (n_chunks <= kKeptChunks ? kKeptUnits * sizeof(Piece) : 0); }
 
 }  // namespace
 
@@ -898,7 +922,7 @@ cudaError_t launch_attn_chunks(const CacheView& cv, const CacheView& lv, const D
   if (e == cudaSuccess && lv.n_kv > 0) e = encode_rows_map(&maps.lv, lv.v, (int64_t)lv.num_pages * lv.n_kv * kPage, kHeadDim, 64, kPage, swz);
   if (e != cudaSuccess) return e;
   static PerDeviceOnce once_plan, once_attn;
-  e = set_dyn_smem_once(plan_kernel, (int)plan_smem(kMaxChunks), once_plan);
+  e = set_dyn_smem_once(plan_kernel, (int)std::max(plan_smem(kMaxChunks), plan_smem(kKeptChunks)), once_plan);
   if (e == cudaSuccess) e = set_dyn_smem_once(attn_chunks_kernel, kSmem, once_attn);
   if (e != cudaSuccess) return e;
   bool ring = false;
