@@ -5,15 +5,15 @@
 // their way and keep a running maximum and sum of exponentials each.  The slice's k best tokens need no second pass: the k-th largest of
 // the 256 threads' maxima is a lower bound of the k-th largest logit, and only the threads that reach it, k and a few, have logits that
 // do.  Those are read again (from L2), go to a list, and the list's k best are put in order.  A second kernel, one CTA per group, joins the
-// rows' sums and takes the k best of the sorted lists one by one.
+// rows' sums and picks the k best of the sorted lists in the same way.
 // Tokens of one row are ordered by their logits alone; where rows meet, scores are 64-bit (sums of exponentials are 32-bit
 // within a slice, 64-bit across slices), so that neighbours are not swapped by the rounding of a normaliser.
-// Bound by the one read of the logits in principle (10 us for 32 x 8 beams over 128K in bf16); measured 25 us: the slices 18, of which the
+// Bound by the one read of the logits in principle (10 us for 32 x 8 beams over 128K in bf16); measured 22.4 us: the slices 18, of which the
 // pass over the logits is about 11 (the special function unit's rate for one exponential per logit is 8), launch, first loads, bound and
-// lists the rest; the second kernel 8.  4 beams over 32K: 11 us, two launches of 4 and 7 us, chains of dependent loads, reductions
-// and k rounds.
+// lists the rest; the second kernel 4 to 5.  4 beams over 32K: 8.6 us, two launches and chains of dependent loads and reductions.
 // Tried and left: a list that grows during the pass under a bound from its first chunk (the slices 26 us: additions were 40 % of the
-// instructions), logits of short slices kept in registers for the list and the second kernel launched ahead (no difference).
+// instructions); k rounds over the lists' heads in the second kernel (8 us; still there for lists that do not fit); logits of short
+// slices kept in registers for the list and the second kernel launched ahead (no difference).
 #include <type_traits>
 
 #include "rtp_device.cuh"
@@ -129,9 +129,6 @@ __device__ __forceinline__ void rule_out(uint4 (&w)[N], H) {
 #pragma unroll
   for (int v = 0; v < N; ++v) w[v] = make_uint4(f(w[v].x), f(w[v].y), f(w[v].z), f(w[v].w));
 }
-// A thread's i-th logit, counted from its first one (in a chunk as in several that follow each other).
-template <int VN>
-__device__ __forceinline__ int token_of(int i) { return (i / VN) * kThreads * VN + i % VN; }
 // Two numbers at a time.
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   float2 r;
@@ -194,11 +191,10 @@ __device__ __noinline__ uint4 edge_piece(const T* base, int t0, int lo, int hi) 
 }
 __device__ __forceinline__ uint4 ld_piece(const void* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
 
-template <class T, int EL>
+template <class T>
 __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_constant__ BeamArgs a) {
   chain_wait();
-  constexpr int VN = Vec<T>::n, NV = EL / VN, kChunk = kThreads * EL;
-  static_assert(EL % VN == 0, "");
+  constexpr int VN = Vec<T>::n, NV = 2, kChunk = kThreads * NV * VN;   // (a chunk: 8 KB)
   __shared__ __align__(16) uint2 s_list[kList];    // ordered key, token
   __shared__ __align__(16) uint2 s_sel[kSelect];
   __shared__ uint2 s_best[RTP_MAX_BEAM_K];
@@ -488,11 +484,16 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
   }
 }
 
-// One CTA per group.  The rows' normalisers, then all lists as 64-bit scores in shared memory where they fit, then k rounds in which every
-// lane knows the best of the lists list = thread, thread + threads, ...; a single warp does the rounds where 32 lanes have few lists each.
+// One CTA per group.  The rows' normalisers, then the lists' entries as 64-bit scores in shared memory; those that reach a bound (a few more
+// than k) are ranked against each other.  Where the lists do not fit, or many are equal, k rounds take one entry each: every lane knows the
+// best of the lists list = thread, thread + threads, ..; a single warp does the rounds where 32 lanes have few lists each.
 // Lists are in the order of (beam, token): the slices of a row hold disjoint, ascending ranges of tokens, and a list is sorted.  So of
-// equal scores the lower list goes first.
-constexpr int kPickCached = 3400;                  // entries in shared memory
+// equal scores the lower entry goes first.
+constexpr int kPickCached = 3200;                  // entries in shared memory
+constexpr int kPickFew = 256;                      // entries that are ranked against each other
+__device__ __forceinline__ double score_of(uint64_t key) {
+  return __longlong_as_double((long long)((key >> 63) ? key & 0x7fffffffffffffffull : ~key));
+}
 __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_constant__ BeamArgs a, const int cached) {
   chain_wait();
   extern __shared__ __align__(16) unsigned char smem_pick[];
@@ -503,6 +504,10 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_consta
   __shared__ double s_off[RTP_MAX_BEAMS];                  // score of a token with the row's largest logit
   __shared__ float s_max[RTP_MAX_BEAMS];                   // that logit
   __shared__ int s_state[RTP_MAX_BEAMS];                   // 1: ended, 2: no token has a probability
+  __shared__ __align__(16) uint64_t s_top[kTops];
+  __shared__ unsigned long long s_low;
+  __shared__ int s_n;
+  __shared__ uint4 s_few[kPickFew];                        // key, entry
   __shared__ uint4 s_best[2][kWarps];                      // score (ordered, 64 bits), list, token of each warp's best
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t row0 = (int64_t)blockIdx.x * a.n_beams;
@@ -563,15 +568,73 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_consta
     return (u >> 63) ? ~u : u | 0x8000000000000000ull;
   };
   if (cached) {
+    uint64_t best = 0;                                     // the thread's best entry (no score has key 0)
     auto keep = [&](int e, const Cand& c) {
       const int l = e / a.k;
-      if (e - l * a.k < s_cnt[l]) s_key[e] = entry(l, c, s_tok[e]);
+      const uint64_t key = e - l * a.k < s_cnt[l] ? entry(l, c, s_tok[e]) : 0ull;
+      s_key[e] = key;
+      best = max(best, key);
     };
 #pragma unroll
     for (int j = 0; j < kEarly; ++j)
       if (tid + j * kThreads < cached) keep(tid + j * kThreads, early[j]);
     for (int e = tid + kEarly * kThreads; e < cached; e += kThreads) keep(e, cand[e]);
+    // The k-th largest of 64 keys, each the best of four threads': what is among the k best reaches it, and little else does.
+    uint64_t four = max(best, __shfl_xor_sync(0xffffffffu, best, 1));
+    four = max(four, __shfl_xor_sync(0xffffffffu, four, 2));
+    if ((lane & 3) == 0) s_top[tid >> 2] = four;
+    if (tid == 0) {
+      s_low = ~0ull;
+      s_n = 0;
+    }
     __syncthreads();
+    int more = 0;                                          // keys above this one, a quarter of them in each of its threads
+#pragma unroll
+    for (int i = 0; i < kTops / 4; i += 2) {
+      const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(s_top + (lane & 3) * (kTops / 4) + i);
+      more += (o.x > four) + (o.y > four);
+    }
+    more += __shfl_xor_sync(0xffffffffu, more, 1);
+    more += __shfl_xor_sync(0xffffffffu, more, 2);
+    const uint64_t mine = more < a.k ? four : ~0ull;
+    const uint32_t h = __reduce_min_sync(0xffffffffu, (uint32_t)(mine >> 32));
+    const uint32_t lo = __reduce_min_sync(0xffffffffu, (uint32_t)(mine >> 32) == h ? (uint32_t)mine : 0xffffffffu);
+    if (lane == 0) atomicMin(&s_low, (unsigned long long)h << 32 | lo);
+    __syncthreads();
+    const uint64_t bound = max((uint64_t)s_low, (uint64_t)1);
+    if (best >= bound)
+      for (int e = tid; e < cached; e += kThreads)
+        if (s_key[e] >= bound) {
+          const int to = atomicAdd(&s_n, 1);
+          if (to < kPickFew) s_few[to] = make_uint4((uint32_t)(s_key[e] >> 32), (uint32_t)s_key[e], (uint32_t)e, 0u);
+        }
+    __syncthreads();
+    const int n = s_n;
+    if (n <= kPickFew) {                                   // (else many are equal, and are taken one by one)
+      for (int c = tid; c < n; c += kThreads) {
+        const uint4 me = s_few[c];
+        const uint64_t key = (uint64_t)me.x << 32 | me.y;
+        int rank = 0;
+#pragma unroll 4
+        for (int o = 0; o < n; ++o) {
+          const uint4 u = s_few[o];
+          const uint64_t other = (uint64_t)u.x << 32 | u.y;
+          rank += other > key || (other == key && u.z < me.z);
+        }
+        if (rank < a.k) {
+          const int64_t at = (int64_t)blockIdx.x * a.k + rank;
+          a.parent[at] = (int32_t)(row0 + me.z / (unsigned)a.k / (unsigned)a.n_slices);
+          a.token[at] = s_tok[me.z];
+          a.scores_out[at] = (float)score_of(key);
+        }
+      }
+      for (int i = n + tid; i < a.k; i += kThreads) {
+        const int64_t at = (int64_t)blockIdx.x * a.k + i;
+        a.parent[at] = a.token[at] = -1;
+        a.scores_out[at] = -INFINITY;
+      }
+      return;
+    }
   }
   const int threads = lists <= 128 ? 32 : kThreads;        // that do the rounds
   if (tid >= threads) return;
@@ -616,8 +679,7 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_consta
     if (warp == 0 && ((i & 31) == 31 || i + 1 == a.k) && (i & ~31) + lane <= i) {
       const int64_t at = (int64_t)blockIdx.x * a.k + (i & ~31) + lane;
       const bool any = (won.x | won.y) != 0u;
-      const uint64_t u = ((uint64_t)won.x << 32) | won.y;
-      const double score = __longlong_as_double((long long)((u >> 63) ? u & 0x7fffffffffffffffull : ~u));
+      const double score = score_of(((uint64_t)won.x << 32) | won.y);
       a.parent[at] = any ? (int32_t)(row0 + won.z / a.n_slices) : -1;
       a.token[at] = any ? (int32_t)won.w : -1;
       a.scores_out[at] = any ? (float)score : -INFINITY;
@@ -629,35 +691,30 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_consta
   }
 }
 
-// How a row is cut: chunks of 4096 logits, of 2048 if they are 32-bit or in calls that would leave SMs idle; and as many slices as make one wave of four CTAs
-// per SM, each of whole chunks.
+// How a row is cut: as many slices as make one wave of four CTAs per SM, each of two whole chunks at least (of one: 11.2 us instead of 9.1 for
+// 15 rows of 50001 in 32 bits, whose second kernel then has twice the lists).
 struct BeamCut {
-  int el, chunks, slices;                          // logits per thread and chunk, chunks per slice, slices per row
+  int chunks, slices;                              // chunks per slice, slices per row
 };
-BeamCut beam_cut(int64_t rows, int64_t vocab, bool wide, int sm_count) {
+BeamCut beam_cut(int64_t rows, int64_t vocab, int bytes, int sm_count) {
   BeamCut c;
-  c.el = !wide && rows * vocab >= (int64_t)sm_count * kThreads * 32 ? 16 : 8;
-  const int64_t chunks = (vocab + (int64_t)kThreads * c.el - 1) / ((int64_t)kThreads * c.el);
-  const int64_t want = std::max<int64_t>(1, std::min(chunks, (int64_t)4 * sm_count / rows));
+  const int64_t chunk = kThreads * 32 / bytes, chunks = (vocab + chunk - 1) / chunk;
+  const int64_t want = std::max<int64_t>(1, std::min(chunks / 2, (int64_t)4 * sm_count / rows));
   c.chunks = (int)((chunks + want - 1) / want);
   c.slices = (int)((chunks + c.chunks - 1) / c.chunks);
   return c;
 }
 
 template <class T>
-cudaError_t launch_slices(const BeamArgs& a, int el, int64_t rows, cudaStream_t st) {
-  const dim3 grid((unsigned)(rows * a.n_slices)), block(kThreads);
-  auto kernel = beam_slice_kernel<T, 8>;
-  if constexpr (sizeof(T) == 2)
-    if (el == 16) kernel = beam_slice_kernel<T, 16>;
-  (void)launch_chained(kernel, grid, block, 0, st, a);
+cudaError_t launch_slices(const BeamArgs& a, int64_t rows, cudaStream_t st) {
+  (void)launch_chained(beam_slice_kernel<T>, dim3((unsigned)(rows * a.n_slices)), dim3(kThreads), 0, st, a);
   return cudaGetLastError();
 }
 
 }  // namespace
 
 size_t beam_workspace_bytes(int64_t rows, int64_t vocab, int k, int sm_count) {
-  const int64_t lists = rows * std::max(beam_cut(rows, vocab, false, sm_count).slices, beam_cut(rows, vocab, true, sm_count).slices);
+  const int64_t lists = rows * std::max(beam_cut(rows, vocab, 4, sm_count).slices, beam_cut(rows, vocab, 2, sm_count).slices);
   return (size_t)lists * (k * sizeof(Cand) + sizeof(float2) + sizeof(int32_t)) + 2 * 256;
 }
 
@@ -665,7 +722,7 @@ cudaError_t launch_beam_select(const void* logits, int format, int64_t row_strid
                                const float* scores, const int32_t* finished, int pad_token, int k, int32_t* parent, int32_t* token,
                                float* scores_out, void* ws, int32_t* status, int sm_count, cudaStream_t st) {
   const int64_t rows = n_groups * n_beams;
-  const BeamCut cut = beam_cut(rows, vocab, format == RTP_LOGITS_F32, sm_count);
+  const BeamCut cut = beam_cut(rows, vocab, format == RTP_LOGITS_F32 ? 4 : 2, sm_count);
   BeamArgs a = {logits, row_stride, n_beams, (int32_t)vocab, k, cut.slices, cut.chunks, pad_token, scores, finished,
                 nullptr, nullptr, nullptr, parent, token, scores_out, status};
   const int64_t lists = rows * a.n_slices, group_lists = (int64_t)n_beams * a.n_slices;
@@ -676,8 +733,8 @@ cudaError_t launch_beam_select(const void* logits, int format, int64_t row_strid
   a.stat = reinterpret_cast<float2*>(p);
   p += (size_t)lists * sizeof(float2);
   a.count = reinterpret_cast<int32_t*>(p);
-  cudaError_t e = format == RTP_LOGITS_F32 ? launch_slices<float>(a, cut.el, rows, st)
-                  : format == RTP_LOGITS_BF16 ? launch_slices<__nv_bfloat16>(a, cut.el, rows, st) : launch_slices<__half>(a, cut.el, rows, st);
+  cudaError_t e = format == RTP_LOGITS_F32 ? launch_slices<float>(a, rows, st)
+                  : format == RTP_LOGITS_BF16 ? launch_slices<__nv_bfloat16>(a, rows, st) : launch_slices<__half>(a, rows, st);
   if (e != cudaSuccess) return e;
   const int cached = group_lists * k <= kPickCached ? (int)(group_lists * k) : 0;
   (void)launch_chained(beam_pick_kernel, dim3((unsigned)n_groups), dim3(kThreads), (size_t)cached * 12 + 2 * group_lists, st, a, cached);
