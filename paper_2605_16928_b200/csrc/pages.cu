@@ -453,7 +453,8 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(int32_t* __restri
 // is read has to be read before any is written.  Columns of the table do not depend on one another: a CTA takes eight of them (a 32-byte
 // sector of every row), reads what all sources hold there into shared memory, and then writes.  Entries that do not change, those of
 // a prompt that all hypotheses share, cost a read only; counts move by one for each entry that does.
-// 256 sequences of 513 pages, all moved: 10 us (1 MB of table at most: a chain of loads, a hash of the destinations, atomics); 4 of 65: 2.6.
+// 256 sequences of 513 pages, all moved: 7 us (1 MB of table at most: a chain of loads, a hash of the destinations, atomics; four requests of
+// a thread are on their way together, one: 10 us); 4 of 65: 3.
 constexpr int kReorderCols = 8;
 
 // The first request that names each destination: open addressing over twice as many places as there are requests.
@@ -475,46 +476,61 @@ __global__ void __launch_bounds__(kRowThreads) reorder_kernel(int32_t* __restric
   extern __shared__ __align__(16) unsigned char smem_reorder[];
   int2* places = reinterpret_cast<int2*>(smem_reorder);            // [mask + 1]
   int* dst_of = reinterpret_cast<int*>(places + mask + 1);         // [n], -1: nothing is done
-  int* held = dst_of + n;                                          // [n][8] entries of the sources, or [n] lengths
+  int* held = dst_of + n;                                          // [n][8] entries of the sources, or lengths in the first of the eight
   const int tid = threadIdx.x;
   const bool lens = blockIdx.x == gridDim.x - 1;                   // the last CTA moves the lengths
   const int col = blockIdx.x * kReorderCols + (tid & (kReorderCols - 1));
+  const int c = tid & (kReorderCols - 1);
+  constexpr int kStep = kRowThreads / kReorderCols, kAtOnce = 4;   // requests of all threads, and of a thread that are on their way together
   for (unsigned h = tid; h <= mask; h += kRowThreads) places[h] = make_int2(-1, 0x7fffffff);
   __syncthreads();
   for (int i = tid; i < n; i += kRowThreads) {
     const int dst = dst_seqs[i];
-    const bool ok = (unsigned)dst < (unsigned)batch;
-    dst_of[i] = ok ? dst : -1;
-    if (ok) atomicMin(&places[place_of(places, mask, dst)].y, i);
+    if ((unsigned)dst < (unsigned)batch) atomicMin(&places[place_of(places, mask, dst)].y, i);
   }
-  bool bad = false;
-  for (int i = tid / kReorderCols; i < n; i += kRowThreads / kReorderCols) {
-    const int src = src_seqs[i];
-    const bool ok = (unsigned)src < (unsigned)batch;
-    if (lens) {
-      if ((tid & (kReorderCols - 1)) == 0) held[i] = ok ? seq_lens[src] : 0;
-    } else if (col < max_pages) {
-      held[i * kReorderCols + (tid & (kReorderCols - 1))] = ok ? table[(int64_t)src * max_pages + col] : -1;
+  for (int i0 = tid / kReorderCols; i0 < n; i0 += kAtOnce * kStep) {
+    int got[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int i = i0 + u * kStep, src = i < n ? src_seqs[i] : -1;
+      const bool ok = (unsigned)src < (unsigned)batch;
+      got[u] = lens ? (ok && c == 0 ? seq_lens[src] : 0) : ok && col < max_pages ? table[(int64_t)src * max_pages + col] : -1;
     }
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u)
+      if (i0 + u * kStep < n) held[(i0 + u * kStep) * kReorderCols + c] = got[u];
   }
   __syncthreads();
-  for (int i = tid / kReorderCols; i < n; i += kRowThreads / kReorderCols) {
-    const int dst = dst_of[i];
-    if (dst < 0 || (unsigned)src_seqs[i] >= (unsigned)batch || places[place_of(places, mask, dst)].y != i) {
-      bad = true;
-      continue;
+  bool bad = false;
+  for (int i = tid; i < n; i += kRowThreads) {
+    const int dst = dst_seqs[i];
+    const bool ok = (unsigned)dst < (unsigned)batch && (unsigned)src_seqs[i] < (unsigned)batch && places[place_of(places, mask, dst)].y == i;
+    dst_of[i] = ok ? dst : -1;
+    bad = bad || !ok;
+  }
+  __syncthreads();
+  for (int i0 = tid / kReorderCols; i0 < n; i0 += kAtOnce * kStep) {
+    int dst[kAtOnce], old[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int i = i0 + u * kStep;
+      dst[u] = i < n ? dst_of[i] : -1;
+      old[u] = !lens && dst[u] >= 0 && col < max_pages ? table[(int64_t)dst[u] * max_pages + col] : -1;
     }
-    if (lens) {
-      if ((tid & (kReorderCols - 1)) == 0) seq_lens[dst] = held[i];
-    } else if (col < max_pages) {
-      int32_t* to = table + (int64_t)dst * max_pages + col;
-      const int old = *to, now = held[i * kReorderCols + (tid & (kReorderCols - 1))];
-      if (old != now) {
-        *to = now;
-        if (page_ok(old, num_pages)) atomicSub(refs + old, 1);
-        if (page_ok(now, num_pages)) atomicAdd(refs + now, 1);
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      if (dst[u] < 0) continue;
+      const int now = held[(i0 + u * kStep) * kReorderCols + c];
+      if (lens) {
+        if (c == 0) seq_lens[dst[u]] = now;
+      } else if (col < max_pages) {
+        if (old[u] != now) {
+          table[(int64_t)dst[u] * max_pages + col] = now;
+          if (page_ok(old[u], num_pages)) atomicSub(refs + old[u], 1);
+          if (page_ok(now, num_pages)) atomicAdd(refs + now, 1);
+        }
+        bad = bad || now >= num_pages;
       }
-      bad = bad || now >= num_pages;
     }
   }
   if (bad) set_status(status, RTP_ERR_INVALID);
