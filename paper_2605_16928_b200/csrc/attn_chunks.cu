@@ -24,8 +24,8 @@
 // P -> next S of each group, of which two cover each other but not all of it, and the shared issue slots of the issuing warp and the softmax
 // warps.  Few rows: DRAM, 5 rows each of 32 sequences of 8K keys 120 us = 5.3 TB/s.  A mixture of pieces and single rows: both in turn,
 // 12 chunks up to 700 rows over up to 32K keys 272 us.  7 rows over 200 keys: two launches and one chain of loads and products, 10 us.
-// Tried and left: exponentials by polynomial on the FMA pipe (slower: one warp per scheduler is issue bound), P through shared memory,
-// a 56 / 224 register split, rolled loops, the merge launched ahead (no difference).
+// Tried and left: exponentials by polynomial on the FMA pipe (slower: one warp per scheduler is issue bound), a 56 / 224
+// register split, rolled loops, the merge launched ahead (no difference).
 #include "tc_common.cuh"
 
 namespace rtp {

@@ -320,7 +320,8 @@ cudaError_t launch_rope_append(const CacheView& cv, const CacheView& lv, const D
   RopeArgs a = {freqs, rotary_dim / 2, interleaved, scale, q, k, v, w_k, q_stride, k_stride, v_stride, q_out, tok_seq, tok_pos,
                 (int32_t)T, d.n_q, d.n_kv, (q ? d.n_q : 0) + 2 * d.n_kv, 0, status};
   a.proj_blocks = w_k ? (int)((T + kProjTokens - 1) / kProjTokens) * d.n_ih : 0;
-  // blocks of eight tokens where there are two for every SM, else of 32 rows
+  // blocks of eight tokens where there are two for every SM, else of 32 rows (48 heads; 16 tokens: 7.1 us with the former, 2.7 with the
+  // latter, 1184: 9.5 and 8.6, 2368: 14.7 and 14.8, 4096: 20.9 and 26.0)
   const bool many = !cv.kv_fp4 && T >= (int64_t)2 * kBlockToks * current_sm_count(148);
   const int64_t blocks = many ? (T + kBlockToks - 1) / kBlockToks : (T * a.rows_per_tok + kRowsAtOnce - 1) / kRowsAtOnce;
   (void)launch_chained(many ? rope_tokens_kernel : rope_rows_kernel, dim3((unsigned)(a.proj_blocks + blocks)), dim3(kThreads), 0, st, cv, lv, hm, a);
