@@ -604,7 +604,9 @@ rtp_status rtp_dense_attn_decode(rtp_ctx* ctx, const rtp_params* params, const r
  * of range: RTP_ERR_INVALID in the status word; such rows see the keys that there are, chunks with wrong offsets are left out.
  * K and V of all positions up to a chunk's last row are taken as finite: one that is not may reach every row of its tile of 128 keys.
  * bf16 caches (RTP_ERR_UNSUPPORTED on a 4-bit one).  On a truncated cache a chunk of local heads needs ring_pages * 64 >= window +
- * its rows + 64, unless its sequence has not outgrown the pool: else it is left out and RTP_ERR_CAPACITY recorded.  n_chunks <= 8192.
+ * (the sequence's tokens from the chunk's first row on: seq_lens - chunk_start, which is its rows only if it ends the sequence) + 64,
+ * unless its sequence fits into the pool (seq_lens <= (sink_pages + ring_pages) * 64): else it is left out, all its heads, and
+ * RTP_ERR_CAPACITY is recorded.  n_chunks <= 8192.
  * workspace: rtp_chunk_workspace_bytes(params, n_chunks, R) (RTP_ERR_CAPACITY). */
 #define RTP_CHUNK_DENSE 0
 #define RTP_CHUNK_LOCAL 1

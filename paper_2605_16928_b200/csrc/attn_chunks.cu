@@ -178,8 +178,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     int keys = (unsigned)seq < (unsigned)cv.batch ? max(0, min(cv.seq_lens[seq], cv.cap_tokens)) : 0;
     if (start < 0) keys = 0;
     if (rows > 0 && (int64_t)start + rows > keys) bad = true;
-    // a ring has to hold the window of the chunk's first row when the last one has been appended
-    if (rows > 0 && a.ring_tokens && a.ring_tokens < (int64_t)window + rows + kPage && (int64_t)start + rows > a.pool_tokens) {
+    // a ring has to hold the window of the chunk's first row when the sequence's last token has been appended, be it of this chunk or not
+    if (rows > 0 && a.ring_tokens && keys > a.pool_tokens && a.ring_tokens < (int64_t)window + ((int64_t)keys - start) + kPage) {
       rows = 0;
       set_status(status, RTP_ERR_CAPACITY);
     }
