@@ -169,8 +169,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
   bool bad = false;
   for (int c = c0; c < c1; ++c) {
     const int64_t lo = a.offsets[c], hi = a.offsets[c + 1];
-    const int seq = a.seq[c], start = a.start[c];
-    int rows = (int)(hi - lo);
+    const int seq = a.seq[c];
+    int start = a.start[c], rows = (int)(hi - lo);
     if (lo < 0 || hi < lo || hi > a.R) {       // no rows of the call
       rows = 0;
       bad = true;
@@ -178,6 +178,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const __grid_constan
     int keys = (unsigned)seq < (unsigned)cv.batch ? max(0, min(cv.seq_lens[seq], cv.cap_tokens)) : 0;
     if (start < 0) keys = 0;
     if (rows > 0 && (int64_t)start + rows > keys) bad = true;
+    // positions, those of a tile's unused rows included, stay within 32 bits (rows that far behind the end see the same keys in front of it)
+    start = max(0, min(start, 0x7fffffff - rows - 2 * span));
     // a ring has to hold the window of the chunk's first row when the sequence's last token has been appended, be it of this chunk or not
     if (rows > 0 && a.ring_tokens && keys > a.pool_tokens && a.ring_tokens < (int64_t)window + ((int64_t)keys - start) + kPage) {
       rows = 0;
