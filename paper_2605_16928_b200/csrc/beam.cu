@@ -6,8 +6,9 @@
 // the 256 threads' maxima is a lower bound of the k-th largest logit, and only the threads that reach it, k and a few, have logits that
 // do.  Those are read again (from L2), go to a list, and the list's k best are put in order.  A second kernel, one CTA per group, joins the
 // rows' sums and picks the k best of the sorted lists in the same way.
-// Tokens of one row are ordered by their logits alone; where rows meet, scores are 64-bit (sums of exponentials are 32-bit
-// within a slice, 64-bit across slices), so that neighbours are not swapped by the rounding of a normaliser.
+// Tokens of one row are ordered by their logits, or rather by scores[beam] + logit in 64 bits: where a large score swallows the differences
+// (all of them, at -infinity), tokens are equal and the lower one goes first.  Where rows meet, scores are 64-bit (sums of exponentials
+// are 32-bit within a slice, 64-bit across slices), so that neighbours are not swapped by the rounding of a normaliser.
 // Bound by the one read of the logits in principle (10 us for 32 x 8 beams over 128K in bf16); measured 22.4 us: the slices 18, of which the
 // pass over the logits is about 11 (the special function unit's rate for one exponential per logit is 8), launch, first loads, bound and
 // lists the rest; the second kernel 4 to 5.  4 beams over 32K: 8.6 us, two launches and chains of dependent loads and reductions.
@@ -189,6 +190,27 @@ __device__ __noinline__ uint4 edge_piece(const T* base, int t0, int lo, int hi) 
   for (int i = 0; i < Vec<T>::n; ++i) e[i] = t0 + i >= lo && t0 + i < hi ? base[t0 + i] : T(-INFINITY);
   return *reinterpret_cast<const uint4*>(e);
 }
+// What a logit counts as beside the others of its row: what is left of score + x, in 64 bits, when the score is taken off again.  That is x
+// itself where the score is below 2^26 |x| (64 bits then keep more than half of what is between two 32-bit numbers), and a function of the
+// sum alone, of which 32 bits hold all: the difference is x, or a multiple of the sum's last place that is as small as x.
+__device__ __forceinline__ float counts_as(float x, float score) {
+  if (fabsf(score) < 0x1p26f * fabsf(x)) return x;
+  const double sum = (double)score + (double)x;
+  return sum == -(double)INFINITY ? -INFINITY : (float)(sum - (double)score);
+}
+__device__ __forceinline__ uint32_t counts_as_key(uint32_t key, float score) { return okey(counts_as(okey_to_float(key), score) + 0.f); }
+constexpr uint32_t kLowest = 0x007fffffu, kLargest = 0xff7fffffu;   // keys of -infinity and of the largest number
+// The keys low .. high that count like `key`.
+__device__ __noinline__ uint2 alike(uint32_t key, float score) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t as = counts_as_key(key, score);
+  const uint32_t low = (uint32_t)warp_search_first(kLowest, key, lane, [&](uint32_t u) { return counts_as_key(u, score) >= as; });
+  return make_uint2(low, (uint32_t)(warp_search_first(key, kLargest, lane, [&](uint32_t u) { return counts_as_key(u, score) > as; }) - 1));
+}
+// The keys of a list, as they count.
+__device__ __noinline__ void settle(uint2* list, int n, float score) {
+  for (int i = threadIdx.x; i < n; i += kThreads) list[i].x = counts_as_key(list[i].x, score);
+}
 __device__ __forceinline__ uint4 ld_piece(const void* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
 
 template <class T>
@@ -201,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
   __shared__ __align__(16) uint32_t s_top[kTops];
   __shared__ uint32_t s_range[2];
   __shared__ uint8_t s_column[kThreads];
-  __shared__ float s_max[kWarps], s_sum[kWarps];
+  __shared__ float s_max[kWarps], s_sum[kWarps], s_score;
   __shared__ int s_n, s_sel_n, s_columns, s_scan[kWarps];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t row = blockIdx.x / a.n_slices;
@@ -247,6 +269,13 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
 #pragma unroll
     for (int v = 0; v < 2 * NV; ++v) two_pieces(c * kChunk + tid * VN + v * kThreads * VN, wa[v], wb[v]);
   };
+  // the beam's score, which is needed after the pass
+  if (tid == 0) {
+    if (a.scores)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(&s_score)), "l"(a.scores + row) : "memory");
+    else
+      s_score = 0.f;
+  }
   float m = -INFINITY, sum = 0.f;
   // (The maximum is taken off first: the largest logit's term is 1 and nothing else, so that rows with one certain token each are equal, and
   // the type's largest values times log2(e) would be no numbers.)
@@ -285,6 +314,11 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
     }
   }
   // ---- the slice's k best
+  float score = 0.f;
+  bool plain = true;                               // the score swallows nothing of what may be on the list
+  auto range = [&](uint32_t key) -> uint2 {        // of keys that count like this one; most often it is the only one
+    return key < kLowest || score == 0.f || fabsf(score) < 0x1p26f * fabsf(okey_to_float(key)) ? make_uint2(key, key) : alike(key, score);
+  };
   int n = 0;                                       // entries of the list (the same in all threads, like what follows)
   uint32_t least = 0;                              // the list takes keys from here on
   // The largest bound that k threads' keys reach (or that a few more do), or 0.  The k-th largest of 64 keys, each the largest of four
@@ -334,6 +368,10 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
   };
   auto order = [&]() {
     __syncthreads();
+    if (!plain) {
+      settle(s_list, n, score);
+      __syncthreads();
+    }
     const uint2* v = s_list;
     int count = n;
     if (n > kShort) {
@@ -365,15 +403,19 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
     n = min(n, a.k);
     for (int i = tid; i < n; i += kThreads) s_list[i] = s_best[i];
     if (tid == 0) s_n = n;
-    least = max(least, s_best[a.k - 1].x);         // (n is k: there were more)
+    least = max(least, range(s_best[a.k - 1].x).x);   // (n is k: there were more)
     __syncthreads();
   };
-  // Threads whose maximum reaches the bound have what is to be looked at again: few of them, unless more equal the bound than that.  Then it is
-  // what lies above it, and of the equal ones the first in the order of their tokens.
+  // Threads whose maximum reaches the bound, or what counts like it, have what is to be looked at again: few of them, unless more equal the
+  // bound than that.  Then it is what lies above it, and of the equal ones the first in the order of their tokens.
   const uint32_t key = c_lo * kChunk + tid * VN < stop ? okey(m + 0.f) : 0u;   // orders like the maximum (-0 is 0); 0: no token
+  if (tid == 0) asm volatile("cp.async.wait_all;" ::: "memory");
   const uint32_t bound = search(key);
-  const bool few = __syncthreads_count(key >= bound) <= a.k + kSlack;
-  least = few ? max(bound, 1u) : bound + 1;
+  score = s_score < INFINITY ? s_score : -INFINITY;        // (as the second kernel takes it)
+  const uint2 equal = range(max(bound, 1u));       // (1: less than any logit's key)
+  plain = score == 0.f || fabsf(score) < 0x1p26f * okey_to_float(equal.x);   // (no key of the list will be less)
+  const bool few = __syncthreads_count(key >= equal.x) <= a.k + kSlack;
+  least = few ? equal.x : equal.y + 1;
   if (tid == 0) s_n = s_columns = 0;
   __syncthreads();
   if (key >= least) s_column[atomicAdd(&s_columns, 1)] = (uint8_t)tid;
@@ -419,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
         if (n > kKeep) cut();
       }
   }
-  if (!few && bound && n < a.k) {
+  if (!few && n < a.k) {
     int need = a.k - n;
 #pragma unroll 1
     for (int p = 0; p < pieces && need > 0; ++p) {
@@ -437,7 +479,10 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
         unpack(w, x, T());
 #pragma unroll
         for (int i = 0; i < VN; ++i)
-          if (t0 + i < stop && (x[i] < INFINITY ? okey(x[i] + 0.f) : okey(-INFINITY)) == bound) eq |= 1u << i;
+          if (t0 + i < stop) {
+            const uint32_t u = x[i] < INFINITY ? okey(x[i] + 0.f) : okey(-INFINITY);
+            eq |= (uint32_t)(u >= equal.x && u <= equal.y) << i;
+          }
       }
       const int cnt = __popc(eq);
       int s = cnt;
