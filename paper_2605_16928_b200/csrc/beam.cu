@@ -737,14 +737,19 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_consta
 }
 
 // How a row is cut: as many slices as make one wave of four CTAs per SM, each of two whole chunks at least (of one: 11.2 us instead of 9.1 for
-// 15 rows of 50001 in 32 bits, whose second kernel then has twice the lists).
+// 15 rows of 50001 in 32 bits, whose second kernel then has twice the lists) and of 32 at most.  The latter keeps a row's normaliser right to
+// 2^-16 however long it is: a thread then adds up 16 times, at 2^-24 for the sum and 2^-22 + 2^-24 for the factor where its maximum rose
+// (2^-17.5 in all); a term's exponential is 2^-22 off, and its distance d from the maximum 2.3 x 2^-24 d (of 2^30 terms, those that count
+// are at 18 on the average at most: 2^-18.6); sums within a step, over lanes and warps take 24 roundings of 2^-24, exponentials
+// across warps and slices 2^-22 each.
+constexpr int kMostChunks = 32;
 struct BeamCut {
   int chunks, slices;                              // chunks per slice, slices per row
 };
 BeamCut beam_cut(int64_t rows, int64_t vocab, int bytes, int sm_count) {
   BeamCut c;
   const int64_t chunk = kThreads * 32 / bytes, chunks = (vocab + chunk - 1) / chunk;
-  const int64_t want = std::max<int64_t>(1, std::min(chunks / 2, (int64_t)4 * sm_count / rows));
+  const int64_t want = std::max<int64_t>({1, std::min(chunks / 2, (int64_t)4 * sm_count / rows), (chunks + kMostChunks - 1) / kMostChunks});
   c.chunks = (int)((chunks + want - 1) / want);
   c.slices = (int)((chunks + c.chunks - 1) / c.chunks);
   return c;
@@ -782,7 +787,13 @@ cudaError_t launch_beam_select(const void* logits, int format, int64_t row_strid
                   : format == RTP_LOGITS_BF16 ? launch_slices<__nv_bfloat16>(a, rows, st) : launch_slices<__half>(a, rows, st);
   if (e != cudaSuccess) return e;
   const int cached = group_lists * k <= kPickCached ? (int)(group_lists * k) : 0;
-  (void)launch_chained(beam_pick_kernel, dim3((unsigned)n_groups), dim3(kThreads), (size_t)cached * 12 + 2 * group_lists, st, a, cached);
+  const size_t smem = (size_t)cached * 12 + 2 * group_lists;
+  if (smem > kPickCached * 12 + 2048) {            // (two bytes for each of up to 2^31 / 2^16 lists and one per beam: vocabularies of millions)
+    static PerDeviceOnce once;
+    e = set_dyn_smem_once(beam_pick_kernel, 2 * ((1 << 15) + RTP_MAX_BEAMS), once);
+    if (e != cudaSuccess) return e;
+  }
+  (void)launch_chained(beam_pick_kernel, dim3((unsigned)n_groups), dim3(kThreads), smem, st, a, cached);
   return cudaGetLastError();
 }
 
