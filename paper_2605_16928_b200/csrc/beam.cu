@@ -184,11 +184,16 @@ __device__ __forceinline__ uint4 join(const uint4& lo, const uint4& hi, int s) {
 }
 // A piece of which only the logits lo .. hi - 1 exist: the others are -infinity.
 template <class T>
-__device__ __noinline__ uint4 edge_piece(const T* base, int t0, int lo, int hi) {
+struct __align__(16) Piece {
   T e[Vec<T>::n];
+};
+template <class T>
+__device__ __noinline__ uint4 edge_piece(const T* base, int t0, int lo, int hi) {
+  static_assert(sizeof(Piece<T>) == sizeof(uint4) && alignof(Piece<T>) == alignof(uint4), "read as one");
+  Piece<T> p;
 #pragma unroll
-  for (int i = 0; i < Vec<T>::n; ++i) e[i] = t0 + i >= lo && t0 + i < hi ? base[t0 + i] : T(-INFINITY);
-  return *reinterpret_cast<const uint4*>(e);
+  for (int i = 0; i < Vec<T>::n; ++i) p.e[i] = t0 + i >= lo && t0 + i < hi ? base[t0 + i] : T(-INFINITY);
+  return *reinterpret_cast<const uint4*>(&p);
 }
 // What a logit counts as beside the others of its row: what is left of score + x, in 64 bits, when the score is taken off again.  That is x
 // itself where the score is below 2^26 |x| (64 bits then keep more than half of what is between two 32-bit numbers), and a function of the
