@@ -932,14 +932,19 @@ cudaError_t launch_attn_chunks(const CacheView& cv, const CacheView& lv, const D
   const ChunkArgs a = {chunk_seq, chunk_start, row_offsets, (int32_t)n_chunks, d.group, bmp, R,
                        ring ? (int64_t)lv.ring_pages * kPage : 0, ring ? (int64_t)lv.max_pages * kPage : 0};
   (void)launch_chained(plan_kernel, dim3(1), dim3(plan.n_ctas <= 512 ? 512 : kPlanThreads), plan_smem(n_chunks), st, a, cv, hu, plan, d.n_sink, d.window, status);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return e;              // (without its plan the attention would take what the workspace holds for one)
   (void)launch_chained(attn_chunks_kernel, dim3(plan.n_ctas), dim3(kThreads), (size_t)kSmem, st, maps, cv, lv, hu, plan, d, bmp, out, lse, status);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
   // sequences that are too short to be cut need no merge
   if (((int64_t)std::max(cv.max_pages, lv.max_pages) * kPage + kTile - 1) / kTile >= 2 * kSnap) {
     const int rows = (int)std::min<int64_t>(R, 2 * bmp) * d.group;
     const int64_t blocks = std::min<int64_t>(((int64_t)plan.n_ctas * rows + kMergeWarps - 1) / kMergeWarps, (int64_t)8 * sm_count);
     (void)launch_chained(merge_kernel, dim3((unsigned)blocks), dim3(kMergeWarps * 32), 0, st, hu, plan, d.group, bmp, d.n_q, rows, out, lse);
+    return cudaGetLastError();
   }
-  return cudaGetLastError();
+  return cudaSuccess;
 }
 
 }  // namespace rtp
