@@ -35,7 +35,8 @@ EXPORTS = [
 ]
 
 
-_LOGITS = {}   # dtype -> logits_format (torch is not imported here)
+_LOGITS = {}   # dtype -> logits_format; filled by _types, like the three types (torch is imported by whoever has arrays, not here)
+_BF16 = _F32 = _INT32 = None
 
 
 class RtpError(RuntimeError):
@@ -203,22 +204,35 @@ def _enough_counts(where: str, cache, page_refs):
         raise RtpError(RTP_ERR_INVALID, where, f"page_refs has {page_refs.shape[0]} counts for {cache.num_pages} pages")
 
 
+def _types():
+    """The types of the checks below, which compare them by identity: a few tens of nanoseconds each."""
+    global _BF16, _F32, _INT32
+    import torch
+    _BF16, _F32, _INT32 = torch.bfloat16, torch.float32, torch.int32
+    _LOGITS.update({torch.float32: RTP_LOGITS_F32, torch.bfloat16: RTP_LOGITS_BF16, torch.float16: RTP_LOGITS_F16})
+
+
 def _rows_of(where: str, name: str, x, n: int, heads: int) -> int:
     """Token stride of rows [n, heads, 128] whose heads lie side by side (a slice of a projection's output, for instance)."""
     s = x.stride()
-    if x.shape != (n, heads, 128) or s[2] != 1 or (s[1] != 128 and heads > 1) or x.element_size() != 2:
-        raise RtpError(RTP_ERR_INVALID, where, f"{name} has to be 16-bit [{n} tokens, {heads}, 128], its heads side by side")
+    if x.shape != (n, heads, 128) or s[2] != 1 or (s[1] != 128 and heads > 1) or x.dtype is not _BF16:
+        raise RtpError(RTP_ERR_INVALID, where, f"{name} has to be bf16 [{n} tokens, {heads}, 128], its heads side by side")
     return s[0] if n > 1 else heads * 128
 
 
 def _is_rows(x, n: int, heads: int) -> bool:
-    """Dense 16-bit rows [n, heads, 128]."""
-    return x.is_contiguous() and x.numel() == n * heads * 128 and x.element_size() == 2 and x.dim() == 3
+    """Dense bf16 rows [n, heads, 128]."""
+    return x.is_contiguous() and x.numel() == n * heads * 128 and x.dtype is _BF16 and x.dim() == 3
 
 
 def _is_i32(x) -> bool:
-    """A dense array of 32-bit values."""
-    return x.element_size() == 4 and x.is_contiguous()
+    """A dense array of int32."""
+    return x.dtype is _INT32 and x.is_contiguous()
+
+
+def _is_f32(x) -> bool:
+    """A dense array of fp32."""
+    return x.dtype is _F32 and x.is_contiguous()
 
 
 class Rope:
@@ -230,6 +244,7 @@ class Rope:
                                         or freqs.numel() != rotary_dim // 2):
             raise RtpError(RTP_ERR_INVALID, "Rope", f"freqs has to be float64 [{rotary_dim // 2}]")
         self.freqs, self.rotary_dim, self.interleaved, self.scale = freqs, int(rotary_dim), bool(interleaved), float(scale)
+        self.device = getattr(freqs, "device", None)   # (None: an address)
 
 
 class Params:
@@ -367,20 +382,28 @@ def rtp_kv_append(ctx, params, cache, k_new, v_new, tok_seq, tok_pos, status, st
 def rtp_rope_append(ctx, params, cache, rope: Rope, q, k, v, q_out, w_k, tok_seq, tok_pos, status, stream=None):
     """q [T, query heads, 128], k, v [T, KV heads, 128]: unrotated rows, dense or slices of one projection's output; q_out dense
     (q and q_out None: keys and values only); w_k: index projections, or None."""
+    if _BF16 is None:
+        _types()
     c = params.c
     n, n_q, n_kv = tok_seq.numel(), c.n_q_heads, c.n_kv_heads
     sq, pq, po = 0, None, None
     if q is not None and q_out is not None:
         sq, pq, po = _rows_of("rtp_rope_append", "q", q, n, n_q), q.data_ptr(), q_out.data_ptr()
         if not _is_rows(q_out, n, n_q):
-            raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", f"q_out has to be dense 16-bit [{n} tokens, {n_q}, 128]")
+            raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", f"q_out has to be dense bf16 [{n} tokens, {n_q}, 128]")
     elif q is not None or q_out is not None:
         raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", "q and q_out go together")
     sk, sv = _rows_of("rtp_rope_append", "k", k, n, n_kv), _rows_of("rtp_rope_append", "v", v, n, n_kv)
     if tok_pos.numel() != n or not (_is_i32(tok_seq) and _is_i32(tok_pos)):
         raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", f"tok_seq and tok_pos have to be contiguous int32 [{n}]")
-    rc = ctx.lib.rtp_rope_append(ctx.h, C.byref(c), C.byref(cache), _ptr(rope.freqs), rope.rotary_dim, rope.interleaved, rope.scale, pq,
-                                 sq, k.data_ptr(), sk, v.data_ptr(), sv, po, None if w_k is None else w_k.data_ptr(), tok_seq.data_ptr(),
+    dev = k.device
+    if rope.device != dev and rope.device is not None:
+        raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", f"the frequencies lie on {rope.device}, the rows on {dev}")
+    if w_k is not None and (w_k.dtype is not _BF16 or w_k.device != dev or not w_k.is_contiguous() or w_k.shape != (c.n_index_heads, 128, 16)):
+        raise RtpError(RTP_ERR_INVALID, "rtp_rope_append", f"w_k has to be contiguous bf16 [{c.n_index_heads} index heads, 128, 16] on {dev}")
+    pf = rope.freqs if rope.device is None else rope.freqs.data_ptr()
+    rc = ctx.lib.rtp_rope_append(ctx.h, C.byref(c), C.byref(cache), pf, rope.rotary_dim, rope.interleaved, rope.scale, pq, sq,
+                                 k.data_ptr(), sk, v.data_ptr(), sv, po, None if w_k is None else w_k.data_ptr(), tok_seq.data_ptr(),
                                  tok_pos.data_ptr(), n, _ptr(status), _stream(stream))
     if rc:
         ctx._check(rc, "rtp_rope_append")
@@ -415,6 +438,8 @@ def rtp_cache_fork(ctx, params, cache, page_refs, src_seqs, dst_seqs, status, st
 
 def rtp_cache_reorder(ctx, params, cache, page_refs, src_seqs, dst_seqs, status, stream=None):
     """Sequence dst_seqs[i] becomes what src_seqs[i] was, all at once (src may be dst, and may be named several times)."""
+    if _BF16 is None:
+        _types()
     _same_length("rtp_cache_reorder", src_seqs, dst_seqs)
     if not (_is_i32(src_seqs) and _is_i32(dst_seqs) and _is_i32(page_refs)):
         raise RtpError(RTP_ERR_INVALID, "rtp_cache_reorder", "src_seqs, dst_seqs and page_refs have to be contiguous int32")
@@ -453,20 +478,19 @@ def rtp_beam_workspace_bytes(rows: int, vocab: int, k: int) -> int:
 def rtp_beam_select(ctx, logits, scores, finished, pad_token, parent, token, scores_out, workspace, status, stream=None):
     """logits [rows, vocab] (fp32, bf16 or fp16; rows may be strided), rows = groups x beams; scores fp32 [rows] or None; finished int32
     [rows] or None; parent, token int32 and scores_out fp32 [groups, k]: written."""
+    if _BF16 is None:
+        _types()
     rows, vocab = logits.shape
     shape = parent.shape
     groups, k = shape
     beams = rows // groups if groups else 1
-    fmt, st = _LOGITS.get(logits.dtype), logits.stride()
-    if fmt is None:
-        fmt = _LOGITS.setdefault(logits.dtype, {"torch.float32": RTP_LOGITS_F32, "torch.bfloat16": RTP_LOGITS_BF16,
-                                                "torch.float16": RTP_LOGITS_F16}.get(str(logits.dtype), -1))
+    fmt, st = _LOGITS.get(logits.dtype, -1), logits.stride()
     if (groups * beams != rows or token.shape != shape or scores_out.shape != shape or st[1] != 1 or fmt < 0
-            or not (_is_i32(parent) and _is_i32(token) and _is_i32(scores_out))
-            or (scores is not None and (scores.numel() != rows or not _is_i32(scores)))
+            or not (_is_i32(parent) and _is_i32(token) and _is_f32(scores_out))
+            or (scores is not None and (scores.numel() != rows or not _is_f32(scores)))
             or (finished is not None and (finished.numel() != rows or not _is_i32(finished)))):
-        raise RtpError(RTP_ERR_INVALID, "rtp_beam_select", "logits [groups x beams, vocabulary] in 32 or 16 bits, scores and finished one 32-bit "
-                       "value a row, parent, token and scores_out 32-bit [groups, k], contiguous but for the logits' rows")
+        raise RtpError(RTP_ERR_INVALID, "rtp_beam_select", "logits [groups x beams, vocabulary] fp32, bf16 or fp16, scores fp32 and finished int32, one "
+                       "a row, parent and token int32 and scores_out fp32 [groups, k], contiguous but for the logits' rows")
     rc = ctx.lib.rtp_beam_select(ctx.h, logits.data_ptr(), fmt, st[0] if rows > 1 else vocab, groups, beams, vocab, _ptr(scores),
                                  _ptr(finished), pad_token, k, parent.data_ptr(), token.data_ptr(), scores_out.data_ptr(),
                                  workspace.data_ptr(), workspace.nbytes, _ptr(status), _stream(stream))
@@ -610,12 +634,14 @@ def rtp_attn_chunks(ctx, params, cache, q, chunk_seq, chunk_start, row_offsets, 
                     stream=None):
     """q, out: [rows, query heads, 128]; chunk c: rows row_offsets[c] .. row_offsets[c + 1] - 1 at positions chunk_start[c] .. of
     sequence chunk_seq[c]; kv_heads: None (all) or the KV heads that are computed."""
+    if _BF16 is None:
+        _types()
     n, rows, n_q = chunk_seq.numel(), q.shape[0], params.c.n_q_heads
     if chunk_start.numel() != n or row_offsets.numel() != n + 1 or not (
             _is_rows(q, rows, n_q) and _is_rows(out, rows, n_q) and _is_i32(chunk_seq) and _is_i32(chunk_start) and _is_i32(row_offsets)
-            and (lse is None or (lse.numel() == rows * n_q and _is_i32(lse)))) or q.shape != out.shape:
+            and (lse is None or (lse.numel() == rows * n_q and _is_f32(lse)))) or q.shape != out.shape:
         raise RtpError(RTP_ERR_INVALID, "rtp_attn_chunks", f"{n} chunks and {rows} rows: chunk_start [{n}] and row_offsets [{n + 1}] have to be contiguous int32, "
-                       f"q and out dense 16-bit [{rows}, {n_q}, 128], lse 32-bit [{rows}, {n_q}]")
+                       f"q and out dense bf16 [{rows}, {n_q}, 128], lse fp32 [{rows}, {n_q}]")
     arr, n_heads = None, 0
     if kv_heads is not None:
         n_heads = len(kv_heads)
