@@ -285,8 +285,8 @@ class BeamPath:
         path.prompts(lengths); out = path.attend(layer, q, k, v) for every layer; path.begin(logits of each prompt's last row)
         path.advance();        out = path.attend(layer, q, k, v) for every layer; path.choose(logits of the hypotheses)      (a step)
 
-    ``tokens`` [groups x beams] are the tokens to go on with, ``parents`` the rows that they continue (None of a first choice),
-    ``scores`` the sums of log-probabilities and ``finished`` what has ended with ``end_token``.  Nothing is read back; a step writes to
+    ``tokens`` [groups x beams] are the tokens to go on with, ``parents`` the rows that they continue (of a first choice: row
+    g * n_beams, where the prompt lies), ``scores`` the sums of log-probabilities and ``finished`` what has ended with ``end_token``.  Nothing is read back; a step writes to
     the same arrays every time and may be captured into a graph.  ``status`` as in PagePool."""
 
     def __init__(self, pools, rope: rb.Rope, n_groups: int, n_beams: int, vocab: int, max_rows: int, pattern: int = rb.RTP_CHUNK_BY_HEAD,
@@ -351,6 +351,7 @@ class BeamPath:
         if logits.shape[0] != self.n_groups:
             raise rb.RtpError(rb.RTP_ERR_INVALID, "BeamPath.begin", f"logits of {logits.shape[0]} rows, not of {self.n_groups}")
         self._select(logits, None, None)
+        self.parents.mul_(self.n_beams)            # (the selection's rows were the groups)
         if self.n_beams > 1:
             src = self.seqs.view(self.n_groups, self.n_beams)[:, :1].expand(-1, self.n_beams - 1).contiguous().view(-1)
             dst = self.seqs.view(self.n_groups, self.n_beams)[:, 1:].contiguous().view(-1)
