@@ -320,7 +320,7 @@ class BeamPath:
             p.reserve(seqs, n)
             p.seq_lens[:self.seqs.shape[0]:self.n_beams] = n
         self.batch = (seqs, torch.zeros(self.n_groups, **i32), torch.tensor([0, *itertools.accumulate(lengths)], **i32),
-                      torch.repeat_interleave(seqs, n), torch.cat([torch.arange(x, **i32) for x in lengths]))
+                      torch.repeat_interleave(seqs, n, output_size=sum(lengths)), torch.cat([torch.arange(x, **i32) for x in lengths]))
 
     def advance(self):
         """Room for one token of every hypothesis, behind its last one."""
