@@ -295,6 +295,8 @@ class BeamPath:
         B, first = n_groups * n_beams, pools[0]
         if any(p.seq_lens.shape[0] < B or p.cache is None for p in pools) or not 1 <= n_beams <= min(vocab, rb.RTP_MAX_BEAMS) or n_groups < 1:
             raise rb.RtpError(rb.RTP_ERR_INVALID, "BeamPath", f"pools of {B} sequences with their arrays, 1 <= beams <= {rb.RTP_MAX_BEAMS} and the vocabulary")
+        if any(p.cache.kv_format != rb.RTP_KV_BF16 for p in pools):
+            raise rb.RtpError(rb.RTP_ERR_UNSUPPORTED, "BeamPath", "a 4-bit pool: its attention (rtp_attn_chunks) reads bf16 pages")
         self.pools, self.rope, self.pattern, self.pad_token, self.end_token = list(pools), rope, pattern, pad_token, end_token
         self.ctx, self.n_groups, self.n_beams, self.vocab, self.max_rows = rb.Context(), n_groups, n_beams, vocab, max(max_rows, B)
         dev = first.seq_lens.device
