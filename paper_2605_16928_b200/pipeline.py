@@ -286,8 +286,13 @@ class BeamPath:
         path.advance();        out = path.attend(layer, q, k, v) for every layer; path.choose(logits of the hypotheses)      (a step)
 
     ``tokens`` [groups x beams] are the tokens to go on with, ``parents`` the rows that they continue (of a first choice: row
-    g * n_beams, where the prompt lies), ``scores`` the sums of log-probabilities and ``finished`` what has ended with ``end_token``.  Nothing is read back; a step writes to
-    the same arrays every time and may be captured into a graph.  ``status`` as in PagePool."""
+    g * n_beams, where the prompt lies), ``scores`` the sums of log-probabilities and ``finished`` what has ended with ``end_token``.
+    Nothing is read back; a step writes to the same arrays every time and may be captured into a graph.  Its shape is the same every
+    time, too: a hypothesis that has ended goes on taking room, with ``pad_token``.
+
+    ``status`` as in PagePool.  Where a pool has something to report after its pages were asked for (it is full: RTP_ERR_CAPACITY),
+    no sequence of any pool grows, by ``prompts`` or ``advance``, until ``status_code`` has read and cleared it: the call can be made
+    again when sequences have been freed.  What follows a call that failed is not to be used."""
 
     def __init__(self, pools, rope: rb.Rope, n_groups: int, n_beams: int, vocab: int, max_rows: int, pattern: int = rb.RTP_CHUNK_BY_HEAD,
                  pad_token: int = 0, end_token: int = -1):
@@ -312,6 +317,11 @@ class BeamPath:
         self.workspace = torch.empty(ws, dtype=torch.uint8, device=dev)
         self.batch = None
 
+    def _granted(self):
+        """[1], on the device: 1 if no pool has anything to report, else 0."""
+        status = self.pools[0].status if len(self.pools) == 1 else torch.cat([p.status for p in self.pools]).amax(0, keepdim=True)
+        return (status == rb.RTP_OK).int()
+
     def prompts(self, lengths):
         """One prompt a group, by its number of tokens: pages for them in every pool.  The sequences have to be empty."""
         if len(lengths) != self.n_groups or min(lengths) < 1 or sum(lengths) > self.max_rows:
@@ -320,7 +330,9 @@ class BeamPath:
         seqs, n = self.seqs[::self.n_beams].contiguous(), torch.tensor(lengths, **i32)
         for p in self.pools:
             p.reserve(seqs, n)
-            p.seq_lens[:self.seqs.shape[0]:self.n_beams] = n
+        granted = n * self._granted()
+        for p in self.pools:
+            p.seq_lens[:self.seqs.shape[0]:self.n_beams] = granted
         self.batch = (seqs, torch.zeros(self.n_groups, **i32), torch.tensor([0, *itertools.accumulate(lengths)], **i32),
                       torch.repeat_interleave(seqs, n, output_size=sum(lengths)), torch.cat([torch.arange(x, **i32) for x in lengths]))
 
@@ -329,7 +341,9 @@ class BeamPath:
         self.positions.copy_(self.pools[0].seq_lens[:self.seqs.shape[0]])
         for p in self.pools:
             p.reserve(self.seqs, self.ones)
-            p.seq_lens[:self.seqs.shape[0]] += 1
+        granted = self._granted()
+        for p in self.pools:
+            p.seq_lens[:self.seqs.shape[0]] += granted
         self.batch = (self.seqs, self.positions, self.offsets, self.seqs, self.positions)
 
     def attend(self, layer: int, q, k, v, out=None, lse=None, w_k=None):
