@@ -360,7 +360,7 @@ rtp_status rtp_cache_compact(rtp_ctx* ctx, const rtp_params* params, const rtp_c
  * A logit of -infinity is ruled out: its score is -infinity, and it is taken behind all others only.  NaN and +infinity count as
  * -infinity, RTP_ERR_INVALID is recorded (also for a score that is NaN or +infinity).  Scores are compared in 64 bits.  Within a beam
  * scores[b] + logit, so formed, decides: logits that a large score makes equal (all of a beam's, at -infinity) go by their tokens.
- * (Whether differences count that only the normaliser swallows, less than 2^-52 of it, is left open.)  A row's
+ * (Sums that become one only when the normaliser is taken off, less than 2^-51 of the two apart, may count as equal.)  A row's
  * normaliser is right to 2^-16 and the same for rows of equal logits, zeros of either sign being equal.
  * n_beams <= 64, k <= 64, k <= n_beams * vocab.  workspace: rtp_beam_workspace_bytes(n_groups * n_beams, vocab, k). */
 #define RTP_LOGITS_F32 0

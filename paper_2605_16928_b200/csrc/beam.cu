@@ -553,7 +553,7 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_consta
   uint8_t* s_cnt = s_at + a.n_beams * a.n_slices;                        // [lists]: entries of each
   __shared__ double s_off[RTP_MAX_BEAMS];                  // score of a token with the row's largest logit
   __shared__ float s_max[RTP_MAX_BEAMS];                   // that logit
-  __shared__ int s_state[RTP_MAX_BEAMS];                   // 1: ended, 2: no token has a probability
+  __shared__ int s_state[RTP_MAX_BEAMS];                   // 1: ended, 2: all scores are -infinity
   __shared__ __align__(16) uint64_t s_top[kTops];
   __shared__ unsigned long long s_low;
   __shared__ int s_n;
@@ -598,10 +598,11 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const __grid_consta
         set_status(a.status, RTP_ERR_INVALID);
         off = -(double)INFINITY;
       }
-      s_state[b] = ended ? 1 : m == -INFINITY ? 2 : 0;
+      // (the maximum as it counts beside the score: what is left of the others is on the same grid, and no two sums become one)
+      s_max[b] = counts_as(m, (float)off);
+      s_state[b] = ended ? 1 : m == -INFINITY || off == -(double)INFINITY ? 2 : 0;
       if (!ended && m != -INFINITY) off -= log(z);
       s_off[b] = off;
-      s_max[b] = m;
     }
   }
   __syncthreads();
