@@ -20,10 +20,12 @@
 // S and P of a group share 128 columns: S of its next job is issued behind the P V that reads P, and the tensor core runs them in order.
 //
 // Bound and measured (8 KV heads, groups of 4, device time).  Long chunks: the tensor cores, 2048 rows over 32K keys 830 us = 1283 TFLOP/s
-// of 1694 that a library product reaches (1000 us by the prefill kernel of the other calls); what is missing is the chain S -> softmax ->
+// of 1694 that a library product reaches (1000 us by the prefill kernel of the other calls), by itself; call after call, under the 1000 W limit,
+// 965 us = 1104 of the 1395 that the product sustains there.  What is missing is the chain S -> softmax ->
 // P -> next S of each group, of which two cover each other but not all of it, and the shared issue slots of the issuing warp and the softmax
-// warps.  Few rows: DRAM, 5 rows each of 32 sequences of 8K keys 120 us = 5.3 TB/s.  A mixture of pieces and single rows: both in turn,
-// 12 chunks up to 700 rows over up to 32K keys 272 us.  7 rows over 200 keys: two launches and one chain of loads and products, 10 us.
+// warps.  Few rows: DRAM, 5 rows each of 32 sequences of 8K keys 119 us = 5.4 TB/s.  A mixture of pieces and single rows: both in turn,
+// 12 chunks up to 700 rows over up to 32K keys 272 us by itself, 305 call after call.  7 rows over 200 keys: two launches and one chain of
+// loads and products, 10.6 us.
 // Tried and left: exponentials by polynomial on the FMA pipe (slower: one warp per scheduler is issue bound), a 56 / 224
 // register split, rolled loops, the merge launched ahead (no difference).
 #include "tc_common.cuh"
@@ -690,7 +692,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_chunks_kernel(const __grid_c
           const float2 sc22 = make_float2(sc2, sc2), mb2 = make_float2(-mb, -mb);
           float2 rs0 = make_float2(0.f, 0.f), rs1 = rs0;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {        // P is rounded to bf16 for the MMA; the sum is of the 32-bit values
+          // P is rounded to bf16, V's type, which the product's other operand has to have (with the output's own rounding the result is 0.0021 to
+          // 0.0024 off 64 bits, relative and in the mean; 0.0017 without); the sum is of the 32-bit values
+          for (int h = 0; h < 2; ++h) {
             uint32_t pk[32];
 #pragma unroll
             for (int e = 0; e < 32; ++e) {

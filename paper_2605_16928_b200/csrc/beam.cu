@@ -9,9 +9,9 @@
 // Tokens of one row are ordered by their logits, or rather by scores[beam] + logit in 64 bits: where a large score swallows the differences
 // (all of them, at -infinity), tokens are equal and the lower one goes first.  Where rows meet, scores are 64-bit (sums of exponentials
 // are 32-bit within a slice, 64-bit across slices), so that neighbours are not swapped by the rounding of a normaliser.
-// Bound by the one read of the logits in principle (10 us for 32 x 8 beams over 128K in bf16); measured 22.4 us: the slices 18, of which the
+// Bound by the one read of the logits in principle (10 us for 32 x 8 beams over 128K in bf16); measured 22.7 us: the slices 18, of which the
 // pass over the logits is about 11 (the special function unit's rate for one exponential per logit is 8), launch, first loads, bound and
-// lists the rest; the second kernel 4 to 5.  4 beams over 32K: 8.6 us, two launches and chains of dependent loads and reductions.
+// lists the rest; the second kernel 4 to 5.  4 beams over 32K: 9.0 us, two launches and chains of dependent loads and reductions.
 // Tried and left: a list that grows during the pass under a bound from its first chunk (the slices 26 us: additions were 40 % of the
 // instructions); k rounds over the lists' heads in the second kernel (8 us; still there for lists that do not fit); logits of short
 // slices kept in registers for the list and the second kernel launched ahead (no difference).
@@ -539,7 +539,9 @@ __global__ void __launch_bounds__(kThreads, 4) beam_slice_kernel(const __grid_co
 // best of the lists list = thread, thread + threads, ..; a single warp does the rounds where 32 lanes have few lists each.
 // Lists are in the order of (beam, token): the slices of a row hold disjoint, ascending ranges of tokens, and a list is sorted.  So of
 // equal scores the lower entry goes first.
-constexpr int kPickCached = 3200;                  // entries in shared memory
+// Entries in shared memory: what the 48 KB hold that a kernel has without asking, beside the rest.  8 rows of 128K in 32 bits, 32 slices each: 3072
+// entries (k = 12) 15.8 us, ranked; 3328 (k = 13) 18.2 and 4096 (k = 16) 20.0 in rounds, which cost about 0.6 us each.
+constexpr int kPickCached = 3200;
 constexpr int kPickFew = 256;                      // entries that are ranked against each other
 __device__ __forceinline__ double score_of(uint64_t key) {
   return __longlong_as_double((long long)((key >> 63) ? key & 0x7fffffffffffffffull : ~key));
