@@ -356,7 +356,8 @@ rtp_status rtp_cache_compact(rtp_ctx* ctx, const rtp_params* params, const rtp_c
  *            (b, pad_token) with its score unchanged
  * parent     DEVICE int32 [n_groups, k]: ROW of the continued hypothesis (g * n_beams + b: what rtp_cache_reorder takes if
  *            sequences are numbered like rows); token DEVICE int32 [n_groups, k]; scores_out DEVICE fp32 [n_groups, k]; best first.
- *            Where a group has fewer than k continuations (ended ones): -1, -1, -infinity behind them.
+ *            Where a group has fewer than k continuations (ended ones): -1, -1, -infinity behind them.  None of the three may
+ *            overlap an input.
  * A logit of -infinity is ruled out: its score is -infinity, and it is taken behind all others only.  NaN and +infinity count as
  * -infinity, RTP_ERR_INVALID is recorded (also for a score that is NaN or +infinity).  Scores are compared in 64 bits.  Within a beam
  * scores[b] + logit, so formed, decides: logits that a large score makes equal (all of a beam's, at -infinity) go by their tokens.
